@@ -392,6 +392,151 @@ typedef struct {
 hidet_status_t hidet_row_schedule(int32_t dtype, int32_t softmax, int64_t rows, int64_t cols, hidet_row_schedule_t* out);
 
 /*
+ * Fused attention: scores, softmax and the product with the values in one kernel, no score ever in memory.
+ *
+ *   x[i][j] = scale * (q_i . k_j);   x = softcap * tanh(x / softcap) if softcap > 0;   x -= slopes[head] * |pos_i - j|
+ *   out_i = sum_j softmax_j(x[i][j]) v_j over the keys j that query i sees;   lse_i = ln sum_j exp(x[i][j])
+ *
+ * Query i of seq_q stands at position pos_i = i + seq_k - seq_q (the queries are the last positions of the keys).  Which keys
+ * it sees:
+ *   ranges == NULL   all; with causal, j <= pos_i; with window > 0, pos_i - j < window and (where not causal) j - pos_i < window;
+ *   ranges           begin <= j < end, the two numbers that ranges[batch][seq_q][2] holds for it (cut to 0 .. seq_k); what
+ *                    document, prefix and padding masks come to (hidet_attention_ranges).  causal and window must be 0.
+ * A query that sees no key, or only keys of score -inf, has output 0 and lse -inf.  Keys and values that a query does not see
+ * have no influence on it, whatever they hold (infinities and NaN too).
+ *
+ * dtype is HIDET_F16 or HIDET_BF16 (of q, k, v and out); scores, maxima, sums and products are accumulated in fp32; the weights
+ * exp(x - max) are rounded to dtype for the product with the values, their sum is not.  heads is a multiple of kv_heads: query
+ * head h reads key head h / (heads / kv_heads).  head_dim is a multiple of 8, at most 128.  Each tensor is given by its first
+ * element and three strides in elements (batch entry, head, position); the head_dim elements of a vector are contiguous, no
+ * alignment beyond the element's is needed, input strides may be 0.  lse (may be NULL; hidet_attention_backward needs it) is
+ * dense fp32 [batch][heads][seq_q]; slopes [heads] fp32.
+ *
+ * Work that is too small for the device otherwise is cut along the keys into splits, whose partial results meet in the workspace:
+ * DEVICE memory, 16-byte aligned, hidet_attention_workspace_bytes() for as many as the library would like; with less (or
+ * NULL) it cuts into fewer.  Results differ by the order of fp32 sums only, and are the same for the same arguments and workspace
+ * size.  Calls that share a workspace must be ordered on one stream.
+ *
+ * batch, heads or seq_q of 0 is an OK no-op; seq_k == 0 gives outputs of 0.  HIDET_ERR_UNSUPPORTED: other dtypes or head_dim, a
+ * key or value stride between positions of 2^23 or more, seq_q * heads / kv_heads or seq_k of 2^29 or more, tensors that span 2^47
+ * elements or more.  Overlaps of out or lse with an input are not allowed.
+ */
+typedef struct {
+  void* data;
+  int64_t stride_batch, stride_head, stride_row;
+} hidet_heads_t;
+typedef struct {
+  uint32_t struct_size; /* sizeof(hidet_attention_options_t) */
+  int32_t causal;
+  float scale;          /* finite */
+  float softcap;        /* 0: none */
+  int64_t window;       /* 0: none */
+  const float* slopes;  /* DEVICE, [heads]; NULL: none */
+  const int32_t* ranges; /* DEVICE, [batch][seq_q][2]; NULL: none */
+} hidet_attention_options_t;
+hidet_status_t hidet_attention(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
+                               int64_t head_dim, const hidet_heads_t* q, const hidet_heads_t* k, const hidet_heads_t* v,
+                               const hidet_heads_t* out, float* lse, const hidet_attention_options_t* options, void* workspace,
+                               int64_t workspace_bytes, void* stream);
+int64_t hidet_attention_workspace_bytes(int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
+                                        int64_t head_dim);
+/*
+ * ranges[batch][seq_q][2] of a batch whose keys are cut into documents (runs of equal numbers in documents[batch][seq_k]; a
+ * negative number is padding: it sees nothing and nobody sees it) and begin with a prefix that all queries of a document see
+ * (prefix[batch]: that many positions from the document's start).  Either may be NULL: one document, no prefix.  Within its
+ * document a query sees all keys; with causal those up to its own position, and the prefix; with window > 0 those less than
+ * window positions away (not together with a prefix: HIDET_ERR_INVALID_ARG).  A query before the first key (seq_q > seq_k) is in
+ * no document and sees nothing.  All DEVICE memory, dense.
+ */
+hidet_status_t hidet_attention_ranges(int64_t batch, int64_t seq_q, int64_t seq_k, const int32_t* documents, const int32_t* prefix,
+                                      int32_t causal, int64_t window, int32_t* ranges, void* stream);
+
+/*
+ * The backward pass of hidet_attention, with the same options: the gradients of q, k and v from that of out (grad_out), given out
+ * and lse of the forward call.  With P = exp(x - lse) and D_i = grad_out_i . out_i,
+ *   dS = P (grad_out . V^T - D) dx/d(scale q.k);  grad_q = scale dS K;  grad_k = scale dS^T Q;  grad_v = P^T grad_out,
+ * summed over the query heads that share a key head.  P and dS are rounded to dtype as operands of these products; sums are
+ * fp32, in an order that depends on the sizes alone: no atomics, the same arguments give the same bits.  Slopes have no gradient.
+ * All three gradients are written whole (zeros where nothing was seen), in their own strides; infinities and NaN in what a query
+ * does not see have no influence, as in the forward pass.  The workspace is needed: HIDET_ERR_INVALID_ARG if it is smaller than
+ * hidet_attention_backward_workspace_bytes.  Limits and no-ops as for hidet_attention.
+ */
+hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
+                                        int64_t head_dim, const hidet_heads_t* grad_out, const hidet_heads_t* q, const hidet_heads_t* k,
+                                        const hidet_heads_t* v, const hidet_heads_t* out, const float* lse, const hidet_heads_t* grad_q,
+                                        const hidet_heads_t* grad_k, const hidet_heads_t* grad_v,
+                                        const hidet_attention_options_t* options, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
+                                                 int64_t head_dim);
+
+/*
+ * Rotary positions: y = x with the pairs of its first rotary_dim elements turned by position * frequencies[j] (radians),
+ *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t),   t = position * frequencies[j], negated if inverse,
+ * where pair j is elements (j, j + rotary_dim / 2), or (2 j, 2 j + 1) if interleaved; the rest of a vector is copied.  inverse is
+ * the backward pass: the gradient of x from that of y, with the same amplitude.
+ * x and y are [batch][heads][seq][head_dim] of dtype (any of the three), given as for hidet_attention; y may be x itself (the same
+ * strides), no other overlap.  frequencies: DEVICE, fp64 [rotary_dim / 2].  Position of token s of batch entry b:
+ * positions[b * positions_stride + s] (DEVICE, int32), or first_position + s if positions is NULL.  Angles are reduced in fp64:
+ * positions up to 2^31 keep theirs to 2^-22 of a turn.
+ * batch, heads or seq of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: head_dim above 4096, 2^29 tokens, 2^20 heads.
+ */
+hidet_status_t hidet_rope(int32_t dtype, int64_t batch, int64_t heads, int64_t seq, int64_t head_dim, int64_t rotary_dim,
+                          const hidet_heads_t* x, const hidet_heads_t* y, const double* frequencies, const int32_t* positions,
+                          int64_t positions_stride, int64_t first_position, int32_t interleaved, int32_t inverse, float amplitude,
+                          void* stream);
+/*
+ * The usual frequencies, base^(-2 j / rotary_dim), into `frequencies`, HOST memory [rotary_dim / 2]; scaled for contexts longer
+ * than a model was trained with:
+ *   HIDET_ROPE_LINEAR  all divided by factor (positions pressed together)
+ *   HIDET_ROPE_BASE    base * factor^(rotary_dim / (rotary_dim - 2)): the slowest divided by factor, the fastest kept
+ *   HIDET_ROPE_BANDS   by the turns that a frequency makes in original_length positions: up to low_turns divided by factor,
+ *                      from high_turns on kept, in between the two mixed in proportion
+ */
+typedef enum { HIDET_ROPE_PLAIN = 0, HIDET_ROPE_LINEAR = 1, HIDET_ROPE_BASE = 2, HIDET_ROPE_BANDS = 3 } hidet_rope_scaling_t;
+hidet_status_t hidet_rope_frequencies(int64_t rotary_dim, double base, int32_t scaling, double factor, double low_turns,
+                                      double high_turns, double original_length, double* frequencies);
+
+/*
+ * A cache of keys and values in pages, shared by the sequences of a batch: element d of head h of the token at position t of
+ * sequence s lies at  page * stride_page + (t % page_size) * stride_slot + h * stride_head + d  of k and of v, with
+ * page = tables[s * table_stride + t / page_size].  lengths[s] is the number of tokens that the sequence has in the cache, the
+ * new ones of a call among them (cut to table_width * page_size).  A page number outside 0 .. num_pages - 1 stands for no page:
+ * nothing is written there and its keys are not seen.  Page sizes need not be powers of two, strides are free (both tensors
+ * share them; the head_dim elements are contiguous), offsets are 64 bits wide.  All but the structure itself is DEVICE memory.
+ *
+ * A call serves a ragged batch: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of `tokens` rows (starts:
+ * DEVICE, ascending, [seqs + 1]; cut to 0 .. tokens), and they are the sequence's last positions: its i-th new token stands at
+ * position lengths[s] - (starts[s + 1] - starts[s]) + i.  Rows of no sequence are left as they are.  max_new bounds the new
+ * tokens of a sequence (it sizes the grid); of a sequence with more only the first max_new are worked on.
+ *
+ * hidet_cache_append writes k and v [tokens][heads][head_dim] of the cache's dtype (any of the three) into the pages.  Two tokens
+ * for the same place (a page that two sequences share): one of them is kept, which one is not defined.
+ * hidet_cache_attention is hidet_attention (its options with causal = 1 and no ranges; q, out: [tokens][heads][head_dim], dtypes
+ * F16 and BF16) of every new token over its sequence's keys up to its own position.  lse (may be NULL) is [tokens][heads].  The
+ * workspace is as there; hidet_cache_attention_workspace_bytes gives its size.
+ * hidet_heads_t::stride_batch is ignored.  seqs, tokens, heads or max_new of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: head_dim not a
+ * multiple of 8 (or, for the attention, above 128; for append, 4096), 2^29 tokens or rows.
+ */
+typedef struct {
+  uint32_t struct_size; /* sizeof(hidet_cache_t) */
+  int32_t dtype;
+  void* k;
+  void* v;
+  int64_t num_pages, page_size, heads, head_dim;
+  int64_t stride_page, stride_slot, stride_head; /* elements */
+  const int32_t* tables;                         /* [seqs][table_stride], table_width of each row in use */
+  int64_t table_width, table_stride;
+  const int32_t* lengths; /* [seqs] */
+  int64_t seqs;
+} hidet_cache_t;
+hidet_status_t hidet_cache_append(const hidet_cache_t* cache, int64_t tokens, int64_t max_new, const hidet_heads_t* k,
+                                  const hidet_heads_t* v, const int32_t* starts, void* stream);
+hidet_status_t hidet_cache_attention(const hidet_cache_t* cache, int64_t heads, int64_t tokens, int64_t max_new, const hidet_heads_t* q,
+                                     const hidet_heads_t* out, float* lse, const int32_t* starts,
+                                     const hidet_attention_options_t* options, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t hidet_cache_attention_workspace_bytes(const hidet_cache_t* cache, int64_t heads, int64_t max_new, int64_t window);
+
+/*
  * Task mappings (Section 5.1): the compile-time mappings the kernels are built from, plus the
  * paper's worked examples, evaluated on the host so that tests can compare them with the
  * definitions.  `expr` receives a string such as "repeat(4,1)*spatial(16,8)".  hidet_taskmap_tasks

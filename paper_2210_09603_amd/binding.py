@@ -24,6 +24,7 @@ HIDET_ACT_NONE, HIDET_ACT_RELU = 0, 1
 HIDET_MAP_PLAIN, HIDET_MAP_HEAD_SPLIT = 0, 1
 HIDET_PROLOGUE_NONE, HIDET_PROLOGUE_RELU = 0, 1
 HIDET_REDUCE_SUM, HIDET_REDUCE_MAX, HIDET_REDUCE_MEAN = 0, 1, 2
+HIDET_ROPE_PLAIN, HIDET_ROPE_LINEAR, HIDET_ROPE_BASE, HIDET_ROPE_BANDS = 0, 1, 2, 3
 
 _DTYPES = {torch.float32: HIDET_F32, torch.float16: HIDET_F16, torch.bfloat16: HIDET_BF16}
 
@@ -57,6 +58,21 @@ class hidet_row_schedule_t(ctypes.Structure):
         ("workgroups", _i64), ("launches", _i64)]
 
 
+class hidet_heads_t(ctypes.Structure):
+    _fields_ = [("data", _vp), ("stride_batch", _i64), ("stride_head", _i64), ("stride_row", _i64)]
+
+
+class hidet_attention_options_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("causal", _i32), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                ("window", _i64), ("slopes", _vp), ("ranges", _vp)]
+
+
+class hidet_cache_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("dtype", _i32), ("k", _vp), ("v", _vp)] + [
+        (n, _i64) for n in ("num_pages", "page_size", "heads", "head_dim", "stride_page", "stride_slot", "stride_head")] + [
+        ("tables", _vp), ("table_width", _i64), ("table_stride", _i64), ("lengths", _vp), ("seqs", _i64)]
+
+
 class HidetError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -74,7 +90,9 @@ EXPORTS = (
     "hidet_softmax_rows", "hidet_host_div", "hidet_conv2d_splitk_workspace_bytes", "hidet_static_scratch_bytes",
     "hidet_batched_gemm_splitk_static", "hidet_conv2d_pack_weights", "hidet_conv2d_implicit_gemm_packed",
     "hidet_tune_conv2d_packed", "hidet_row_schedule", "hidet_conv2d_untuned_config",
-    "hidet_gemm_untuned_config", "hidet_conv2d_patch_rows", "hidet_conv2d_untuned_form",
+    "hidet_gemm_untuned_config", "hidet_conv2d_patch_rows", "hidet_conv2d_untuned_form", "hidet_attention",
+    "hidet_attention_workspace_bytes", "hidet_attention_backward", "hidet_attention_backward_workspace_bytes", "hidet_attention_ranges", "hidet_rope", "hidet_rope_frequencies", "hidet_cache_append",
+    "hidet_cache_attention", "hidet_cache_attention_workspace_bytes",
 )
 
 _lib = None
@@ -137,6 +155,21 @@ def lib():
         L.hidet_probe_scratch_bytes.restype = _i64
         L.hidet_probe_launch_floor.argtypes = [_vp, _i32, ctypes.POINTER(ctypes.c_float)]
         L.hidet_probe_stream_bandwidth.argtypes = [_vp, _i64, _i32, _vp, ctypes.POINTER(ctypes.c_float)]
+        hp, op, cp = ctypes.POINTER(hidet_heads_t), ctypes.POINTER(hidet_attention_options_t), ctypes.POINTER(hidet_cache_t)
+        L.hidet_attention.argtypes = [_i32] + [_i64] * 6 + [hp] * 4 + [_vp, op, _vp, _i64, _vp]
+        L.hidet_attention_workspace_bytes.argtypes = [_i64] * 6
+        L.hidet_attention_workspace_bytes.restype = _i64
+        L.hidet_attention_backward.argtypes = [_i32] + [_i64] * 6 + [hp] * 5 + [_vp] + [hp] * 3 + [op, _vp, _i64, _vp]
+        L.hidet_attention_backward_workspace_bytes.argtypes = [_i64] * 6
+        L.hidet_attention_backward_workspace_bytes.restype = _i64
+        L.hidet_attention_ranges.argtypes = [_i64] * 3 + [_vp, _vp, _i32, _i64, _vp, _vp]
+        L.hidet_rope.argtypes = [_i32] + [_i64] * 5 + [hp, hp, _vp, _vp, _i64, _i64, _i32, _i32, ctypes.c_float, _vp]
+        f64 = ctypes.c_double
+        L.hidet_rope_frequencies.argtypes = [_i64, f64, _i32, f64, f64, f64, f64, ctypes.POINTER(f64)]
+        L.hidet_cache_append.argtypes = [cp, _i64, _i64, hp, hp, _vp, _vp]
+        L.hidet_cache_attention.argtypes = [cp, _i64, _i64, _i64, hp, hp, _vp, _vp, op, _vp, _i64, _vp]
+        L.hidet_cache_attention_workspace_bytes.argtypes = [cp, _i64, _i64, _i64]
+        L.hidet_cache_attention_workspace_bytes.restype = _i64
         L.hidet_status_string.argtypes = [_i32]
         L.hidet_status_string.restype = ctypes.c_char_p
         L.hidet_version.restype = ctypes.c_char_p
@@ -554,6 +587,228 @@ def _softmax_rows(x, y, stream):
     _, _, ldy = _rows_view(y)
     st = lib().hidet_softmax_rows(_dtype(x), rows, cols, _ptr(x), ldx, _ptr(y), ldy, _stream(stream))
     _check(st, "hidet_softmax_rows")
+
+
+# ---- attention, its positions and its cache ---------------------------------------------------------------------------
+# These run on the device that their tensors are on, whichever is current: on `stream`, or on that device's current stream.
+def _on(tensors, stream):
+    """(context that makes the tensors' device current, stream handle)."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if t.device.type != "cuda":
+            raise ValueError("tensors must be on the GPU")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("tensors are on different devices")
+    if stream is not None:
+        return torch.cuda.device(device), stream.cuda_stream
+    return torch.cuda.device(device), torch.cuda.current_stream(device).cuda_stream
+
+
+def _heads(t):
+    """hidet_heads_t of a [batch, heads, rows, head_dim] tensor, or of [rows, heads, head_dim]."""
+    s = t.stride()
+    if s[-1] != 1 and t.shape[-1] > 1:
+        raise ValueError("the last dimension must be contiguous")
+    if t.dim() == 4:
+        return hidet_heads_t(t.data_ptr(), s[0], s[1], s[2])
+    return hidet_heads_t(t.data_ptr(), 0, s[1], s[0])
+
+
+def _whole32(t, shape, what):
+    """Address of a dense int32 tensor of that shape, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a dense int32 tensor of shape %s" % (what, tuple(shape)))
+    return t.data_ptr()
+
+
+def _float32(t, shape, what):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError("%s must be a dense float32 tensor of shape %s" % (what, tuple(shape)))
+    return t.data_ptr()
+
+
+def _options(scale, head_dim, causal, window, softcap, slopes, ranges, heads, ranges_shape):
+    o = hidet_attention_options_t()
+    o.struct_size = ctypes.sizeof(hidet_attention_options_t)
+    o.causal, o.window, o.softcap = int(causal), window, softcap
+    o.scale = head_dim ** -0.5 if scale is None else scale
+    o.slopes = _float32(slopes, (heads,), "slopes")
+    o.ranges = _whole32(ranges, ranges_shape, "ranges")
+    return o
+
+
+def _attention_shapes(q, k, v, *like_q):
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3]:
+        raise ValueError("need q [batch, heads, seq_q, head_dim] and k, v [batch, kv_heads, seq_k, head_dim]")
+    for t in like_q:
+        if t.shape != q.shape:
+            raise ValueError("expected shape %s, got %s" % (tuple(q.shape), tuple(t.shape)))
+    for t in (k, v) + like_q:
+        if t.dtype != q.dtype:
+            raise ValueError("tensors must agree in dtype")
+    batch, heads, seq_q, dim = q.shape
+    return batch, heads, k.shape[1], seq_q, k.shape[2], dim
+
+
+def hidet_attention(q, k, v, out, lse=None, scale=None, causal=False, window=0, softcap=0.0, slopes=None, ranges=None,
+                    workspace=None, stream=None):
+    """out = softmax(scores(q, k)) . v; q, out [batch, heads, seq_q, head_dim], k, v [batch, kv_heads, seq_k, head_dim], any
+    strides with a contiguous last dimension.  scale: head_dim ** -0.5 if None.  lse [batch, heads, seq_q] float32 is written where
+    given.  ranges [batch, seq_q, 2] int32 (hidet_attention_ranges) stands in for causal and window."""
+    sizes = _attention_shapes(q, k, v, out)
+    batch, heads, _, seq_q, _, dim = sizes
+    o = _options(scale, dim, causal, window, softcap, slopes, ranges, heads, (batch, seq_q, 2))
+    wp, wb = _ws(workspace)
+    device, handle = _on((q, k, v, out, lse, slopes, ranges, workspace), stream)
+    with device:
+        st = lib().hidet_attention(_dtype(q), *sizes, _heads(q), _heads(k), _heads(v), _heads(out),
+                                   _float32(lse, (batch, heads, seq_q), "lse"), o, wp, wb, handle)
+    _check(st, "hidet_attention")
+
+
+def hidet_attention_workspace_bytes(q, k):
+    """Workspace bytes of hidet_attention on these tensors (0: none is wanted)."""
+    return lib().hidet_attention_workspace_bytes(q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3])
+
+
+def hidet_attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, scale=None, causal=False, window=0,
+                             softcap=0.0, slopes=None, ranges=None, stream=None):
+    """Writes the gradients of q, k and v from that of out, with the options, out and lse of the forward call."""
+    sizes = _attention_shapes(q, k, v, grad_out, out, grad_q)
+    batch, heads, _, seq_q, _, dim = sizes
+    for t in (grad_k, grad_v):
+        if t.shape != k.shape or t.dtype != q.dtype:
+            raise ValueError("grad_k and grad_v must agree with k in shape and dtype")
+    o = _options(scale, dim, causal, window, softcap, slopes, ranges, heads, (batch, seq_q, 2))
+    wp, wb = _ws(workspace)
+    device, handle = _on((grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, slopes, ranges, workspace), stream)
+    with device:
+        st = lib().hidet_attention_backward(_dtype(q), *sizes, _heads(grad_out), _heads(q), _heads(k), _heads(v), _heads(out),
+                                            _float32(lse, (batch, heads, seq_q), "lse"), _heads(grad_q), _heads(grad_k),
+                                            _heads(grad_v), o, wp, wb, handle)
+    _check(st, "hidet_attention_backward")
+
+
+def hidet_attention_backward_workspace_bytes(q, k):
+    """Workspace bytes of hidet_attention_backward on these tensors."""
+    return lib().hidet_attention_backward_workspace_bytes(q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3])
+
+
+def hidet_attention_ranges(ranges, keys=None, documents=None, prefix=None, causal=False, window=0, stream=None):
+    """Fills ranges [batch, seq_q, 2] (int32) with the keys that every query sees: documents [batch, keys] int32 (runs of equal
+    numbers, negative: padding), prefix [batch] int32; `keys`: their number, seq_q or the documents' if None."""
+    if ranges.dim() != 3:
+        raise ValueError("ranges must be [batch, seq_q, 2]")
+    batch, seq_q, _ = ranges.shape
+    if keys is None:
+        keys = seq_q if documents is None else documents.shape[-1]
+    device, handle = _on((ranges, documents, prefix), stream)
+    with device:
+        st = lib().hidet_attention_ranges(batch, seq_q, keys, _whole32(documents, (batch, keys), "documents"),
+                                          _whole32(prefix, (batch,), "prefix"), int(causal), window,
+                                          _whole32(ranges, (batch, seq_q, 2), "ranges"), handle)
+    _check(st, "hidet_attention_ranges")
+
+
+def hidet_rope(x, y, frequencies, positions=None, first_position=0, interleaved=False, inverse=False, amplitude=1.0, stream=None):
+    """y = x [batch, heads, seq, head_dim] with its first 2 * len(frequencies) elements turned (y may be x); frequencies: float64 on
+    the GPU; positions: int32 [batch, seq] or [seq], or first_position, first_position + 1, ...  inverse: the backward pass."""
+    if x.dim() != 4 or x.shape != y.shape or x.dtype != y.dtype:
+        raise ValueError("x and y must be [batch, heads, seq, head_dim] and agree in shape and dtype")
+    batch, heads, seq, dim = x.shape
+    if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous():
+        raise ValueError("frequencies must be a dense float64 vector")
+    pp, ps = None, 0
+    if positions is not None:
+        if positions.dtype != torch.int32 or tuple(positions.shape) not in ((batch, seq), (seq,)) or (
+                seq > 1 and positions.stride(-1) != 1):
+            raise ValueError("positions must be int32 of shape %s or %s with contiguous rows" % ((batch, seq), (seq,)))
+        pp, ps = positions.data_ptr(), positions.stride(0) if positions.dim() == 2 else 0
+    device, handle = _on((x, y, frequencies, positions), stream)
+    with device:
+        st = lib().hidet_rope(_dtype(x), batch, heads, seq, dim, 2 * frequencies.shape[0], _heads(x), _heads(y),
+                              frequencies.data_ptr(), pp, ps, first_position, int(interleaved), int(inverse), amplitude, handle)
+    _check(st, "hidet_rope")
+
+
+def hidet_rope_frequencies(rotary_dim, base=10000.0, scaling=HIDET_ROPE_PLAIN, factor=1.0, low_turns=1.0, high_turns=4.0,
+                           original_length=8192.0):
+    """The frequencies of hidet_rope as a float64 CPU tensor of rotary_dim / 2 elements."""
+    out = torch.empty(max(rotary_dim, 0) // 2, dtype=torch.float64)
+    _check(lib().hidet_rope_frequencies(rotary_dim, base, scaling, factor, low_turns, high_turns, original_length,
+                                        ctypes.cast(out.data_ptr(), ctypes.POINTER(ctypes.c_double))), "hidet_rope_frequencies")
+    return out
+
+
+def make_cache(k_pages, v_pages, tables, lengths):
+    """hidet_cache_t over k_pages, v_pages [pages, page_size, kv_heads, head_dim] (the same strides), tables [seqs, width] int32 and
+    lengths [seqs] int32, all on one device.  It holds their addresses: they are to be filled in place."""
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or k_pages.dtype != v_pages.dtype or k_pages.stride() != v_pages.stride():
+        raise ValueError("k_pages and v_pages must be [pages, page_size, kv_heads, head_dim] and agree in shape, dtype and strides")
+    if k_pages.stride(3) != 1 and k_pages.shape[3] > 1:
+        raise ValueError("the last dimension must be contiguous")
+    if tables.dim() != 2 or tables.dtype != torch.int32 or (tables.shape[1] > 1 and tables.stride(1) != 1):
+        raise ValueError("tables must be int32 [seqs, width] with contiguous rows")
+    c = hidet_cache_t()
+    c.struct_size = ctypes.sizeof(hidet_cache_t)
+    c._keep = (k_pages, v_pages, tables, lengths)  # (the structure holds raw addresses)
+    c.dtype = _dtype(k_pages)
+    c.k, c.v = k_pages.data_ptr(), v_pages.data_ptr()
+    c.num_pages, c.page_size, c.heads, c.head_dim = k_pages.shape
+    c.stride_page, c.stride_slot, c.stride_head, _ = k_pages.stride()
+    c.seqs, c.table_width = tables.shape
+    c.tables, c.table_stride = tables.data_ptr(), max(tables.stride(0), tables.shape[1]) if tables.shape[0] <= 1 else tables.stride(0)
+    c.lengths = _whole32(lengths, (tables.shape[0],), "lengths")
+    return c
+
+
+def _new_tokens(cache, tensors, starts):
+    for t in tensors:
+        if t.dim() != 3 or t.shape != tensors[0].shape or t.shape[2] != cache.head_dim:
+            raise ValueError("need tensors [tokens, heads, %d] of one shape" % cache.head_dim)
+        if _dtype(t) != cache.dtype:
+            raise ValueError("tensors must have the cache's dtype")
+    return _whole32(starts, (cache.seqs + 1,), "starts")
+
+
+def hidet_cache_append(cache, k, v, starts, max_new, stream=None):
+    """Writes the new tokens' k and v [tokens, kv_heads, head_dim] into the pages of `cache` (make_cache): rows starts[s] to
+    starts[s + 1] are the last positions of sequence s; starts [seqs + 1] int32; at most max_new of each sequence."""
+    sp = _new_tokens(cache, (k, v), starts)
+    if k.shape[1] != cache.heads:
+        raise ValueError("the cache has %d heads" % cache.heads)
+    device, handle = _on((k, v, starts) + cache._keep, stream)
+    with device:
+        st = lib().hidet_cache_append(cache, k.shape[0], max_new, _heads(k), _heads(v), sp, handle)
+    _check(st, "hidet_cache_append")
+
+
+def hidet_cache_attention(cache, q, out, starts, max_new, scale=None, window=0, softcap=0.0, slopes=None, lse=None, workspace=None,
+                          stream=None):
+    """Attention of the new tokens' q [tokens, heads, head_dim] over their sequences' keys in `cache` up to their own position; rows
+    of `out` behind the last sequence stay as they are.  lse [tokens, heads] float32 is written where given."""
+    sp = _new_tokens(cache, (q, out), starts)
+    tokens, heads, dim = q.shape
+    o = _options(scale, dim, True, window, softcap, slopes, None, heads, None)
+    wp, wb = _ws(workspace)
+    device, handle = _on((q, out, lse, slopes, starts, workspace) + cache._keep, stream)
+    with device:
+        st = lib().hidet_cache_attention(cache, heads, tokens, max_new, _heads(q), _heads(out), _float32(lse, (tokens, heads), "lse"), sp,
+                                         o, wp, wb, handle)
+    _check(st, "hidet_cache_attention")
+
+
+def hidet_cache_attention_workspace_bytes(cache, q, max_new, window=0):
+    """Workspace bytes of hidet_cache_attention for queries like q (0: none is wanted)."""
+    return lib().hidet_cache_attention_workspace_bytes(cache, q.shape[1], max_new, window)
 
 
 def hidet_conv2d_untuned_config(dtype, x_shape, w_shape, stride=(1, 1), pad=(0, 0), packed=False):

@@ -1,0 +1,96 @@
+// Host side of the attention entry points: checks of what a caller describes, and how work is cut.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "../../include/hidet_mi355x.h"
+#include "attention.hpp"
+
+namespace hidet {
+namespace attn {
+
+constexpr long long kMaxRows = 1LL << 29;    // of a kv head's queries, and of keys: positions and their differences stay in 32 bits
+constexpr long long kMaxSpan = 1LL << 47;    // elements that a tensor spans
+constexpr long long kMaxStride = 1LL << 23;  // between keys: 64 rows of them are reached by a 32-bit byte offset
+constexpr long long kMaxBlocks = 1LL << 24;  // of 512 threads: below 2^32 work items
+
+inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// strides >= 0 and (n0 - 1) * s0 + (n1 - 1) * s1 + (n2 - 1) * s2 + dim < 2^47
+inline hidet_status_t check_span(const long long (&n)[3], const long long (&s)[3], long long dim) {
+  long long span = dim;
+  for (int i = 0; i < 3; ++i) {
+    if (s[i] < 0) return HIDET_ERR_INVALID_ARG;
+    if (n[i] > 1 && s[i] > kMaxSpan / (n[i] - 1)) return HIDET_ERR_UNSUPPORTED;
+    if (n[i] > 1) span += (n[i] - 1) * s[i];
+    if (span >= kMaxSpan) return HIDET_ERR_UNSUPPORTED;
+  }
+  return HIDET_OK;
+}
+// A tensor of vectors of 2-byte elements; `written`: no two elements of it may be the same.
+inline hidet_status_t check_heads(const hidet_heads_t* t, long long batch, long long heads, long long rows, long long dim, bool written) {
+  if (!t || !t->data) return HIDET_ERR_INVALID_ARG;
+  const long long n[3] = {batch, heads, rows}, s[3] = {t->stride_batch, t->stride_head, t->stride_row};
+  if (hidet_status_t st = check_span(n, s, dim); st != HIDET_OK) return st;
+  if (written)
+    for (int i = 0; i < 3; ++i)
+      if (n[i] > 1 && s[i] < dim) return HIDET_ERR_INVALID_ARG;
+  return is_aligned(t->data, 2) ? HIDET_OK : HIDET_ERR_ALIGNMENT;
+}
+inline Strides strides_of(const hidet_heads_t* t) { return Strides{t->stride_batch, t->stride_head, t->stride_row}; }
+
+inline hidet_status_t check_options(const hidet_attention_options_t* o) {
+  if (!o || o->struct_size != sizeof(hidet_attention_options_t)) return HIDET_ERR_INVALID_ARG;
+  if (!std::isfinite(o->scale) || !std::isfinite(o->softcap) || o->softcap < 0 || o->window < 0 || o->causal < 0 || o->causal > 1)
+    return HIDET_ERR_INVALID_ARG;
+  if (o->ranges && (o->causal || o->window)) return HIDET_ERR_INVALID_ARG;
+  if (!is_aligned(o->slopes, 4) || !is_aligned(o->ranges, 4)) return HIDET_ERR_ALIGNMENT;
+  return HIDET_OK;
+}
+// (a window of 2^30 hides nothing of 2^29 positions)
+inline int window_of(long long window) { return window >= (1LL << 30) ? 0 : (int)window; }
+// scores that are no positive multiple of the products take the form with a score of their own
+inline bool is_extra(const hidet_attention_options_t* o) { return o->softcap > 0 || o->slopes || !(o->scale > 0); }
+
+// How the work of `entries` (batch entries x kv heads) of `rows` rows each over up to `keys` keys is cut.
+struct Cut {
+  bool stream;     // the kernel of few rows
+  int row_tiles, splits;
+};
+inline long long split_bytes(long long entries, long long rows, int dp) { return entries * rows * (dp + 2) * 4; }
+Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room);
+
+inline int padded_dim(long long dim) { return dim <= 64 ? 64 : 128; }
+
+template <typename T, int DP, bool PAGED, bool EXTRA>
+hipError_t launch_forward(const Args& p, const Cut& c, hipStream_t stream) {
+  const long long blocks = (long long)p.batch * p.kv_heads * c.row_tiles * c.splits;
+  if (c.stream)
+    hipLaunchKernelGGL((stream_kernel<T, DP, PAGED, EXTRA>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), 0, stream, p);
+  else
+    hipLaunchKernelGGL((tile_kernel<T, DP, PAGED, EXTRA>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (c.splits > 1) {
+    const long long rows = (long long)p.batch * p.kv_heads * p.seq_q * p.group;
+    hipLaunchKernelGGL((join_kernel<T, DP, PAGED>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, p);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+template <bool PAGED>
+hipError_t dispatch_forward(int dtype, bool extra, const Args& p, const Cut& c, hipStream_t stream) {
+  const bool wide = padded_dim(p.dim) == 128;
+  if (dtype == HIDET_F16) {
+    if (wide) return extra ? launch_forward<f16, 128, PAGED, true>(p, c, stream) : launch_forward<f16, 128, PAGED, false>(p, c, stream);
+    return extra ? launch_forward<f16, 64, PAGED, true>(p, c, stream) : launch_forward<f16, 64, PAGED, false>(p, c, stream);
+  }
+  if (wide) return extra ? launch_forward<bf16, 128, PAGED, true>(p, c, stream) : launch_forward<bf16, 128, PAGED, false>(p, c, stream);
+  return extra ? launch_forward<bf16, 64, PAGED, true>(p, c, stream) : launch_forward<bf16, 64, PAGED, false>(p, c, stream);
+}
+
+}  // namespace attn
+}  // namespace hidet

@@ -1,0 +1,436 @@
+"""Fused attention and its backward pass against the float64 oracle: sizes, head layouts, masks, strides, values that must not matter,
+splits, streams, graphs."""
+import numpy as np
+import pytest
+import torch
+
+from attention_helpers import TYPES, assert_within, bounds, f64
+from oracle import attention as oa
+from paper_2210_09603_amd import binding as hb
+
+pytestmark = pytest.mark.gpu
+
+
+def _draw(g, shape, dtype, layout):
+    """A [batch, heads, rows, dim] tensor: dense, seen through [batch, rows, heads, dim], or a slice of a wider odd-sized buffer."""
+    b, h, n, d = shape
+    x = torch.from_numpy(g.standard_normal(shape).astype(np.float32)).to(TYPES[dtype]).cuda()
+    if layout == "dense":
+        return x
+    if layout == "tokens":
+        return x.transpose(1, 2).contiguous().transpose(1, 2)
+    buf = torch.zeros(b * n * (h + 2) * (d + 3) + 5, dtype=TYPES[dtype], device="cuda")
+    view = buf[5:5 + b * n * (h + 2) * (d + 3)].view(b, n, h + 2, d + 3)[:, :, 1:h + 1, 1:d + 1].transpose(1, 2)
+    view.copy_(x)
+    return view
+
+
+def _surrounded(shape, dtype, layout):
+    """A tensor to write to, in a buffer of sevens: (view, function that checks that nothing beside it changed)."""
+    b, h, n, d = shape
+    if layout == "odd":
+        buf = torch.full((b * n * (h + 2) * (d + 3) + 5,), 7.0, dtype=TYPES[dtype], device="cuda")
+        view = buf[5:].view(b, n, h + 2, d + 3)[:, :, 1:h + 1, 1:d + 1].transpose(1, 2)
+    else:
+        buf = torch.full((16 + b * h * n * d + 16,), 7.0, dtype=TYPES[dtype], device="cuda")
+        view = buf[16:-16].view(b, h, n, d) if layout == "dense" else buf[16:-16].view(b, n, h, d).transpose(1, 2)
+
+    def check(what):
+        keep = view.clone()
+        view.fill_(7.0)
+        assert bool((buf == 7.0).all()), what + ": wrote beside its output"
+        view.copy_(keep)
+
+    return view, check
+
+
+def _run(seed, dtype, b, h, hk, n, m, d, layout="dense", causal=False, window=0, softcap=0.0, slopes=False, ranges=None, scale=None,
+         poison=None, split=False, back=True):
+    g = np.random.Generator(np.random.PCG64(seed))
+    q, k, v = _draw(g, (b, h, n, d), dtype, layout), _draw(g, (b, hk, m, d), dtype, layout), _draw(g, (b, hk, m, d), dtype, layout)
+    dout = _draw(g, (b, h, n, d), dtype, layout)
+    sl = torch.tensor([2.0 ** (-8.0 * (i + 1) / h) for i in range(h)], device="cuda") if slopes else None
+    rg = None
+    if ranges is not None:
+        rg = torch.from_numpy(ranges.astype(np.int32)).cuda()
+        see = np.stack([oa.in_ranges(r, m) for r in ranges])
+    else:
+        see = np.stack([oa.sees(n, m, causal, window)] * b)
+    if poison is not None:
+        poison(q, k, v, dout, see)
+    out, check_out = _surrounded((b, h, n, d), dtype, layout)
+    out.fill_(float("nan"))
+    lse = torch.full((b, h, n), float("nan"), device="cuda")
+    opts = dict(scale=scale, causal=causal, window=window, softcap=softcap, slopes=sl, ranges=rg)
+    ws = None
+    if split:
+        size = hb.hidet_attention_workspace_bytes(q, k)
+        assert size > 0, "this size is not split"
+        ws = torch.full((size // 4,), float("nan"), device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse, workspace=ws, **opts)
+    torch.cuda.synchronize()
+    what = "%s %s" % (dtype, (b, h, hk, n, m, d))
+    sc = d ** -0.5 if scale is None else scale
+    args = (f64(q), f64(k), f64(v), see, sc, softcap, None if sl is None else f64(sl))
+    if not back:
+        want, bound = bounds(dtype, *args)
+    else:
+        grads = []
+        for shape in ((b, h, n, d), (b, hk, m, d), (b, hk, m, d)):
+            t, check = _surrounded(shape, dtype, layout)
+            t.fill_(float("nan"))
+            grads.append((t, check))
+        size = hb.hidet_attention_backward_workspace_bytes(q, k)
+        ws2 = torch.full((max(size, 4) // 4,), float("nan"), device="cuda")
+        hb.hidet_attention_backward(dout, q, k, v, out, lse, *(t for t, _ in grads), ws2, **opts)
+        torch.cuda.synchronize()
+        want, bound = bounds(dtype, *args, grad_out=f64(dout))
+        for name, (t, check), w, e in zip(("dq", "dk", "dv"), grads, want[2:], bound[2:]):
+            assert_within(t, w, e, what + " " + name)
+            check(what + " " + name)
+    assert_within(out, want[0], bound[0], what + " out")
+    assert_within(lse, want[1], bound[1], what + " lse")
+    check_out(what)
+    return out, lse
+
+
+SIZES = [  # batch, heads, kv heads, queries, keys, dim
+    (1, 1, 1, 1, 1, 64), (2, 3, 1, 1, 7, 64), (1, 2, 2, 2, 1, 8), (1, 2, 1, 31, 33, 40), (2, 4, 2, 65, 64, 64), (1, 4, 4, 64, 65, 72),
+    (1, 2, 1, 127, 129, 128), (1, 7, 1, 50, 50, 128), (1, 3, 3, 200, 300, 96), (2, 2, 1, 300, 200, 64), (1, 1, 1, 129, 517, 120),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", SIZES, ids=str)
+def test_full_and_causal(size, dtype):
+    for i, causal in enumerate((False, True)):  # (fewer keys than queries: the first queries see nothing)
+        _run(1000 + 10 * SIZES.index(size) + i, dtype, *size, causal=causal, layout=("dense", "tokens", "odd")[SIZES.index(size) % 3])
+
+
+@pytest.mark.parametrize("window", [1, 2, 33, 64, 150, 1 << 40])
+@pytest.mark.parametrize("causal", [False, True])
+def test_window(window, causal):
+    _run(2000 + window % 997, "bf16", 1, 4, 2, 90, 190, 64, causal=causal, window=window)
+    _run(2100 + window % 997, "f16", 1, 2, 2, 190, 90, 128, causal=causal, window=window, layout="odd")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 24])
+def test_cap_and_slopes(dtype, dim):
+    for i, (softcap, slopes) in enumerate(((0.7, False), (30.0, False), (0.0, True), (5.0, True))):
+        _run(3000 + 7 * i + dim, dtype, 1, 6, 2, 70, 100, dim, causal=i % 2 == 0, softcap=softcap, slopes=slopes)
+
+
+def test_scales_of_any_sign():
+    for i, scale in enumerate((0.0, -0.2, 1.0)):
+        _run(3100 + i, "f16", 1, 2, 1, 40, 70, 64, scale=scale)
+
+
+def _random_ranges(g, b, n, m):
+    lo, hi = g.integers(-5, m, (b, n)), g.integers(-5, m + 9, (b, n))
+    r = np.stack([lo, hi], -1)
+    r[:, ::7] = (0, m)
+    r[:, 3::11] = (5, 5)
+    return r
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [(2, 4, 2, 70, 130, 64), (1, 3, 1, 150, 150, 128), (3, 1, 1, 33, 5, 16)], ids=str)
+def test_ranges(size, dtype):
+    g = np.random.Generator(np.random.PCG64(size[3]))
+    r = _random_ranges(g, size[0], size[3], size[4])
+    _run(4000 + size[3], dtype, *size, ranges=r, slopes=True)
+    r[:] = 0  # nobody sees anything
+    out, lse = _run(4100 + size[3], dtype, *size, ranges=r)
+    assert bool((out == 0).all()) and bool((lse == -np.inf).all())
+
+
+def test_no_keys_and_no_queries():
+    q = torch.randn(2, 4, 5, 64, device="cuda").half()
+    k = torch.empty(2, 2, 0, 64, device="cuda", dtype=torch.float16)
+    out, lse, dq = torch.full_like(q, 3.0), torch.zeros(2, 4, 5, device="cuda"), torch.full_like(q, 3.0)
+    hb.hidet_attention(q, k, k, out, lse=lse)
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k), dtype=torch.uint8, device="cuda")
+    hb.hidet_attention_backward(q, q, k, k, out, lse, dq, torch.empty_like(k), torch.empty_like(k), ws)
+    assert bool((out == 0).all()) and bool((lse == -np.inf).all()) and bool((dq == 0).all())
+    none = torch.empty(2, 4, 0, 64, device="cuda", dtype=torch.float16)
+    kv = torch.randn(2, 2, 9, 64, device="cuda").half()
+    dk, dv = torch.full_like(kv, 3.0), torch.full_like(kv, 3.0)
+    hb.hidet_attention(none, kv, kv, none)
+    hb.hidet_attention_backward(none, none, kv, kv, none, torch.empty(2, 4, 0, device="cuda"), none, dk, dv, None)
+    assert bool((dk == 0).all()) and bool((dv == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 104])
+def test_what_nobody_sees_and_what_others_see_has_no_influence(dtype, dim):
+    def padding(q, k, v, g, see):  # keys and queries that take no part, and the gradients of the latter
+        for b in range(len(see)):
+            none = torch.from_numpy(~see[b].any(0)).cuda()
+            k[b][:, none] = float("nan")
+            v[b][:, none] = float("inf")
+            alone = torch.from_numpy(~see[b].any(1)).cuda()
+            q[b][:, alone] = float("nan")
+            g[b][:, alone] = float("inf")
+
+    lens = np.array([90, 0, 41])
+    r = np.zeros((3, 100, 2), dtype=int)
+    for b, length in enumerate(lens):
+        r[b, :length, 1] = np.arange(1, length + 1)
+    _run(5000 + dim, dtype, 3, 2, 1, 100, 100, dim, ranges=r, poison=padding)
+
+
+def test_a_poisoned_key_reaches_only_the_queries_that_see_it():
+    g = np.random.Generator(np.random.PCG64(5))
+    for dtype in ("f16", "bf16"):
+        q, k, v, dout = (_draw(g, (1, 4, 100, 64), dtype, "dense") for _ in range(4))
+        k, v = k[:, :2].contiguous(), v[:, :2].contiguous()
+        clean = [t.clone() for t in (k, v)]
+        v[0, 0, 60, 3] = float("inf")
+        k[0, 1, 70, 5] = float("nan")
+        outs = []
+        for kk, vv in ((k, v), clean):
+            out, lse = torch.empty_like(q), torch.empty(1, 4, 100, device="cuda")
+            dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(k)
+            ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k), dtype=torch.uint8, device="cuda")
+            hb.hidet_attention(q, kk, vv, out, lse=lse, causal=True)
+            hb.hidet_attention_backward(dout, q, kk, vv, out, lse, dq, dk, dv, ws, causal=True)
+            outs.append([out, lse, dq, dk, dv])
+        (out, lse, dq, dk, dv), want = outs
+        u = 4 * {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+
+        def same(a, b):  # (computed another way: a few roundings apart)
+            assert float((a.float() - b.float()).abs().max()) <= u * max(1.0, float(b.float().abs().max()))
+
+        same(out[:, :2, :60], want[0][:, :2, :60])
+        same(out[:, 2:, :70], want[0][:, 2:, :70])
+        same(dq[:, :2, :60], want[2][:, :2, :60])
+        same(dq[:, 2:, :70], want[2][:, 2:, :70])
+        assert bool(torch.isinf(out[:, :2, 60:, 3]).all()) and bool(torch.isnan(out[:, 2:, 70:]).all())
+        same(out[:, :2, :, :3], want[0][:, :2, :, :3])  # (an infinite value spoils its own dimension only)
+        assert bool(torch.isnan(lse[:, 2:, 70:]).all())
+        same(lse[:, :2], want[1][:, :2])
+        # every query of these heads that sees the key is spoilt, and with it the keys that such a query sees: all of them
+        assert bool(torch.isnan(dk[:, 1]).all()) and bool(torch.isnan(dv[:, 1]).all())
+
+
+def test_large_scores_and_flat_ones():
+    def grow(q, k, v, g, see):  # maxima that grow from tile to tile by far more than the slack before a rescale
+        q.copy_(torch.ones_like(q))
+        k.copy_((torch.arange(k.shape[2], device="cuda") / 8.0).to(k.dtype)[None, None, :, None].expand_as(k))
+
+    def shrink(q, k, v, g, see):
+        grow(q, k, v, g, see)
+        k.copy_(-k)
+
+    def flat(q, k, v, g, see):
+        q.zero_()
+
+    for i, poison in enumerate((grow, shrink, flat)):
+        _run(6000 + i, "f16", 1, 1, 1, 40, 400, 64, poison=poison)
+        _run(6010 + i, "bf16", 1, 2, 1, 140, 300, 128, poison=poison, causal=True)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [(1, 2, 1, 1, 9000, 64), (1, 8, 1, 3, 5000, 128), (1, 4, 2, 90, 3000, 128), (1, 2, 2, 200, 2500, 80)], ids=str)
+def test_splits(size, dtype):
+    a, la = _run(7000 + size[3], dtype, *size, causal=True, split=True, back=False)
+    b, lb = _run(7000 + size[3], dtype, *size, causal=True, split=True, back=False)
+    assert torch.equal(a, b) and torch.equal(la, lb)
+    _run(7000 + size[3], dtype, *size, causal=True, split=False, back=False)
+    g = np.random.Generator(np.random.PCG64(1))
+    r = _random_ranges(g, size[0], size[3], size[4])  # (some rows see little or nothing: empty splits)
+    r[:, 0] = (17, 40)
+    _run(7100 + size[3], dtype, *size, ranges=r, split=True, back=False, softcap=3.0)
+
+
+def test_a_workspace_that_is_too_small_for_all_splits_serves_fewer():
+    g = np.random.Generator(np.random.PCG64(8))
+    q, k, v = (_draw(g, (1, 2, n, 64), "f16", "dense") for n in (1, 8192, 8192))
+    size = hb.hidet_attention_workspace_bytes(q, k)
+    outs = []
+    for part in (0, 100, size // 3 // 16 * 16, size):
+        guard = torch.full((part + 64,), 0x5A, dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q)
+        hb.hidet_attention(q, k, v, out, workspace=guard[:part] if part else None)
+        assert bool((guard[part:] == 0x5A).all())
+        outs.append(out)
+    for o in outs[1:]:
+        assert float((o.float() - outs[0].float()).abs().max()) <= 2e-3  # (outputs below 1/4: two roundings to fp16 are 2.4e-4)
+
+
+def test_shared_inputs_with_stride_zero():
+    g = np.random.Generator(np.random.PCG64(9))
+    q = _draw(g, (3, 4, 20, 64), "bf16", "tokens")
+    k, v = (_draw(g, (1, 1, 50, 64), "bf16", "dense").expand(3, 2, 50, 64) for _ in range(2))
+    see = np.ones((3, 20, 50), bool)
+    out, lse = torch.empty_like(q), torch.empty(3, 4, 20, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse)
+    want, bound = bounds("bf16", f64(q), f64(k), f64(v), see, 0.125)
+    assert_within(out, want[0], bound[0], "out")
+    assert_within(lse, want[1], bound[1], "lse")
+
+
+@pytest.mark.parametrize("n,m", [(5, 5), (1500, 1500), (40, 2100), (300, 100), (4097, 4097)])
+def test_attention_ranges(n, m):
+    g = np.random.Generator(np.random.PCG64(n + m))
+    docs = np.repeat(g.integers(-1, 4, m), g.integers(1, 1 + max(2, m // 6), m))[:m].astype(np.int32)
+    prefix = np.array([int(g.integers(0, m + 3)), 2], dtype=np.int32)
+    documents = np.stack([docs, np.roll(docs, 3)])
+    for use_docs, use_prefix, causal, window in ((1, 0, 1, 0), (1, 0, 0, 0), (1, 1, 1, 0), (0, 1, 1, 0), (1, 0, 1, 3), (1, 0, 0, 4), (0, 0, 1, 0), (0, 0, 0, 2)):
+        r = torch.full((2, n, 2), -99, dtype=torch.int32, device="cuda")
+        hb.hidet_attention_ranges(r, keys=m, documents=torch.from_numpy(documents).cuda() if use_docs else None,
+                                  prefix=torch.from_numpy(prefix).cuda() if use_prefix else None, causal=bool(causal), window=window)
+        got = r.cpu().numpy()
+        rows = sorted({0, 1, n // 2, n - 1} | set(g.integers(0, n, 40).tolist())) if n > 200 else range(n)
+        for b in range(2):
+            at = np.arange(n) + m - n
+            lo, hi = got[b, :, 0], got[b, :, 1]
+            d = documents[b] if use_docs else np.zeros(m, dtype=int)
+            for i in rows:
+                want = np.zeros(m, dtype=bool)
+                if at[i] >= 0 and d[at[i]] >= 0:  # (a query before the first key is in no document)
+                    s = at[i]
+                    while s > 0 and d[s - 1] == d[at[i]]:
+                        s -= 1
+                    e = at[i] + 1
+                    while e < m and d[e] == d[at[i]]:
+                        e += 1
+                    j = np.arange(m)
+                    want = (j >= s) & (j < e)
+                    if window:
+                        want &= (np.abs(j - at[i]) < window)
+                    if causal:
+                        want &= (j <= at[i]) | (j < s + (prefix[b] if use_prefix else 0))
+                    want &= (j >= s) & (j < e)
+                have = np.zeros(m, dtype=bool)
+                have[max(lo[i], 0):max(hi[i], 0)] = True
+                assert np.array_equal(have, want), (use_docs, use_prefix, causal, window, b, i)
+
+
+def test_documents_and_prefixes_through_the_kernels():
+    docs = np.array([[0] * 30 + [1] * 70 + [-1] * 20, [5] * 120], dtype=np.int32)
+    prefix = np.array([10, 50], dtype=np.int32)
+    for causal, pre in ((True, False), (True, True), (False, False)):
+        see = np.stack([oa.sees(120, 120, causal, 0, docs[b], prefix[b] if pre else 0) for b in range(2)])
+        r = torch.empty(2, 120, 2, dtype=torch.int32, device="cuda")
+        hb.hidet_attention_ranges(r, documents=torch.from_numpy(docs).cuda(), prefix=torch.from_numpy(prefix).cuda() if pre else None, causal=causal)
+        ranges = r.cpu().numpy()
+        assert np.array_equal(np.stack([oa.in_ranges(x, 120) for x in ranges]), see)
+        _run(8000 + causal + 2 * pre, "bf16", 2, 4, 2, 120, 120, 64, ranges=ranges)
+
+
+def test_gradients_against_differences():
+    """The forward kernel itself, differenced: a step that fp16 inputs hold exactly, in a direction of ones and minus ones."""
+    g = np.random.Generator(np.random.PCG64(17))
+    shape_q, shape_k = (1, 2, 24, 64), (1, 1, 40, 64)
+    q, k, v = (torch.from_numpy(np.round(g.standard_normal(s) * 16) / 16).cuda() for s in (shape_q, shape_k, shape_k))
+    dout = torch.from_numpy(np.round(g.standard_normal(shape_q) * 16) / 16).cuda()
+    opts = dict(causal=True, softcap=4.0, slopes=torch.tensor([0.1, 0.3], device="cuda"))
+
+    def loss(q, k, v):  # (differences of an output rounded to fp16: its oracle has the same definition in 64 bits)
+        see = np.ones((1, 24, 40), bool) & oa.sees(24, 40, causal=True)[None]
+        return float((oa.attention(f64(q), f64(k), f64(v), see, 0.125, 4.0, [float(np.float32(0.1)), float(np.float32(0.3))])[0] * f64(dout)).sum())
+
+    h = torch.float16
+    out, lse = torch.empty(shape_q, dtype=h, device="cuda"), torch.empty(1, 2, 24, device="cuda")
+    grads = [torch.empty(s, dtype=h, device="cuda") for s in (shape_q, shape_k, shape_k)]
+    args = [t.to(h) for t in (q, k, v)]
+    hb.hidet_attention(*args, out, lse=lse, **opts)
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(args[0], args[1]), dtype=torch.uint8, device="cuda")
+    hb.hidet_attention_backward(dout.to(h), *args, out, lse, *grads, ws, **opts)
+    for which in range(3):
+        t = [q, k, v]
+        direction = torch.from_numpy(g.choice([-1.0, 1.0], t[which].shape)).cuda()
+        ends = []
+        for step in (1e-4, -1e-4):
+            moved = list(t)
+            moved[which] = t[which] + step * direction
+            ends.append(loss(*moved))
+        want = (ends[0] - ends[1]) / 2e-4
+        got = float((f64(grads[which]) * f64(direction)).sum())
+        # a sum of n gradients of random sign, each off by 2^-10 of itself and of its terms: sqrt(n) of the largest, generously
+        n = grads[which].numel()
+        assert abs(got - want) <= 2.0 ** -9 * n ** 0.5 * float(grads[which].float().abs().max()) + 1e-5, which
+
+
+def _chain(q, k, v, dout, bufs, stream=None):
+    out, lse, dq, dk, dv, ws, r, docs = bufs
+    hb.hidet_attention_ranges(r, documents=docs, causal=True, stream=stream)
+    hb.hidet_attention(q, k, v, out, lse=lse, ranges=r, workspace=ws, stream=stream)
+    hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, ranges=r, stream=stream)
+
+
+def _chain_state(seed=3):
+    g = np.random.Generator(np.random.PCG64(seed))
+    q, dout = (_draw(g, (2, 4, 150, 64), "bf16", "tokens") for _ in range(2))
+    k, v = (_draw(g, (2, 2, 150, 64), "bf16", "tokens") for _ in range(2))
+    docs = torch.tensor([[0] * 70 + [1] * 80, [2] * 149 + [-1]], dtype=torch.int32, device="cuda")
+    size = max(hb.hidet_attention_workspace_bytes(q, k), hb.hidet_attention_backward_workspace_bytes(q, k))
+
+    def bufs():
+        return (torch.empty_like(q), torch.empty(2, 4, 150, device="cuda"), torch.empty_like(q), torch.empty_like(k), torch.empty_like(k),
+                torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty(2, 150, 2, dtype=torch.int32, device="cuda"), docs)
+
+    return q, k, v, dout, bufs
+
+
+def test_graph_replays_match_eager_calls():
+    q, k, v, dout, make = _chain_state()
+    eager, captured = make(), make()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _chain(q, k, v, dout, captured)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _chain(q, k, v, dout, captured)
+    for step in range(4):
+        q.add_(0.25)
+        v.mul_(-1.0)
+        for t in captured[:6]:
+            t.zero_()
+        graph.replay()
+        _chain(q, k, v, dout, eager)
+        torch.cuda.synchronize()
+        for a, b in zip(eager[:5], captured[:5]):
+            assert torch.equal(a, b), step
+
+
+def test_on_another_stream():
+    q, k, v, dout, make = _chain_state(4)
+    a, b = make(), make()
+    _chain(q, k, v, dout, a)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    _chain(q, k, v, dout, b, stream=side)
+    side.synchronize()
+    for x, y in zip(a[:5], b[:5]):
+        assert torch.equal(x, y)
+
+
+def test_a_training_step_from_tokens_to_gradients():
+    """rope -> attention -> backward -> rope backward, as a step runs them, against the oracle's chain of the same."""
+    g = np.random.Generator(np.random.PCG64(23))
+    x, kx, v, dout = (_draw(g, s, "bf16", "tokens") for s in ((2, 4, 90, 64), (2, 2, 90, 64), (2, 2, 90, 64), (2, 4, 90, 64)))
+    f = hb.hidet_rope_frequencies(64).cuda()
+    pos = torch.arange(90, dtype=torch.int32, device="cuda").expand(2, 90).contiguous() + 1000
+    q, k = torch.empty_like(x), torch.empty_like(kx)
+    hb.hidet_rope(x, q, f, positions=pos)
+    hb.hidet_rope(kx, k, f, positions=pos)
+    out, lse = torch.empty_like(q), torch.empty(2, 4, 90, device="cuda")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k), dtype=torch.uint8, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse, causal=True)
+    hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, causal=True)
+    hb.hidet_rope(dq, dq, f, positions=pos, inverse=True)
+    hb.hidet_rope(dk, dk, f, positions=pos, inverse=True)
+    p, ff = pos.cpu().numpy(), f.cpu().numpy()
+    see = np.stack([oa.sees(90, 90, causal=True)] * 2)
+    q64, k64 = oa.rope(f64(x), p, ff), oa.rope(f64(kx), p, ff)
+    wq, wk, wv = oa.attention_grad(f64(dout), q64, k64, f64(v), see, 0.125)
+    wq, wk = oa.rope(wq, p, ff, inverse=True), oa.rope(wk, p, ff, inverse=True)
+    for got, want, name in ((dq, wq, "dq"), (dk, wk, "dk"), (dv, wv, "dv")):
+        # seven roundings of 2^-8 / sqrt(3) in a row at most (inputs, weights, dS, gradient, turned gradient), relative to the whole
+        assert np.linalg.norm(f64(got) - want) <= 7 * 2.0 ** -8 / 3 ** 0.5 * np.linalg.norm(want), name
