@@ -110,25 +110,30 @@ __device__ __forceinline__ typename Frag8<T>::type col_frag(const unsigned char*
 // register, so that nothing has to stay reserved while they run; they are waited for by wait_all_and_meet or wait_loads.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void load_to_lds(const void* base, unsigned offset, unsigned lds) {
-  const void* copy;  // (the scalar unit's copy of an address that a vector instruction may just have written)
-  asm volatile(
-      "s_mov_b32 m0, %3\n\t"
-      "s_mov_b64 %0, %2\n\t"
-      "global_load_lds_dwordx4 %1, %0"
-      : "=&s"(copy)
-      : "v"(offset), "s"(base), "s"(lds)
-      : "memory", "m0");
-}
-__device__ __forceinline__ void load_to_lds(const void* at, unsigned lds) {
-  asm volatile(
-      "s_mov_b32 m0, %1\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %0, off"
-      :
-      : "v"(at), "s"(lds)
-      : "memory", "m0");
-}
+struct DirectLoad {
+  // from `offset` bytes behind `base`, which the scalar unit copies (a load may read a scalar register that a vector instruction has
+  // written five wait states later at the earliest)
+  static __device__ __forceinline__ void at(const void* base, unsigned offset, unsigned lds) {
+    const void* copy;
+    asm volatile(
+        "s_mov_b32 m0, %3\n\t"
+        "s_mov_b64 %0, %2\n\t"
+        "global_load_lds_dwordx4 %1, %0"
+        : "=&s"(copy)
+        : "v"(offset), "s"(base), "s"(lds)
+        : "memory", "m0");
+  }
+  // from an address of the lane's own
+  static __device__ __forceinline__ void at(const void* address, unsigned lds) {
+    asm volatile(
+        "s_mov_b32 m0, %1\n\t"
+        "s_nop 3\n\t"
+        "global_load_lds_dwordx4 %0, off"
+        :
+        : "v"(address), "s"(lds)
+        : "memory", "m0");
+  }
+};
 #pragma clang diagnostic pop
 // All loads of this wavefront have arrived and all its LDS reads are back; then the workgroup meets.
 __device__ __forceinline__ void wait_all_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
@@ -618,8 +623,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
         const unsigned low = __shfl((int)(unsigned)ahead, from), high = __shfl((int)(unsigned)(ahead >> 32), from);
         const long long off = (long long)(((unsigned long long)high << 32) | low) + load_chunk * 8;
         if (loads) {
-          load_to_lds(kbase + off, to + i * 4096);
-          load_to_lds(vbase + off, to + 2 * STAGE + i * 4096);
+          DirectLoad::at(kbase + off, to + i * 4096);
+          DirectLoad::at(vbase + off, to + 2 * STAGE + i * 4096);
         }
       }
     } else {
@@ -635,8 +640,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
           vo = ((unsigned)row * (unsigned)p.vs.row + load_chunk * 8) * 2;
         }
         if (loads) {
-          load_to_lds(kt, ko, to + i * 4096);
-          load_to_lds(vt, vo, to + 2 * STAGE + i * 4096);
+          DirectLoad::at(kt, ko, to + i * 4096);
+          DirectLoad::at(vt, vo, to + 2 * STAGE + i * 4096);
         }
       }
     }

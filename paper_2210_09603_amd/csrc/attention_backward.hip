@@ -247,8 +247,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
       const unsigned ko = ((unsigned)row * (unsigned)p.ks.row + load_chunk * 8) * 2;
       const unsigned vo = ((unsigned)row * (unsigned)p.vs.row + load_chunk * 8) * 2;
       if (loads) {
-        load_to_lds(kt, ko, to + i * 4096);
-        load_to_lds(vt, vo, to + 2 * STAGE + i * 4096);
+        DirectLoad::at(kt, ko, to + i * 4096);
+        DirectLoad::at(vt, vo, to + 2 * STAGE + i * 4096);
       }
     }
   };
@@ -376,8 +376,8 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void dkv_kernel(const BackAr
       const T* qr = reinterpret_cast<const T*>(p.q) + (long long)e.b * p.qs.batch + (long long)head * p.qs.head + (long long)token * p.qs.row;
       const T* gr = reinterpret_cast<const T*>(b.dout) + (long long)e.b * b.dos.batch + (long long)head * b.dos.head + (long long)token * b.dos.row;
       if (loads) {
-        load_to_lds(qr + load_chunk * 8, dst + i * 4096);
-        load_to_lds(gr + load_chunk * 8, dst + 2 * STAGE + i * 4096);
+        DirectLoad::at(qr + load_chunk * 8, dst + i * 4096);
+        DirectLoad::at(gr + load_chunk * 8, dst + 2 * STAGE + i * 4096);
       }
     }
   };
