@@ -188,7 +188,7 @@ def built_for():
     return "torch %s, Python %d.%d" % (torch.__version__, sys.version_info[0], sys.version_info[1])
 
 
-def _load_host_calls(L):
+def _host_module():
     if not os.path.exists(HOST_CALLS_PATH):
         raise RuntimeError("host extension missing: %s (build it with `python -m paper_2210_09603_amd.build`)" % HOST_CALLS_PATH)
     loader = importlib.machinery.ExtensionFileLoader("_host_calls", HOST_CALLS_PATH)
@@ -197,13 +197,27 @@ def _load_host_calls(L):
     if module.built_for != built_for():
         raise RuntimeError("host extension %s was built for %s, this is %s (run `python -m paper_2210_09603_amd.build`)"
                            % (HOST_CALLS_PATH, module.built_for, built_for()))
-    entry = (L.hidet_gemm_cfg, L.hidet_batched_gemm_cfg, L.hidet_conv2d_implicit_gemm_cfg,
-             L.hidet_conv2d_implicit_gemm_packed, L.hidet_softmax_rows, L.hidet_reduce_rows)
+    return module
+
+
+def _of_the_process():
+    """What tells a forked process, the current device and its current stream."""
     c = torch._C
     unavailable = lambda *a: None  # (a torch without the GPU: the general path says so)
-    return module.Calls(tuple(ctypes.cast(f, _vp).value for f in entry), hidet_epilogue_t,
-                        getattr(c, "_cuda_isInBadFork", unavailable), getattr(c, "_cuda_getDevice", unavailable),
-                        getattr(c, "_cuda_getCurrentRawStream", unavailable))
+    return (getattr(c, "_cuda_isInBadFork", unavailable), getattr(c, "_cuda_getDevice", unavailable),
+            getattr(c, "_cuda_getCurrentRawStream", unavailable))
+
+
+def _load_host_calls(L):
+    entry = (L.hidet_gemm_cfg, L.hidet_batched_gemm_cfg, L.hidet_conv2d_implicit_gemm_cfg,
+             L.hidet_conv2d_implicit_gemm_packed, L.hidet_softmax_rows, L.hidet_reduce_rows)
+    return _host_module().Calls(tuple(ctypes.cast(f, _vp).value for f in entry), hidet_epilogue_t, *_of_the_process())
+
+
+def _load_attention_calls(L):
+    entry = (L.hidet_attention, L.hidet_attention_backward, L.hidet_attention_ranges, L.hidet_rope, L.hidet_cache_append,
+             L.hidet_cache_attention)
+    return _host_module().AttentionCalls(tuple(ctypes.cast(f, _vp).value for f in entry), hidet_cache_t, *_of_the_process())
 
 
 def _calls():
@@ -211,6 +225,16 @@ def _calls():
     if _host_calls is None:
         _host_calls = _load_host_calls(lib())
     return _host_calls
+
+
+_attention_calls = None
+
+
+def _attn():
+    global _attention_calls
+    if _attention_calls is None:
+        _attention_calls = _load_attention_calls(lib())
+    return _attention_calls
 
 
 def _check(status, where):
@@ -663,6 +687,14 @@ def hidet_attention(q, k, v, out, lse=None, scale=None, causal=False, window=0, 
     """out = softmax(scores(q, k)) . v; q, out [batch, heads, seq_q, head_dim], k, v [batch, kv_heads, seq_k, head_dim], any
     strides with a contiguous last dimension.  scale: head_dim ** -0.5 if None.  lse [batch, heads, seq_q] float32 is written where
     given.  ranges [batch, seq_q, 2] int32 (hidet_attention_ranges) stands in for causal and window."""
+    st = (_attention_calls or _attn()).attention(q, k, v, out, lse, scale, causal, window, softcap, slopes, ranges, workspace, stream)
+    if st < 0:
+        _attention(q, k, v, out, lse, scale, causal, window, softcap, slopes, ranges, workspace, stream)
+    else:
+        _check(st, "hidet_attention")
+
+
+def _attention(q, k, v, out, lse, scale, causal, window, softcap, slopes, ranges, workspace, stream):
     sizes = _attention_shapes(q, k, v, out)
     batch, heads, _, seq_q, _, dim = sizes
     o = _options(scale, dim, causal, window, softcap, slopes, ranges, heads, (batch, seq_q, 2))
@@ -682,6 +714,17 @@ def hidet_attention_workspace_bytes(q, k):
 def hidet_attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, scale=None, causal=False, window=0,
                              softcap=0.0, slopes=None, ranges=None, stream=None):
     """Writes the gradients of q, k and v from that of out, with the options, out and lse of the forward call."""
+    st = (_attention_calls or _attn()).attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, scale,
+                                                            causal, window, softcap, slopes, ranges, stream)
+    if st < 0:
+        _attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, scale, causal, window, softcap, slopes, ranges,
+                            stream)
+    else:
+        _check(st, "hidet_attention_backward")
+
+
+def _attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, scale, causal, window, softcap, slopes,
+                        ranges, stream):
     sizes = _attention_shapes(q, k, v, grad_out, out, grad_q)
     batch, heads, _, seq_q, _, dim = sizes
     for t in (grad_k, grad_v):
@@ -704,12 +747,20 @@ def hidet_attention_backward_workspace_bytes(q, k):
 
 def hidet_attention_ranges(ranges, keys=None, documents=None, prefix=None, causal=False, window=0, stream=None):
     """Fills ranges [batch, seq_q, 2] (int32) with the keys that every query sees: documents [batch, keys] int32 (runs of equal
-    numbers, negative: padding), prefix [batch] int32; `keys`: their number, seq_q or the documents' if None."""
+    numbers, negative: padding), prefix [batch] int32; `keys`: their number, the documents' or seq_q if None."""
+    if keys is None:
+        keys = (ranges if documents is None else documents).shape[1]
+    st = (_attention_calls or _attn()).attention_ranges(ranges, keys, documents, prefix, causal, window, stream)
+    if st < 0:
+        _attention_ranges(ranges, keys, documents, prefix, causal, window, stream)
+    else:
+        _check(st, "hidet_attention_ranges")
+
+
+def _attention_ranges(ranges, keys, documents, prefix, causal, window, stream):
     if ranges.dim() != 3:
         raise ValueError("ranges must be [batch, seq_q, 2]")
     batch, seq_q, _ = ranges.shape
-    if keys is None:
-        keys = seq_q if documents is None else documents.shape[-1]
     device, handle = _on((ranges, documents, prefix), stream)
     with device:
         st = lib().hidet_attention_ranges(batch, seq_q, keys, _whole32(documents, (batch, keys), "documents"),
@@ -721,6 +772,14 @@ def hidet_attention_ranges(ranges, keys=None, documents=None, prefix=None, causa
 def hidet_rope(x, y, frequencies, positions=None, first_position=0, interleaved=False, inverse=False, amplitude=1.0, stream=None):
     """y = x [batch, heads, seq, head_dim] with its first 2 * len(frequencies) elements turned (y may be x); frequencies: float64 on
     the GPU; positions: int32 [batch, seq] or [seq], or first_position, first_position + 1, ...  inverse: the backward pass."""
+    st = (_attention_calls or _attn()).rope(x, y, frequencies, positions, first_position, interleaved, inverse, amplitude, stream)
+    if st < 0:
+        _rope(x, y, frequencies, positions, first_position, interleaved, inverse, amplitude, stream)
+    else:
+        _check(st, "hidet_rope")
+
+
+def _rope(x, y, frequencies, positions, first_position, interleaved, inverse, amplitude, stream):
     if x.dim() != 4 or x.shape != y.shape or x.dtype != y.dtype:
         raise ValueError("x and y must be [batch, heads, seq, head_dim] and agree in shape and dtype")
     batch, heads, seq, dim = x.shape
@@ -760,6 +819,8 @@ def make_cache(k_pages, v_pages, tables, lengths):
     c = hidet_cache_t()
     c.struct_size = ctypes.sizeof(hidet_cache_t)
     c._keep = (k_pages, v_pages, tables, lengths)  # (the structure holds raw addresses)
+    one = k_pages.is_cuda and all(t.device == k_pages.device for t in c._keep)
+    c._device = k_pages.device.index if one else -1  # (of the calls that need no look at each tensor)
     c.dtype = _dtype(k_pages)
     c.k, c.v = k_pages.data_ptr(), v_pages.data_ptr()
     c.num_pages, c.page_size, c.heads, c.head_dim = k_pages.shape
@@ -782,6 +843,14 @@ def _new_tokens(cache, tensors, starts):
 def hidet_cache_append(cache, k, v, starts, max_new, stream=None):
     """Writes the new tokens' k and v [tokens, kv_heads, head_dim] into the pages of `cache` (make_cache): rows starts[s] to
     starts[s + 1] are the last positions of sequence s; starts [seqs + 1] int32; at most max_new of each sequence."""
+    st = (_attention_calls or _attn()).cache_append(cache, k, v, starts, max_new, stream)
+    if st < 0:
+        _cache_append(cache, k, v, starts, max_new, stream)
+    else:
+        _check(st, "hidet_cache_append")
+
+
+def _cache_append(cache, k, v, starts, max_new, stream):
     sp = _new_tokens(cache, (k, v), starts)
     if k.shape[1] != cache.heads:
         raise ValueError("the cache has %d heads" % cache.heads)
@@ -795,6 +864,14 @@ def hidet_cache_attention(cache, q, out, starts, max_new, scale=None, window=0, 
                           stream=None):
     """Attention of the new tokens' q [tokens, heads, head_dim] over their sequences' keys in `cache` up to their own position; rows
     of `out` behind the last sequence stay as they are.  lse [tokens, heads] float32 is written where given."""
+    st = (_attention_calls or _attn()).cache_attention(cache, q, out, starts, max_new, scale, window, softcap, slopes, lse, workspace, stream)
+    if st < 0:
+        _cache_attention(cache, q, out, starts, max_new, scale, window, softcap, slopes, lse, workspace, stream)
+    else:
+        _check(st, "hidet_cache_attention")
+
+
+def _cache_attention(cache, q, out, starts, max_new, scale, window, softcap, slopes, lse, workspace, stream):
     sp = _new_tokens(cache, (q, out), starts)
     tokens, heads, dim = q.shape
     o = _options(scale, dim, True, window, softcap, slopes, None, heads, None)

@@ -7,88 +7,102 @@ using namespace hidet::attn;
 namespace hidet {
 namespace attn {
 
-// Rows beyond 32 run in tiles of 128.  Splits: as many as give every compute unit its workgroups, as long as each keeps some
-// tiles of keys.
+// Up to 32 rows run in the kernel of few rows, more in tiles of 128.  A split is a fixed number of tiles of keys, so that the
+// sequences of a ragged batch give pieces of equal length.
+//   Few rows: 512 workgroups fill the device, which is worth a partial result for 16 tiles of 32 keys (one sequence of 131000 keys, 2 kv
+//   heads: 40 us with 16, 42 with 32, 56 with 64); up to 2048 even out a ragged batch, as long as 64 tiles remain (64 sequences of 100 to
+//   8000 keys, 8 kv heads: 222 us; 241 with 1024, 232 with 4096 of 16).
+//   Tiles of 128 rows: where they leave compute units without any, and 8 tiles of 64 keys remain (more, and the second kernel costs
+//   what it gains: 36 x 8 tiles of 1021 keys, 64 dimensions, 32 us whole and 26 + 10 split).
 Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room) {
   Cut c;
   c.stream = rows <= 32;
-  const long long tile = c.stream ? 32 : 128;
+  const long long tile = c.stream ? 32 : 128, tile_keys = c.stream ? kStreamKeys : kTileKeys;
   c.row_tiles = (int)((rows + tile - 1) / tile);
-  const long long blocks = entries * c.row_tiles, wanted = 512;
-  const long long least = c.stream ? 2 * kStreamWaves * kStreamKeys : 4 * kTileKeys;  // keys of a split
-  long long splits = blocks >= wanted ? 1 : std::min((wanted + blocks - 1) / blocks, (keys + least - 1) / least);
-  splits = std::min(splits, room / split_bytes(entries, rows, dp));
-  c.splits = (int)std::max(1LL, splits);
+  const long long blocks = entries * c.row_tiles, tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys);
+  const auto wish = [&](long long workgroups, long long least) { return std::min((workgroups + blocks - 1) / blocks, tiles / least); };
+  long long splits = c.stream ? std::max(wish(512, 16), wish(2048, 64)) : wish(256, 8);
+  splits = std::max(1LL, std::min(splits, room / split_bytes(entries, rows, dp)));
+  const long long share = (tiles + splits - 1) / splits;
+  c.share = (int)share;
+  c.splits = (int)((tiles + share - 1) / share);
   return c;
 }
 
 namespace {
 
-// What a query may see of its document, from the run of equal document numbers around it.  One workgroup a batch entry walks over
-// its positions: every thread owns a contiguous piece, knows the runs within it, and gets the start of its first run from the
-// pieces before it and the end of its last run from those behind it (maxima and minima over the 1024 pieces in LDS).
-constexpr int kRangeThreads = 1024;
+// What a query may see of its document: the run of equal document numbers around it.  A workgroup has 1024 positions; it looks for
+// the last run that begins before them and the first that ends behind them in the whole row (coalesced, all loads independent: a row
+// of 4096 takes the time of one), and within them every thread finds the borders around its position in its wavefront's bit mask, or
+// in those of the other wavefronts.
+constexpr int kRangeThreads = 1024, kRangeWaves = kRangeThreads / 64;
 __global__ __launch_bounds__(kRangeThreads) void ranges_kernel(const int* documents, const int* prefix, int* ranges, int seq_q, int seq_k,
                                                                int causal, int window) {
-  __shared__ int starts[kRangeThreads], ends[kRangeThreads];
-  const int tid = threadIdx.x, b = blockIdx.x;
-  const int piece = (seq_k + kRangeThreads - 1) / kRangeThreads;
-  const int first = min(tid * piece, seq_k), last = min(first + piece, seq_k);
+  __shared__ unsigned long long masks[kRangeWaves + 1];
+  __shared__ int outer[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.y;
+  const int first = blockIdx.x * kRangeThreads, at = first + tid;
   const int* doc = documents ? documents + (long long)b * seq_k : nullptr;
   const int skipped = seq_k - seq_q;
   int* out = ranges + (long long)b * seq_q * 2;
-  const int pre = prefix ? max(prefix[b], 0) : 0;
-  auto put = [&](int at, int start, int end, int number) {
-    const int i = at - skipped;
-    if (i < 0) return;
+  int start = 0, end = seq_k, number = 0;
+  if (doc) {
+    if (tid < 2) outer[tid] = tid ? seq_k : 0;
+    __syncthreads();
+    const int last = min(first + kRangeThreads, seq_k);
+    int before = 0, behind = seq_k;
+#pragma unroll 4
+    for (int i = tid; i < seq_k; i += kRangeThreads) {
+      const bool border = i == 0 || doc[i] != doc[i - 1];  // (a run begins here)
+      if (border && i <= first) before = max(before, i);
+      if (border && i >= last) behind = min(behind, i);
+    }
+    if (before > 0) atomicMax(&outer[0], before);  // (whole numbers: the order changes nothing)
+    if (behind < seq_k) atomicMin(&outer[1], behind);
+    const bool border = at < seq_k && (at == 0 || doc[at] != doc[at - 1]);
+    number = at < seq_k ? doc[at] : 0;
+    const unsigned long long mask = __ballot(border);
+    if (lane == 0) masks[wave] = mask;
+    __syncthreads();
+    start = outer[0];
+    end = outer[1];
+    const unsigned long long up_to = mask & (~0ull >> (63 - lane)), beyond = lane < 63 ? mask >> (lane + 1) : 0;
+    if (up_to) {
+      start = first + wave * 64 + 63 - __builtin_clzll(up_to);
+    } else {
+      for (int i = wave - 1; i >= 0; --i)
+        if (masks[i]) {
+          start = first + i * 64 + 63 - __builtin_clzll(masks[i]);
+          break;
+        }
+    }
+    if (beyond) {
+      end = at + 1 + __builtin_ctzll(beyond);
+    } else {
+      for (int i = wave + 1; i < kRangeWaves; ++i)
+        if (masks[i]) {
+          end = first + i * 64 + __builtin_ctzll(masks[i]);
+          break;
+        }
+    }
+  }
+  if (at < seq_k && at >= skipped) {
+    const int pre = prefix ? max(prefix[b], 0) : 0;
     int lo = start, hi = end;
     if (causal) {
       hi = min(hi, at + 1);
-      if (pre) hi = max(hi, min(end, pre < end - start ? start + pre : end));
+      if (pre) hi = max(hi, pre < end - start ? start + pre : end);
     }
     if (window) {
       lo = max(lo, at - window + 1);
-      if (!causal) hi = window < hi - at ? at + window : hi;
+      if (!causal && window < hi - at) hi = at + window;
     }
     if (number < 0) lo = hi = 0;
-    out[2 * i] = lo;
-    out[2 * i + 1] = hi;
-  };
-  if (doc) {
-    // the last position in the piece that begins a run, the first that ends one (the position behind it)
-    int start = -1, end = 0x7fffffff;
-    for (int at = first; at < last; ++at)
-      if (at == 0 || doc[at] != doc[at - 1]) {
-        start = at;
-        if (end == 0x7fffffff && at > first) end = at;
-      }
-    if (first < last && end == 0x7fffffff && (last == seq_k || doc[last] != doc[last - 1])) end = last;
-    starts[tid] = start;
-    ends[tid] = end;
-    __syncthreads();
-    for (int step = 1; step < kRangeThreads; step <<= 1) {
-      const int s = tid >= step ? starts[tid - step] : -1, t = tid + step < kRangeThreads ? ends[tid + step] : 0x7fffffff;
-      __syncthreads();
-      starts[tid] = max(starts[tid], s);
-      ends[tid] = min(ends[tid], t);
-      __syncthreads();
-    }
-    // runs of the piece in turn; `end` is found ahead of the run's positions
-    int run = tid > 0 ? starts[tid - 1] : 0;
-    for (int at = first; at < last;) {
-      const int number = doc[at];
-      if (at == 0 || number != doc[at - 1]) run = at;
-      int stop = at + 1;
-      while (stop < last && doc[stop] == number) ++stop;
-      int finish = stop;
-      if (stop == last && last < seq_k && doc[last] == number) finish = ends[tid + 1];
-      for (; at < stop; ++at) put(at, run, finish, number);
-    }
-  } else {
-    for (int at = tid; at < seq_k; at += kRangeThreads) put(at, 0, seq_k, 0);
+    out[2 * (at - skipped)] = lo;
+    out[2 * (at - skipped) + 1] = hi;
   }
-  // queries before the first key's position
-  for (int i = tid; i < -skipped; i += kRangeThreads) out[2 * i] = out[2 * i + 1] = 0;
+  // queries before the first key
+  for (int i = at; i < -skipped; i += gridDim.x * kRangeThreads) out[2 * i] = out[2 * i + 1] = 0;
 }
 
 }  // namespace
@@ -159,7 +173,8 @@ hidet_status_t hidet_attention(int32_t dtype, int64_t batch, int64_t heads, int6
   if (batch * kv_heads * c.row_tiles > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
   p.row_tiles = c.row_tiles;
   p.splits = c.splits;
-  return dispatch_forward<false>(dtype, is_extra(options), p, c, (hipStream_t)stream) == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
+  p.share = c.share;
+  return dispatch_forward<false>(dtype, form_of(options), p, c, (hipStream_t)stream) == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }
 
 hidet_status_t hidet_attention_ranges(int64_t batch, int64_t seq_q, int64_t seq_k, const int32_t* documents, const int32_t* prefix,
@@ -167,9 +182,10 @@ hidet_status_t hidet_attention_ranges(int64_t batch, int64_t seq_q, int64_t seq_
   if (batch < 0 || seq_q < 0 || seq_k < 0 || causal < 0 || causal > 1 || window < 0 || (prefix && window)) return HIDET_ERR_INVALID_ARG;
   if (batch == 0 || seq_q == 0) return HIDET_OK;
   if (!ranges) return HIDET_ERR_INVALID_ARG;
-  if (seq_q >= kMaxRows || seq_k >= kMaxRows || batch > (1LL << 21)) return HIDET_ERR_UNSUPPORTED;
+  if (seq_q >= kMaxRows || seq_k >= kMaxRows || batch >= (1LL << 16) || batch * (seq_k + kRangeThreads) > (1LL << 31)) return HIDET_ERR_UNSUPPORTED;
   if (!is_aligned(documents, 4) || !is_aligned(prefix, 4) || !is_aligned(ranges, 4)) return HIDET_ERR_ALIGNMENT;
-  hipLaunchKernelGGL(ranges_kernel, dim3((unsigned)batch), dim3(kRangeThreads), 0, (hipStream_t)stream, documents, prefix, ranges, (int)seq_q,
+  const unsigned pieces = (unsigned)((std::max(seq_k, (int64_t)1) + kRangeThreads - 1) / kRangeThreads);
+  hipLaunchKernelGGL(ranges_kernel, dim3(pieces, (unsigned)batch), dim3(kRangeThreads), 0, (hipStream_t)stream, documents, prefix, ranges, (int)seq_q,
                      (int)seq_k, causal, window_of(window));
   return hipGetLastError() == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }

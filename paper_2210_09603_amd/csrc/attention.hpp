@@ -53,6 +53,7 @@ struct Args {
   int batch, heads, kv_heads, group, seq_q, seq_k, dim;
   int causal, window;     // window 0: none
   int row_tiles, splits;
+  int share;              // tiles of keys of a split
   float scale, softcap;   // softcap 0: none
 };
 
@@ -80,27 +81,40 @@ struct Frag8<bf16> {
   using type = bf16x8;
 };
 
-// Rows first..first+31 as the operand with a row per lane: chunk column 2 * step + lane / 32.
-template <typename T, int CPR>
-__device__ __forceinline__ typename Frag8<T>::type row_frag(const unsigned char* tile, int lane, int first, int step) {
-  const int row = lane & 31;
-  const int c = (2 * step + (lane >> 5)) ^ swz<CPR>(row);
-  return __builtin_bit_cast(typename Frag8<T>::type, *reinterpret_cast<const u32x4*>(tile + ((first + row) * CPR + c) * 16));
-}
+// Where a lane reads, as byte offsets from a tile: worked out once, so that a read costs an addition at most.
+template <int DP>
+struct ReadMap {
+  static constexpr int CPR = DP / 8, KS = DP / 16, DT = DP / 32;
+  unsigned row[KS];     // as a row: chunk column 2 * step + lane / 32 of row lane % 32
+  unsigned col[DT][2];  // as a column: 4 rows of the group's 16 lanes, and those 8 below
+  __device__ __forceinline__ explicit ReadMap(int lane) {
+    const int r = lane & 31, s = lane & 15, h = lane >> 5;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) row[ks] = (r * CPR + ((2 * ks + h) ^ swz<CPR>(r))) * 16;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int chunk = d * 4 + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1), c = 8 * i + 4 * h + (s >> 2);
+        col[d][i] = (c * CPR + (chunk ^ swz<CPR>(c))) * 16 + (s & 1) * 8;
+      }
+  }
+};
+typedef __attribute__((address_space(3))) const u32x4 LdsChunk;
+typedef __attribute__((address_space(3))) i16x4 LdsQuad;
 
+// Rows first..first+31 of the tile at LDS address `tile` as the operand with a row per lane.
+template <typename T, int DP>
+__device__ __forceinline__ typename Frag8<T>::type row_frag(const ReadMap<DP>& m, unsigned tile, int first, int step) {
+  return __builtin_bit_cast(typename Frag8<T>::type, *(LdsChunk*)(__UINTPTR_TYPE__)(tile + m.row[step] + first * DP * 2));
+}
 // Columns 32 * dt..+31 as the operand with a column per lane; its 8 values are rows first + {0..3, 8..11} + 4 * (lane / 32).
-template <typename T, int CPR>
-__device__ __forceinline__ typename Frag8<T>::type col_frag(const unsigned char* tile, int lane, int first, int dt) {
-  const int s = lane & 15, h = lane >> 5;
-  const int chunk = dt * 4 + 2 * ((lane >> 4) & 1) + ((s & 3) >> 1);
+template <typename T, int DP>
+__device__ __forceinline__ typename Frag8<T>::type col_frag(const ReadMap<DP>& m, unsigned tile, int first, int dt) {
   u32x2 part[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = 8 * i + 4 * h + (s >> 2);
-    const unsigned char* at = tile + ((first + row) * CPR + (chunk ^ swz<CPR>(row))) * 16 + (s & 1) * 8;
-    part[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                            (__attribute__((address_space(3))) i16x4*)(const_cast<unsigned char*>(at))));
-  }
+  for (int i = 0; i < 2; ++i)
+    part[i] = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsQuad*)(__UINTPTR_TYPE__)(tile + m.col[dt][i] + first * DP * 2)));
   const u32x4 v = {part[0][0], part[0][1], part[1][0], part[1][1]};
   return __builtin_bit_cast(typename Frag8<T>::type, v);
 }
@@ -138,6 +152,10 @@ struct DirectLoad {
 // All loads of this wavefront have arrived and all its LDS reads are back; then the workgroup meets.
 __device__ __forceinline__ void wait_all_and_meet() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Nothing is outstanding, and the compiler knows it: where a register that it loaded was first used inside a loop, it would wait
+// there for all loads in flight, the direct ones among them, in every round (a capped prompt of 4096 x 32 heads: 240 us).
+__device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0); }
+
 __device__ __forceinline__ unsigned lds_address(const void* p) {
   return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p;
 }
@@ -173,25 +191,41 @@ __device__ __forceinline__ float wave_sum(float v) {
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
 // ---- scores -----------------------------------------------------------------------------------------------------------
+// What a score is besides scale * q.k, a template parameter of the kernels: an exponential and a reciprocal an element for the cap
+// (half of such a kernel's vector time), two instructions for the bias.
+enum : int { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2 };  // PLAIN: scale > 0 and nothing else
+
 // The score to base 2 of a product: scale and cap as they stand in Args, slope for the query's head.
+template <int FORM>
 struct Score {
-  float factor;       // to base 2; with a cap: 2 log2(e) scale / cap, so that exp2 of it is e^2y
-  float cap;          // cap * log2(e); 0: none
-  float slope;        // slope * log2(e)
+  float factor;  // to base 2; with a cap: 2 log2(e) scale / cap, so that exp2 of it is e^2y
+  float cap;     // cap * log2(e)
+  float slope;   // slope * log2(e)
   __device__ __forceinline__ Score(const Args& p, float slope_of_head) {
-    factor = p.softcap > 0 ? 2.0f * kLog2e * p.scale / p.softcap : p.scale * kLog2e;
+    factor = FORM & FORM_CAP ? 2.0f * kLog2e * p.scale / p.softcap : p.scale * kLog2e;
     cap = p.softcap * kLog2e;
     slope = slope_of_head * kLog2e;
   }
-  // tanh(y) = 1 - 2 / (e^2y + 1): off by some 2^-23, which is what the score's own rounding to fp32 is off for scores near
-  // the cap
-  __device__ __forceinline__ float tanh_of(float dot) const {
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_fast(dot * factor) + 1.0f);
+  // 1 / (e^2y + 1), of which tanh(y) is 1 - 2 r and its derivative 4 r (1 - r): off by some 2^-23, which is what the score's own
+  // rounding to fp32 is off for scores near the cap
+  __device__ __forceinline__ float share(float dot) const { return __builtin_amdgcn_rcpf(exp2_fast(dot * factor) + 1.0f); }
+  // (distances beyond 2^24 are rounded to fp32, 2^-24 of themselves)
+  __device__ __forceinline__ float biased(float x, float distance) const {
+    if constexpr (FORM & FORM_BIAS) return __builtin_fmaf(-slope, __builtin_fabsf(distance), x);
+    return x;
   }
-  __device__ __forceinline__ float operator()(float dot, int distance) const {
-    float x = cap > 0 ? cap * tanh_of(dot) : dot * factor;
-    // (no slope: a distance of any size adds nothing, not even to an infinite score)
-    return x - slope * (float)(distance < 0 ? -distance : distance);
+  __device__ __forceinline__ float operator()(float dot, float distance) const {
+    return biased(FORM & FORM_CAP ? __builtin_fmaf(-2.0f * cap, share(dot), cap) : dot * factor, distance);
+  }
+  // the same with its derivative to the uncapped score
+  __device__ __forceinline__ float operator()(float dot, float distance, float& derivative) const {
+    if constexpr (FORM & FORM_CAP) {
+      const float r = share(dot);
+      derivative = 4.0f * r * (1.0f - r);
+      return biased(__builtin_fmaf(-2.0f * cap, r, cap), distance);
+    }
+    derivative = 1.0f;
+    return biased(dot * factor, distance);
   }
 };
 
@@ -235,28 +269,51 @@ struct Row {
   int token, head;  // head: of all heads
   int lo, hi;       // keys that it sees: lo <= j < hi; none: 0, 0
 };
+// The keys from lo to hi that the query at position `at` sees where there are no ranges; lo and hi never fall from a query to the next.
+// None: lo >= hi.
+template <bool PAGED>
+__device__ __forceinline__ void seen_from(const Args& p, const Entry& e, int at, int& lo, int& hi) {
+  lo = max(p.window ? at - p.window + 1 : 0, 0);
+  if (PAGED || p.causal)
+    hi = at + 1;
+  else
+    hi = p.window && p.window < e.keys - at ? at + p.window : e.keys;  // (at + window may pass 32 bits)
+  hi = min(hi, e.keys);
+}
 template <bool PAGED>
 __device__ __forceinline__ Row make_row(const Args& p, const Entry& e, int r) {
   Row w;
   w.token = p.d_group.div(r);
   w.head = e.kv * p.group + (r - w.token * p.group);
-  const int at = w.token + e.shift;
   if (!PAGED && p.ranges) {
     const int* range = p.ranges + ((long long)e.b * p.seq_q + w.token) * 2;
-    w.lo = range[0];
-    w.hi = range[1];
+    w.lo = max(range[0], 0);
+    w.hi = min(range[1], e.keys);
   } else {
-    // (at + window may pass 32 bits)
-    w.lo = p.window ? at - p.window + 1 : 0;
-    if (PAGED || p.causal)
-      w.hi = at + 1;
-    else
-      w.hi = p.window && p.window < e.keys - at ? at + p.window : e.keys;
+    seen_from<PAGED>(p, e, w.token + e.shift, w.lo, w.hi);
   }
-  w.lo = max(w.lo, 0);
-  w.hi = min(w.hi, e.keys);
   if (w.lo >= w.hi) w.lo = w.hi = 0;
   return w;
+}
+
+// Of the rows first..last: from the first to the last key + 1 that any of them sees, and the keys that all of them see.
+struct Seen {
+  int lo, hi, full_lo, full_hi;
+};
+// `w`: one of the rows in each half of a wavefront, all of them in its 32 lanes
+template <bool PAGED>
+__device__ __forceinline__ Seen seen_by(const Args& p, const Entry& e, const Row& w, int first, int last) {
+  Seen s;
+  if (!PAGED && p.ranges) {
+    s.lo = wave_min(w.lo < w.hi ? w.lo : 0x7fffffff);
+    s.hi = wave_max(w.hi);
+    s.full_lo = wave_max(w.lo);
+    s.full_hi = wave_min(w.hi);
+  } else {
+    seen_from<PAGED>(p, e, p.d_group.div(first) + e.shift, s.lo, s.full_hi);
+    seen_from<PAGED>(p, e, p.d_group.div(last) + e.shift, s.full_lo, s.hi);
+  }
+  return s;
 }
 
 template <bool PAGED>
@@ -350,14 +407,15 @@ struct State {
 // A tile of 32 * KT keys: s holds the products with the queries.  P goes to p (the operand of the second product), its sum and
 // maximum to the state.  `first`: key of register 0 of lane 0; MASKED: some query does not see some of the keys.
 // `there`: bit j: key j of the tile is on a page of the cache (only looked at where MASKED).
-template <typename T, int DP, bool EXTRA, int KT>
-__device__ __forceinline__ void softmax_tile(State<T, DP>& st, f32x16 (&s)[KT], typename Frag8<T>::type (&p)[2 * KT], const Score& score,
+template <typename T, int DP, int FORM, int KT>
+__device__ __forceinline__ void softmax_tile(State<T, DP>& st, f32x16 (&s)[KT], typename Frag8<T>::type (&p)[2 * KT], const Score<FORM>& score,
                                              int first, int lo, int hi, int at, int half, bool masked, unsigned long long there) {
-  if constexpr (EXTRA) {
+  if constexpr (FORM != FORM_PLAIN) {
+    const float distance = (float)(at - first - 4 * half);
 #pragma unroll
     for (int t = 0; t < KT; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[t][r] = score(s[t][r], at - (first + 4 * half + 32 * t + 8 * (r >> 2) + (r & 3)));
+      for (int r = 0; r < 16; ++r) s[t][r] = score(s[t][r], distance - (float)(32 * t + 8 * (r >> 2) + (r & 3)));
   }
   if (masked) {
     const int from = lo - first - 4 * half;
@@ -377,19 +435,19 @@ __device__ __forceinline__ void softmax_tile(State<T, DP>& st, f32x16 (&s)[KT], 
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
   top = max_of_halves(top);
-  const float factor = EXTRA ? 1.0f : score.factor;
+  const float factor = FORM != FORM_PLAIN ? 1.0f : score.factor;
   // (a first maximum is larger than none by any measure)
   if (__any((top - st.top) * factor > kSlack || (st.top == kNoMax && top != kNoMax))) st.raise(top, factor);
-  float sum = 0.0f;
+  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
   for (int t = 0; t < KT; ++t)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const float e = EXTRA ? exp2_fast(s[t][r] - st.shift) : exp2_fast(__builtin_fmaf(s[t][r], factor, -st.shift));
-      sum += e;
+      const float e = FORM != FORM_PLAIN ? exp2_fast(s[t][r] - st.shift) : exp2_fast(__builtin_fmaf(s[t][r], factor, -st.shift));
+      sum[r & 3] += e;
       p[2 * t + (r >> 3)][r & 7] = from_f32<T>(e);
     }
-  st.sum += sum;
+  st.sum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 // ---- results --------------------------------------------------------------------------------------------------------------
@@ -408,12 +466,12 @@ __device__ __forceinline__ Part part_of(const Args& p, int b, int kv, int z, int
 // One query again, by all lanes of a wavefront: only the keys that it sees take part, each with its own multiplication.  Where
 // a masked key or value is infinite or NaN the tiled products multiply it by a zero and their sums become NaN; the rows that
 // come out not finite are computed by this definition instead.  Rare, and slow: a few hundred cycles a key.
-template <typename T, int DP, bool PAGED>
+template <typename T, int DP, bool PAGED, int FORM>
 __device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e, int r, int from, int to, int z) {
   constexpr int E = DP / 64;
   const int lane = threadIdx.x & 63;
   const Row w = make_row<PAGED>(p, e, r);
-  const Score score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   const T* q = reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w);
   const T* k = keys_of<T, PAGED>(p, e, p.k, p.ks);
   const T* v = keys_of<T, PAGED>(p, e, p.v, p.vs);
@@ -435,7 +493,7 @@ __device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e,
 #pragma unroll
     for (int i = 0; i < E; ++i)
       if (lane * E + i < p.dim) dot = __builtin_fmaf(mine[i], to_f32(k[ko + lane * E + i]), dot);
-    const float x = score(wave_sum(dot), w.token + e.shift - j);
+    const float x = score(wave_sum(dot), (float)(w.token + e.shift - j));
     if (x == kNoMax) continue;  // (weight 0: as a masked key)
     if (!(x <= top)) {
       const float shrink = top == kNoMax ? 0.0f : exp2_fast(top - x);
@@ -475,7 +533,7 @@ __device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e,
 }
 
 // Stores a wavefront's 32 rows: the finished output, or the sums of a split.  `r0`: its first row.
-template <typename T, int DP, bool PAGED>
+template <typename T, int DP, bool PAGED, int FORM>
 __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, DP>& st, int r0, int rows, const Row& w, int from, int to, int z) {
   const int lane = threadIdx.x & 63, half = lane >> 5, r = r0 + (lane & 31);
   const float sum = sum_of_halves(st.sum);
@@ -491,6 +549,7 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
   if (p.splits > 1) {
     if (mine) {
       const Part part = part_of<DP>(p, e.b, e.kv, z, r);
+      if (sum > 0.0f)  // (the sums of nothing are not read)
 #pragma unroll
       for (int t = 0; t < State<T, DP>::DT; ++t)
 #pragma unroll
@@ -522,7 +581,7 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
   while (again) {
     const int i = __builtin_ctz(again);
     again &= again - 1;
-    if (r0 + i < rows) row_by_definition<T, DP, PAGED>(p, e, r0 + i, from, to, z);
+    if (r0 + i < rows) row_by_definition<T, DP, PAGED, FORM>(p, e, r0 + i, from, to, z);
   }
 }
 
@@ -535,14 +594,25 @@ constexpr int tile_lds_bytes() {
   return 2 * 2 * kTileKeys * DP * 2;
 }
 
-// Workgroups are dealt to the 8 XCDs in turn, each with an L2 of its own: every XCD gets a contiguous run of the work, so that
-// the row tiles of a kv head read its keys from the same L2.
-__device__ __forceinline__ int xcd_run(int w, int n) {
-  const int x = w & 7, each = n >> 3, rest = n & 7;
-  return x * each + min(x, rest) + (w >> 3);
+// Workgroups are dealt to the 8 XCDs in turn, each with an L2 of its own: the pieces of an entry (a batch entry's or sequence's kv head)
+// go to one XCD, one entry after the other, so that they read its keys from the same L2; every eighth entry, so that the heads of a
+// long sequence are spread.  What is left of the entries is cut into contiguous runs.  (Chunks of 4 prompts of 37 to 512 tokens, 8 kv
+// heads: 206 us with runs of all of them, which gave two XCDs the longest prompt.)
+struct Place {
+  int entry, piece;
+};
+__device__ __forceinline__ Place place_of(int w, int entries, int pieces) {
+  const int whole = (entries & ~7) * pieces;
+  if (w < whole) {
+    const int j = w >> 3, turn = j / pieces;
+    return Place{turn * 8 + (w & 7), j - turn * pieces};
+  }
+  const int n = (entries & 7) * pieces, v = w - whole, x = v & 7, each = n >> 3, rest = n & 7;
+  const int at = x * each + min(x, rest) + (v >> 3), turn = at / pieces;
+  return Place{(entries & ~7) + turn, at - turn * pieces};
 }
 
-template <typename T, int DP, bool PAGED, bool EXTRA>
+template <typename T, int DP, bool PAGED, int FORM>
 __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   constexpr int CPR = DP / 8, STAGE = kTileKeys * CPR * 16, NL = kTileKeys * CPR / 256, RPP = 256 / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
@@ -550,51 +620,52 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   __shared__ int bounds[4][2];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = xcd_run(blockIdx.x, gridDim.x);
-  const int z = id % p.splits;
-  id /= p.splits;
-  const int tile = p.row_tiles - 1 - id % p.row_tiles;  // (causal: the longest first)
-  id /= p.row_tiles;
-  const Entry e = make_entry<PAGED>(p, id / p.kv_heads, id % p.kv_heads);
+  const Place place = place_of(blockIdx.x, p.batch * p.kv_heads, p.row_tiles * p.splits);
+  const int z = place.piece % p.splits, tile = p.row_tiles - 1 - place.piece / p.splits;  // (causal: the longest first)
+  const Entry e = make_entry<PAGED>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
   const int rows = e.tokens * p.group, r0 = tile * 128 + wave * 32;
   if (tile * 128 >= rows) return;  // (the whole workgroup)
 
   // (rows past the last are the last again, and not stored)
   const Row w = make_row<PAGED>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
-  const bool sees = w.lo < w.hi;
-  const int wave_lo = wave_min(sees ? w.lo : 0x7fffffff), wave_hi = wave_max(w.hi);
-  const int full_lo = wave_max(w.lo), full_hi = wave_min(w.hi);
-  if (lane == 0) {
-    bounds[wave][0] = wave_lo;
-    bounds[wave][1] = wave_hi;
+  const Seen mine = seen_by<PAGED>(p, e, w, min(r0, rows - 1), min(r0 + 31, rows - 1));
+  int begin, end;  // of the workgroup
+  if (!PAGED && p.ranges) {
+    if (lane == 0) {
+      bounds[wave][0] = mine.lo;
+      bounds[wave][1] = mine.hi;
+    }
+  } else {
+    const Seen all = seen_by<PAGED>(p, e, w, tile * 128, min(tile * 128 + 127, rows - 1));
+    begin = all.lo;
+    end = all.hi;
   }
   State<T, DP> st;
   st.clear();
   load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w), half, p.dim, st.q);
-  const Score score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   const bool narrow = p.dim < DP;
   if (narrow)  // the chunks past the head's dimension, which no load fills
     for (int i = tid; i < 4 * STAGE / 16; i += 256) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
-  int begin = 0x7fffffff, end = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    begin = min(begin, bounds[i][0]);
-    end = max(end, bounds[i][1]);
+  if (!PAGED && p.ranges) {
+    begin = min(min(bounds[0][0], bounds[1][0]), min(bounds[2][0], bounds[3][0]));
+    end = max(max(bounds[0][1], bounds[1][1]), max(bounds[2][1], bounds[3][1]));
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    end = __builtin_amdgcn_readfirstlane(end);
   }
-  begin = __builtin_amdgcn_readfirstlane(begin);
-  end = __builtin_amdgcn_readfirstlane(end);
   if (begin >= end) begin = end = 0;
   // this split's share of the tiles, the first of which begins with the first key that anyone sees
-  const int all = (end - begin + kTileKeys - 1) / kTileKeys, share = (all + p.splits - 1) / p.splits;
-  const int t0 = min(all, z * share), t1 = min(all, t0 + share);
+  const int all = (end - begin + kTileKeys - 1) / kTileKeys;
+  const int t0 = min(all, z * p.share), t1 = z + 1 < p.splits ? min(all, t0 + p.share) : all;
 
   const T* kbase = keys_of<T, PAGED>(p, e, p.k, p.ks);
   const T* vbase = keys_of<T, PAGED>(p, e, p.v, p.vs);
   const int load_row = tid / CPR, load_chunk = (tid % CPR) ^ swz<CPR>(load_row);
   const bool loads = load_chunk * 8 < p.dim;
-  const unsigned lds = lds_address(smem) + wave * 1024;
+  const unsigned lds0 = lds_address(smem), lds = lds0 + wave * 1024;
+  const ReadMap<DP> map(lane);
   unsigned koff[NL], voff[NL];
   if constexpr (!PAGED) {
 #pragma unroll
@@ -647,6 +718,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
     }
   };
 
+  settle();
   if (t0 < t1) {
     look_up(t0);
     there_now = there_next;
@@ -662,74 +734,69 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
       if (t + 2 < t1) look_up(t + 2);
     }
     const int first = begin + t * kTileKeys;
-    if (first >= wave_hi || first + kTileKeys <= wave_lo) continue;
-    const unsigned char* keys = smem + (t & 1) * STAGE;
-    const unsigned char* values = keys + 2 * STAGE;
+    if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
+    const unsigned keys = lds0 + (t & 1) * STAGE, values = keys + 2 * STAGE;
     f32x16 s[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s[i] = mfma_op(row_frag<T, CPR>(keys, lane, i * 32, ks), st.q[ks], s[i]);
+      for (int ks = 0; ks < KS; ++ks) s[i] = mfma_op(row_frag<T, DP>(map, keys, i * 32, ks), st.q[ks], s[i]);
     }
-    const bool masked = first < full_lo || first + kTileKeys > full_hi || (PAGED && ~there != 0);
+    const bool masked = first < mine.full_lo || first + kTileKeys > mine.full_hi || (PAGED && ~there != 0);
     Frag pf[4];
-    softmax_tile<T, DP, EXTRA, 2>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
+    softmax_tile<T, DP, FORM, 2>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, CPR>(values, lane, c * 16, d), pf[c], st.o[d]);
+      for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
   }
-  finish<T, DP, PAGED>(p, e, st, r0, rows, w, begin + t0 * kTileKeys, min(end, begin + t1 * kTileKeys), z);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kTileKeys, min(end, begin + t1 * kTileKeys), z);
 }
 
 // ---- the kernel of few rows ---------------------------------------------------------------------------------------------------
-// At most 32 rows, over many keys: memory bound, so that what counts are the bytes in flight.  A wavefront of the 8 in a workgroup
-// streams tiles of 32 keys of its own, without meeting the others before the end: keys straight into the registers that the
-// products want, values through registers into 8 KB of LDS of its own (they are read as columns), both asked for one tile ahead:
-// 16 KB a wavefront, 128 KB a compute unit at 128 dimensions.
-constexpr int kStreamWaves = 8, kStreamKeys = 32;
+// At most 32 rows, over many keys: memory bound, so that what counts are the bytes in flight.  A wavefront streams tiles of 32 keys of
+// its own, without meeting the others before the end: whole rows through registers, asked for one tile ahead (16 KB a wavefront, 128 KB
+// a compute unit at 128 dimensions), into 16 KB of LDS of its own, where the products read them as rows and as columns.  Workgroups
+// of 4 wavefronts, so that one begins and ends beside another.
+constexpr int kStreamWaves = 4, kStreamKeys = 32;
 
-template <typename T, int DP, bool PAGED, bool EXTRA>
+template <typename T, int DP, bool PAGED, int FORM>
 __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args p) {
-  constexpr int CPR = DP / 8, NV = kStreamKeys * CPR / 64, RPP = 64 / CPR, KS = DP / 16, DT = DP / 32;
+  constexpr int CPR = DP / 8, NL = kStreamKeys * CPR / 64, RPP = 64 / CPR, KS = DP / 16, DT = DP / 32;
   constexpr int TILE = kStreamKeys * CPR * 16;
   constexpr int JOIN = 32 * (DP + 4) * 4;  // fp32 sums of 32 rows
   using Frag = typename Frag8<T>::type;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kStreamWaves * TILE > kStreamWaves / 2 * JOIN ? kStreamWaves * TILE : kStreamWaves / 2 * JOIN];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[kStreamWaves * 2 * TILE > kStreamWaves / 2 * JOIN ? kStreamWaves * 2 * TILE : kStreamWaves / 2 * JOIN];
   __shared__ float stat[kStreamWaves][32][2];
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  int id = xcd_run(blockIdx.x, gridDim.x);
-  const int z = id % p.splits;
-  id /= p.splits;
+  // (workgroups share no keys; dealt to the XCDs in turn by kv head and sequence, so that each gets its part of every sequence, the first
+  // splits of all before the second ones, which only long sequences have)
+  int id = blockIdx.x;
   const int tile = id % p.row_tiles;
   id /= p.row_tiles;
+  const int entries = p.batch * p.kv_heads, z = id / entries;
+  id -= z * entries;
   const Entry e = make_entry<PAGED>(p, id / p.kv_heads, id % p.kv_heads);
   const int rows = e.tokens * p.group, r0 = tile * 32;
   if (r0 >= rows) return;
 
   const Row w = make_row<PAGED>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
-  const bool sees = w.lo < w.hi;
-  int begin = wave_min(sees ? w.lo : 0x7fffffff);
-  const int end = wave_max(w.hi);
-  const int full_lo = wave_max(w.lo), full_hi = wave_min(w.hi);
-  if (begin >= end) begin = end;
-  State<T, DP> st;
-  st.clear();
-  load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w), half, p.dim, st.q);
-  const Score score(p, p.slopes ? p.slopes[w.head] : 0.0f);
-
-  const int all = (end - begin + kStreamKeys - 1) / kStreamKeys, share = (all + p.splits - 1) / p.splits;
-  const int t0 = min(all, z * share), t1 = min(all, t0 + share);
+  const Seen seen = seen_by<PAGED>(p, e, w, r0, min(r0 + 31, rows - 1));
+  const int end = seen.hi, begin = min(seen.lo, end);
+  const int all = (end - begin + kStreamKeys - 1) / kStreamKeys;
+  const int t0 = min(all, z * p.share), t1 = z + 1 < p.splits ? min(all, t0 + p.share) : all;
   const T* kbase = keys_of<T, PAGED>(p, e, p.k, p.ks);
   const T* vbase = keys_of<T, PAGED>(p, e, p.v, p.vs);
-  unsigned char* mine = smem + wave * TILE;
-  const int v_row = lane / CPR, v_chunk = lane % CPR;
+  unsigned char* mine = smem + wave * 2 * TILE;
+  const unsigned keys = lds_address(mine), values = keys + TILE;
+  const int load_row = lane / CPR, load_chunk = lane % CPR;
+  const bool loads = load_chunk * 8 < p.dim;
 
-  u32x4 kr[KS], vr[NV];
+  u32x4 kr[NL], vr[NL];
   long long ko_next = 0, vo_next = 0;
   bool there_next = true;
   auto look_up = [&](int t) {  // lane's key, lane % 32 of tile t
@@ -739,20 +806,20 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
     vo_next = PAGED ? ko_next : key_offset<PAGED>(p, e, p.vs, j, there);
     there_next = there;
   };
+  auto from_lane = [&](long long v, int lane_of_row) {
+    const unsigned low = __shfl((int)(unsigned)v, lane_of_row), high = __shfl((int)(unsigned)(v >> 32), lane_of_row);
+    return (long long)(((unsigned long long)high << 32) | low) + load_chunk * 8;
+  };
   auto request = [&]() {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int d = ks * 16 + half * 8;
-      kr[ks] = u32x4{0, 0, 0, 0};
-      if (d < p.dim) kr[ks] = reinterpret_cast<const Chunk16*>(kbase + ko_next + d)->v;
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int from = i * RPP + v_row;
-      const unsigned low = __shfl((int)(unsigned)vo_next, from), high = __shfl((int)(unsigned)(vo_next >> 32), from);
-      const long long off = (long long)(((unsigned long long)high << 32) | low) + v_chunk * 8;
-      vr[i] = u32x4{0, 0, 0, 0};
-      if (v_chunk * 8 < p.dim) vr[i] = reinterpret_cast<const Chunk16*>(vbase + off)->v;
+    for (int i = 0; i < NL; ++i) {
+      const long long ko = from_lane(ko_next, i * RPP + load_row);
+      const long long vo = PAGED ? ko : from_lane(vo_next, i * RPP + load_row);
+      kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+      if (loads) {
+        kr[i] = reinterpret_cast<const Chunk16*>(kbase + ko)->v;
+        vr[i] = reinterpret_cast<const Chunk16*>(vbase + vo)->v;
+      }
     }
   };
 
@@ -764,32 +831,38 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
     request();
     if (t + kStreamWaves < t1) look_up(t + kStreamWaves);
   }
+  State<T, DP> st;
+  st.clear();
+  load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w), half, p.dim, st.q);
+  const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  const ReadMap<DP> map(lane);
   for (; t < t1; t += kStreamWaves) {
     const int first = begin + t * kStreamKeys;
-    f32x16 s[1];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = mfma_op(__builtin_bit_cast(Frag, kr[ks]), st.q[ks], s[0]);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int row = i * RPP + v_row;
-      *reinterpret_cast<u32x4*>(mine + (row * CPR + (v_chunk ^ swz<CPR>(row))) * 16) = vr[i];
+    for (int i = 0; i < NL; ++i) {
+      const int row = i * RPP + load_row, to = (row * CPR + (load_chunk ^ swz<CPR>(row))) * 16;
+      *reinterpret_cast<u32x4*>(mine + to) = kr[i];
+      *reinterpret_cast<u32x4*>(mine + TILE + to) = vr[i];
     }
+    asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order: its writes, then its reads)
     const unsigned long long there = there_now & 0xffffffffull;
     if (t + kStreamWaves < t1) {
       there_now = __ballot(there_next);
       request();
       if (t + 2 * kStreamWaves < t1) look_up(t + 2 * kStreamWaves);
     }
-    const bool masked = first < full_lo || first + kStreamKeys > full_hi || (PAGED && there != 0xffffffffull);
+    f32x16 s[1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s[0] = mfma_op(row_frag<T, DP>(map, keys, 0, ks), st.q[ks], s[0]);
+    const bool masked = first < seen.full_lo || first + kStreamKeys > seen.full_hi || (PAGED && there != 0xffffffffull);
     Frag pf[2];
-    softmax_tile<T, DP, EXTRA, 1>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
-    asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order: its writes, then its reads)
+    softmax_tile<T, DP, FORM, 1>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, CPR>(mine, lane, c * 16, d), pf[c], st.o[d]);
+      for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
     asm volatile("" ::: "memory");
   }
 
@@ -843,47 +916,139 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
   st.top = top;
   st.shift = next;
   st.sum = half == 0 ? sum : 0.0f;
-  finish<T, DP, PAGED>(p, e, st, r0, rows, w, begin + t0 * kStreamKeys, min(end, begin + t1 * kStreamKeys), z);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kStreamKeys, min(end, begin + t1 * kStreamKeys), z);
 }
 
 // ---- joining the splits -----------------------------------------------------------------------------------------------------
-// One wavefront a row: the splits' sums to one maximum, in ascending order.
+// The order of additions depends on the number of splits alone.  A few splits: DP / 4 lanes a row, whose splits' sums and maxima are
+// all asked for at once.
 template <typename T, int DP, bool PAGED>
 __global__ __launch_bounds__(256) void join_kernel(const Args p) {
-  constexpr int E = DP / 64;
-  const int lane = threadIdx.x & 63, per_entry = p.seq_q * p.group;
-  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int LANES = DP / 4, ROWS = 256 / LANES, U = 4;
+  const int per_entry = p.seq_q * p.group, d = (threadIdx.x % LANES) * 4;
+  const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / LANES;
   if (row >= (long long)p.batch * p.kv_heads * per_entry) return;
   const int entry = (int)(row / per_entry), r = (int)(row - (long long)entry * per_entry);
   const Entry e = make_entry<PAGED>(p, entry / p.kv_heads, entry % p.kv_heads);
   if (r >= e.tokens * p.group) return;
+  float top = kNoMax, sum = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  for (int z0 = 0; z0 < p.splits; z0 += U) {
+    f32x4 v[U];
+    float m[U], s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const Part part = part_of<DP>(p, e.b, e.kv, min(z0 + u, p.splits - 1), r);
+      m[u] = z0 + u < p.splits ? part.stat[0] : kNoMax;
+      s[u] = part.stat[1];
+      v[u] = *reinterpret_cast<const f32x4*>(part.sums + d);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (m[u] == kNoMax) continue;  // (nothing was seen, and no sums were written)
+      const float next = m[u] > top || m[u] != m[u] ? m[u] : top;
+      const float old = top == kNoMax ? 0.0f : exp2_fast(top - next), now = exp2_fast(m[u] - next);
+      sum = sum * old + now * s[u];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] = acc[c] * old + now * v[u][c];
+      top = next;
+    }
+  }
   const Row w = make_row<PAGED>(p, e, r);
-  float top = kNoMax;
+  const bool none = top == kNoMax;
+  if (d < p.dim) {
+    T four[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : acc[c] / sum);
+    __builtin_memcpy(reinterpret_cast<Chunk8*>(reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w) + d), four, 8);
+  }
+  if (d == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (top + __builtin_log2f(sum)) * kLn2;
+}
+// Many: a workgroup a row, four splits of it in flight in each half or quarter of a wavefront.
+template <typename T, int DP, bool PAGED>
+__global__ __launch_bounds__(256) void join_many_kernel(const Args p) {
+  constexpr int WAVES = 4;
+  constexpr int LANES = DP / 4, GROUPS = 64 / LANES, ROWS = 1;
+  __shared__ __attribute__((aligned(16))) float meet[4][DP + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_entry = p.seq_q * p.group;
+  const long long row = (long long)blockIdx.x * ROWS + wave / WAVES;
+  const int part_of_row = wave % WAVES;
+  const bool exists = row < (long long)p.batch * p.kv_heads * per_entry;
+  const int entry = exists ? (int)(row / per_entry) : 0, r = exists ? (int)(row - (long long)entry * per_entry) : 0;
+  const Entry e = make_entry<PAGED>(p, entry / p.kv_heads, entry % p.kv_heads);
+  const bool mine = exists && r < e.tokens * p.group;
+  const int d = (lane % LANES) * 4, group = lane / LANES;
+  float top = kNoMax, sum = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
   bool nan = false;
-  for (int z = 0; z < p.splits; ++z) {
-    const float m = part_of<DP>(p, e.b, e.kv, z, r).stat[0];
-    nan |= m != m;
-    top = fmaxf(top, m);
-  }
-  const float next = top == kNoMax ? 0.0f : top;
-  float sum = 0.0f, acc[E];
+  if (mine) {
+    // (the maximum over all splits, by every wavefront of the row)
+    for (int z = lane; z < p.splits; z += 64) {
+      const float m = part_of<DP>(p, e.b, e.kv, z, r).stat[0];
+      nan |= m != m;
+      top = fmaxf(top, m);
+    }
 #pragma unroll
-  for (int i = 0; i < E; ++i) acc[i] = 0.0f;
-  for (int z = 0; z < p.splits; ++z) {
-    const Part part = part_of<DP>(p, e.b, e.kv, z, r);
-    const float m = part.stat[0];
-    if (m == kNoMax) continue;
-    const float weight = exp2_fast(m - next);
-    sum += weight * part.stat[1];
+    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+    nan = __any(nan);
+    const float next = top == kNoMax ? 0.0f : top;
+    for (int z0 = part_of_row * 64; z0 < p.splits; z0 += WAVES * 64) {
+      float weight = 0.0f;
+      if (z0 + lane < p.splits) {
+        const Part part = part_of<DP>(p, e.b, e.kv, z0 + lane, r);
+        if (part.stat[0] != kNoMax) {
+          weight = exp2_fast(part.stat[0] - next);
+          sum += weight * part.stat[1];
+        }
+      }
+      const int count = min(64, p.splits - z0);
+      for (int i = 0; i < count; i += 4 * GROUPS) {
+        f32x4 v[4];
+        float w[4];
 #pragma unroll
-    for (int i = 0; i < E; ++i) acc[i] += weight * part.sums[lane * E + i];
+        for (int u = 0; u < 4; ++u) {
+          const int z = i + u * GROUPS + group;
+          w[u] = __shfl(weight, z & 63);
+          v[u] = f32x4{0, 0, 0, 0};
+          if (z >= count) w[u] = 0.0f;
+          if (w[u] != 0.0f) v[u] = *reinterpret_cast<const f32x4*>(part_of<DP>(p, e.b, e.kv, z0 + z, r).sums + d);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(w[u], v[u][c], acc[c]);
+      }
+    }
+    sum = wave_sum(sum);
+#pragma unroll
+    for (int m = 32; m >= LANES; m >>= 1)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) acc[c] += __shfl_xor(acc[c], m);
   }
+  {
+    if (group == 0) *reinterpret_cast<f32x4*>(&meet[wave][d]) = acc;
+    if (lane == 0) meet[wave][DP] = sum;
+    __syncthreads();
+    if (part_of_row != 0) return;
+    acc = f32x4{0, 0, 0, 0};
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      acc += *reinterpret_cast<const f32x4*>(&meet[wave + i][d]);
+      sum += meet[wave + i][DP];
+    }
+  }
+  if (!mine) return;
   if (nan) sum = __builtin_nanf("");
-  T* out = reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w);
+  const Row w = make_row<PAGED>(p, e, r);
   const bool none = top == kNoMax && !nan;
+  const float next = top == kNoMax ? 0.0f : top;
+  if (group == 0 && d < p.dim) {
+    T four[4];
 #pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (lane * E + i < p.dim) out[lane * E + i] = from_f32<T>(none ? 0.0f : acc[i] / sum);
+    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : acc[c] / sum);
+    __builtin_memcpy(reinterpret_cast<Chunk8*>(reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w) + d), four, 8);
+  }
   if (lane == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (next + __builtin_log2f(sum)) * kLn2;
 }
 

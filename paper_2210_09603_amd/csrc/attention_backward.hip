@@ -19,6 +19,8 @@ using namespace hidet::attn;
 
 namespace {
 
+constexpr float kLift = 1024.0f, kLiftBits = 10.0f;
+
 struct BackArgs {
   Args f;  // f.lse: of the forward pass; f.out: its output
   const void* dout;
@@ -26,24 +28,38 @@ struct BackArgs {
   void* dk;
   void* dv;
   Strides dos, dqs, dks, dvs;
-  float* delta;   // [batch][heads][seq_q]
+  float* info;    // of every row of a kv head, see row_info
   int4* seen;     // [batch][row_groups]: of 32 rows, the first and last + 1 of the keys that any of them sees; that all of them see
+  float* part;    // partial sums of the splits: dQ's [split][kv row][DP], then dK's and dV's [split][entry][key][2][DP]
   int row_groups;
   int key_tiles;
+  int dq_splits, dq_share;    // share: tiles of keys of a split
+  int dkv_splits, dkv_share;  // share: tiles of rows
+  int regular;    // 32 rows hold whole tokens, and offsets within them fit 32 bits
 };
 
-constexpr float kLift = 1024.0f, kLiftBits = 10.0f;
+// What the second kernel needs to know of a row, as the first leaves it: for 4 rows each in turn, so that a lane reads those of its 4
+// rows at once, and padded to whole tiles by rows that nobody is seen by.
+//   0  lse to base 2, less the lift     1  D, divided by the lift     2, 3  first key seen, their number
+//   4  position, 5  slope to base 2 (with a bias only: 8 fields, else 4)
+template <int FORM>
+__device__ __forceinline__ float* row_info(const BackArgs& b, const Entry& e, int r, int field) {
+  constexpr int FIELDS = FORM & FORM_BIAS ? 8 : 4;
+  const long long rows = (long long)b.f.row_tiles * 128, entry = (long long)e.b * b.f.kv_heads + e.kv;
+  return b.info + (entry * rows + (r & ~3)) * FIELDS + field * 4 + (r & 3);
+}
+
 
 __device__ __forceinline__ float lse_to_base_2(float lse) { return lse == kNoMax ? __builtin_huge_valf() : lse * kLog2e; }
 
 // Rows that come out not finite, again: only what a query sees takes part (see the forward pass).
-template <typename T, int DP>
+template <typename T, int DP, int FORM>
 __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry& e, int r, float delta) {
   constexpr int E = DP / 64;
   const Args& p = b.f;
   const int lane = threadIdx.x & 63;
   const Row w = make_row<false>(p, e, r);
-  const Score score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   const T* q = reinterpret_cast<const T*>(p.q) + query_offset<false>(p, e, p.qs, w);
   const T* g = reinterpret_cast<const T*>(b.dout) + query_offset<false>(p, e, b.dos, w);
   const T* k = keys_of<T, false>(p, e, p.k, p.ks);
@@ -69,13 +85,10 @@ __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry&
     }
     dot = wave_sum(dot);
     dp = wave_sum(dp);
-    const float prob = exp2_fast(score(dot, w.token + e.shift - j) - lse);
+    float derivative;
+    const float prob = exp2_fast(score(dot, (float)(w.token + e.shift - j), derivative) - lse);
     if (prob == 0.0f) continue;
-    float ds = prob * (dp - delta);
-    if (p.softcap > 0) {
-      const float t = score.tanh_of(dot);
-      ds *= 1.0f - t * t;
-    }
+    const float ds = prob * (dp - delta) * derivative;
     bool finite = false;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -90,25 +103,25 @@ __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry&
     if (lane * E + i < p.dim) to[lane * E + i] = from_f32<T>(acc[i] * p.scale);
 }
 
-template <typename T, int DP>
-__device__ __forceinline__ void dkv_by_definition(const BackArgs& b, const Entry& e, int j) {
+template <typename T, int DP, int FORM>
+__device__ __forceinline__ void dkv_by_definition(const BackArgs& b, const Entry& e, int j, bool for_dv) {
   constexpr int E = DP / 64;
   const Args& p = b.f;
   const int lane = threadIdx.x & 63;
   const T* k = keys_of<T, false>(p, e, p.k, p.ks) + (long long)j * p.ks.row;
   const T* v = keys_of<T, false>(p, e, p.v, p.vs) + (long long)j * p.vs.row;
-  float mk[E], mv[E], dk[E], dv[E];
+  float mk[E], mv[E], acc[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const int d = lane * E + i;
     mk[i] = d < p.dim ? to_f32(k[d]) : 0.0f;
     mv[i] = d < p.dim ? to_f32(v[d]) : 0.0f;
-    dk[i] = dv[i] = 0.0f;
+    acc[i] = 0.0f;
   }
   for (int r = 0; r < e.tokens * p.group; ++r) {
     const Row w = make_row<false>(p, e, r);
     if (j < w.lo || j >= w.hi) continue;
-    const Score score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+    const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
     const T* q = reinterpret_cast<const T*>(p.q) + query_offset<false>(p, e, p.qs, w);
     const T* g = reinterpret_cast<const T*>(b.dout) + query_offset<false>(p, e, b.dos, w);
     float dot = 0.0f, dp = 0.0f, mq[E], mg[E];
@@ -123,30 +136,23 @@ __device__ __forceinline__ void dkv_by_definition(const BackArgs& b, const Entry
     dot = wave_sum(dot);
     dp = wave_sum(dp);
     const long long at = lse_offset<false>(p, e, w);
-    const float prob = exp2_fast(score(dot, w.token + e.shift - j) - lse_to_base_2(p.lse[at]));
+    float derivative;
+    const float prob = exp2_fast(score(dot, (float)(w.token + e.shift - j), derivative) - lse_to_base_2(p.lse[at]));
     if (prob == 0.0f) continue;
-    float ds = prob * (dp - b.delta[at]);
-    if (p.softcap > 0) {
-      const float t = score.tanh_of(dot);
-      ds *= 1.0f - t * t;
-    }
+    const float ds = prob * (dp - kLift * *row_info<FORM>(b, e, r, 1)) * derivative;
     bool finite = false;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      dk[i] += ds * mq[i];
-      dv[i] += prob * mg[i];
-      finite |= dk[i] == dk[i] || dv[i] == dv[i];
+      acc[i] += for_dv ? prob * mg[i] : ds * mq[i];
+      finite |= acc[i] == acc[i];
     }
     if (!__any(finite)) break;
   }
-  T* to_k = reinterpret_cast<T*>(b.dk) + (long long)e.b * b.dks.batch + (long long)e.kv * b.dks.head + (long long)j * b.dks.row;
-  T* to_v = reinterpret_cast<T*>(b.dv) + (long long)e.b * b.dvs.batch + (long long)e.kv * b.dvs.head + (long long)j * b.dvs.row;
+  const Strides& s = for_dv ? b.dvs : b.dks;
+  T* to = reinterpret_cast<T*>(for_dv ? b.dv : b.dk) + (long long)e.b * s.batch + (long long)e.kv * s.head + (long long)j * s.row;
 #pragma unroll
   for (int i = 0; i < E; ++i)
-    if (lane * E + i < p.dim) {
-      to_k[lane * E + i] = from_f32<T>(dk[i] * p.scale);
-      to_v[lane * E + i] = from_f32<T>(dv[i]);
-    }
+    if (lane * E + i < p.dim) to[lane * E + i] = from_f32<T>(for_dv ? acc[i] : acc[i] * p.scale);
 }
 
 // A transposed accumulator (lane = vector, registers = its dimensions) to the vector's memory, times `by`.
@@ -173,9 +179,27 @@ __device__ __forceinline__ bool all_finite(const f32x16 (&acc)[DT]) {
   return finite;
 }
 
+template <int DT>
+__device__ __forceinline__ void store_part(float* to, const f32x16 (&acc)[DT], int half) {
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<f32x4*>(to + 32 * t + 8 * g + 4 * half) = f32x4{acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]};
+}
+template <int DP>
+__device__ __forceinline__ float* dq_part(const BackArgs& b, int z, const Entry& e, int r) {
+  const long long per_entry = (long long)b.f.seq_q * b.f.group;
+  return b.part + (((long long)z * b.f.batch * b.f.kv_heads + (long long)e.b * b.f.kv_heads + e.kv) * per_entry + r) * DP;
+}
+template <int DP>
+__device__ __forceinline__ float* dkv_part(const BackArgs& b, int z, const Entry& e, int key) {
+  return b.part + (((long long)z * b.f.batch * b.f.kv_heads + (long long)e.b * b.f.kv_heads + e.kv) * b.f.seq_k + key) * (2 * DP);
+}
+
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
 // The forward kernel's walk, with dout and out beside q.
-template <typename T, int DP, bool EXTRA>
+template <typename T, int DP, int FORM>
 __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   constexpr int CPR = DP / 8, STAGE = kTileKeys * CPR * 16, NL = kTileKeys * CPR / 256, RPP = 256 / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
@@ -184,22 +208,26 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-  int id = xcd_run(blockIdx.x, gridDim.x);
-  const int tile = p.row_tiles - 1 - id % p.row_tiles;
-  id /= p.row_tiles;
-  const Entry e = make_entry<false>(p, id / p.kv_heads, id % p.kv_heads);
+  const Place place = place_of(blockIdx.x, p.batch * p.kv_heads, p.row_tiles * b.dq_splits);
+  const int z = place.piece % b.dq_splits, tile = p.row_tiles - 1 - place.piece / b.dq_splits;
+  const Entry e = make_entry<false>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
   const int rows = e.tokens * p.group, r0 = tile * 128 + wave * 32;
 
   const Row w = make_row<false>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
-  const bool sees = w.lo < w.hi;
-  const int wave_lo = wave_min(sees ? w.lo : 0x7fffffff), wave_hi = wave_max(w.hi);
-  const int full_lo = wave_max(w.lo), full_hi = wave_min(w.hi);
-  if (lane == 0) {
-    bounds[wave][0] = wave_lo;
-    bounds[wave][1] = wave_hi;
-    if (e.kv == 0 && r0 < rows) b.seen[(long long)e.b * b.row_groups + (r0 >> 5)] = int4{wave_lo, wave_hi, full_lo, full_hi};
+  const Seen mine = seen_by<false>(p, e, w, min(r0, rows - 1), min(r0 + 31, rows - 1));
+  int begin, end;  // of the workgroup
+  if (p.ranges) {
+    if (lane == 0) {
+      bounds[wave][0] = mine.lo;
+      bounds[wave][1] = mine.hi;
+    }
+  } else {
+    const Seen all = seen_by<false>(p, e, w, tile * 128, min(tile * 128 + 127, rows - 1));
+    begin = all.lo;
+    end = all.hi;
   }
+  if (lane == 0 && e.kv == 0 && z == 0 && r0 < rows) b.seen[(long long)e.b * b.row_groups + (r0 >> 5)] = int4{mine.lo, mine.hi, mine.full_lo, mine.full_hi};
   Frag q[KS], g[KS];
   load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<false>(p, e, p.qs, w), half, p.dim, q);
   load_row_frags<T, DP>(reinterpret_cast<const T*>(b.dout) + query_offset<false>(p, e, b.dos, w), half, p.dim, g);
@@ -215,27 +243,38 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   delta = sum_of_halves(delta);
   const long long stat = lse_offset<false>(p, e, w);
   const float lse = lse_to_base_2(p.lse[stat]);
-  if (half == 0 && r0 + lane < rows) b.delta[stat] = delta;
-  const Score score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  if (half == 0 && z == 0) {
+    const int r = r0 + lane;
+    const bool is = r < rows;
+    *row_info<FORM>(b, e, r, 0) = (is ? lse : __builtin_huge_valf()) - kLiftBits;
+    *row_info<FORM>(b, e, r, 1) = is ? delta * (1.0f / kLift) : 0.0f;
+    *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 2)) = w.lo;
+    *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 3)) = is ? w.hi - w.lo : 0;
+    if constexpr (FORM & FORM_BIAS) {
+      *row_info<FORM>(b, e, r, 4) = (float)at;
+      *row_info<FORM>(b, e, r, 5) = p.slopes ? p.slopes[w.head] * kLog2e : 0.0f;
+    }
+  }
+  const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   if (p.dim < DP)
     for (int i = tid; i < 4 * STAGE / 16; i += 256) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
-  int begin = 0x7fffffff, end = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    begin = min(begin, bounds[i][0]);
-    end = max(end, bounds[i][1]);
+  if (p.ranges) {
+    begin = min(min(bounds[0][0], bounds[1][0]), min(bounds[2][0], bounds[3][0]));
+    end = max(max(bounds[0][1], bounds[1][1]), max(bounds[2][1], bounds[3][1]));
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    end = __builtin_amdgcn_readfirstlane(end);
   }
-  begin = __builtin_amdgcn_readfirstlane(begin);
-  end = __builtin_amdgcn_readfirstlane(end);
   if (begin >= end) begin = end = 0;
-  const int tiles = (end - begin + kTileKeys - 1) / kTileKeys;
+  const int all = (end - begin + kTileKeys - 1) / kTileKeys;
+  const int t0 = min(all, z * b.dq_share), t1 = z + 1 < b.dq_splits ? min(all, t0 + b.dq_share) : all;
 
   const T* kbase = keys_of<T, false>(p, e, p.k, p.ks);
   const T* vbase = keys_of<T, false>(p, e, p.v, p.vs);
   const int load_row = tid / CPR, load_chunk = (tid % CPR) ^ swz<CPR>(load_row);
   const bool loads = load_chunk * 8 < p.dim;
-  const unsigned lds = lds_address(smem) + wave * 1024;
+  const unsigned lds0 = lds_address(smem), lds = lds0 + wave * 1024;
+  const ReadMap<DP> map(lane);
   auto request = [&](int t) {
     const unsigned to = lds + (t & 1) * STAGE;
     const int first = begin + t * kTileKeys, last = end - 1 - first;
@@ -257,43 +296,48 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
-  if (tiles > 0) request(0);
-  for (int t = 0; t < tiles; ++t) {
+  settle();
+  if (t0 < t1) request(t0);
+  for (int t = t0; t < t1; ++t) {
     wait_all_and_meet();
-    if (t + 1 < tiles) request(t + 1);
+    if (t + 1 < t1) request(t + 1);
     const int first = begin + t * kTileKeys;
-    if (first >= wave_hi || first + kTileKeys <= wave_lo) continue;
-    const unsigned char* keys = smem + (t & 1) * STAGE;
-    const unsigned char* values = keys + 2 * STAGE;
-    const bool masked = first < full_lo || first + kTileKeys > full_hi;
+    if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
+    const unsigned keys = lds0 + (t & 1) * STAGE, values = keys + 2 * STAGE;
+    const bool masked = first < mine.full_lo || first + kTileKeys > mine.full_hi;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       f32x16 s, dp;
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, CPR>(keys, lane, c * 32, ks), q[ks], s);
+      for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, keys, c * 32, ks), q[ks], s);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, CPR>(values, lane, c * 32, ks), g[ks], dp);
+      for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, values, c * 32, ks), g[ks], dp);
       const int base = first + c * 32 + 4 * half;
+      const float distance = (float)(at - base);
       Frag ds[2];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = base + 8 * (r >> 2) + (r & 3);
-        float x = EXTRA ? score(s[r], at - j) - lse : __builtin_fmaf(s[r], score.factor, -lse);
-        float d = exp2_fast(x) * (dp[r] - delta);
-        if (EXTRA && score.cap > 0) {
-          const float th = score.tanh_of(s[r]);
-          d *= 1.0f - th * th;
-        }
+        float derivative = 1.0f, x;
+        if constexpr (FORM == FORM_PLAIN)
+          x = __builtin_fmaf(s[r], score.factor, -lse);
+        else
+          x = score(s[r], distance - (float)(8 * (r >> 2) + (r & 3)), derivative) - lse;
+        float d = exp2_fast(x) * (dp[r] - delta) * derivative;
         if (masked) d = (unsigned)(j - w.lo) < (unsigned)(w.hi - w.lo) ? d : 0.0f;
         ds[r >> 3][r & 7] = from_f32<T>(d);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, CPR>(keys, lane, c * 32 + h * 16, d), ds[h], acc[d]);
+        for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, DP>(map, keys, c * 32 + h * 16, d), ds[h], acc[d]);
     }
+  }
+  if (b.dq_splits > 1) {
+    if (r0 + (lane & 31) < rows) store_part<DT>(dq_part<DP>(b, z, e, r0 + (lane & 31)), acc, half);
+    return;
   }
   const unsigned long long odd = __ballot(!all_finite(acc));
   unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
@@ -304,40 +348,81 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
     const int i = __builtin_ctz(again);
     again &= again - 1;
     const float its = __shfl(delta, i);
-    if (r0 + i < rows) dq_by_definition<T, DP>(b, e, r0 + i, its);
+    if (r0 + i < rows) dq_by_definition<T, DP, FORM>(b, e, r0 + i, its);
   }
 }
 
-// ---- dK, dV -------------------------------------------------------------------------------------------------------------
-// A workgroup of 4 wavefronts keeps 128 keys and values, 32 a wavefront, in registers with their two sums (192 registers at 128
-// dimensions) and walks over the rows that see one of them in tiles of 64 rows of q and dout, one tile ahead of it in LDS.
-constexpr int kTileRows = 64;
+// The splits of a query's sum, in ascending order; one wavefront a query.
+template <typename T, int DP, int FORM>
+__global__ __launch_bounds__(256) void dq_join_kernel(const BackArgs b) {
+  constexpr int E = DP / 64;
+  const Args& p = b.f;
+  const int lane = threadIdx.x & 63, per_entry = p.seq_q * p.group;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= (long long)p.batch * p.kv_heads * per_entry) return;
+  const int entry = (int)(row / per_entry), r = (int)(row - (long long)entry * per_entry);
+  const Entry e = make_entry<false>(p, entry / p.kv_heads, entry % p.kv_heads);
+  float acc[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) acc[i] = 0.0f;
+#pragma unroll 4
+  for (int z = 0; z < b.dq_splits; ++z) {
+    const float* from = dq_part<DP>(b, z, e, r) + lane * E;
+#pragma unroll
+    for (int i = 0; i < E; ++i) acc[i] += from[i];
+  }
+  bool finite = true;
+#pragma unroll
+  for (int i = 0; i < E; ++i) finite &= __builtin_fabsf(acc[i]) < __builtin_huge_valf();
+  const Row w = make_row<false>(p, e, r);
+  if (!__all(finite)) {
+    dq_by_definition<T, DP, FORM>(b, e, r, kLift * *row_info<FORM>(b, e, r, 1));
+    return;
+  }
+  T* to = reinterpret_cast<T*>(b.dq) + query_offset<false>(p, e, b.dqs, w);
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (lane * E + i < p.dim) to[lane * E + i] = from_f32<T>(acc[i] * p.scale);
+}
 
-template <typename T, int DP, bool EXTRA>
-__global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void dkv_kernel(const BackArgs b) {
-  constexpr int CPR = DP / 8, STAGE = kTileRows * CPR * 16, NL = kTileRows * CPR / 256, RPP = 256 / CPR, KS = DP / 16, DT = DP / 32;
+// ---- dK, dV -------------------------------------------------------------------------------------------------------------
+// A workgroup of 8 wavefronts works on 64 keys and walks over the rows that see one of them in tiles of 128 rows of q and dout,
+// which arrive in LDS one tile ahead.  4 wavefronts share 32 keys and meet in LDS at the end.  Up to 64 dimensions each of them takes
+// 32 of the tile's rows and sums dK and dV.  Beyond, two sum dK and two dV, each of 64 rows: the scores are computed for either sum
+// (5 products for 4), which halves what a wavefront keeps -- a sum, its keys and values, 128 registers at 128 dimensions -- so that two
+// wavefronts fit a SIMD, one of each kind.
+// Microseconds for 2 x 4096 positions of 16 heads on 4, 128 dimensions, no mask: 800; both sums in a wavefront, one a SIMD, waiting for
+// LDS half of the time, 1237; the same with the values in LDS, two a SIMD and 44 registers spilled, 1200.  For 3 x 1021 positions of 12
+// heads, 64 dimensions: both sums in a wavefront 48, apart 53.
+constexpr int kTileRows = 128, kBlockKeys = 64, kDkvThreads = 512;
+
+template <typename T, int DP, int FORM>
+__global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
+  constexpr int CPR = DP / 8, STAGE = kTileRows * CPR * 16, NL = kTileRows * CPR / kDkvThreads, RPP = kDkvThreads / CPR, KS = DP / 16, DT = DP / 32;
+  constexpr bool BOTH = DP == 64;
+  constexpr int GROUPS = BOTH ? 1 : 2, SUMS = BOTH ? 2 : 1;
+  constexpr int FIELDS = FORM & FORM_BIAS ? 8 : 4, INFO = kTileRows * FIELDS * 4;  // bytes of a tile's row_info
   using Frag = typename Frag8<T>::type;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[4 * STAGE];  // q of two stages, dout of two
-  __shared__ __attribute__((aligned(16))) float row_lse[2][kTileRows], row_delta[2][kTileRows], row_slope[2][kTileRows];
-  __shared__ __attribute__((aligned(16))) int row_lo[2][kTileRows], row_count[2][kTileRows], row_at[2][kTileRows];
-  __shared__ int4 tile_seen[2][2];
-  __shared__ int bounds[4][2];
+  __shared__ __attribute__((aligned(256))) unsigned char smem[4 * STAGE];  // q of two stages, dout of two
+  __shared__ __attribute__((aligned(16))) unsigned char info[2 * INFO];
+  __shared__ int bounds[8][2];
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool for_dv = !BOTH && wave >= 4;
+  const int part = BOTH ? wave >> 1 : ((wave >> 1) & 1) * 2;  // the first of its GROUPS groups of 32 rows
 
-  int id = xcd_run(blockIdx.x, gridDim.x);
-  const int tile = id % b.key_tiles;  // (causal: the longest first)
-  id /= b.key_tiles;
-  const Entry e = make_entry<false>(p, id / p.kv_heads, id % p.kv_heads);
+  const Place place = place_of(blockIdx.x, p.batch * p.kv_heads, b.key_tiles * b.dkv_splits);
+  const int z = place.piece % b.dkv_splits, tile = place.piece / b.dkv_splits;  // (causal: the longest first)
+  const Entry e = make_entry<false>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
   const int rows = e.tokens * p.group;
-  const int block_key = tile * 128, key0 = block_key + wave * 32, key = key0 + (lane & 31);
-  const int block_end = min(block_key + 128, e.keys);
+  const int block_key = tile * kBlockKeys, key0 = block_key + (wave & 1) * 32, key = key0 + (lane & 31);
+  const int block_end = min(block_key + kBlockKeys, e.keys);
 
   // the first and last groups of 32 rows that see a key of the block
   const int groups = (rows + 31) >> 5;
   const int4* seen = b.seen + (long long)e.b * b.row_groups;
   int from = 0x7fffffff, to = 0;
-  for (int i = tid; i < groups; i += 256)
+  for (int i = tid; i < groups; i += kDkvThreads)
     if (seen[i].x < block_end && seen[i].y > block_key) {
       from = min(from, i);
       to = i + 1;
@@ -353,192 +438,311 @@ __global__ __launch_bounds__(256, DP == 64 ? 2 : 1) void dkv_kernel(const BackAr
   load_row_frags<T, DP>(keys_of<T, false>(p, e, p.k, p.ks) + (long long)mine * p.ks.row, half, p.dim, kf);
   load_row_frags<T, DP>(keys_of<T, false>(p, e, p.v, p.vs) + (long long)mine * p.vs.row, half, p.dim, vf);
   if (p.dim < DP)
-    for (int i = tid; i < 4 * STAGE / 16; i += 256) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
+    for (int i = tid; i < 4 * STAGE / 16; i += kDkvThreads) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 8; ++i) {
     from = min(from, bounds[i][0]);
     to = max(to, bounds[i][1]);
   }
   from = __builtin_amdgcn_readfirstlane(from);
   to = __builtin_amdgcn_readfirstlane(to);
-  const int t0 = from < to ? from >> 1 : 0, t1 = from < to ? (to + 1) >> 1 : 0;  // tiles of 64 rows
+  const int first_tile = from < to ? from >> 2 : 0, last_tile = from < to ? (to + 3) >> 2 : 0;
+  const int t0 = min(last_tile, first_tile + z * b.dkv_share), t1 = z + 1 < b.dkv_splits ? min(last_tile, t0 + b.dkv_share) : last_tile;
 
   const int load_row = tid / CPR, load_chunk = (tid % CPR) ^ swz<CPR>(load_row);
   const bool loads = load_chunk * 8 < p.dim;
-  const unsigned lds = lds_address(smem) + wave * 1024;
+  const unsigned lds0 = lds_address(smem), lds = lds0 + wave * 1024, info0 = lds_address(info);
+  const ReadMap<DP> map(lane);
+  const T* qbase = reinterpret_cast<const T*>(p.q) + (long long)e.b * p.qs.batch + (long long)e.kv * p.group * p.qs.head;
+  const T* gbase = reinterpret_cast<const T*>(b.dout) + (long long)e.b * b.dos.batch + (long long)e.kv * p.group * b.dos.head;
+  // regular: RPP rows lie alike everywhere
+  const int load_token = p.d_group.div(load_row), load_head = load_row - load_token * p.group, step_tokens = p.d_group.div(RPP);
+  const unsigned qoff = ((unsigned)load_token * (unsigned)p.qs.row + (unsigned)load_head * (unsigned)p.qs.head + load_chunk * 8) * 2;
+  const unsigned goff = ((unsigned)load_token * (unsigned)b.dos.row + (unsigned)load_head * (unsigned)b.dos.head + load_chunk * 8) * 2;
+  const float* rinfo = row_info<FORM>(b, e, 0, 0);
   auto request = [&](int t) {
     const unsigned dst = lds + (t & 1) * STAGE;
+    if (wave * 1024 < INFO) DirectLoad::at(rinfo + (long long)t * (INFO / 4), tid * 16, info0 + (t & 1) * INFO + wave * 1024);
+    if (b.regular && (t + 1) * kTileRows <= rows) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (loads) {
+          const long long token = (long long)(t * NL + i) * step_tokens;
+          DirectLoad::at(qbase + token * p.qs.row, qoff, dst + i * (kDkvThreads * 16));
+          DirectLoad::at(gbase + token * b.dos.row, goff, dst + 2 * STAGE + i * (kDkvThreads * 16));
+        }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int r = min(t * kTileRows + i * RPP + load_row, rows - 1);  // (rows past the last: the last again, seen by nobody)
-      const int token = p.d_group.div(r), head = e.kv * p.group + (r - token * p.group);
-      const T* qr = reinterpret_cast<const T*>(p.q) + (long long)e.b * p.qs.batch + (long long)head * p.qs.head + (long long)token * p.qs.row;
-      const T* gr = reinterpret_cast<const T*>(b.dout) + (long long)e.b * b.dos.batch + (long long)head * b.dos.head + (long long)token * b.dos.row;
+      const int token = p.d_group.div(r), head = r - token * p.group;
+      const T* qr = qbase + (long long)head * p.qs.head + (long long)token * p.qs.row;
+      const T* gr = gbase + (long long)head * b.dos.head + (long long)token * b.dos.row;
       if (loads) {
-        DirectLoad::at(qr + load_chunk * 8, dst + i * 4096);
-        DirectLoad::at(gr + load_chunk * 8, dst + 2 * STAGE + i * 4096);
+        DirectLoad::at(qr + load_chunk * 8, dst + i * (kDkvThreads * 16));
+        DirectLoad::at(gr + load_chunk * 8, dst + 2 * STAGE + i * (kDkvThreads * 16));
       }
-    }
-  };
-  // what thread i < 64 knows of row i of a tile
-  float next_lse = 0, next_delta = 0, next_slope = 0;
-  int next_lo = 0, next_count = 0, next_at = 0;
-  int4 next_seen = {0, 0, 0, 0};
-  auto look_up = [&](int t) {
-    if (tid < kTileRows) {
-      const int r = t * kTileRows + tid;
-      const Row w = make_row<false>(p, e, min(r, rows - 1));
-      const long long stat = lse_offset<false>(p, e, w);
-      next_lse = lse_to_base_2(p.lse[stat]);
-      next_delta = b.delta[stat];
-      next_lo = w.lo;
-      next_count = r < rows ? w.hi - w.lo : 0;
-      next_at = w.token + e.shift;
-      if (EXTRA) next_slope = p.slopes ? p.slopes[w.head] * kLog2e : 0.0f;
-      if (tid < 2) {
-        const int i = 2 * t + tid;
-        next_seen = seen[min(i, groups - 1)];
-        if (i >= groups || (i + 1) * 32 > rows) next_seen.z = 0x7fffffff;  // (rows past the last: never seen by all)
-        if (i >= groups) next_seen.y = 0;
-      }
-    }
-  };
-  auto put = [&](int t) {
-    const int s = t & 1;
-    if (tid < kTileRows) {
-      row_lse[s][tid] = next_lse - kLiftBits;
-      row_delta[s][tid] = next_delta * (1.0f / kLift);
-      row_lo[s][tid] = next_lo;
-      row_count[s][tid] = next_count;
-      row_at[s][tid] = next_at;
-      if (EXTRA) row_slope[s][tid] = next_slope;
-      if (tid < 2) tile_seen[s][tid] = next_seen;
     }
   };
 
-  f32x16 dk[DT], dv[DT];
+  f32x16 acc[SUMS][DT];  // dK, dV or both, transposed: lane = key
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
+  for (int i = 0; i < SUMS; ++i)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dk[d][r] = dv[d][r] = 0.0f;
-  Score score(p, 0.0f);
-  if (t0 < t1) {
-    request(t0);
-    look_up(t0);
-    put(t0);
-  }
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
+  const Score<FORM> all_scores(p, 0.0f);
+  const float at_key = (float)key;
+  settle();
+  if (t0 < t1) request(t0);
   for (int t = t0; t < t1; ++t) {
+    // (which groups of 32 rows take part: asked for before the wait)
+    const int4 seen0 = seen[min(4 * t + part, groups - 1)], seen1 = seen[min(4 * t + part + GROUPS - 1, groups - 1)];
     wait_all_and_meet();
-    if (t + 1 < t1) {
-      request(t + 1);
-      look_up(t + 1);
-    }
-    const unsigned char* qs = smem + (t & 1) * STAGE;
-    const unsigned char* gs = qs + 2 * STAGE;
-    const int st = t & 1;
+    if (t + 1 < t1) request(t + 1);
+    const unsigned qs = lds0 + (t & 1) * STAGE, gs = qs + 2 * STAGE;
+    const float* of_rows = reinterpret_cast<const float*>(info + (t & 1) * INFO);
+#pragma unroll 1
+    for (int c = 0; c < GROUPS; ++c) {
+      const int row = (part + c) * 32, behind = t * kTileRows + row + 32;
+      if ((c ? seen1.x : seen0.x) >= key0 + 32 || (c ? seen1.y : seen0.y) <= key0 || behind - 32 >= rows) continue;
+      const bool masked = (c ? seen1.z : seen0.z) > key0 || (c ? seen1.w : seen0.w) < key0 + 32 || behind > rows;
+      f32x16 s;
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const int4 group = tile_seen[st][c];
-      if (__builtin_amdgcn_readfirstlane(group.x) >= key0 + 32 || __builtin_amdgcn_readfirstlane(group.y) <= key0) continue;
-      const bool masked = __builtin_amdgcn_readfirstlane(group.z) > key0 || __builtin_amdgcn_readfirstlane(group.w) < key0 + 32;
-      f32x16 s, dp;
+      for (int r = 0; r < 16; ++r) s[r] = 0.0f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+      for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, qs, row, ks), kf[ks], s);
+      f32x16 dp;
+      if (!for_dv) {
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, CPR>(qs, lane, c * 32, ks), kf[ks], s);
+        for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, CPR>(gs, lane, c * 32, ks), vf[ks], dp);
-      Frag pf[2], ds[2];
+        for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, gs, row, ks), vf[ks], dp);
+      }
+      Score<FORM> score = all_scores;
+      float derivative[16];
 #pragma unroll
-      for (int gq = 0; gq < 4; ++gq) {
-        const int i = c * 32 + 8 * gq + 4 * half;
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(&row_lse[st][i]);
-        const f32x4 delta = *reinterpret_cast<const f32x4*>(&row_delta[st][i]);
-        float prob[4], d[4];
+      for (int g = 0; g < 4; ++g) {  // P
+        const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
+        const f32x4 lse = *reinterpret_cast<const f32x4*>(quad);
+        f32x4 at = {0, 0, 0, 0}, slope = {0, 0, 0, 0};
+        if constexpr (FORM & FORM_BIAS) {
+          at = *reinterpret_cast<const f32x4*>(quad + 16);
+          slope = *reinterpret_cast<const f32x4*>(quad + 20);
+        }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float dot = s[4 * gq + u];
-          float deriv = 1.0f;
-          if constexpr (EXTRA) {
-            float x = dot * score.factor;
-            if (score.cap > 0) {
-              const float th = score.tanh_of(dot);
-              x = score.cap * th;
-              deriv = 1.0f - th * th;
-            }
-            x -= row_slope[st][i + u] * (float)abs(row_at[st][i + u] - key);
-            prob[u] = exp2_fast(x - lse[u]);
+          const int r = 4 * g + u;
+          if constexpr (FORM == FORM_PLAIN) {
+            s[r] = exp2_fast(__builtin_fmaf(s[r], score.factor, -lse[u]));
           } else {
-            prob[u] = exp2_fast(__builtin_fmaf(dot, score.factor, -lse[u]));
+            score.slope = slope[u];
+            s[r] = exp2_fast(score(s[r], at[u] - at_key, derivative[r]) - lse[u]);
           }
-          d[u] = prob[u] * __builtin_fmaf(dp[4 * gq + u], 1.0f / kLift, -delta[u]);
-          if (EXTRA) d[u] *= deriv;
         }
-        if (masked) {
-          const int4 first = *reinterpret_cast<const int4*>(&row_lo[st][i]), count = *reinterpret_cast<const int4*>(&row_count[st][i]);
+      }
+      if (!for_dv) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {  // dS
+          const f32x4 delta = *reinterpret_cast<const f32x4*>(of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4) + 4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = 4 * g + u;
+            dp[r] = s[r] * __builtin_fmaf(dp[r], 1.0f / kLift, -delta[u]);
+            if constexpr (FORM & FORM_CAP) dp[r] *= derivative[r];
+          }
+        }
+      }
+      if (!BOTH && !for_dv) s = dp;
+      if (masked) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
+          const int4 first = *reinterpret_cast<const int4*>(quad + 8), count = *reinterpret_cast<const int4*>(quad + 12);
           const int f4[4] = {first.x, first.y, first.z, first.w}, c4[4] = {count.x, count.y, count.z, count.w};
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const bool in = (unsigned)(key - f4[u]) < (unsigned)c4[u];
-            prob[u] = in ? prob[u] : 0.0f;
-            d[u] = in ? d[u] : 0.0f;
+            s[4 * g + u] = in ? s[4 * g + u] : 0.0f;
+            if constexpr (BOTH) dp[4 * g + u] = in ? dp[4 * g + u] : 0.0f;
           }
         }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          pf[gq >> 1][4 * (gq & 1) + u] = from_f32<T>(prob[u]);
-          ds[gq >> 1][4 * (gq & 1) + u] = from_f32<T>(d[u]);
-        }
       }
+      Frag w[SUMS][2];  // both: dS, P
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        w[0][r >> 3][r & 7] = from_f32<T>(BOTH ? dp[r] : s[r]);
+        if constexpr (BOTH) w[SUMS - 1][r >> 3][r & 7] = from_f32<T>(s[r]);
+      }
+      const unsigned from_rows = for_dv ? gs : qs;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          dv[d] = mfma_op(col_frag<T, CPR>(gs, lane, c * 32 + h * 16, d), pf[h], dv[d]);
-          dk[d] = mfma_op(col_frag<T, CPR>(qs, lane, c * 32 + h * 16, d), ds[h], dk[d]);
+          acc[0][d] = mfma_op(col_frag<T, DP>(map, from_rows, row + h * 16, d), w[0][h], acc[0][d]);
+          if constexpr (BOTH) acc[SUMS - 1][d] = mfma_op(col_frag<T, DP>(map, gs, row + h * 16, d), w[SUMS - 1][h], acc[SUMS - 1][d]);
         }
     }
-    if (t + 1 < t1) put(t + 1);
   }
-  const unsigned long long odd = __ballot(!(all_finite(dk) && all_finite(dv)));
-  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
-  if (key < e.keys && !((again >> (lane & 31)) & 1)) {
-    store_columns<T, DT>(reinterpret_cast<T*>(b.dk) + (long long)e.b * b.dks.batch + (long long)e.kv * b.dks.head + (long long)key * b.dks.row, dk,
-                         half, p.dim, p.scale);
-    store_columns<T, DT>(reinterpret_cast<T*>(b.dv) + (long long)e.b * b.dvs.batch + (long long)e.kv * b.dvs.head + (long long)key * b.dvs.row, dv,
-                         half, p.dim, 1.0f / kLift);
+  // the wavefronts of a sum meet: four (two of them onto two, one onto one), or two
+  const int lead = BOTH ? 0 : wave & 4;  // the first wavefront of the kind
+#pragma unroll
+  for (int step = BOTH ? 4 : 2; step >= 2; step >>= 1) {
+    __syncthreads();
+    const int mate = wave - lead;
+    f32x4* meet = reinterpret_cast<f32x4*>(smem) + ((mate & (step - 1)) + lead / 2) * (SUMS * DT * 4 * 64) + lane;
+    if (mate >= step && mate < 2 * step) {
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            meet[((i * DT + d) * 4 + g) * 64] = f32x4{acc[i][d][4 * g], acc[i][d][4 * g + 1], acc[i][d][4 * g + 2], acc[i][d][4 * g + 3]};
+    }
+    __syncthreads();
+    if (mate < step) {
+#pragma unroll
+      for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const f32x4 other = meet[((i * DT + d) * 4 + g) * 64];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) acc[i][d][4 * g + u] += other[u];
+          }
+    }
   }
-  again = __builtin_amdgcn_readfirstlane(again);
-  while (again) {
-    const int i = __builtin_ctz(again);
-    again &= again - 1;
-    if (key0 + i < e.keys) dkv_by_definition<T, DP>(b, e, key0 + i);
+  if (part) return;
+#pragma unroll
+  for (int i = 0; i < SUMS; ++i) {
+    const bool is_dv = for_dv || i == 1;
+    if (b.dkv_splits > 1) {
+      if (key < e.keys) store_part<DT>(dkv_part<DP>(b, z, e, key) + (is_dv ? DP : 0), acc[i], half);
+      continue;
+    }
+    const unsigned long long odd = __ballot(!all_finite(acc[i]));
+    unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
+    const Strides& to_s = is_dv ? b.dvs : b.dks;
+    T* out = reinterpret_cast<T*>(is_dv ? b.dv : b.dk) + (long long)e.b * to_s.batch + (long long)e.kv * to_s.head + (long long)key * to_s.row;
+    if (key < e.keys && !((again >> (lane & 31)) & 1)) store_columns<T, DT>(out, acc[i], half, p.dim, is_dv ? 1.0f / kLift : p.scale);
+    again = __builtin_amdgcn_readfirstlane(again);
+    while (again) {
+      const int at = __builtin_ctz(again);
+      again &= again - 1;
+      if (key0 + at < e.keys) dkv_by_definition<T, DP, FORM>(b, e, key0 + at, is_dv);
+    }
   }
 }
 
-template <typename T, int DP, bool EXTRA>
+// The splits of a key's two sums, in ascending order; one wavefront a key.
+template <typename T, int DP, int FORM>
+__global__ __launch_bounds__(256) void dkv_join_kernel(const BackArgs b) {
+  constexpr int E = DP / 64;
+  const Args& p = b.f;
+  const int lane = threadIdx.x & 63;
+  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= (long long)p.batch * p.kv_heads * p.seq_k) return;
+  const int entry = (int)(at / p.seq_k), key = (int)(at - (long long)entry * p.seq_k);
+  const Entry e = make_entry<false>(p, entry / p.kv_heads, entry % p.kv_heads);
+  float dk[E], dv[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) dk[i] = dv[i] = 0.0f;
+#pragma unroll 4
+  for (int z = 0; z < b.dkv_splits; ++z) {
+    const float* from = dkv_part<DP>(b, z, e, key) + lane * E;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      dk[i] += from[i];
+      dv[i] += from[DP + i];
+    }
+  }
+  bool finite = true;
+#pragma unroll
+  for (int i = 0; i < E; ++i) finite &= __builtin_fabsf(dk[i]) < __builtin_huge_valf() && __builtin_fabsf(dv[i]) < __builtin_huge_valf();
+  if (!__all(finite)) {
+    dkv_by_definition<T, DP, FORM>(b, e, key, false);
+    dkv_by_definition<T, DP, FORM>(b, e, key, true);
+    return;
+  }
+  T* to_k = reinterpret_cast<T*>(b.dk) + (long long)e.b * b.dks.batch + (long long)e.kv * b.dks.head + (long long)key * b.dks.row;
+  T* to_v = reinterpret_cast<T*>(b.dv) + (long long)e.b * b.dvs.batch + (long long)e.kv * b.dvs.head + (long long)key * b.dvs.row;
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (lane * E + i < p.dim) {
+      to_k[lane * E + i] = from_f32<T>(dk[i] * p.scale);
+      to_v[lane * E + i] = from_f32<T>(dv[i] * (1.0f / kLift));
+    }
+}
+
+template <typename T, int DP, int FORM>
 hipError_t launch(const BackArgs& b, hipStream_t stream) {
   const Args& p = b.f;
   const long long entries = (long long)p.batch * p.kv_heads;
   if (p.seq_q > 0) {
-    hipLaunchKernelGGL((dq_kernel<T, DP, EXTRA>), dim3((unsigned)(entries * p.row_tiles)), dim3(256), 0, stream, b);
+    hipLaunchKernelGGL((dq_kernel<T, DP, FORM>), dim3((unsigned)(entries * p.row_tiles * b.dq_splits)), dim3(256), 0, stream, b);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (b.dq_splits > 1) {
+      const long long rows = entries * p.seq_q * p.group;
+      hipLaunchKernelGGL((dq_join_kernel<T, DP, FORM>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, b);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
   }
   if (p.seq_k > 0) {
-    hipLaunchKernelGGL((dkv_kernel<T, DP, EXTRA>), dim3((unsigned)(entries * b.key_tiles)), dim3(256), 0, stream, b);
-    return hipGetLastError();
+    hipLaunchKernelGGL((dkv_kernel<T, DP, FORM>), dim3((unsigned)(entries * b.key_tiles * b.dkv_splits)), dim3(kDkvThreads), 0, stream, b);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (b.dkv_splits > 1) {
+      hipLaunchKernelGGL((dkv_join_kernel<T, DP, FORM>), dim3((unsigned)((entries * p.seq_k + 3) / 4)), dim3(256), 0, stream, b);
+      return hipGetLastError();
+    }
   }
   return hipSuccess;
 }
+template <typename T, int DP>
+hipError_t dispatch_form(int form, const BackArgs& b, hipStream_t stream) {
+  switch (form) {
+    case FORM_PLAIN: return launch<T, DP, FORM_PLAIN>(b, stream);
+    case FORM_BIAS: return launch<T, DP, FORM_BIAS>(b, stream);
+    case FORM_CAP: return launch<T, DP, FORM_CAP>(b, stream);
+    default: return launch<T, DP, FORM_CAP | FORM_BIAS>(b, stream);
+  }
+}
 template <typename T>
-hipError_t dispatch(bool extra, const BackArgs& b, hipStream_t stream) {
-  if (padded_dim(b.f.dim) == 128) return extra ? launch<T, 128, true>(b, stream) : launch<T, 128, false>(b, stream);
-  return extra ? launch<T, 64, true>(b, stream) : launch<T, 64, false>(b, stream);
+hipError_t dispatch(int form, const BackArgs& b, hipStream_t stream) {
+  return padded_dim(b.f.dim) == 128 ? dispatch_form<T, 128>(form, b, stream) : dispatch_form<T, 64>(form, b, stream);
 }
 
 long long row_groups_of(long long rows) { return (rows + 31) / 32; }
-long long delta_bytes(long long batch, long long heads, long long seq_q) { return (batch * heads * seq_q * 4 + 15) / 16 * 16; }
+// (of all forms: with a bias twice the fields)
+long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
+
+// How the two kernels' work is cut: tiles of 128 rows and of 64 keys, and these into splits where they would leave compute units
+// without work, as long as a split keeps some tiles of the other axis.
+struct BackCut {
+  int row_tiles, key_tiles, dq_splits, dq_share, dkv_splits, dkv_share;
+  long long part_bytes;
+};
+void split(long long blocks, long long tiles, long long wanted, long long least, int& splits, int& share) {
+  long long n = blocks >= wanted ? 1 : (wanted + blocks - 1) / blocks;
+  n = std::max(1LL, std::min(n, tiles / least));
+  share = (int)std::max(1LL, (tiles + n - 1) / n);
+  splits = (int)std::max(1LL, (tiles + share - 1) / share);
+}
+BackCut cut_backward(long long entries, long long rows, long long keys, int dp) {
+  BackCut c;
+  c.row_tiles = (int)((rows + 127) / 128);
+  c.key_tiles = (int)((keys + kBlockKeys - 1) / kBlockKeys);
+  split(std::max(1LL, entries * c.row_tiles), (keys + kTileKeys - 1) / kTileKeys, 256, 8, c.dq_splits, c.dq_share);
+  split(std::max(1LL, entries * c.key_tiles), (rows + kTileRows - 1) / kTileRows, 512, 4, c.dkv_splits, c.dkv_share);
+  const long long dq = c.dq_splits > 1 ? c.dq_splits * entries * rows * dp * 4 : 0;
+  const long long dkv = c.dkv_splits > 1 ? c.dkv_splits * entries * keys * dp * 8 : 0;
+  c.part_bytes = std::max(dq, dkv);
+  return c;
+}
 
 }  // namespace
 
@@ -546,12 +750,12 @@ extern "C" {
 
 int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
                                                  int64_t head_dim) {
-  (void)seq_k;
-  (void)head_dim;
-  if (batch <= 0 || kv_heads <= 0 || heads <= 0 || heads % kv_heads != 0 || seq_q <= 0) return 0;
+  if (batch <= 0 || kv_heads <= 0 || heads <= 0 || heads % kv_heads != 0 || seq_q <= 0 || seq_k < 0 || head_dim <= 0 || head_dim > 128) return 0;
   const long long group = heads / kv_heads;
-  if (group >= kMaxRows || seq_q >= kMaxRows || seq_q * group >= kMaxRows || batch > kMaxBlocks || kv_heads > kMaxBlocks) return 0;
-  return delta_bytes(batch, heads, seq_q) + batch * row_groups_of(seq_q * group) * 16;
+  if (group >= kMaxRows || seq_q >= kMaxRows || seq_q * group >= kMaxRows || seq_k >= kMaxRows || batch > kMaxBlocks || kv_heads > kMaxBlocks)
+    return 0;
+  return info_bytes(batch * kv_heads, seq_q * group) + batch * row_groups_of(seq_q * group) * 16 +
+         cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim)).part_bytes;
 }
 
 hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
@@ -597,8 +801,8 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
     b.dos = strides_of(grad_out);
     b.dq = grad_q->data;
     b.dqs = strides_of(grad_q);
-    b.delta = static_cast<float*>(workspace);
-    b.seen = reinterpret_cast<int4*>(static_cast<char*>(workspace) + delta_bytes(batch, heads, seq_q));
+    b.info = static_cast<float*>(workspace);
+    b.seen = reinterpret_cast<int4*>(static_cast<char*>(workspace) + info_bytes(batch * kv_heads, seq_q * group));
   }
   if (seq_k > 0) {
     p.k = k->data;
@@ -625,13 +829,22 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
   p.scale = options->scale;
   p.softcap = options->softcap;
   p.splits = 1;
-  p.row_tiles = (int)((seq_q * group + 127) / 128);
+  const BackCut c = cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim));
+  p.row_tiles = c.row_tiles;
   b.row_groups = (int)row_groups_of(seq_q * group);
-  b.key_tiles = (int)((seq_k + 127) / 128);
-  if (batch * kv_heads * std::max(p.row_tiles, b.key_tiles) > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
-  const bool extra = is_extra(options);
+  b.key_tiles = c.key_tiles;
+  b.dq_splits = c.dq_splits;
+  b.dq_share = c.dq_share;
+  // (without queries there is no workspace, and nothing to add up)
+  b.dkv_splits = seq_q > 0 ? c.dkv_splits : 1;
+  b.dkv_share = c.dkv_share;
+  if (seq_q > 0) b.part = reinterpret_cast<float*>(reinterpret_cast<char*>(b.seen) + batch * b.row_groups * 16);
+  const auto near = [&](const Strides& s) { return s.row < (1LL << 23) && s.head < (1LL << 23); };
+  b.regular = group <= 32 && 32 % group == 0 && near(p.qs) && near(b.dos);
+  if (batch * kv_heads * std::max((long long)c.row_tiles * c.dq_splits, (long long)c.key_tiles * c.dkv_splits) > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
+  const int form = form_of(options);
   const hipStream_t s = (hipStream_t)stream;
-  const hipError_t e = dtype == HIDET_F16 ? dispatch<f16>(extra, b, s) : dispatch<bf16>(extra, b, s);
+  const hipError_t e = dtype == HIDET_F16 ? dispatch<f16>(form, b, s) : dispatch<bf16>(form, b, s);
   return e == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }
 

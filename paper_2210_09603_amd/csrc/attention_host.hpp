@@ -53,43 +53,50 @@ inline hidet_status_t check_options(const hidet_attention_options_t* o) {
 }
 // (a window of 2^30 hides nothing of 2^29 positions)
 inline int window_of(long long window) { return window >= (1LL << 30) ? 0 : (int)window; }
-// scores that are no positive multiple of the products take the form with a score of their own
-inline bool is_extra(const hidet_attention_options_t* o) { return o->softcap > 0 || o->slopes || !(o->scale > 0); }
+// (scores that are no positive multiple of the products take the form with a score of their own: a slope of 0 where there is none)
+inline int form_of(const hidet_attention_options_t* o) {
+  return (o->softcap > 0 ? FORM_CAP : 0) | (o->slopes || (o->softcap == 0 && !(o->scale > 0)) ? FORM_BIAS : 0);
+}
 
 // How the work of `entries` (batch entries x kv heads) of `rows` rows each over up to `keys` keys is cut.
 struct Cut {
-  bool stream;     // the kernel of few rows
-  int row_tiles, splits;
+  bool stream;  // the kernel of few rows
+  int row_tiles, splits, share;
 };
 inline long long split_bytes(long long entries, long long rows, int dp) { return entries * rows * (dp + 2) * 4; }
 Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room);
 
 inline int padded_dim(long long dim) { return dim <= 64 ? 64 : 128; }
 
-template <typename T, int DP, bool PAGED, bool EXTRA>
+template <typename T, int DP, bool PAGED, int FORM>
 hipError_t launch_forward(const Args& p, const Cut& c, hipStream_t stream) {
   const long long blocks = (long long)p.batch * p.kv_heads * c.row_tiles * c.splits;
   if (c.stream)
-    hipLaunchKernelGGL((stream_kernel<T, DP, PAGED, EXTRA>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), 0, stream, p);
+    hipLaunchKernelGGL((stream_kernel<T, DP, PAGED, FORM>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), 0, stream, p);
   else
-    hipLaunchKernelGGL((tile_kernel<T, DP, PAGED, EXTRA>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (c.splits > 1) {
-    const long long rows = (long long)p.batch * p.kv_heads * p.seq_q * p.group;
-    hipLaunchKernelGGL((join_kernel<T, DP, PAGED>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, p);
-    return hipGetLastError();
+    hipLaunchKernelGGL((tile_kernel<T, DP, PAGED, FORM>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || c.splits == 1) return e;
+  const long long rows = (long long)p.batch * p.kv_heads * p.seq_q * p.group;
+  if (c.splits > 16)
+    hipLaunchKernelGGL((join_many_kernel<T, DP, PAGED>), dim3((unsigned)rows), dim3(256), 0, stream, p);
+  else
+    hipLaunchKernelGGL((join_kernel<T, DP, PAGED>), dim3((unsigned)((rows + 1024 / DP - 1) / (1024 / DP))), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+template <typename T, int DP, bool PAGED>
+hipError_t dispatch_form(int form, const Args& p, const Cut& c, hipStream_t stream) {
+  switch (form) {
+    case FORM_PLAIN: return launch_forward<T, DP, PAGED, FORM_PLAIN>(p, c, stream);
+    case FORM_BIAS: return launch_forward<T, DP, PAGED, FORM_BIAS>(p, c, stream);
+    case FORM_CAP: return launch_forward<T, DP, PAGED, FORM_CAP>(p, c, stream);
+    default: return launch_forward<T, DP, PAGED, FORM_CAP | FORM_BIAS>(p, c, stream);
   }
-  return hipSuccess;
 }
 template <bool PAGED>
-hipError_t dispatch_forward(int dtype, bool extra, const Args& p, const Cut& c, hipStream_t stream) {
+hipError_t dispatch_forward(int dtype, int form, const Args& p, const Cut& c, hipStream_t stream) {
   const bool wide = padded_dim(p.dim) == 128;
-  if (dtype == HIDET_F16) {
-    if (wide) return extra ? launch_forward<f16, 128, PAGED, true>(p, c, stream) : launch_forward<f16, 128, PAGED, false>(p, c, stream);
-    return extra ? launch_forward<f16, 64, PAGED, true>(p, c, stream) : launch_forward<f16, 64, PAGED, false>(p, c, stream);
-  }
-  if (wide) return extra ? launch_forward<bf16, 128, PAGED, true>(p, c, stream) : launch_forward<bf16, 128, PAGED, false>(p, c, stream);
-  return extra ? launch_forward<bf16, 64, PAGED, true>(p, c, stream) : launch_forward<bf16, 64, PAGED, false>(p, c, stream);
+  if (dtype == HIDET_F16) return wide ? dispatch_form<f16, 128, PAGED>(form, p, c, stream) : dispatch_form<f16, 64, PAGED>(form, p, c, stream);
+  return wide ? dispatch_form<bf16, 128, PAGED>(form, p, c, stream) : dispatch_form<bf16, 64, PAGED>(form, p, c, stream);
 }
 
 }  // namespace attn

@@ -241,7 +241,8 @@ hidet_status_t hidet_cache_attention(const hidet_cache_t* cache, int64_t heads, 
   if (entries * c.row_tiles > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
   p.row_tiles = c.row_tiles;
   p.splits = c.splits;
-  return dispatch_forward<true>(cache->dtype, is_extra(options), p, c, (hipStream_t)stream) == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
+  p.share = c.share;
+  return dispatch_forward<true>(cache->dtype, form_of(options), p, c, (hipStream_t)stream) == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }
 
 }  // extern "C"

@@ -13,6 +13,9 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+#include <initializer_list>
+
 #include "../../include/hidet_mi355x.h"
 
 namespace {
@@ -324,13 +327,359 @@ void calls_dealloc(PyObject* self) {
   Py_TYPE(self)->tp_free(self);
 }
 
+// ---- attention, its positions and its cache -----------------------------------------------------------------------------------
+struct AttentionCalls {
+  PyObject_HEAD
+  decltype(&hidet_attention) attention;
+  decltype(&hidet_attention_backward) backward;
+  decltype(&hidet_attention_ranges) ranges;
+  decltype(&hidet_rope) rope;
+  decltype(&hidet_cache_append) append;
+  decltype(&hidet_cache_attention) cache_attention;
+  PyObject *cache_type, *in_bad_fork, *get_device, *get_stream;
+};
+
+// Exact strided tensors on one GPU.  A missing one (None) counts as fine where it is optional.
+class Tensors {
+ public:
+  bool ok = true;
+  const at::Tensor* get(PyObject* o, bool optional = false) {
+    if (o == Py_None && optional) return nullptr;
+    if (!THPVariable_CheckExact(o)) return fail();
+    const at::Tensor& x = THPVariable_Unpack(o);
+    if (!x.defined() || x.layout() != at::kStrided || !x.has_storage() || !x.is_cuda()) return fail();
+    const int index = x.device().index();
+    if (device_ >= 0 && index != device_) return fail();
+    device_ = index;
+    return &x;
+  }
+  // with a known shape and type, dense
+  const at::Tensor* dense(PyObject* o, at::ScalarType type, std::initializer_list<int64_t> shape, bool optional = true) {
+    const at::Tensor* x = get(o, optional);
+    if (x && (x->scalar_type() != type || x->sizes() != at::IntArrayRef(shape.begin(), shape.size()) || !x->is_contiguous())) return fail();
+    return x;
+  }
+  // vectors along the last axis of 3 or 4
+  const at::Tensor* vectors(PyObject* o, hidet_heads_t& h, int64_t dim) {
+    const at::Tensor* x = get(o);
+    if (!x || x->dim() != dim || (x->stride(dim - 1) != 1 && x->size(dim - 1) > 1)) return fail();
+    h.data = x->data_ptr();
+    h.stride_batch = dim == 4 ? x->stride(0) : 0;
+    h.stride_head = x->stride(1);
+    h.stride_row = x->stride(dim == 4 ? 2 : 0);
+    return x;
+  }
+  bool on(int64_t device) const { return device_ == device; }
+  int64_t device() const { return device_; }
+
+ private:
+  const at::Tensor* fail() {
+    ok = false;
+    return nullptr;
+  }
+  int64_t device_ = -1;
+};
+int32_t type_of(const at::Tensor* x) {
+  switch (x->scalar_type()) {
+    case at::kFloat: return HIDET_F32;
+    case at::kHalf: return HIDET_F16;
+    case at::kBFloat16: return HIDET_BF16;
+    default: return -1;
+  }
+}
+bool real(PyObject* o, double& v) {
+  if (PyFloat_CheckExact(o)) {
+    v = PyFloat_AS_DOUBLE(o);
+    return true;
+  }
+  int64_t w;
+  if (!whole(o, w)) return false;
+  v = (double)w;
+  return true;
+}
+template <class P>
+P* address(const at::Tensor* x) {
+  return x ? static_cast<P*>(x->data_ptr()) : nullptr;
+}
+int64_t bytes_of(const at::Tensor* x) { return x ? x->numel() * (int64_t)x->element_size() : 0; }
+
+// The stream given, or the current one; the tensors' device has to be the current one.
+bool stream_on(const AttentionCalls* c, PyObject* o, const Tensors& t, void*& out) {
+  bool ok = false;
+  PyObject* bad = PyObject_CallNoArgs(c->in_bad_fork);
+  if (bad == Py_False) {
+    if (PyObject* device = PyObject_CallNoArgs(c->get_device)) {
+      int64_t index;
+      if (whole(device, index) && t.on(index)) {
+        PyObject* v = o != Py_None ? PyObject_GetAttrString(o, "cuda_stream") : PyObject_CallOneArg(c->get_stream, device);
+        ok = v != nullptr && PyLong_CheckExact(v);
+        if (ok) out = PyLong_AsVoidPtr(v);
+        Py_XDECREF(v);
+      }
+      Py_DECREF(device);
+    }
+  }
+  Py_XDECREF(bad);
+  if (PyErr_Occurred()) {
+    PyErr_Clear();
+    return false;
+  }
+  return ok;
+}
+
+// scale, causal, window, softcap, slopes, ranges: the options of a call with `heads` heads
+bool options_of(Tensors& t, PyObject* scale, PyObject* causal, PyObject* window, PyObject* softcap, PyObject* slopes, PyObject* ranges,
+                int64_t batch, int64_t heads, int64_t rows, int64_t dim, hidet_attention_options_t& o) {
+  o.struct_size = sizeof(o);
+  double v;
+  if (scale == Py_None) {
+    if (dim <= 0) return false;
+    o.scale = (float)(1.0 / std::sqrt((double)dim));
+  } else {
+    if (!real(scale, v)) return false;
+    o.scale = (float)v;
+  }
+  if (!flag(causal, o.causal) || !whole(window, o.window) || !real(softcap, v)) return false;
+  o.softcap = (float)v;
+  o.slopes = address<const float>(t.dense(slopes, at::kFloat, {heads}));
+  o.ranges = address<const int32_t>(t.dense(ranges, at::kInt, {batch, rows, 2}));
+  return t.ok;
+}
+
+// attention(q, k, v, out, lse, scale, causal, window, softcap, slopes, ranges, workspace, stream)
+PyObject* call_attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 13)) return nullptr;
+  const AttentionCalls* c = reinterpret_cast<const AttentionCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    hidet_heads_t hq, hk, hv, ho;
+    const at::Tensor *q = t.vectors(a[0], hq, 4), *k = t.vectors(a[1], hk, 4), *v = t.vectors(a[2], hv, 4), *out = t.vectors(a[3], ho, 4);
+    if (!t.ok) return kGeneral;
+    const int32_t type = type_of(q);
+    const int64_t batch = q->size(0), heads = q->size(1), rows = q->size(2), dim = q->size(3);
+    if (type < 0 || k->sizes() != v->sizes() || out->sizes() != q->sizes() || k->size(0) != batch || k->size(3) != dim) return kGeneral;
+    if (k->scalar_type() != q->scalar_type() || v->scalar_type() != q->scalar_type() || out->scalar_type() != q->scalar_type()) return kGeneral;
+    float* lse = address<float>(t.dense(a[4], at::kFloat, {batch, heads, rows}));
+    hidet_attention_options_t o;
+    if (!options_of(t, a[5], a[6], a[7], a[8], a[9], a[10], batch, heads, rows, dim, o)) return kGeneral;
+    const at::Tensor* ws = t.get(a[11], true);
+    void* stream;
+    if (!t.ok || !stream_on(c, a[12], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->attention(type, batch, heads, k->size(1), rows, k->size(2), dim, &hq, &hk, &hv, &ho, lse, &o, address<void>(ws), bytes_of(ws), stream);
+    });
+  });
+}
+
+// attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, workspace, scale, causal, window, softcap, slopes, ranges, stream)
+PyObject* call_attention_backward(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 17)) return nullptr;
+  const AttentionCalls* c = reinterpret_cast<const AttentionCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    hidet_heads_t h[8];
+    const at::Tensor* x[8];
+    const int from[8] = {0, 1, 2, 3, 4, 6, 7, 8};  // grad_out, q, k, v, out, grad_q, grad_k, grad_v
+    for (int i = 0; i < 8; ++i) {
+      x[i] = t.vectors(a[from[i]], h[i], 4);
+      if (!t.ok) return kGeneral;
+    }
+    const at::Tensor *q = x[1], *k = x[2];
+    const int32_t type = type_of(q);
+    const int64_t batch = q->size(0), heads = q->size(1), rows = q->size(2), dim = q->size(3);
+    if (type < 0 || k->size(0) != batch || k->size(3) != dim) return kGeneral;
+    for (int i = 0; i < 8; ++i) {
+      const at::Tensor* like = i == 2 || i == 3 || i >= 6 ? k : q;
+      if (x[i]->sizes() != like->sizes() || x[i]->scalar_type() != q->scalar_type()) return kGeneral;
+    }
+    const float* lse = address<const float>(t.dense(a[5], at::kFloat, {batch, heads, rows}));
+    const at::Tensor* ws = t.get(a[9], true);
+    hidet_attention_options_t o;
+    if (!options_of(t, a[10], a[11], a[12], a[13], a[14], a[15], batch, heads, rows, dim, o)) return kGeneral;
+    void* stream;
+    if (!t.ok || !stream_on(c, a[16], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->backward(type, batch, heads, k->size(1), rows, k->size(2), dim, &h[0], &h[1], &h[2], &h[3], &h[4], lse, &h[5], &h[6], &h[7], &o,
+                         address<void>(ws), bytes_of(ws), stream);
+    });
+  });
+}
+
+// attention_ranges(ranges, keys, documents, prefix, causal, window, stream)
+PyObject* call_attention_ranges(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 7)) return nullptr;
+  const AttentionCalls* c = reinterpret_cast<const AttentionCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    const at::Tensor* r = t.get(a[0]);
+    int64_t keys, window;
+    int32_t causal;
+    if (!r || r->dim() != 3 || r->size(2) != 2 || r->scalar_type() != at::kInt || !r->is_contiguous()) return kGeneral;
+    if (!whole(a[1], keys) || !flag(a[4], causal) || !whole(a[5], window)) return kGeneral;
+    const int32_t* documents = address<const int32_t>(t.dense(a[2], at::kInt, {r->size(0), keys}));
+    const int32_t* prefix = address<const int32_t>(t.dense(a[3], at::kInt, {r->size(0)}));
+    void* stream;
+    if (!t.ok || !stream_on(c, a[6], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->ranges(r->size(0), r->size(1), keys, documents, prefix, causal, window, address<int32_t>(r), stream);
+    });
+  });
+}
+
+// rope(x, y, frequencies, positions, first_position, interleaved, inverse, amplitude, stream)
+PyObject* call_rope(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 9)) return nullptr;
+  const AttentionCalls* c = reinterpret_cast<const AttentionCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    hidet_heads_t hx, hy;
+    const at::Tensor *x = t.vectors(a[0], hx, 4), *y = t.vectors(a[1], hy, 4), *f = t.get(a[2]), *p = t.get(a[3], true);
+    if (!t.ok || y->sizes() != x->sizes() || y->scalar_type() != x->scalar_type()) return kGeneral;
+    if (f->scalar_type() != at::kDouble || f->dim() != 1 || !f->is_contiguous()) return kGeneral;
+    const int64_t batch = x->size(0), seq = x->size(2);
+    int64_t each = 0, first;
+    if (p) {
+      if (p->scalar_type() != at::kInt || p->dim() < 1 || p->dim() > 2 || p->size(-1) != seq || (seq > 1 && p->stride(-1) != 1)) return kGeneral;
+      if (p->dim() == 2) {
+        if (p->size(0) != batch) return kGeneral;
+        each = p->stride(0);
+      }
+    }
+    const int32_t type = type_of(x);
+    int32_t interleaved, inverse;
+    double amplitude;
+    if (type < 0 || !whole(a[4], first) || !flag(a[5], interleaved) || !flag(a[6], inverse) || !real(a[7], amplitude)) return kGeneral;
+    void* stream;
+    if (!stream_on(c, a[8], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->rope(type, batch, x->size(1), seq, x->size(3), 2 * f->size(0), &hx, &hy, address<const double>(f), address<const int32_t>(p), each,
+                     first, interleaved, inverse, (float)amplitude, stream);
+    });
+  });
+}
+
+// The cache descriptor of a call, borrowed from the ctypes structure for as long as this lives; `_device` is that of its tensors.
+class CacheArg {
+ public:
+  CacheArg(const AttentionCalls* c, PyObject* o) {
+    if ((PyObject*)Py_TYPE(o) != c->cache_type) return;
+    PyObject* device = PyObject_GetAttrString(o, "_device");
+    const bool known = device && whole(device, device_);
+    Py_XDECREF(device);
+    if (!known || PyObject_GetBuffer(o, &view_, PyBUF_SIMPLE) != 0) {
+      PyErr_Clear();
+      return;
+    }
+    held_ = true;
+    ok_ = view_.len == (Py_ssize_t)sizeof(hidet_cache_t);
+  }
+  ~CacheArg() {
+    if (held_) PyBuffer_Release(&view_);
+  }
+  CacheArg(const CacheArg&) = delete;
+  CacheArg& operator=(const CacheArg&) = delete;
+  const hidet_cache_t* get() const { return static_cast<const hidet_cache_t*>(view_.buf); }
+  bool holds(const Tensors& t, const at::Tensor* x) const {
+    return ok_ && t.on(device_) && type_of(x) == get()->dtype && x->size(2) == get()->head_dim;
+  }
+  bool ok() const { return ok_; }
+
+ private:
+  Py_buffer view_;
+  int64_t device_ = -2;
+  bool held_ = false, ok_ = false;
+};
+
+// cache_append(cache, k, v, starts, max_new, stream)
+PyObject* call_cache_append(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 6)) return nullptr;
+  const AttentionCalls* c = reinterpret_cast<const AttentionCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    hidet_heads_t hk, hv;
+    const CacheArg cache(c, a[0]);
+    const at::Tensor *k = t.vectors(a[1], hk, 3), *v = t.vectors(a[2], hv, 3);
+    if (!t.ok || !cache.ok() || !cache.holds(t, k) || !cache.holds(t, v) || k->sizes() != v->sizes() || k->size(1) != cache.get()->heads) return kGeneral;
+    const int32_t* starts = address<const int32_t>(t.dense(a[3], at::kInt, {cache.get()->seqs + 1}, false));
+    int64_t max_new;
+    void* stream;
+    if (!t.ok || !whole(a[4], max_new) || !stream_on(c, a[5], t, stream)) return kGeneral;
+    return without_lock([&] { return c->append(cache.get(), k->size(0), max_new, &hk, &hv, starts, stream); });
+  });
+}
+
+// cache_attention(cache, q, out, starts, max_new, scale, window, softcap, slopes, lse, workspace, stream)
+PyObject* call_cache_attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 12)) return nullptr;
+  const AttentionCalls* c = reinterpret_cast<const AttentionCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    hidet_heads_t hq, ho;
+    const CacheArg cache(c, a[0]);
+    const at::Tensor *q = t.vectors(a[1], hq, 3), *out = t.vectors(a[2], ho, 3);
+    if (!t.ok || !cache.ok() || !cache.holds(t, q) || !cache.holds(t, out) || q->sizes() != out->sizes()) return kGeneral;
+    const int64_t tokens = q->size(0), heads = q->size(1);
+    const int32_t* starts = address<const int32_t>(t.dense(a[3], at::kInt, {cache.get()->seqs + 1}, false));
+    float* lse = address<float>(t.dense(a[9], at::kFloat, {tokens, heads}));
+    hidet_attention_options_t o;
+    if (!options_of(t, a[5], Py_True, a[6], a[7], a[8], Py_None, 0, heads, 0, q->size(2), o)) return kGeneral;
+    const at::Tensor* ws = t.get(a[10], true);
+    int64_t max_new;
+    void* stream;
+    if (!t.ok || !whole(a[4], max_new) || !stream_on(c, a[11], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->cache_attention(cache.get(), heads, tokens, max_new, &hq, &ho, lse, starts, &o, address<void>(ws), bytes_of(ws), stream);
+    });
+  });
+}
+
+// AttentionCalls((addresses of the six entry points), cache type, in_bad_fork, get_device, get_stream)
+PyObject* attention_calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
+  unsigned long long at[6];
+  PyObject *cache_type, *in_bad_fork, *get_device, *get_stream;
+  if (!PyArg_ParseTuple(args, "(KKKKKK)OOOO", &at[0], &at[1], &at[2], &at[3], &at[4], &at[5], &cache_type, &in_bad_fork, &get_device, &get_stream))
+    return nullptr;
+  for (unsigned long long a : at) {
+    if (a == 0) {
+      PyErr_SetString(PyExc_ValueError, "null entry point");
+      return nullptr;
+    }
+  }
+  AttentionCalls* c = reinterpret_cast<AttentionCalls*>(type->tp_alloc(type, 0));
+  if (!c) return nullptr;
+  c->attention = reinterpret_cast<decltype(c->attention)>((uintptr_t)at[0]);
+  c->backward = reinterpret_cast<decltype(c->backward)>((uintptr_t)at[1]);
+  c->ranges = reinterpret_cast<decltype(c->ranges)>((uintptr_t)at[2]);
+  c->rope = reinterpret_cast<decltype(c->rope)>((uintptr_t)at[3]);
+  c->append = reinterpret_cast<decltype(c->append)>((uintptr_t)at[4]);
+  c->cache_attention = reinterpret_cast<decltype(c->cache_attention)>((uintptr_t)at[5]);
+  c->cache_type = Py_NewRef(cache_type);
+  c->in_bad_fork = Py_NewRef(in_bad_fork);
+  c->get_device = Py_NewRef(get_device);
+  c->get_stream = Py_NewRef(get_stream);
+  return reinterpret_cast<PyObject*>(c);
+}
+void attention_calls_dealloc(PyObject* self) {
+  AttentionCalls* c = reinterpret_cast<AttentionCalls*>(self);
+  Py_XDECREF(c->cache_type);
+  Py_XDECREF(c->in_bad_fork);
+  Py_XDECREF(c->get_device);
+  Py_XDECREF(c->get_stream);
+  Py_TYPE(self)->tp_free(self);
+}
+
 using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 PyMethodDef method(const char* name, Fast f) { return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}; }
 PyMethodDef g_methods[] = {method("gemm", call_gemm<2>),         method("batched_gemm", call_gemm<3>),
                            method("conv2d", call_conv<false>),   method("conv2d_packed", call_conv<true>),
                            method("softmax_rows", call_softmax), method("reduce_rows", call_reduce),
                            {nullptr, nullptr, 0, nullptr}};
+PyMethodDef g_attention_methods[] = {method("attention", call_attention),       method("attention_backward", call_attention_backward),
+                                     method("rope", call_rope),                 method("attention_ranges", call_attention_ranges),
+                                     method("cache_append", call_cache_append), method("cache_attention", call_cache_attention),
+                                     {nullptr, nullptr, 0, nullptr}};
 PyTypeObject g_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+PyTypeObject g_attention_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -342,11 +691,18 @@ PyMODINIT_FUNC PyInit__host_calls() {
   g_type.tp_new = calls_new;
   g_type.tp_dealloc = calls_dealloc;
   g_type.tp_methods = g_methods;
-  if (PyType_Ready(&g_type) < 0) return nullptr;
+  g_attention_type.tp_name = "_host_calls.AttentionCalls";
+  g_attention_type.tp_basicsize = sizeof(AttentionCalls);
+  g_attention_type.tp_flags = Py_TPFLAGS_DEFAULT;
+  g_attention_type.tp_new = attention_calls_new;
+  g_attention_type.tp_dealloc = attention_calls_dealloc;
+  g_attention_type.tp_methods = g_attention_methods;
+  if (PyType_Ready(&g_type) < 0 || PyType_Ready(&g_attention_type) < 0) return nullptr;
   PyObject* m = PyModule_Create(&g_module);
   if (!m) return nullptr;
   // (what this was compiled for: the binding refuses it under another torch or Python, whose tensors it would misread)
   if (PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject*>(&g_type)) < 0 ||
+      PyModule_AddObjectRef(m, "AttentionCalls", reinterpret_cast<PyObject*>(&g_attention_type)) < 0 ||
       PyModule_AddStringConstant(m, "built_for", HIDET_BUILT_FOR) < 0) {
     Py_DECREF(m);
     return nullptr;
