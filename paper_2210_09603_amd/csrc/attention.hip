@@ -7,21 +7,27 @@ using namespace hidet::attn;
 namespace hidet {
 namespace attn {
 
-// Up to 32 rows run in the kernel of few rows, more in tiles of 128.  A split is a fixed number of tiles of keys, so that the
-// sequences of a ragged batch give pieces of equal length.
+// Which kernel: up to 32 rows, or little work on keys that more than one wavefront can share, runs in pieces of 32 rows, where 4
+// wavefronts share the keys; the rest in tiles of 128 rows.  Microseconds in pieces and in tiles, heads of 64 dimensions with as many
+// causal keys as rows: 12 heads of 128 5.8 and 6.1, of 512 8.5 and 11.1, of 1024 17.7 and 16.5; 48 heads of 128 5.9 and 6.1, of 256 8.0 and
+// 7.9; one head of 64 rows 5.5 and 4.7.
+//
+// Splits: one is a fixed number of tiles of keys, so that the sequences of a ragged batch give pieces of equal length.
 //   Few rows: 512 workgroups fill the device, which is worth a partial result for 16 tiles of 32 keys (one sequence of 131000 keys, 2 kv
-//   heads: 40 us with 16, 42 with 32, 56 with 64); up to 2048 even out a ragged batch, as long as 64 tiles remain (64 sequences of 100 to
-//   8000 keys, 8 kv heads: 222 us; 241 with 1024, 232 with 4096 of 16).
+//   heads: 39 us with 16, 40 with 32, 56 with 64); up to 2048 even out a ragged batch, as long as 64 tiles remain (64 sequences of 100 to
+//   8000 keys, 8 kv heads: 220 us; 231 with 1024 workgroups, 225 with 4096 of 16 tiles).
 //   Tiles of 128 rows: where they leave compute units without any, and 8 tiles of 64 keys remain (more, and the second kernel costs
-//   what it gains: 36 x 8 tiles of 1021 keys, 64 dimensions, 32 us whole and 26 + 10 split).
-Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room) {
+//   what it gains: 36 x 8 tiles of 1021 keys, 64 dimensions, 32 us whole and 26 + 10 split).  Of a ragged batch's tiles some have no
+//   rows: four times as many (chunks of 4 prompts of 37 to 512 tokens over 4096 keys: 157 us, 192 with a quarter).
+Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room, bool ragged) {
   Cut c;
-  c.stream = rows <= 32;
+  const long long pieces = entries * ((rows + 31) / 32);
+  c.stream = rows <= 32 || (keys > kTileKeys && pieces <= 256 && pieces * ((keys + 31) / 32) <= 4096);
   const long long tile = c.stream ? 32 : 128, tile_keys = c.stream ? kStreamKeys : kTileKeys;
   c.row_tiles = (int)((rows + tile - 1) / tile);
   const long long blocks = entries * c.row_tiles, tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys);
   const auto wish = [&](long long workgroups, long long least) { return std::min((workgroups + blocks - 1) / blocks, tiles / least); };
-  long long splits = c.stream ? std::max(wish(512, 16), wish(2048, 64)) : wish(256, 8);
+  long long splits = c.stream ? std::max(wish(512, 16), wish(2048, 64)) : wish(ragged ? 1024 : 256, 8);
   splits = std::max(1LL, std::min(splits, room / split_bytes(entries, rows, dp)));
   const long long share = (tiles + splits - 1) / splits;
   c.share = (int)share;
@@ -116,7 +122,7 @@ int64_t hidet_attention_workspace_bytes(int64_t batch, int64_t heads, int64_t kv
   const long long group = heads / kv_heads;
   if (group > kMaxRows || seq_q >= kMaxRows || seq_q * group >= kMaxRows || batch > kMaxBlocks || kv_heads > kMaxBlocks) return 0;
   const int dp = padded_dim(head_dim);
-  const Cut c = cut_work(batch * kv_heads, seq_q * group, seq_k, dp, 1LL << 62);
+  const Cut c = cut_work(batch * kv_heads, seq_q * group, seq_k, dp, 1LL << 62, false);
   return c.splits > 1 ? c.splits * split_bytes(batch * kv_heads, seq_q * group, dp) : 0;
 }
 
@@ -169,7 +175,7 @@ hidet_status_t hidet_attention(int32_t dtype, int64_t batch, int64_t heads, int6
   p.window = window_of(options->window);
   p.scale = options->scale;
   p.softcap = options->softcap;
-  const Cut c = cut_work(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim), workspace ? workspace_bytes : 0);
+  const Cut c = cut_work(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim), workspace ? workspace_bytes : 0, false);
   if (batch * kv_heads * c.row_tiles > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
   p.row_tiles = c.row_tiles;
   p.splits = c.splits;

@@ -331,18 +331,28 @@ __device__ __forceinline__ long long lse_offset(const Args& p, const Entry& e, c
     return ((long long)e.b * p.heads + w.head) * p.seq_q + w.token;
 }
 
-// Where a key is: its offset from the entry's keys, in elements; `there` says whether its page is one of the cache's.
+// Where a key is.  What is asked of the table and what is made of it are apart: a loop asks one tile ahead of the keys' own loads, and
+// using the answer at once would wait for every load in flight.
+struct KeyPlace {
+  int page, row;  // row: slot of the page, or the key where there are no pages
+};
 template <bool PAGED>
-__device__ __forceinline__ long long key_offset(const Args& p, const Entry& e, const Strides& s, int j, bool& there) {
+__device__ __forceinline__ KeyPlace find_key(const Args& p, const Entry& e, int j) {
   if constexpr (PAGED) {
-    const int at = p.d_page.div(j), slot = j - at * p.page_size;
-    const int page = e.table[at];
-    there = (unsigned)page < (unsigned)p.num_pages;
-    return (long long)(there ? page : 0) * s.batch + (long long)slot * s.row;
+    const int at = p.d_page.div(j);
+    return KeyPlace{e.table[at], j - at * p.page_size};
   } else {
-    there = true;
-    return (long long)j * s.row;
+    return KeyPlace{0, j};
   }
+}
+template <bool PAGED>
+__device__ __forceinline__ bool is_there(const Args& p, const KeyPlace& k) {  // (its page is one of the cache's)
+  return !PAGED || (unsigned)k.page < (unsigned)p.num_pages;
+}
+// its offset from the entry's keys, in elements; of no page: some page's
+template <bool PAGED>
+__device__ __forceinline__ long long key_offset(const Args& p, const Strides& s, const KeyPlace& k) {
+  return (PAGED ? (long long)(is_there<PAGED>(p, k) ? k.page : 0) * s.batch : 0) + (long long)k.row * s.row;
 }
 template <typename T, bool PAGED>
 __device__ __forceinline__ const T* keys_of(const Args& p, const Entry& e, const void* base, const Strides& s) {
@@ -485,10 +495,9 @@ __device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e,
   from = max(from, w.lo);
   to = min(to, w.hi);
   for (int j = from; j < to; ++j) {
-    bool there;
-    const long long ko = key_offset<PAGED>(p, e, p.ks, j, there);
-    if (!there) continue;
-    const long long vo = key_offset<PAGED>(p, e, p.vs, j, there);
+    const KeyPlace place = find_key<PAGED>(p, e, j);
+    if (!is_there<PAGED>(p, place)) continue;
+    const long long ko = key_offset<PAGED>(p, p.ks, place), vo = key_offset<PAGED>(p, p.vs, place);
     float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < E; ++i)
@@ -674,45 +683,49 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
       voff[i] = ((unsigned)(i * RPP + load_row) * (unsigned)p.vs.row + load_chunk * 8) * 2;
     }
   }
-  // paged: where lane l's key of the tile after the next is
-  long long ahead = 0;
-  unsigned long long there_next = ~0ull, there_now = ~0ull;
+  KeyPlace next = {0, 0};  // paged: where lane l's key of the tile after the next is
+  unsigned long long there = ~0ull, there_next = ~0ull;
   auto look_up = [&](int t) {
-    if constexpr (PAGED) {
-      bool there;
-      ahead = key_offset<PAGED>(p, e, p.ks, min(begin + t * kTileKeys + lane, end - 1), there);
-      there_next = __ballot(there);
-    }
+    if constexpr (PAGED) next = find_key<PAGED>(p, e, min(begin + t * kTileKeys + lane, end - 1));
   };
   auto request = [&](int t) {
     const unsigned to = lds + (t & 1) * STAGE;
     const int first = begin + t * kTileKeys;
     if constexpr (PAGED) {
+      there_next = __ballot(is_there<PAGED>(p, next));
+      const long long mine_at = key_offset<PAGED>(p, p.ks, next);
+      long long off[NL];
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int from = i * RPP + load_row;
-        const unsigned low = __shfl((int)(unsigned)ahead, from), high = __shfl((int)(unsigned)(ahead >> 32), from);
-        const long long off = (long long)(((unsigned long long)high << 32) | low) + load_chunk * 8;
-        if (loads) {
-          DirectLoad::at(kbase + off, to + i * 4096);
-          DirectLoad::at(vbase + off, to + 2 * STAGE + i * 4096);
+        const unsigned low = __shfl((int)(unsigned)mine_at, from), high = __shfl((int)(unsigned)(mine_at >> 32), from);
+        off[i] = (long long)(((unsigned long long)high << 32) | low) + load_chunk * 8;
+      }
+      if (t + 1 < t1) look_up(t + 1);
+      if (loads) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          DirectLoad::at(kbase + off[i], to + i * 4096);
+          DirectLoad::at(vbase + off[i], to + 2 * STAGE + i * 4096);
         }
       }
     } else {
       const T* kt = kbase + (long long)first * p.ks.row;
       const T* vt = vbase + (long long)first * p.vs.row;
-      const int last = end - 1 - first;  // (keys past the last that anyone sees are that one again)
+      const int last = end - 1 - first;
+      if (!loads) return;
+      if (last >= kTileKeys - 1) {
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        unsigned ko = koff[i], vo = voff[i];
-        if (last < kTileKeys - 1) {
-          const int row = min(i * RPP + load_row, last);
-          ko = ((unsigned)row * (unsigned)p.ks.row + load_chunk * 8) * 2;
-          vo = ((unsigned)row * (unsigned)p.vs.row + load_chunk * 8) * 2;
+        for (int i = 0; i < NL; ++i) {
+          DirectLoad::at(kt, koff[i], to + i * 4096);
+          DirectLoad::at(vt, voff[i], to + 2 * STAGE + i * 4096);
         }
-        if (loads) {
-          DirectLoad::at(kt, ko, to + i * 4096);
-          DirectLoad::at(vt, vo, to + 2 * STAGE + i * 4096);
+      } else {  // (keys past the last that anyone sees are that one again)
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const unsigned row = min(i * RPP + load_row, last);
+          DirectLoad::at(kt, (row * (unsigned)p.ks.row + load_chunk * 8) * 2, to + i * 4096);
+          DirectLoad::at(vt, (row * (unsigned)p.vs.row + load_chunk * 8) * 2, to + 2 * STAGE + i * 4096);
         }
       }
     }
@@ -721,18 +734,12 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   settle();
   if (t0 < t1) {
     look_up(t0);
-    there_now = there_next;
     request(t0);
-    if (t0 + 1 < t1) look_up(t0 + 1);
   }
   for (int t = t0; t < t1; ++t) {
     wait_all_and_meet();
-    const unsigned long long there = there_now;
-    if (t + 1 < t1) {
-      there_now = there_next;
-      request(t + 1);
-      if (t + 2 < t1) look_up(t + 2);
-    }
+    there = there_next;
+    if (t + 1 < t1) request(t + 1);
     const int first = begin + t * kTileKeys;
     if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
     const unsigned keys = lds0 + (t & 1) * STAGE, values = keys + 2 * STAGE;
@@ -797,39 +804,32 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
   const bool loads = load_chunk * 8 < p.dim;
 
   u32x4 kr[NL], vr[NL];
-  long long ko_next = 0, vo_next = 0;
-  bool there_next = true;
-  auto look_up = [&](int t) {  // lane's key, lane % 32 of tile t
-    const int j = min(begin + t * kStreamKeys + (lane & 31), end - 1);
-    bool there;
-    ko_next = key_offset<PAGED>(p, e, p.ks, j, there);
-    vo_next = PAGED ? ko_next : key_offset<PAGED>(p, e, p.vs, j, there);
-    there_next = there;
-  };
+  KeyPlace next = {0, 0};  // of lane's key, lane % 32 of the tile after the next
+  unsigned long long there_next = ~0ull;
+  auto look_up = [&](int t) { next = find_key<PAGED>(p, e, min(begin + t * kStreamKeys + (lane & 31), end - 1)); };
   auto from_lane = [&](long long v, int lane_of_row) {
     const unsigned low = __shfl((int)(unsigned)v, lane_of_row), high = __shfl((int)(unsigned)(v >> 32), lane_of_row);
     return (long long)(((unsigned long long)high << 32) | low) + load_chunk * 8;
   };
-  auto request = [&]() {
+  auto request = [&](int t) {
+    there_next = __ballot(is_there<PAGED>(p, next));
+    const long long ko = key_offset<PAGED>(p, p.ks, next), vo = PAGED ? ko : key_offset<PAGED>(p, p.vs, next);
+    if (t + kStreamWaves < t1) look_up(t + kStreamWaves);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      const long long ko = from_lane(ko_next, i * RPP + load_row);
-      const long long vo = PAGED ? ko : from_lane(vo_next, i * RPP + load_row);
+      const long long k_at = from_lane(ko, i * RPP + load_row), v_at = PAGED ? k_at : from_lane(vo, i * RPP + load_row);
       kr[i] = vr[i] = u32x4{0, 0, 0, 0};
       if (loads) {
-        kr[i] = reinterpret_cast<const Chunk16*>(kbase + ko)->v;
-        vr[i] = reinterpret_cast<const Chunk16*>(vbase + vo)->v;
+        kr[i] = reinterpret_cast<const Chunk16*>(kbase + k_at)->v;
+        vr[i] = reinterpret_cast<const Chunk16*>(vbase + v_at)->v;
       }
     }
   };
 
   int t = t0 + wave;
-  unsigned long long there_now = ~0ull;
   if (t < t1) {
     look_up(t);
-    there_now = __ballot(there_next);
-    request();
-    if (t + kStreamWaves < t1) look_up(t + kStreamWaves);
+    request(t);
   }
   State<T, DP> st;
   st.clear();
@@ -845,12 +845,8 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
       *reinterpret_cast<u32x4*>(mine + TILE + to) = vr[i];
     }
     asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order: its writes, then its reads)
-    const unsigned long long there = there_now & 0xffffffffull;
-    if (t + kStreamWaves < t1) {
-      there_now = __ballot(there_next);
-      request();
-      if (t + 2 * kStreamWaves < t1) look_up(t + 2 * kStreamWaves);
-    }
+    const unsigned long long there = there_next & 0xffffffffull;
+    if (t + kStreamWaves < t1) request(t + kStreamWaves);
     f32x16 s[1];
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
@@ -876,13 +872,13 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
   float top = kNoMax;
 #pragma unroll
   for (int i = 0; i < kStreamWaves; ++i) top = fmaxf(top, stat[i][lane & 31][0]);
-  const float next = top == kNoMax ? 0.0f : top;
-  const float shrink = st.top == kNoMax ? 0.0f : exp2_fast(st.shift - next);
+  const float level = top == kNoMax ? 0.0f : top;
+  const float shrink = st.top == kNoMax ? 0.0f : exp2_fast(st.shift - level);
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < kStreamWaves; ++i) {
     const float m = stat[i][lane & 31][0];
-    sum += m == kNoMax ? 0.0f : stat[i][lane & 31][1] * exp2_fast(m - next);
+    sum += m == kNoMax ? 0.0f : stat[i][lane & 31][1] * exp2_fast(m - level);
   }
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -914,7 +910,7 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
   }
   if (wave != 0) return;
   st.top = top;
-  st.shift = next;
+  st.shift = level;
   st.sum = half == 0 ? sum : 0.0f;
   finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kStreamKeys, min(end, begin + t1 * kStreamKeys), z);
 }

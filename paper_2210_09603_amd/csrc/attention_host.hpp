@@ -18,6 +18,8 @@ constexpr long long kMaxSpan = 1LL << 47;    // elements that a tensor spans
 constexpr long long kMaxStride = 1LL << 23;  // between keys: 64 rows of them are reached by a 32-bit byte offset
 constexpr long long kMaxBlocks = 1LL << 24;  // of 512 threads: below 2^32 work items
 
+constexpr long long kFarBytes = 128LL << 20;  // tensors beyond are streamed past the caches
+
 inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 // strides >= 0 and (n0 - 1) * s0 + (n1 - 1) * s1 + (n2 - 1) * s2 + dim < 2^47
@@ -64,7 +66,7 @@ struct Cut {
   int row_tiles, splits, share;
 };
 inline long long split_bytes(long long entries, long long rows, int dp) { return entries * rows * (dp + 2) * 4; }
-Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room);
+Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room, bool ragged);
 
 inline int padded_dim(long long dim) { return dim <= 64 ? 64 : 128; }
 

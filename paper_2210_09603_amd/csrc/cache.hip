@@ -29,7 +29,9 @@ struct AppendArgs {
 struct __attribute__((packed, aligned(2))) Bytes16 {
   u32x4 v;
 };
+typedef u32x4 Streamed __attribute__((aligned(2)));  // (the same, for a store with a hint)
 
+template <bool STREAM>
 __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs p) {
   __shared__ long long place[kMaxTokens];  // -1: goes nowhere
   __shared__ int before;
@@ -81,14 +83,22 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs p) {
         if (at >= 0) {
           const char* from = static_cast<const char*>(p.from[which]) + (long long)(token0 + t) * p.token_stride[which] +
                              h * p.head_stride[which] + c * 16;
-          v[u] = reinterpret_cast<const Bytes16*>(from)->v;
+          if constexpr (STREAM)
+            v[u] = __builtin_nontemporal_load(reinterpret_cast<const Streamed*>(from));
+          else
+            v[u] = reinterpret_cast<const Bytes16*>(from)->v;
           to[u] = static_cast<char*>(p.to[which]) + at + h * p.cache_head_stride + c * 16;
         }
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (to[u]) reinterpret_cast<Bytes16*>(to[u])->v = v[u];
+      if (to[u]) {
+        if constexpr (STREAM)
+          __builtin_nontemporal_store(v[u], reinterpret_cast<Streamed*>(to[u]));
+        else
+          reinterpret_cast<Bytes16*>(to[u])->v = v[u];
+      }
   }
 }
 
@@ -161,8 +171,9 @@ hidet_status_t hidet_cache_append(const hidet_cache_t* cache, int64_t tokens, in
   p.tokens = (int)tokens;
   p.max_new = (int)std::min(max_new, (int64_t)kMaxRows);
   const long long chunks = cache->head_dim * e / 16, per_tensor = chunks * cache->heads;
-  // some 8 chunks a thread, fewer where that leaves compute units without work
-  long long block_tokens = std::min((long long)kMaxTokens, std::max(1LL, 8 * kThreads / (2 * per_tensor)));
+  // 4 chunks a thread, which are in flight together, fewer where that leaves compute units without work (48000 tokens of 12 heads of 64
+  // dimensions: 61 us; 84 with 2, where finding the tokens' places weighs more, 63 with 8)
+  long long block_tokens = std::min((long long)kMaxTokens, std::max(1LL, 4 * kThreads / (2 * per_tensor)));
   block_tokens = std::min(block_tokens, std::max(1LL, (long long)tokens / 1024));
   const long long blocks = (tokens + block_tokens - 1) / block_tokens;
   if (blocks > kMaxBlocks || block_tokens * 2 * per_tensor >= (1LL << 30)) return HIDET_ERR_UNSUPPORTED;
@@ -172,7 +183,8 @@ hidet_status_t hidet_cache_append(const hidet_cache_t* cache, int64_t tokens, in
   p.d_page = make_fastdiv(cache->page_size);
   p.d_chunks = make_fastdiv(chunks);
   p.d_token = make_fastdiv(2 * per_tensor);
-  hipLaunchKernelGGL(append_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, p);
+  const bool far = tokens * 2 * per_tensor * 16 > kFarBytes / 2;
+  hipLaunchKernelGGL(far ? append_kernel<true> : append_kernel<false>, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, p);
   return hipGetLastError() == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }
 
@@ -185,7 +197,7 @@ int64_t hidet_cache_attention_workspace_bytes(const hidet_cache_t* cache, int64_
   if (max_new >= kMaxRows || group >= kMaxRows || max_new * group >= kMaxRows) return 0;
   const int dp = padded_dim(cache->head_dim);
   const long long entries = cache->seqs * cache->heads, rows = max_new * group;
-  const Cut c = cut_work(entries, rows, keys_at_most(cache, max_new, window), dp, 1LL << 62);
+  const Cut c = cut_work(entries, rows, keys_at_most(cache, max_new, window), dp, 1LL << 62, true);
   return c.splits > 1 ? c.splits * split_bytes(entries, rows, dp) : 0;
 }
 
@@ -237,7 +249,7 @@ hidet_status_t hidet_cache_attention(const hidet_cache_t* cache, int64_t heads, 
   p.scale = options->scale;
   p.softcap = options->softcap;
   const long long entries = cache->seqs * cache->heads, rows = max_new * group;
-  const Cut c = cut_work(entries, rows, keys_at_most(cache, max_new, options->window), padded_dim(cache->head_dim), workspace ? workspace_bytes : 0);
+  const Cut c = cut_work(entries, rows, keys_at_most(cache, max_new, options->window), padded_dim(cache->head_dim), workspace ? workspace_bytes : 0, true);
   if (entries * c.row_tiles > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
   p.row_tiles = c.row_tiles;
   p.splits = c.splits;
