@@ -16,18 +16,23 @@ namespace attn {
 //   Few rows: 512 workgroups fill the device, which is worth a partial result for 16 tiles of 32 keys (one sequence of 131000 keys, 2 kv
 //   heads: 39 us with 16, 40 with 32, 56 with 64); up to 2048 even out a ragged batch, as long as 64 tiles remain (64 sequences of 100 to
 //   8000 keys, 8 kv heads: 220 us; 231 with 1024 workgroups, 225 with 4096 of 16 tiles).
-//   Tiles of 128 rows: where they leave compute units without any, and 8 tiles of 64 keys remain (more, and the second kernel costs
-//   what it gains: 36 x 8 tiles of 1021 keys, 64 dimensions, 32 us whole and 26 + 10 split).  Of a ragged batch's tiles some have no
-//   rows: four times as many (chunks of 4 prompts of 37 to 512 tokens over 4096 keys: 157 us, 192 with a quarter).
+//   Tiles of 128 rows: up to 512 of them take pairs of wavefronts, and as many splits as leave a compute unit for each (more would be
+//   a second round: 210 tiles of 2068 keys 52 us whole, 69 in halves) of at least 4 tiles of 128 keys (n heads of as many rows as keys, us with plain wavefronts, with pairs, and what is taken: 128 dimensions, 4
+//   heads of 4096 97, 69, 50 split in 2; 8 of 2048 52, 40, 34; 32 of 1024 31, 27, 27; 32 of 2048, 512 tiles, 79 without pairs and 80
+//   with; 64 dimensions, 4 of 4096 59, 45, 33; 12 of 1024 18.7, 17.0, 16.9; 12 of 512 13.1, 12.9, 13.6).  Of a ragged batch's tiles
+//   some have no rows: four times as many (chunks of 4 prompts of 37 to 512 tokens over 4096 keys: 157 us, 192 with a quarter).
 Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room, bool ragged) {
   Cut c;
   const long long pieces = entries * ((rows + 31) / 32);
   c.stream = rows <= 32 || (keys > kTileKeys && pieces <= 256 && pieces * ((keys + 31) / 32) <= 4096);
-  const long long tile = c.stream ? 32 : 128, tile_keys = c.stream ? kStreamKeys : kTileKeys;
+  const long long tile = c.stream ? 32 : 128;
   c.row_tiles = (int)((rows + tile - 1) / tile);
-  const long long blocks = entries * c.row_tiles, tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys);
+  const long long blocks = entries * c.row_tiles;
+  c.pairs = !c.stream && !ragged && blocks < 512 && keys > kTileKeys;
+  const long long tile_keys = c.stream ? kStreamKeys : c.pairs ? 2 * kTileKeys : kTileKeys;
+  const long long tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys);
   const auto wish = [&](long long workgroups, long long least) { return std::min((workgroups + blocks - 1) / blocks, tiles / least); };
-  long long splits = c.stream ? std::max(wish(512, 16), wish(2048, 64)) : wish(ragged ? 1024 : 256, 8);
+  long long splits = c.stream ? std::max(wish(512, 8), wish(2048, 64)) : ragged ? wish(1024, 8) : c.pairs ? std::min(256 / blocks, tiles / 4) : 1;
   splits = std::max(1LL, std::min(splits, room / split_bytes(entries, rows, dp)));
   const long long share = (tiles + splits - 1) / splits;
   c.share = (int)share;
@@ -175,7 +180,9 @@ hidet_status_t hidet_attention(int32_t dtype, int64_t batch, int64_t heads, int6
   p.window = window_of(options->window);
   p.scale = options->scale;
   p.softcap = options->softcap;
-  const Cut c = cut_work(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim), workspace ? workspace_bytes : 0, false);
+  // (a window leaves the 128 rows of a tile no more keys than this)
+  const long long keys = options->window > 0 ? std::min<long long>(seq_k, 2LL * std::min<long long>(options->window, kMaxRows) + 128) : seq_k;
+  const Cut c = cut_work(batch * kv_heads, seq_q * group, keys, padded_dim(head_dim), workspace ? workspace_bytes : 0, false);
   if (batch * kv_heads * c.row_tiles > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
   p.row_tiles = c.row_tiles;
   p.splits = c.splits;

@@ -597,12 +597,8 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
 // ---- the kernel of many rows ------------------------------------------------------------------------------------------------
 // A workgroup of 4 wavefronts works on 128 rows, 32 a wavefront, and walks over the keys that one of them sees in tiles of 64,
 // which arrive in LDS by direct loads one tile ahead (2 stages of 16 KB of keys and of values at 128 dimensions: two workgroups a
-// compute unit, so that one's products run beside the other's exponentials).
-template <int DP>
-constexpr int tile_lds_bytes() {
-  return 2 * 2 * kTileKeys * DP * 2;
-}
-
+// compute unit, so that one's products run beside the other's exponentials).  Where there is not a second workgroup for every compute
+// unit, 8 wavefronts (PAIRS 2): two of them share 32 rows and take the halves of tiles of 128 keys, and meet at the end.
 // Workgroups are dealt to the 8 XCDs in turn, each with an L2 of its own: the pieces of an entry (a batch entry's or sequence's kv head)
 // go to one XCD, one entry after the other, so that they read its keys from the same L2; every eighth entry, so that the heads of a
 // long sequence are spread.  What is left of the entries is cut into contiguous runs.  (Chunks of 4 prompts of 37 to 512 tokens, 8 kv
@@ -621,18 +617,21 @@ __device__ __forceinline__ Place place_of(int w, int entries, int pieces) {
   return Place{(entries & ~7) + turn, at - turn * pieces};
 }
 
-template <typename T, int DP, bool PAGED, int FORM>
-__global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
-  constexpr int CPR = DP / 8, STAGE = kTileKeys * CPR * 16, NL = kTileKeys * CPR / 256, RPP = 256 / CPR, KS = DP / 16, DT = DP / 32;
+template <typename T, int DP, bool PAGED, int FORM, int PAIRS>
+__global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
+  static_assert(PAIRS == 1 || !PAGED, "a wavefront looks up 64 keys");
+  constexpr int THREADS = 256 * PAIRS, TILE = kTileKeys * PAIRS;  // keys of a tile
+  constexpr int CPR = DP / 8, STAGE = TILE * CPR * 16, NL = TILE * CPR / THREADS, RPP = THREADS / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * STAGE];  // keys of two stages, values of two
   __shared__ int bounds[4][2];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int own = (wave >> 2) * kTileKeys;  // the first of its 64 keys of a tile
 
   const Place place = place_of(blockIdx.x, p.batch * p.kv_heads, p.row_tiles * p.splits);
   const int z = place.piece % p.splits, tile = p.row_tiles - 1 - place.piece / p.splits;  // (causal: the longest first)
   const Entry e = make_entry<PAGED>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
-  const int rows = e.tokens * p.group, r0 = tile * 128 + wave * 32;
+  const int rows = e.tokens * p.group, r0 = tile * 128 + (wave & 3) * 32;
   if (tile * 128 >= rows) return;  // (the whole workgroup)
 
   // (rows past the last are the last again, and not stored)
@@ -641,7 +640,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   const Seen mine = seen_by<PAGED>(p, e, w, min(r0, rows - 1), min(r0 + 31, rows - 1));
   int begin, end;  // of the workgroup
   if (!PAGED && p.ranges) {
-    if (lane == 0) {
+    if (lane == 0 && wave < 4) {
       bounds[wave][0] = mine.lo;
       bounds[wave][1] = mine.hi;
     }
@@ -656,7 +655,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   const bool narrow = p.dim < DP;
   if (narrow)  // the chunks past the head's dimension, which no load fills
-    for (int i = tid; i < 4 * STAGE / 16; i += 256) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
+    for (int i = tid; i < 4 * STAGE / 16; i += THREADS) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
   if (!PAGED && p.ranges) {
     begin = min(min(bounds[0][0], bounds[1][0]), min(bounds[2][0], bounds[3][0]));
@@ -666,7 +665,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   }
   if (begin >= end) begin = end = 0;
   // this split's share of the tiles, the first of which begins with the first key that anyone sees
-  const int all = (end - begin + kTileKeys - 1) / kTileKeys;
+  const int all = (end - begin + TILE - 1) / TILE;
   const int t0 = min(all, z * p.share), t1 = z + 1 < p.splits ? min(all, t0 + p.share) : all;
 
   const T* kbase = keys_of<T, PAGED>(p, e, p.k, p.ks);
@@ -686,11 +685,11 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
   KeyPlace next = {0, 0};  // paged: where lane l's key of the tile after the next is
   unsigned long long there = ~0ull, there_next = ~0ull;
   auto look_up = [&](int t) {
-    if constexpr (PAGED) next = find_key<PAGED>(p, e, min(begin + t * kTileKeys + lane, end - 1));
+    if constexpr (PAGED) next = find_key<PAGED>(p, e, min(begin + t * TILE + lane, end - 1));
   };
   auto request = [&](int t) {
     const unsigned to = lds + (t & 1) * STAGE;
-    const int first = begin + t * kTileKeys;
+    const int first = begin + t * TILE;
     if constexpr (PAGED) {
       there_next = __ballot(is_there<PAGED>(p, next));
       const long long mine_at = key_offset<PAGED>(p, p.ks, next);
@@ -705,8 +704,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
       if (loads) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-          DirectLoad::at(kbase + off[i], to + i * 4096);
-          DirectLoad::at(vbase + off[i], to + 2 * STAGE + i * 4096);
+          DirectLoad::at(kbase + off[i], to + i * (THREADS * 16));
+          DirectLoad::at(vbase + off[i], to + 2 * STAGE + i * (THREADS * 16));
         }
       }
     } else {
@@ -714,18 +713,18 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
       const T* vt = vbase + (long long)first * p.vs.row;
       const int last = end - 1 - first;
       if (!loads) return;
-      if (last >= kTileKeys - 1) {
+      if (last >= TILE - 1) {
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
-          DirectLoad::at(kt, koff[i], to + i * 4096);
-          DirectLoad::at(vt, voff[i], to + 2 * STAGE + i * 4096);
+          DirectLoad::at(kt, koff[i], to + i * (THREADS * 16));
+          DirectLoad::at(vt, voff[i], to + 2 * STAGE + i * (THREADS * 16));
         }
       } else {  // (keys past the last that anyone sees are that one again)
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
           const unsigned row = min(i * RPP + load_row, last);
-          DirectLoad::at(kt, (row * (unsigned)p.ks.row + load_chunk * 8) * 2, to + i * 4096);
-          DirectLoad::at(vt, (row * (unsigned)p.vs.row + load_chunk * 8) * 2, to + 2 * STAGE + i * 4096);
+          DirectLoad::at(kt, (row * (unsigned)p.ks.row + load_chunk * 8) * 2, to + i * (THREADS * 16));
+          DirectLoad::at(vt, (row * (unsigned)p.vs.row + load_chunk * 8) * 2, to + 2 * STAGE + i * (THREADS * 16));
         }
       }
     }
@@ -740,9 +739,9 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
     wait_all_and_meet();
     there = there_next;
     if (t + 1 < t1) request(t + 1);
-    const int first = begin + t * kTileKeys;
+    const int first = begin + t * TILE + own;
     if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
-    const unsigned keys = lds0 + (t & 1) * STAGE, values = keys + 2 * STAGE;
+    const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
     f32x16 s[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -759,7 +758,30 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args p) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
   }
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kTileKeys, min(end, begin + t1 * kTileKeys), z);
+  if constexpr (PAIRS == 2) {
+    __syncthreads();
+    float* meet = reinterpret_cast<float*>(smem) + (wave & 3) * (DT * 16 + 2) * 64 + lane;
+    if (wave >= 4) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) meet[(d * 16 + r) * 64] = st.o[d][r];
+      meet[DT * 16 * 64] = st.top == kNoMax ? kNoMax : st.shift;
+      meet[(DT * 16 + 1) * 64] = st.sum;
+    }
+    __syncthreads();
+    if (wave >= 4) return;
+    const float other = meet[DT * 16 * 64], own_level = st.top == kNoMax ? kNoMax : st.shift;
+    const float top = fmaxf(own_level, other), level = top == kNoMax ? 0.0f : top;
+    const float by = own_level == kNoMax ? 0.0f : exp2_fast(own_level - level), by_other = other == kNoMax ? 0.0f : exp2_fast(other - level);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st.o[d][r] = st.o[d][r] * by + meet[(d * 16 + r) * 64] * by_other;
+    st.sum = st.sum * by + meet[(DT * 16 + 1) * 64] * by_other;
+    st.shift = level;
+  }
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * TILE, min(end, begin + t1 * TILE), z);
 }
 
 // ---- the kernel of few rows ---------------------------------------------------------------------------------------------------

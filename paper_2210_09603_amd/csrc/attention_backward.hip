@@ -33,6 +33,7 @@ struct BackArgs {
   float* part;    // partial sums of the splits: dQ's [split][kv row][DP], then dK's and dV's [split][entry][key][2][DP]
   int row_groups;
   int key_tiles;
+  int dq_pairs;               // two wavefronts for 32 rows
   int dq_splits, dq_share;    // share: tiles of keys of a split
   int dkv_splits, dkv_share;  // share: tiles of rows
   int regular;    // 32 rows hold whole tokens, and offsets within them fit 32 bits
@@ -198,27 +199,29 @@ __device__ __forceinline__ float* dkv_part(const BackArgs& b, int z, const Entry
 }
 
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
-// The forward kernel's walk, with dout and out beside q.
-template <typename T, int DP, int FORM>
-__global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
-  constexpr int CPR = DP / 8, STAGE = kTileKeys * CPR * 16, NL = kTileKeys * CPR / 256, RPP = 256 / CPR, KS = DP / 16, DT = DP / 32;
+// The forward kernel's walk, with dout and out beside q, and its pairs of wavefronts.
+template <typename T, int DP, int FORM, int PAIRS>
+__global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
+  constexpr int THREADS = 256 * PAIRS, TILE = kTileKeys * PAIRS;  // keys of a tile
+  constexpr int CPR = DP / 8, STAGE = TILE * CPR * 16, NL = TILE * CPR / THREADS, RPP = THREADS / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * STAGE];
   __shared__ int bounds[4][2];
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int own = (wave >> 2) * kTileKeys;  // the first of its 64 keys of a tile
 
   const Place place = place_of(blockIdx.x, p.batch * p.kv_heads, p.row_tiles * b.dq_splits);
   const int z = place.piece % b.dq_splits, tile = p.row_tiles - 1 - place.piece / b.dq_splits;
   const Entry e = make_entry<false>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
-  const int rows = e.tokens * p.group, r0 = tile * 128 + wave * 32;
+  const int rows = e.tokens * p.group, r0 = tile * 128 + (wave & 3) * 32;
 
   const Row w = make_row<false>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
   const Seen mine = seen_by<false>(p, e, w, min(r0, rows - 1), min(r0 + 31, rows - 1));
   int begin, end;  // of the workgroup
   if (p.ranges) {
-    if (lane == 0) {
+    if (lane == 0 && wave < 4) {
       bounds[wave][0] = mine.lo;
       bounds[wave][1] = mine.hi;
     }
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
     begin = all.lo;
     end = all.hi;
   }
-  if (lane == 0 && e.kv == 0 && z == 0 && r0 < rows) b.seen[(long long)e.b * b.row_groups + (r0 >> 5)] = int4{mine.lo, mine.hi, mine.full_lo, mine.full_hi};
+  if (lane == 0 && wave < 4 && e.kv == 0 && z == 0 && r0 < rows) b.seen[(long long)e.b * b.row_groups + (r0 >> 5)] = int4{mine.lo, mine.hi, mine.full_lo, mine.full_hi};
   Frag q[KS], g[KS];
   load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<false>(p, e, p.qs, w), half, p.dim, q);
   load_row_frags<T, DP>(reinterpret_cast<const T*>(b.dout) + query_offset<false>(p, e, b.dos, w), half, p.dim, g);
@@ -243,7 +246,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   delta = sum_of_halves(delta);
   const long long stat = lse_offset<false>(p, e, w);
   const float lse = lse_to_base_2(p.lse[stat]);
-  if (half == 0 && z == 0) {
+  if (half == 0 && wave < 4 && z == 0) {
     const int r = r0 + lane;
     const bool is = r < rows;
     *row_info<FORM>(b, e, r, 0) = (is ? lse : __builtin_huge_valf()) - kLiftBits;
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   }
   const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   if (p.dim < DP)
-    for (int i = tid; i < 4 * STAGE / 16; i += 256) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
+    for (int i = tid; i < 4 * STAGE / 16; i += THREADS) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
   if (p.ranges) {
     begin = min(min(bounds[0][0], bounds[1][0]), min(bounds[2][0], bounds[3][0]));
@@ -266,7 +269,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
     end = __builtin_amdgcn_readfirstlane(end);
   }
   if (begin >= end) begin = end = 0;
-  const int all = (end - begin + kTileKeys - 1) / kTileKeys;
+  const int all = (end - begin + TILE - 1) / TILE;
   const int t0 = min(all, z * b.dq_share), t1 = z + 1 < b.dq_splits ? min(all, t0 + b.dq_share) : all;
 
   const T* kbase = keys_of<T, false>(p, e, p.k, p.ks);
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   const ReadMap<DP> map(lane);
   auto request = [&](int t) {
     const unsigned to = lds + (t & 1) * STAGE;
-    const int first = begin + t * kTileKeys, last = end - 1 - first;
+    const int first = begin + t * TILE, last = end - 1 - first;
     const T* kt = kbase + (long long)first * p.ks.row;
     const T* vt = vbase + (long long)first * p.vs.row;
 #pragma unroll
@@ -286,8 +289,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
       const unsigned ko = ((unsigned)row * (unsigned)p.ks.row + load_chunk * 8) * 2;
       const unsigned vo = ((unsigned)row * (unsigned)p.vs.row + load_chunk * 8) * 2;
       if (loads) {
-        DirectLoad::at(kt, ko, to + i * 4096);
-        DirectLoad::at(vt, vo, to + 2 * STAGE + i * 4096);
+        DirectLoad::at(kt, ko, to + i * (THREADS * 16));
+        DirectLoad::at(vt, vo, to + 2 * STAGE + i * (THREADS * 16));
       }
     }
   };
@@ -301,9 +304,9 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
   for (int t = t0; t < t1; ++t) {
     wait_all_and_meet();
     if (t + 1 < t1) request(t + 1);
-    const int first = begin + t * kTileKeys;
+    const int first = begin + t * TILE + own;
     if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
-    const unsigned keys = lds0 + (t & 1) * STAGE, values = keys + 2 * STAGE;
+    const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
     const bool masked = first < mine.full_lo || first + kTileKeys > mine.full_hi;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -334,6 +337,22 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(const BackArgs b) {
 #pragma unroll
         for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, DP>(map, keys, c * 32 + h * 16, d), ds[h], acc[d]);
     }
+  }
+  if constexpr (PAIRS == 2) {
+    __syncthreads();
+    float* meet = reinterpret_cast<float*>(smem) + (wave & 3) * (DT * 16 * 64) + lane;
+    if (wave >= 4) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) meet[(d * 16 + r) * 64] = acc[d][r];
+    }
+    __syncthreads();
+    if (wave >= 4) return;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] += meet[(d * 16 + r) * 64];
   }
   if (b.dq_splits > 1) {
     if (r0 + (lane & 31) < rows) store_part<DT>(dq_part<DP>(b, z, e, r0 + (lane & 31)), acc, half);
@@ -684,7 +703,11 @@ hipError_t launch(const BackArgs& b, hipStream_t stream) {
   const Args& p = b.f;
   const long long entries = (long long)p.batch * p.kv_heads;
   if (p.seq_q > 0) {
-    hipLaunchKernelGGL((dq_kernel<T, DP, FORM>), dim3((unsigned)(entries * p.row_tiles * b.dq_splits)), dim3(256), 0, stream, b);
+    const dim3 grid((unsigned)(entries * p.row_tiles * b.dq_splits));
+    if (b.dq_pairs)
+      hipLaunchKernelGGL((dq_kernel<T, DP, FORM, 2>), grid, dim3(512), 0, stream, b);
+    else
+      hipLaunchKernelGGL((dq_kernel<T, DP, FORM, 1>), grid, dim3(256), 0, stream, b);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (b.dq_splits > 1) {
       const long long rows = entries * p.seq_q * p.group;
@@ -720,15 +743,21 @@ long long row_groups_of(long long rows) { return (rows + 31) / 32; }
 // (of all forms: with a bias twice the fields)
 long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
 
-// How the two kernels' work is cut: tiles of 128 rows and of 64 keys, and these into splits where they would leave compute units
-// without work, as long as a split keeps some tiles of the other axis.
+// How the two kernels' work is cut.
+//   dQ: tiles of 128 rows, in pairs of wavefronts as in the forward pass where they are fewer than 512, and then as many splits of at
+//   least 4 tiles of 128 keys as find a compute unit each.  A whole pass (forward, dQ, dK and dV) without and with pairs, us: 6 entries of
+//   3146 rows of 96 dimensions 170 and 152, 9 of 3332 at 128 470 and 429, 36 of 1021 at 64 125 and 122; one fit worse, 4 entries of 1472
+//   rows over 184 keys 47 and 50.
+//   dK and dV: tiles of 64 keys, and where they leave compute units without work splits of at least 2 tiles of 128 rows: 256 workgroups
+//   (512 at 64 dimensions, where two fit a compute unit).  With 512 of at least 4 everywhere: the first of the passes above 220 for 190,
+//   the second 486 for 449, and 285 for 271 of 2 entries of 6599 rows.
 struct BackCut {
   int row_tiles, key_tiles, dq_splits, dq_share, dkv_splits, dkv_share;
+  bool dq_pairs;
   long long part_bytes;
 };
-void split(long long blocks, long long tiles, long long wanted, long long least, int& splits, int& share) {
-  long long n = blocks >= wanted ? 1 : (wanted + blocks - 1) / blocks;
-  n = std::max(1LL, std::min(n, tiles / least));
+void split(long long tiles, long long n, int& splits, int& share) {
+  n = std::max(1LL, n);
   share = (int)std::max(1LL, (tiles + n - 1) / n);
   splits = (int)std::max(1LL, (tiles + share - 1) / share);
 }
@@ -736,8 +765,13 @@ BackCut cut_backward(long long entries, long long rows, long long keys, int dp) 
   BackCut c;
   c.row_tiles = (int)((rows + 127) / 128);
   c.key_tiles = (int)((keys + kBlockKeys - 1) / kBlockKeys);
-  split(std::max(1LL, entries * c.row_tiles), (keys + kTileKeys - 1) / kTileKeys, 256, 8, c.dq_splits, c.dq_share);
-  split(std::max(1LL, entries * c.key_tiles), (rows + kTileRows - 1) / kTileRows, 512, 4, c.dkv_splits, c.dkv_share);
+  const long long row_blocks = std::max(1LL, entries * c.row_tiles), key_blocks = std::max(1LL, entries * c.key_tiles);
+  c.dq_pairs = row_blocks < 512 && keys > kTileKeys;
+  const long long tile_keys = c.dq_pairs ? 2 * kTileKeys : kTileKeys;
+  const long long tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys), row_tiles = std::max(1LL, (rows + kTileRows - 1) / kTileRows);
+  split(tiles, c.dq_pairs ? std::min(256 / row_blocks, tiles / 4) : 1, c.dq_splits, c.dq_share);
+  const long long wanted = dp == 64 ? 512 : 256;
+  split(row_tiles, std::min((wanted + key_blocks - 1) / key_blocks, row_tiles / 2), c.dkv_splits, c.dkv_share);
   const long long dq = c.dq_splits > 1 ? c.dq_splits * entries * rows * dp * 4 : 0;
   const long long dkv = c.dkv_splits > 1 ? c.dkv_splits * entries * keys * dp * 8 : 0;
   c.part_bytes = std::max(dq, dkv);
@@ -833,6 +867,7 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
   p.row_tiles = c.row_tiles;
   b.row_groups = (int)row_groups_of(seq_q * group);
   b.key_tiles = c.key_tiles;
+  b.dq_pairs = c.dq_pairs;
   b.dq_splits = c.dq_splits;
   b.dq_share = c.dq_share;
   // (without queries there is no workspace, and nothing to add up)

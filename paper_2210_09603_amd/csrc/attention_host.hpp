@@ -63,6 +63,7 @@ inline int form_of(const hidet_attention_options_t* o) {
 // How the work of `entries` (batch entries x kv heads) of `rows` rows each over up to `keys` keys is cut.
 struct Cut {
   bool stream;  // the kernel of few rows
+  bool pairs;   // that of many with two wavefronts for 32 rows
   int row_tiles, splits, share;
 };
 inline long long split_bytes(long long entries, long long rows, int dp) { return entries * rows * (dp + 2) * 4; }
@@ -75,8 +76,10 @@ hipError_t launch_forward(const Args& p, const Cut& c, hipStream_t stream) {
   const long long blocks = (long long)p.batch * p.kv_heads * c.row_tiles * c.splits;
   if (c.stream)
     hipLaunchKernelGGL((stream_kernel<T, DP, PAGED, FORM>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), 0, stream, p);
+  else if (!PAGED && c.pairs)
+    hipLaunchKernelGGL((tile_kernel<T, DP, PAGED, FORM, PAGED ? 1 : 2>), dim3((unsigned)blocks), dim3(512), 0, stream, p);
   else
-    hipLaunchKernelGGL((tile_kernel<T, DP, PAGED, FORM>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((tile_kernel<T, DP, PAGED, FORM, 1>), dim3((unsigned)blocks), dim3(256), 0, stream, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || c.splits == 1) return e;
   const long long rows = (long long)p.batch * p.kv_heads * p.seq_q * p.group;
   if (c.splits > 16)

@@ -107,6 +107,30 @@ def test_full_and_causal(size, dtype):
         _run(1000 + 10 * SIZES.index(size) + i, dtype, *size, causal=causal, layout=("dense", "tokens", "odd")[SIZES.index(size) % 3])
 
 
+# (512 tiles of 128 rows: a wavefront for 32 rows, where fewer take two)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [(128, 4, 4, 40, 150, 64), (86, 12, 6, 19, 193, 112)], ids=str)
+def test_many_tiles(size, dtype):
+    _run(22, dtype, *size)
+    _run(22, dtype, *size, causal=True, window=40, softcap=10.0, slopes=True, layout="tokens")
+
+
+def test_many_tiles_under_ranges_with_values_that_must_not_matter():
+    g = np.random.Generator(np.random.PCG64(23))
+    b, n, m = 128, 40, 150
+    ranges = np.sort(g.integers(-20, m + 20, size=(b, n, 2)), axis=2)
+    ranges[::3, ::5] = 7  # (empty)
+    ranges[5] = 0
+
+    def poison(q, k, v, dout, see):
+        for i in range(b):
+            hidden = torch.from_numpy(~see[i].any(0)).cuda()
+            k[i][:, hidden] = float("nan")
+            v[i][:, hidden] = float("inf")
+
+    _run(23, "bf16", b, 4, 4, n, m, 64, ranges=ranges, poison=poison)
+
+
 @pytest.mark.parametrize("window", [1, 2, 33, 64, 150, 1 << 40])
 @pytest.mark.parametrize("causal", [False, True])
 def test_window(window, causal):
