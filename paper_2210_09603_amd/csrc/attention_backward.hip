@@ -30,6 +30,7 @@ struct BackArgs {
   Strides dos, dqs, dks, dvs;
   float* info;    // of every row of a kv head, see row_info
   int4* seen;     // [batch][row_groups]: of 32 rows, the first and last + 1 of the keys that any of them sees; that all of them see
+  int* order;     // [batch][key_tiles]: the blocks of keys, the longest first; null: as they lie
   float* part;    // partial sums of the splits: dQ's [split][kv row][DP], then dK's and dV's [split][entry][key][2][DP]
   int row_groups;
   int key_tiles;
@@ -198,6 +199,48 @@ __device__ __forceinline__ float* dkv_part(const BackArgs& b, int z, const Entry
   return b.part + (((long long)z * b.f.batch * b.f.kv_heads + (long long)e.b * b.f.kv_heads + e.kv) * b.f.seq_k + key) * (2 * DP);
 }
 
+// ---- the order of the second kernel's work -------------------------------------------------------------------------------------
+// Ranges may give blocks of keys work in any order, and what begins last should be short.  One workgroup of the first kernel ranks the
+// blocks, 256 at a time, by how many groups of 32 rows see one of their keys: a sum over the differences at the first block of a group
+// and behind its last.  What a group sees is estimated by its first and last rows; of equal blocks the first comes first, so that
+// every block has one place, whatever the ranges are.  (Packed documents of 146 to 1024 tokens, 8 entries of 64 blocks: dK and dV 172 us
+// as they lie, 138 in order, with the ranking at the start of every workgroup; a group of workgroups that begin at once needs none.)
+constexpr int kTileRows = 128, kBlockKeys = 64, kDkvThreads = 512;
+constexpr int kOrdered = 256;
+template <int THREADS>
+__device__ __forceinline__ void write_order(const BackArgs& b, int batch, int* edges, int* work) {
+  const Args& p = b.f;
+  const int rows = p.seq_q * p.group;
+  const int* ranges = p.ranges + (long long)batch * p.seq_q * 2;
+  int* order = b.order + (long long)batch * b.key_tiles;
+  for (int base = 0; base < b.key_tiles; base += kOrdered) {
+    const int count = min(b.key_tiles - base, kOrdered);
+    for (int i = threadIdx.x; i < kOrdered; i += THREADS) edges[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < b.row_groups; i += THREADS) {
+      const int first = 2 * p.d_group.div(i * 32), last = 2 * p.d_group.div(min(i * 32 + 31, rows - 1));
+      const int lo = max(min(ranges[first], ranges[last]), 0), hi = min(max(ranges[first + 1], ranges[last + 1]), p.seq_k);
+      const int from = max(lo / kBlockKeys - base, 0), to = (hi + kBlockKeys - 1) / kBlockKeys - base;
+      if (lo >= hi || from >= count || to <= 0) continue;
+      atomicAdd(&edges[from], 1);
+      if (to < count) atomicAdd(&edges[to], -1);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += THREADS) {
+      int sum = 0;
+      for (int j = 0; j <= i; ++j) sum += edges[j];
+      work[i] = sum;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += THREADS) {
+      int rank = 0;
+      for (int j = 0; j < count; ++j) rank += work[j] > work[i] || (work[j] == work[i] && j < i);
+      order[base + rank] = base + i;
+    }
+    __syncthreads();
+  }
+}
+
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
 // The forward kernel's walk, with dout and out beside q, and its pairs of wavefronts.
 template <typename T, int DP, int FORM, int PAIRS>
@@ -215,6 +258,8 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   const int z = place.piece % b.dq_splits, tile = p.row_tiles - 1 - place.piece / b.dq_splits;
   const Entry e = make_entry<false>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
   const int rows = e.tokens * p.group, r0 = tile * 128 + (wave & 3) * 32;
+  if (b.order && e.kv == 0 && z == 0 && tile == p.row_tiles / 2)
+    write_order<THREADS>(b, e.b, reinterpret_cast<int*>(smem), reinterpret_cast<int*>(smem) + kOrdered);
 
   const Row w = make_row<false>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
@@ -413,7 +458,6 @@ __global__ __launch_bounds__(256) void dq_join_kernel(const BackArgs b) {
 // Microseconds for 2 x 4096 positions of 16 heads on 4, 128 dimensions, no mask: 800; both sums in a wavefront, one a SIMD, waiting for
 // LDS half of the time, 1237; the same with the values in LDS, two a SIMD and 44 registers spilled, 1200.  For 3 x 1021 positions of 12
 // heads, 64 dimensions: both sums in a wavefront 48, apart 53.
-constexpr int kTileRows = 128, kBlockKeys = 64, kDkvThreads = 512;
 
 template <typename T, int DP, int FORM>
 __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
@@ -431,8 +475,9 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   const int part = BOTH ? wave >> 1 : ((wave >> 1) & 1) * 2;  // the first of its GROUPS groups of 32 rows
 
   const Place place = place_of(blockIdx.x, p.batch * p.kv_heads, b.key_tiles * b.dkv_splits);
-  const int z = place.piece % b.dkv_splits, tile = place.piece / b.dkv_splits;  // (causal: the longest first)
+  const int z = place.piece % b.dkv_splits, turn = place.piece / b.dkv_splits;
   const Entry e = make_entry<false>(p, place.entry / p.kv_heads, place.entry % p.kv_heads);
+  const int tile = b.order ? b.order[(long long)e.b * b.key_tiles + turn] : turn;  // (causal: the longest first)
   const int rows = e.tokens * p.group;
   const int block_key = tile * kBlockKeys, key0 = block_key + (wave & 1) * 32, key = key0 + (lane & 31);
   const int block_end = min(block_key + kBlockKeys, e.keys);
@@ -741,6 +786,7 @@ hipError_t dispatch(int form, const BackArgs& b, hipStream_t stream) {
 
 long long row_groups_of(long long rows) { return (rows + 31) / 32; }
 // (of all forms: with a bias twice the fields)
+long long order_bytes(long long batch, long long key_tiles) { return (batch * key_tiles * 4 + 15) / 16 * 16; }
 long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
 
 // How the two kernels' work is cut.
@@ -788,8 +834,8 @@ int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, i
   const long long group = heads / kv_heads;
   if (group >= kMaxRows || seq_q >= kMaxRows || seq_q * group >= kMaxRows || seq_k >= kMaxRows || batch > kMaxBlocks || kv_heads > kMaxBlocks)
     return 0;
-  return info_bytes(batch * kv_heads, seq_q * group) + batch * row_groups_of(seq_q * group) * 16 +
-         cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim)).part_bytes;
+  const BackCut c = cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim));
+  return info_bytes(batch * kv_heads, seq_q * group) + batch * row_groups_of(seq_q * group) * 16 + order_bytes(batch, c.key_tiles) + c.part_bytes;
 }
 
 hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
@@ -873,7 +919,12 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
   // (without queries there is no workspace, and nothing to add up)
   b.dkv_splits = seq_q > 0 ? c.dkv_splits : 1;
   b.dkv_share = c.dkv_share;
-  if (seq_q > 0) b.part = reinterpret_cast<float*>(reinterpret_cast<char*>(b.seen) + batch * b.row_groups * 16);
+  if (seq_q > 0) {
+    char* order = reinterpret_cast<char*>(b.seen) + batch * b.row_groups * 16;
+    // (more workgroups than begin at once)
+    if (options->ranges && batch * kv_heads * c.key_tiles * c.dkv_splits > 256) b.order = reinterpret_cast<int*>(order);
+    b.part = reinterpret_cast<float*>(order + order_bytes(batch, c.key_tiles));
+  }
   const auto near = [&](const Strides& s) { return s.row < (1LL << 23) && s.head < (1LL << 23); };
   b.regular = group <= 32 && 32 % group == 0 && near(p.qs) && near(b.dos);
   if (batch * kv_heads * std::max((long long)c.row_tiles * c.dq_splits, (long long)c.key_tiles * c.dkv_splits) > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;

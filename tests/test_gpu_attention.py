@@ -131,6 +131,18 @@ def test_many_tiles_under_ranges_with_values_that_must_not_matter():
     _run(23, "bf16", b, 4, 4, n, m, 64, ranges=ranges, poison=poison)
 
 
+# (more blocks of 64 keys than begin at once: the longest first, 256 of an entry at a time)
+@pytest.mark.parametrize("size", [(2, 4, 2, 90, 4500, 64), (1, 2, 1, 33, 17000, 128)], ids=str)
+def test_ranges_over_many_blocks_of_keys(size):
+    b, h, hk, n, m, d = size
+    g = np.random.Generator(np.random.PCG64(24))
+    lo = g.integers(-20, m, size=(b, n, 1))
+    ranges = np.concatenate([lo, lo + g.integers(-5, m // 2, size=(b, n, 1))], axis=2)
+    ranges[0, 3] = (0, m)
+    ranges[-1, 32:64] = 0
+    _run(24, "bf16", b, h, hk, n, m, d, ranges=ranges)
+
+
 @pytest.mark.parametrize("window", [1, 2, 33, 64, 150, 1 << 40])
 @pytest.mark.parametrize("causal", [False, True])
 def test_window(window, causal):
