@@ -16,11 +16,14 @@ namespace attn {
 //   Few rows: 512 workgroups fill the device, which is worth a partial result for 16 tiles of 32 keys (one sequence of 131000 keys, 2 kv
 //   heads: 39 us with 16, 40 with 32, 56 with 64); up to 2048 even out a ragged batch, as long as 64 tiles remain (64 sequences of 100 to
 //   8000 keys, 8 kv heads: 220 us; 231 with 1024 workgroups, 225 with 4096 of 16 tiles).
-//   Tiles of 128 rows: up to 512 of them take pairs of wavefronts, and as many splits as leave a compute unit for each (more would be
-//   a second round: 210 tiles of 2068 keys 52 us whole, 69 in halves) of at least 4 tiles of 128 keys (n heads of as many rows as keys, us with plain wavefronts, with pairs, and what is taken: 128 dimensions, 4
-//   heads of 4096 97, 69, 50 split in 2; 8 of 2048 52, 40, 34; 32 of 1024 31, 27, 27; 32 of 2048, 512 tiles, 79 without pairs and 80
-//   with; 64 dimensions, 4 of 4096 59, 45, 33; 12 of 1024 18.7, 17.0, 16.9; 12 of 512 13.1, 12.9, 13.6).  Of a ragged batch's tiles
-//   some have no rows: four times as many (chunks of 4 prompts of 37 to 512 tokens over 4096 keys: 157 us, 192 with a quarter).
+//   Tiles of 128 rows: while they are no more than the 8 wavefronts that the device takes at once, they run in pairs of wavefronts (256
+//   compute units; two of them each at 64 dimensions, whose tiles are half as large), and in as many splits as leave a compute unit for
+//   each (more would be a second round: 210 tiles of 2068 keys 52 us whole, 69 in halves) of at least 4 tiles of 128 keys.  n heads of as
+//   many rows as keys, us with plain wavefronts, with pairs, and with pairs and splits: 128 dimensions, 4 heads of 4096 97, 69, 50; 8 of
+//   2048 52, 40, 34; 32 of 1024, 256 tiles, 31 and 27; 36 of 1024, 288 tiles, 41 and 51; 64 dimensions, 4 of 4096 59, 45, 33; 12 of 1024
+//   18.7, 17.0, 16.9; 12 of 512 13.1 and 12.9.
+//   Of a ragged batch's tiles some have no rows: 1024 workgroups of at least 8 tiles of 64 keys (chunks of 4 prompts of 37 to 512 tokens
+//   over 4096 keys: 157 us, 192 with 256).
 Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room, bool ragged) {
   Cut c;
   const long long pieces = entries * ((rows + 31) / 32);
@@ -28,7 +31,7 @@ Cut cut_work(long long entries, long long rows, long long keys, int dp, long lon
   const long long tile = c.stream ? 32 : 128;
   c.row_tiles = (int)((rows + tile - 1) / tile);
   const long long blocks = entries * c.row_tiles;
-  c.pairs = !c.stream && !ragged && blocks < 512 && keys > kTileKeys;
+  c.pairs = !c.stream && !ragged && (dp == 64 ? blocks < 512 : blocks <= 256) && keys > kTileKeys;
   const long long tile_keys = c.stream ? kStreamKeys : c.pairs ? 2 * kTileKeys : kTileKeys;
   const long long tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys);
   const auto wish = [&](long long workgroups, long long least) { return std::min((workgroups + blocks - 1) / blocks, tiles / least); };
