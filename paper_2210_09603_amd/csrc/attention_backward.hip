@@ -51,6 +51,9 @@ __device__ __forceinline__ float* row_info(const BackArgs& b, const Entry& e, in
   return b.info + (entry * rows + (r & ~3)) * FIELDS + field * 4 + (r & 3);
 }
 
+// The weight of a query's only key is 1 whatever the score: dS = P (dP - D) is 0, of which the two sums D and dP, in their different
+// orders, would leave a rounding.  (Times 0, so that what is not finite stays so.)
+__device__ __forceinline__ float unless_alone(int keys) { return keys == 1 ? 0.0f : 1.0f; }
 
 __device__ __forceinline__ float lse_to_base_2(float lse) { return lse == kNoMax ? __builtin_huge_valf() : lse * kLog2e; }
 
@@ -90,7 +93,7 @@ __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry&
     float derivative;
     const float prob = exp2_fast(score(dot, (float)(w.token + e.shift - j), derivative) - lse);
     if (prob == 0.0f) continue;
-    const float ds = prob * (dp - delta) * derivative;
+    const float ds = prob * (dp - delta) * derivative * unless_alone(w.hi - w.lo);
     bool finite = false;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -141,7 +144,7 @@ __device__ __forceinline__ void dkv_by_definition(const BackArgs& b, const Entry
     float derivative;
     const float prob = exp2_fast(score(dot, (float)(w.token + e.shift - j), derivative) - lse_to_base_2(p.lse[at]));
     if (prob == 0.0f) continue;
-    const float ds = prob * (dp - kLift * *row_info<FORM>(b, e, r, 1)) * derivative;
+    const float ds = prob * (dp - kLift * *row_info<FORM>(b, e, r, 1)) * derivative * unless_alone(w.hi - w.lo);
     bool finite = false;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -383,6 +386,11 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
         for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, DP>(map, keys, c * 32 + h * 16, d), ds[h], acc[d]);
     }
   }
+  const float by = unless_alone(w.hi - w.lo);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[d][r] *= by;
   if constexpr (PAIRS == 2) {
     __syncthreads();
     float* meet = reinterpret_cast<float*>(smem) + (wave & 3) * (DT * 16 * 64) + lane;
@@ -630,8 +638,10 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const bool in = (unsigned)(key - f4[u]) < (unsigned)c4[u];
-            s[4 * g + u] = in ? s[4 * g + u] : 0.0f;
-            if constexpr (BOTH) dp[4 * g + u] = in ? dp[4 * g + u] : 0.0f;
+            // (a row that sees one key has no whole tile, and comes by here)
+            const float by = for_dv ? 1.0f : unless_alone(c4[u]);
+            s[4 * g + u] = in ? (BOTH ? s[4 * g + u] : s[4 * g + u] * by) : 0.0f;
+            if constexpr (BOTH) dp[4 * g + u] = in ? dp[4 * g + u] * by : 0.0f;
           }
         }
       }

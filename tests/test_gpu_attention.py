@@ -181,6 +181,29 @@ def test_ranges(size, dtype):
     assert bool((out == 0).all()) and bool((lse == -np.inf).all())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [40, 128])
+@pytest.mark.parametrize("softcap", [0.0, 3.0])
+def test_the_only_key_of_a_query_has_no_gradient_of_its_score(dtype, dim, softcap):
+    """Windows of one key, sequences and documents of one token, one key in a longer range: dQ and dK are zeros, not roundings."""
+    g = np.random.Generator(np.random.PCG64(25))
+    for b, h, hk, n, m, window in ((2, 4, 2, 70, 70, 1), (1, 2, 2, 1, 1, 0), (2, 3, 1, 9, 1, 0), (1, 2, 1, 600, 600, 0)):
+        q, dout, out = (_draw(g, (b, h, n, dim), dtype, "dense") for _ in range(3))
+        k, v = (_draw(g, (b, hk, m, dim), dtype, "dense") for _ in range(2))
+        ranges = None
+        if n == 600:
+            at = torch.arange(n, dtype=torch.int32)
+            ranges = torch.stack([(at * 7) % m, (at * 7) % m + 1], dim=1)[None].contiguous().cuda()
+        opts = dict(window=window, softcap=softcap, ranges=ranges)
+        lse = torch.empty(b, h, n, device="cuda")
+        hb.hidet_attention(q, k, v, out, lse=lse, **opts)
+        dq, dk, dv = (torch.full_like(t, 3.0) for t in (q, k, v))
+        ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+        hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, **opts)
+        assert not dq.any() and not dk.any(), (b, h, hk, n, m)
+        assert bool((dv != 3.0).any())
+
+
 def test_no_keys_and_no_queries():
     q = torch.randn(2, 4, 5, 64, device="cuda").half()
     k = torch.empty(2, 2, 0, 64, device="cuda", dtype=torch.float16)
