@@ -659,6 +659,13 @@ def _float32(t, shape, what):
     return t.data_ptr()
 
 
+def _dense_ws(workspace):
+    """_ws() of a workspace that is checked: all of its bytes are written to."""
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace must be a dense tensor")
+    return _ws(workspace)
+
+
 def _options(scale, head_dim, causal, window, softcap, slopes, ranges, heads, ranges_shape):
     o = hidet_attention_options_t()
     o.struct_size = ctypes.sizeof(hidet_attention_options_t)
@@ -698,7 +705,7 @@ def _attention(q, k, v, out, lse, scale, causal, window, softcap, slopes, ranges
     sizes = _attention_shapes(q, k, v, out)
     batch, heads, _, seq_q, _, dim = sizes
     o = _options(scale, dim, causal, window, softcap, slopes, ranges, heads, (batch, seq_q, 2))
-    wp, wb = _ws(workspace)
+    wp, wb = _dense_ws(workspace)
     device, handle = _on((q, k, v, out, lse, slopes, ranges, workspace), stream)
     with device:
         st = lib().hidet_attention(_dtype(q), *sizes, _heads(q), _heads(k), _heads(v), _heads(out),
@@ -731,7 +738,7 @@ def _attention_backward(grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, wor
         if t.shape != k.shape or t.dtype != q.dtype:
             raise ValueError("grad_k and grad_v must agree with k in shape and dtype")
     o = _options(scale, dim, causal, window, softcap, slopes, ranges, heads, (batch, seq_q, 2))
-    wp, wb = _ws(workspace)
+    wp, wb = _dense_ws(workspace)
     device, handle = _on((grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, slopes, ranges, workspace), stream)
     with device:
         st = lib().hidet_attention_backward(_dtype(q), *sizes, _heads(grad_out), _heads(q), _heads(k), _heads(v), _heads(out),
@@ -875,7 +882,7 @@ def _cache_attention(cache, q, out, starts, max_new, scale, window, softcap, slo
     sp = _new_tokens(cache, (q, out), starts)
     tokens, heads, dim = q.shape
     o = _options(scale, dim, True, window, softcap, slopes, None, heads, None)
-    wp, wb = _ws(workspace)
+    wp, wb = _dense_ws(workspace)
     device, handle = _on((q, out, lse, slopes, starts, workspace) + cache._keep, stream)
     with device:
         st = lib().hidet_cache_attention(cache, heads, tokens, max_new, _heads(q), _heads(out), _float32(lse, (tokens, heads), "lse"), sp,

@@ -359,6 +359,10 @@ class Tensors {
     if (x && (x->scalar_type() != type || x->sizes() != at::IntArrayRef(shape.begin(), shape.size()) || !x->is_contiguous())) return fail();
     return x;
   }
+  const at::Tensor* workspace(PyObject* o) {
+    const at::Tensor* x = get(o, true);
+    return x && !x->is_contiguous() ? fail() : x;
+  }
   // vectors along the last axis of 3 or 4
   const at::Tensor* vectors(PyObject* o, hidet_heads_t& h, int64_t dim) {
     const at::Tensor* x = get(o);
@@ -462,7 +466,7 @@ PyObject* call_attention(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     float* lse = address<float>(t.dense(a[4], at::kFloat, {batch, heads, rows}));
     hidet_attention_options_t o;
     if (!options_of(t, a[5], a[6], a[7], a[8], a[9], a[10], batch, heads, rows, dim, o)) return kGeneral;
-    const at::Tensor* ws = t.get(a[11], true);
+    const at::Tensor* ws = t.workspace(a[11]);
     void* stream;
     if (!t.ok || !stream_on(c, a[12], t, stream)) return kGeneral;
     return without_lock([&] {
@@ -493,7 +497,7 @@ PyObject* call_attention_backward(PyObject* self, PyObject* const* a, Py_ssize_t
       if (x[i]->sizes() != like->sizes() || x[i]->scalar_type() != q->scalar_type()) return kGeneral;
     }
     const float* lse = address<const float>(t.dense(a[5], at::kFloat, {batch, heads, rows}));
-    const at::Tensor* ws = t.get(a[9], true);
+    const at::Tensor* ws = t.workspace(a[9]);
     hidet_attention_options_t o;
     if (!options_of(t, a[10], a[11], a[12], a[13], a[14], a[15], batch, heads, rows, dim, o)) return kGeneral;
     void* stream;
@@ -623,7 +627,7 @@ PyObject* call_cache_attention(PyObject* self, PyObject* const* a, Py_ssize_t n)
     float* lse = address<float>(t.dense(a[9], at::kFloat, {tokens, heads}));
     hidet_attention_options_t o;
     if (!options_of(t, a[5], Py_True, a[6], a[7], a[8], Py_None, 0, heads, 0, q->size(2), o)) return kGeneral;
-    const at::Tensor* ws = t.get(a[10], true);
+    const at::Tensor* ws = t.workspace(a[10]);
     int64_t max_new;
     void* stream;
     if (!t.ok || !whole(a[4], max_new) || !stream_on(c, a[11], t, stream)) return kGeneral;

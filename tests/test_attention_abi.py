@@ -203,3 +203,17 @@ def test_the_binding_refuses_what_it_cannot_describe():
         hb.hidet_cache_attention(c, x.float(), x, torch.zeros(4, dtype=torch.int32), 1)
     with pytest.raises(ValueError):
         hb.hidet_rope(q, q, torch.zeros(32))
+
+
+def test_workspaces_that_are_not_dense_are_refused():
+    """(A strided one holds elements that are not its own, an expanded one has fewer bytes than elements.)"""
+    q, k = torch.zeros(1, 2, 3, 16, dtype=torch.float16), torch.zeros(1, 2, 4, 16, dtype=torch.float16)
+    lse = torch.zeros(1, 2, 3)
+    pages, i32 = torch.zeros(2, 4, 2, 16, dtype=torch.float16), lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    cache = hb.make_cache(pages, pages.clone(), i32(1, 2), i32(1))
+    rows = torch.zeros(3, 2, 16, dtype=torch.float16)
+    for ws in (torch.zeros(64)[::2], torch.zeros(1).expand(1 << 20)):
+        for f, args in ((hb.hidet_attention, (q, k, k, q)), (hb.hidet_attention_backward, (q, q, k, k, q, lse, q, k, k)),
+                        (hb.hidet_cache_attention, (cache, rows, rows, i32(2), 3))):
+            with pytest.raises(ValueError, match="dense"):
+                f(*args, workspace=ws)
