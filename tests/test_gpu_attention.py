@@ -1,5 +1,7 @@
 """Fused attention and its backward pass against the float64 oracle: sizes, head layouts, masks, strides, values that must not matter,
 splits, streams, graphs."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -467,6 +469,59 @@ def test_on_another_stream():
     side.synchronize()
     for x, y in zip(a[:5], b[:5]):
         assert torch.equal(x, y)
+
+
+def test_two_threads_on_two_streams():
+    """Calls from several threads at once, each on its own stream with its own buffers."""
+    states = [_chain_state(), _chain_state()]
+    states[1][0].mul_(-0.5)
+    want = []
+    for q, k, v, dout, make in states:
+        want.append(make())
+        _chain(q, k, v, dout, want[-1])
+    torch.cuda.synchronize()
+    got, errors = [make() for *_, make in states], []
+
+    def work(i):
+        try:
+            q, k, v, dout, _ = states[i]
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    _chain(q, k, v, dout, got[i])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for a, b in zip(want, got):
+        for x, y in zip(a[:5], b[:5]):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("group", [1, 3])
+def test_strides_beyond_32_bits(group):
+    """All tensors in one buffer, every position 2^23 - 8 elements behind the last."""
+    n, d, h, stride = 290, 64, 2 * group, (1 << 23) - 8
+    buf = torch.empty(n * stride, dtype=torch.bfloat16, device="cuda")
+    view = lambda at, heads: buf.as_strided((1, heads, n, d), (d, d, stride, 1), at * 8 * d)
+    g = np.random.Generator(np.random.PCG64(26))
+    dense = [torch.from_numpy(g.standard_normal((1, heads, n, d)).astype(np.float32)).to(torch.bfloat16).cuda() for heads in (h, 2, 2, h)]
+    far = [view(i, t.shape[1]) for i, t in enumerate(dense)] + [view(4 + i, heads) for i, heads in enumerate((h, h, 2, 2))]
+    for a, b in zip(far, dense):
+        a.copy_(b)
+    near = dense + [torch.empty_like(t) for t in (dense[0], dense[0], dense[1], dense[2])]
+    for q, k, v, dout, out, dq, dk, dv in (near, far):
+        lse = torch.empty(1, h, n, device="cuda")
+        hb.hidet_attention(q, k, v, out, lse=lse, causal=True, workspace=torch.empty(1 << 22, device="cuda"))
+        ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+        hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, causal=True)
+    for a, b in zip(near[4:], far[4:]):
+        assert torch.equal(a, b)
 
 
 def test_a_training_step_from_tokens_to_gradients():
