@@ -568,13 +568,23 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
       for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
   const Score<FORM> all_scores(p, 0.0f);
   const float at_key = (float)key;
+  // (which groups of 32 rows take part: asked for a tile ahead, and in scalar registers before the next tile's loads are under way, for
+  // which the compiler would otherwise wait)
+  const auto in_scalars = [](const int4& v) {
+    return int4{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z),
+                __builtin_amdgcn_readfirstlane(v.w)};
+  };
+  int4 next0 = seen[min(4 * t0 + part, groups - 1)], next1 = seen[min(4 * t0 + part + GROUPS - 1, groups - 1)];
   settle();
   if (t0 < t1) request(t0);
   for (int t = t0; t < t1; ++t) {
-    // (which groups of 32 rows take part: asked for before the wait)
-    const int4 seen0 = seen[min(4 * t + part, groups - 1)], seen1 = seen[min(4 * t + part + GROUPS - 1, groups - 1)];
     wait_all_and_meet();
-    if (t + 1 < t1) request(t + 1);
+    const int4 seen0 = in_scalars(next0), seen1 = in_scalars(next1);
+    if (t + 1 < t1) {
+      request(t + 1);
+      next0 = seen[min(4 * t + 4 + part, groups - 1)];
+      next1 = seen[min(4 * t + 4 + part + GROUPS - 1, groups - 1)];
+    }
     const unsigned qs = lds0 + (t & 1) * STAGE, gs = qs + 2 * STAGE;
     const float* of_rows = reinterpret_cast<const float*>(info + (t & 1) * INFO);
 #pragma unroll 1
