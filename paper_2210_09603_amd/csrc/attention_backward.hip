@@ -592,17 +592,39 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
       const int row = (part + c) * 32, behind = t * kTileRows + row + 32;
       if ((c ? seen1.x : seen0.x) >= key0 + 32 || (c ? seen1.y : seen0.y) <= key0 || behind - 32 >= rows) continue;
       const bool masked = (c ? seen1.z : seen0.z) > key0 || (c ? seen1.w : seen0.w) < key0 + 32 || behind > rows;
-      f32x16 s;
+      f32x16 s, dp;
+      Frag gcol[BOTH ? 4 : 1], qcol[BOTH ? 4 : 1];
+      if constexpr (BOTH) {
+        // (one workgroup to a compute unit: what a wavefront reads from LDS is asked for well before its products, which the scheduler
+        // does not do of itself; 24 heads over 1449 keys 89 to 84 us)
+        Frag a[KS], g[KS];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+        for (int ks = 0; ks < KS; ++ks) a[ks] = row_frag<T, DP>(map, qs, row, ks);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, qs, row, ks), kf[ks], s);
-      f32x16 dp;
-      if (!for_dv) {
+        for (int ks = 0; ks < KS; ++ks) g[ks] = row_frag<T, DP>(map, gs, row, ks);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, gs, row, ks), vf[ks], dp);
+        for (int ks = 0; ks < KS; ++ks) s = mfma_op(a[ks], kf[ks], s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mfma_op(g[ks], vf[ks], dp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) qcol[i] = col_frag<T, DP>(map, qs, row + (i / DT) * 16, i % DT);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) gcol[i] = col_frag<T, DP>(map, gs, row + (i / DT) * 16, i % DT);
+        __builtin_amdgcn_sched_barrier(0);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, qs, row, ks), kf[ks], s);
+        if (!for_dv) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, gs, row, ks), vf[ks], dp);
+        }
       }
       Score<FORM> score = all_scores;
       float derivative[16];
@@ -666,8 +688,12 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          acc[0][d] = mfma_op(col_frag<T, DP>(map, from_rows, row + h * 16, d), w[0][h], acc[0][d]);
-          if constexpr (BOTH) acc[SUMS - 1][d] = mfma_op(col_frag<T, DP>(map, gs, row + h * 16, d), w[SUMS - 1][h], acc[SUMS - 1][d]);
+          if constexpr (BOTH) {
+            acc[0][d] = mfma_op(qcol[h * DT + d], w[0][h], acc[0][d]);
+            acc[SUMS - 1][d] = mfma_op(gcol[h * DT + d], w[SUMS - 1][h], acc[SUMS - 1][d]);
+          } else {
+            acc[0][d] = mfma_op(col_frag<T, DP>(map, from_rows, row + h * 16, d), w[0][h], acc[0][d]);
+          }
         }
     }
   }
@@ -816,7 +842,7 @@ long long info_bytes(long long entries, long long rows) { return entries * ((row
 //   202 and 227, and so without; one fits worse, 4 entries of 1472
 //   rows over 184 keys 47 and 50.
 //   dK and dV: tiles of 64 keys, and where they leave compute units without work splits of at least 2 tiles of 128 rows: 256 workgroups
-//   (512 at 64 dimensions, where two fit a compute unit).  With 512 of at least 4 everywhere: the first of the passes above 220 for 190,
+//   (512 at 64 dimensions: 24 heads over 1449 keys 199 us for 211).  With 512 of at least 4 everywhere: the first of the passes above 220 for 190,
 //   the second 486 for 449, and 285 for 271 of 2 entries of 6599 rows.
 struct BackCut {
   int row_tiles, key_tiles, dq_splits, dq_share, dkv_splits, dkv_share;
