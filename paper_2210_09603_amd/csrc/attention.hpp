@@ -54,6 +54,7 @@ struct Args {
   int causal, window;     // window 0: none
   int row_tiles, splits;
   int share;              // tiles of keys of a split
+  int flat;               // pieces of a ragged batch, see flat_kernel; 0: splits
   float scale, softcap;   // softcap 0: none
 };
 
@@ -477,7 +478,7 @@ __device__ __forceinline__ Part part_of(const Args& p, int b, int kv, int z, int
 // a masked key or value is infinite or NaN the tiled products multiply it by a zero and their sums become NaN; the rows that
 // come out not finite are computed by this definition instead.  Rare, and slow: a few hundred cycles a key.
 template <typename T, int DP, bool PAGED, int FORM>
-__device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e, int r, int from, int to, int z) {
+__device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e, int r, int from, int to, const Part& rows, bool partial) {
   constexpr int E = DP / 64;
   const int lane = threadIdx.x & 63;
   const Row w = make_row<PAGED>(p, e, r);
@@ -524,8 +525,8 @@ __device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e,
     for (int i = 0; i < E; ++i) acc[i] = sum;
     top = sum;
   }
-  if (p.splits > 1) {
-    const Part part = part_of<DP>(p, e.b, e.kv, z, r);
+  if (partial) {
+    const Part part = {rows.sums + (long long)r * DP, rows.stat + r * 2LL};
 #pragma unroll
     for (int i = 0; i < E; ++i) part.sums[lane * E + i] = acc[i];
     if (lane == 0) {
@@ -541,9 +542,10 @@ __device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e,
   if (lane == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (top + __builtin_log2f(sum)) * kLn2;
 }
 
-// Stores a wavefront's 32 rows: the finished output, or the sums of a split.  `r0`: its first row.
+// Stores a wavefront's 32 rows: the finished output, or the sums of a split, from `to_rows` of row 0 on.  `r0`: its first row.
 template <typename T, int DP, bool PAGED, int FORM>
-__device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, DP>& st, int r0, int rows, const Row& w, int from, int to, int z) {
+__device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, DP>& st, int r0, int rows, const Row& w, int from, int to, const Part& to_rows,
+                                       bool partial) {
   const int lane = threadIdx.x & 63, half = lane >> 5, r = r0 + (lane & 31);
   const float sum = sum_of_halves(st.sum);
   bool finite = true;
@@ -555,9 +557,9 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
   const unsigned long long odd = __ballot(!finite);
   unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
   const bool mine = r < rows && !((again >> (lane & 31)) & 1);
-  if (p.splits > 1) {
+  if (partial) {
     if (mine) {
-      const Part part = part_of<DP>(p, e.b, e.kv, z, r);
+      const Part part = {to_rows.sums + (long long)r * DP, to_rows.stat + r * 2LL};
       if (sum > 0.0f)  // (the sums of nothing are not read)
 #pragma unroll
       for (int t = 0; t < State<T, DP>::DT; ++t)
@@ -590,7 +592,7 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
   while (again) {
     const int i = __builtin_ctz(again);
     again &= again - 1;
-    if (r0 + i < rows) row_by_definition<T, DP, PAGED, FORM>(p, e, r0 + i, from, to, z);
+    if (r0 + i < rows) row_by_definition<T, DP, PAGED, FORM>(p, e, r0 + i, from, to, to_rows, partial);
   }
 }
 
@@ -781,7 +783,8 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
     st.sum = st.sum * by + meet[(DT * 16 + 1) * 64] * by_other;
     st.shift = level;
   }
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * TILE, min(end, begin + t1 * TILE), z);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * TILE, min(end, begin + t1 * TILE),
+                                part_of<DP>(p, e.b, e.kv, z, 0), p.splits > 1);
 }
 
 // ---- the kernel of few rows ---------------------------------------------------------------------------------------------------
@@ -791,33 +794,32 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
 // of 4 wavefronts, so that one begins and ends beside another.
 constexpr int kStreamWaves = 4, kStreamKeys = 32;
 
+// What the wavefronts of a workgroup have for themselves, and to meet in.
+template <int DP>
+struct StreamLds {
+  static constexpr int TILE = kStreamKeys * DP * 2, JOIN = 32 * (DP + 4) * 4;  // JOIN: fp32 sums of 32 rows
+  static constexpr int BYTES = kStreamWaves * 2 * TILE > kStreamWaves / 2 * JOIN ? kStreamWaves * 2 * TILE : kStreamWaves / 2 * JOIN;
+  __attribute__((aligned(16))) unsigned char smem[BYTES];
+  float stat[kStreamWaves][32][2];
+};
+// Rows r0.. of an entry over tiles t0..t1 - 1 of the keys that they see.
 template <typename T, int DP, bool PAGED, int FORM>
-__global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args p) {
+__device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, const Entry& e, int r0, int t0, int t1, const Part& to_rows,
+                                             bool partial) {
   constexpr int CPR = DP / 8, NL = kStreamKeys * CPR / 64, RPP = 64 / CPR, KS = DP / 16, DT = DP / 32;
-  constexpr int TILE = kStreamKeys * CPR * 16;
-  constexpr int JOIN = 32 * (DP + 4) * 4;  // fp32 sums of 32 rows
+  constexpr int TILE = StreamLds<DP>::TILE, JOIN = StreamLds<DP>::JOIN;
   using Frag = typename Frag8<T>::type;
-  __shared__ __attribute__((aligned(16))) unsigned char smem[kStreamWaves * 2 * TILE > kStreamWaves / 2 * JOIN ? kStreamWaves * 2 * TILE : kStreamWaves / 2 * JOIN];
-  __shared__ float stat[kStreamWaves][32][2];
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  // (workgroups share no keys; dealt to the XCDs in turn by kv head and sequence, so that each gets its part of every sequence, the first
-  // splits of all before the second ones, which only long sequences have)
-  int id = blockIdx.x;
-  const int tile = id % p.row_tiles;
-  id /= p.row_tiles;
-  const int entries = p.batch * p.kv_heads, z = id / entries;
-  id -= z * entries;
-  const Entry e = make_entry<PAGED>(p, id / p.kv_heads, id % p.kv_heads);
-  const int rows = e.tokens * p.group, r0 = tile * 32;
-  if (r0 >= rows) return;
-
+  const int rows = e.tokens * p.group;
+  unsigned char* smem = lds.smem;
+  auto& stat = lds.stat;
   const Row w = make_row<PAGED>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
   const Seen seen = seen_by<PAGED>(p, e, w, r0, min(r0 + 31, rows - 1));
   const int end = seen.hi, begin = min(seen.lo, end);
   const int all = (end - begin + kStreamKeys - 1) / kStreamKeys;
-  const int t0 = min(all, z * p.share), t1 = z + 1 < p.splits ? min(all, t0 + p.share) : all;
+  t0 = min(t0, all);
+  t1 = min(t1, all);
   const T* kbase = keys_of<T, PAGED>(p, e, p.k, p.ks);
   const T* vbase = keys_of<T, PAGED>(p, e, p.v, p.vs);
   unsigned char* mine = smem + wave * 2 * TILE;
@@ -934,7 +936,147 @@ __global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args
   st.top = top;
   st.shift = level;
   st.sum = half == 0 ? sum : 0.0f;
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kStreamKeys, min(end, begin + t1 * kStreamKeys), z);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kStreamKeys, min(end, begin + t1 * kStreamKeys), to_rows, partial);
+}
+
+template <typename T, int DP, bool PAGED, int FORM>
+__global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args p) {
+  __shared__ StreamLds<DP> lds;
+  // (workgroups share no keys; dealt to the XCDs in turn by kv head and sequence, so that each gets its part of every sequence, the first
+  // splits of all before the second ones, which only long sequences have)
+  int id = blockIdx.x;
+  const int tile = id % p.row_tiles;
+  id /= p.row_tiles;
+  const int entries = p.batch * p.kv_heads, z = id / entries;
+  id -= z * entries;
+  const Entry e = make_entry<PAGED>(p, id / p.kv_heads, id % p.kv_heads);
+  if (tile * 32 >= e.tokens * p.group) return;
+  stream_tiles<T, DP, PAGED, FORM>(p, lds, e, tile * 32, z * p.share, z + 1 < p.splits ? (z + 1) * p.share : 0x7fffffff,
+                                   part_of<DP>(p, e.b, e.kv, z, 0), p.splits > 1);
+}
+
+// ---- a ragged batch in equal pieces ------------------------------------------------------------------------------------------------
+// The sequences' tiles of 32 keys one behind the other, once for every kv head, cut into as many equal pieces as the device takes workgroups:
+// one may end one sequence and begin others.  What lies in one piece whole is finished there; of the others each piece
+// leaves its sums, and join_flat_kernel adds them in the order of the pieces.  Where the tiles of a sequence begin is worked out by each
+// workgroup (lengths are known on the device alone), and left for the second kernel by one of them.
+constexpr int kFlatSeqs = 1024;
+// (a sequence with new tokens has a tile at least, so that what sees nothing is written as well)
+__device__ __forceinline__ int flat_tiles(const Args& p, int s) {
+  const Entry e = make_entry<true>(p, s, 0);
+  if (e.tokens == 0) return 0;
+  int lo, first_hi, last_lo, hi;
+  seen_from<true>(p, e, e.shift, lo, first_hi);
+  seen_from<true>(p, e, e.tokens - 1 + e.shift, last_lo, hi);
+  return max((hi - min(lo, hi) + kStreamKeys - 1) / kStreamKeys, 1);
+}
+__device__ __forceinline__ int flat_share(const Args& p, int total) { return max((total + p.flat - 1) / p.flat, 1); }
+// sums of a piece's part of a sequence: `begins` if the sequence begins in it
+template <int DP>
+__device__ __forceinline__ Part flat_part(const Args& p, int piece, bool begins, int kv) {
+  const long long rows = (long long)p.seq_q * p.group, slot = ((long long)piece * 2 + begins) * p.kv_heads + kv;
+  float* part = p.part + (kFlatSeqs + 4);
+  return Part{part + slot * rows * DP, part + 2LL * p.flat * p.kv_heads * rows * DP + slot * rows * 2};
+}
+
+template <typename T, int DP, int FORM>
+__global__ __launch_bounds__(64 * kStreamWaves, 2) void flat_kernel(const Args p) {
+  constexpr int THREADS = 64 * kStreamWaves;
+  __shared__ StreamLds<DP> lds;
+  __shared__ int begins[kFlatSeqs + 1], sums[kStreamWaves], found;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int kv = blockIdx.x % p.kv_heads, piece = blockIdx.x / p.kv_heads;
+  int total = 0;
+  for (int s0 = 0; s0 < p.batch; s0 += THREADS) {
+    const int s = s0 + tid;
+    int upto = s < p.batch ? flat_tiles(p, s) : 0;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const int other = __shfl_up(upto, m);
+      if (lane >= m) upto += other;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int before = total;
+#pragma unroll
+    for (int i = 0; i < kStreamWaves; ++i) {
+      if (i < wave) before += sums[i];
+      total += sums[i];
+    }
+    if (s < p.batch) begins[s + 1] = before + upto;
+    __syncthreads();
+  }
+  if (tid == 0) begins[0] = 0;
+  total = __builtin_amdgcn_readfirstlane(total);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int s = tid; s <= p.batch; s += THREADS) reinterpret_cast<int*>(p.part)[s] = begins[s];
+  const int share = flat_share(p, total);
+  if ((long long)piece * share >= total) return;
+  int from = piece * share;
+  const int till = min(total - from, share) + from;
+  for (int s = tid; s < p.batch; s += THREADS)
+    if (begins[s] <= from && from < begins[s + 1]) found = s;
+  __syncthreads();
+  for (int s = __builtin_amdgcn_readfirstlane(found); from < till; ++s) {
+    const int first = __builtin_amdgcn_readfirstlane(begins[s]), last = __builtin_amdgcn_readfirstlane(begins[s + 1]);
+    if (first == last) continue;
+    const int t0 = from - first, t1 = min(last, till) - first;
+    stream_tiles<T, DP, true, FORM>(p, lds, make_entry<true>(p, s, kv), 0, t0, t1, flat_part<DP>(p, piece, t0 == 0, kv),
+                                    t0 > 0 || t1 < last - first);
+    __syncthreads();
+    from = first + t1;
+  }
+}
+
+// One row of a sequence that lies in several pieces, by groups of lanes that take a piece each in turn.
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void join_flat_kernel(const Args p) {
+  constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
+  __shared__ __attribute__((aligned(16))) float meet[GROUPS][DP];
+  __shared__ float stat[GROUPS][2];
+  const int rows = p.seq_q * p.group, r = blockIdx.x % rows, entry = blockIdx.x / rows, s = entry / p.kv_heads, kv = entry - s * p.kv_heads;
+  const int* begins = reinterpret_cast<const int*>(p.part);
+  const int first = begins[s], last = begins[s + 1], share = flat_share(p, begins[p.batch]);
+  if (first == last) return;
+  const int from = first / share, to = (last - 1) / share;
+  if (from == to) return;  // (finished)
+  const Entry e = make_entry<true>(p, s, kv);
+  if (r >= e.tokens * p.group) return;
+  const int group = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
+  float top = kNoMax, sum = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  auto add = [&](float m, float its, const f32x4& v) {
+    const float next = m > top || m != m ? m : top;
+    const float old = top == kNoMax ? 0.0f : exp2_fast(top - next), now = exp2_fast(m - next);
+    sum = sum * old + now * its;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] = acc[c] * old + now * v[c];
+    top = next;
+  };
+  for (int piece = from + group; piece <= to; piece += GROUPS) {
+    const Part part = flat_part<DP>(p, piece, piece == from, kv);
+    const float m = part.stat[r * 2];
+    if (m != kNoMax) add(m, part.stat[r * 2 + 1], *reinterpret_cast<const f32x4*>(part.sums + (long long)r * DP + d));
+  }
+  *reinterpret_cast<f32x4*>(&meet[group][d]) = acc;
+  if (d == 0) {
+    stat[group][0] = top;
+    stat[group][1] = sum;
+  }
+  __syncthreads();
+  if (group != 0) return;
+  for (int g = 1; g < GROUPS; ++g)
+    if (stat[g][0] != kNoMax) add(stat[g][0], stat[g][1], *reinterpret_cast<const f32x4*>(&meet[g][d]));
+  const Row w = make_row<true>(p, e, r);
+  const bool none = top == kNoMax;
+  if (d < p.dim) {
+    T four[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : acc[c] / sum);
+    __builtin_memcpy(reinterpret_cast<Chunk8*>(reinterpret_cast<T*>(p.out) + query_offset<true>(p, e, p.os, w) + d), four, 8);
+  }
+  if (d == 0 && p.lse) p.lse[lse_offset<true>(p, e, w)] = none ? kNoMax : (top + __builtin_log2f(sum)) * kLn2;
 }
 
 // ---- joining the splits -----------------------------------------------------------------------------------------------------

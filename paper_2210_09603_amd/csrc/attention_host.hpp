@@ -74,6 +74,13 @@ inline int padded_dim(long long dim) { return dim <= 64 ? 64 : 128; }
 template <typename T, int DP, bool PAGED, int FORM>
 hipError_t launch_forward(const Args& p, const Cut& c, hipStream_t stream) {
   const long long blocks = (long long)p.batch * p.kv_heads * c.row_tiles * c.splits;
+  if constexpr (PAGED)
+    if (p.flat) {
+      hipLaunchKernelGGL((flat_kernel<T, DP, FORM>), dim3((unsigned)(p.flat * p.kv_heads)), dim3(64 * kStreamWaves), 0, stream, p);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      hipLaunchKernelGGL((join_flat_kernel<T, DP>), dim3((unsigned)(p.batch * p.kv_heads * p.seq_q * p.group)), dim3(256), 0, stream, p);
+      return hipGetLastError();
+    }
   if (c.stream)
     hipLaunchKernelGGL((stream_kernel<T, DP, PAGED, FORM>), dim3((unsigned)blocks), dim3(64 * kStreamWaves), 0, stream, p);
   else if (!PAGED && c.pairs)

@@ -129,6 +129,18 @@ long long keys_at_most(const hidet_cache_t* c, long long max_new, long long wind
   if (window > 0) keys = std::min(keys, std::min<long long>(window, 1LL << 31) + max_new);
   return std::max(keys, 1LL);
 }
+// The pieces of flat_kernel for a kv head, or 0: splits.  Lengths are known on the device alone, and splits are cut for as many keys as the
+// tables have room for: where that is far more than the sequences hold, one split has all of a sequence.  64 sequences, 8 kv heads,
+// splits and pieces, us: room for 131000, lengths 100 to 8000 244 and 204, 100 to 163 27.6 and 23.1, one of 120000 beside 63 of 200 546
+// and 154; room for 8000 and lengths 100 to 8000 222 and 217; room for 2000 and lengths 100 to 163 12.3 and 23, where splits stay:
+// the pieces' second kernel, and the ends of two sequences one after the other.
+int flat_pieces(const hidet_cache_t* c, long long rows, long long keys) {
+  if (rows > 32 || c->seqs > kFlatSeqs || c->seqs * c->heads < 256 || keys < 16384 || (keys / kStreamKeys + 1) * c->seqs >= (1LL << 30)) return 0;
+  return (int)std::max(1LL, 512 / (long long)c->heads);
+}
+long long flat_bytes(const hidet_cache_t* c, long long rows, int pieces, int dp) {
+  return (kFlatSeqs + 4 + 2LL * pieces * c->heads * rows * (dp + 2)) * 4;
+}
 
 }  // namespace
 
@@ -197,7 +209,9 @@ int64_t hidet_cache_attention_workspace_bytes(const hidet_cache_t* cache, int64_
   if (max_new >= kMaxRows || group >= kMaxRows || max_new * group >= kMaxRows) return 0;
   const int dp = padded_dim(cache->head_dim);
   const long long entries = cache->seqs * cache->heads, rows = max_new * group;
-  const Cut c = cut_work(entries, rows, keys_at_most(cache, max_new, window), dp, 1LL << 62, true);
+  const long long keys = keys_at_most(cache, max_new, window);
+  if (const int pieces = flat_pieces(cache, rows, keys)) return flat_bytes(cache, rows, pieces, dp);
+  const Cut c = cut_work(entries, rows, keys, dp, 1LL << 62, true);
   return c.splits > 1 ? c.splits * split_bytes(entries, rows, dp) : 0;
 }
 
@@ -249,7 +263,10 @@ hidet_status_t hidet_cache_attention(const hidet_cache_t* cache, int64_t heads, 
   p.scale = options->scale;
   p.softcap = options->softcap;
   const long long entries = cache->seqs * cache->heads, rows = max_new * group;
-  const Cut c = cut_work(entries, rows, keys_at_most(cache, max_new, options->window), padded_dim(cache->head_dim), workspace ? workspace_bytes : 0, true);
+  const long long keys = keys_at_most(cache, max_new, options->window);
+  const int dp = padded_dim(cache->head_dim), pieces = flat_pieces(cache, rows, keys);
+  if (pieces && workspace && workspace_bytes >= flat_bytes(cache, rows, pieces, dp)) p.flat = pieces;
+  const Cut c = cut_work(entries, rows, keys, dp, workspace ? workspace_bytes : 0, true);
   if (entries * c.row_tiles > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
   p.row_tiles = c.row_tiles;
   p.splits = c.splits;

@@ -183,6 +183,98 @@ def test_lists_that_make_no_sense_reach_nothing():
     assert bool((out == 7.0).all()) and torch.equal(b.k_pages, before)
 
 
+# ---- a ragged batch of many entries: equal pieces of all its keys ----
+RAGGED = [0, 1, 2, 31, 32, 33, 3000, 64, 65, 700, 5, 1, 0, 2100, 96, 97, 300, 301, 12, 40, 41, 42, 1500, 3, 8, 9, 10, 128, 129, 1000, 6, 700]
+
+
+def _ragged(seed, dtype, dim, poison=False, **kw):
+    """32 sequences of 0 to 3000 tokens, 0 to 4 of them new, 8 kv heads; one of them without a page in its middle."""
+    new = [min(n, (i * 7) % 5) for i, n in enumerate(RAGGED)]
+    new[4] = new[30] = 0
+    b = Batch(seed, dtype, RAGGED, new, 16, 8, dim, 48, pad=3, width=350, **kw)
+    b.table[9, 3] = -1
+    b.tables.copy_(torch.from_numpy(b.table))
+    if poison:  # (whatever no sequence owns)
+        own = torch.zeros(b.k_pages.shape[:2], dtype=torch.bool)
+        for s, n in enumerate(RAGGED):
+            for t in range(n):
+                if b.table[s, t // 48] >= 0:
+                    own[int(b.table[s, t // 48]), t % 48] = True
+        for x in (b.k_pages, b.v_pages):
+            x[~own.cuda()] = float("nan")
+    return b
+
+
+@pytest.mark.parametrize("dtype,dim,poison", [("f16", 64, False), ("bf16", 128, False), ("bf16", 40, True), ("f16", 128, True)])
+def test_ragged_batches_in_equal_pieces(dtype, dim, poison):
+    b = _ragged(dim, dtype, dim, poison)
+    slopes = torch.tensor([2.0 ** -(i / 2 + 1) for i in range(16)], device="cuda")
+    for kw in (dict(), dict(window=100), dict(window=2500), dict(softcap=5.0, slopes=slopes)):
+        if poison and "window" not in kw and kw:
+            continue
+        for workspace in (True, False):
+            q, out, lse = b.run(workspace=workspace, **kw)
+            b.check(q, out, lse, what=str(kw), **{k: f64(v) if k == "slopes" else v for k, v in kw.items()})
+
+
+def test_ragged_pieces_of_one_token_and_of_a_wide_table():
+    """One long sequence among short ones, a table that would hold a hundred times as many tokens."""
+    lengths = [9000 if i == 13 else 1 + i % 70 for i in range(64)]
+    b = Batch(3, "bf16", lengths, [1] * 64, 32, 8, 128, 16, width=4096)
+    q, out, lse = b.run()
+    b.check(q, out, lse)
+    again = torch.zeros_like(out)
+    ws = torch.full((hb.hidet_cache_attention_workspace_bytes(b.cache, q, 1) // 4,), 3e38, device="cuda")
+    hb.hidet_cache_attention(b.cache, q, again, b.starts, 1, workspace=ws)
+    assert torch.equal(out, again)
+
+
+def test_ragged_pieces_under_a_wide_window():
+    lengths = [20000 if i == 3 else 17100 if i == 20 else 1 + 9 * i for i in range(32)]
+    b = Batch(4, "f16", lengths, [1 + i % 2 for i in range(31)] + [0], 8, 8, 64, 64)
+    q, out, lse = b.run(window=17000)
+    b.check(q, out, lse, window=17000)
+
+
+def test_ragged_pieces_captured_while_lengths_grow():
+    b = _ragged(11, "f16", 64)
+    q = b.rows(16)
+    ws = torch.empty(hb.hidet_cache_attention_workspace_bytes(b.cache, q, 4), dtype=torch.uint8, device="cuda")
+    outs = [torch.zeros_like(q) for _ in range(2)]
+    call = lambda out: hb.hidet_cache_attention(b.cache, q, out, b.starts, 4, workspace=ws)
+    call(outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(outs[1])
+    for shrink in (0, 100, 500, 3, 0):
+        b.lens.copy_(_ints([n if i % 3 else max(n - shrink, min(n, 4)) for i, n in enumerate(RAGGED)]))
+        outs[1].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        outs[0].zero_()
+        call(outs[0])
+        torch.cuda.synchronize()
+        assert torch.equal(*outs), shrink
+
+
+def test_ragged_lists_that_make_no_sense_reach_nothing():
+    """Starts and lengths out of any order: no index leaves its tensor, and nothing hangs."""
+    b = _ragged(12, "bf16", 64)
+    q = b.rows(16)
+    g = np.random.Generator(np.random.PCG64(5))
+    ws = torch.empty(hb.hidet_cache_attention_workspace_bytes(b.cache, q, 4), dtype=torch.uint8, device="cuda")
+    for lengths, starts, table in ((2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1), (10 ** 4, 100, 60)):
+        b.lens.copy_(torch.from_numpy(g.integers(-lengths, lengths, size=32).astype(np.int32)))
+        b.starts.copy_(torch.from_numpy(g.integers(-starts, starts, size=33).astype(np.int32)))
+        b.tables.copy_(torch.from_numpy(g.integers(-table, table, size=b.table.shape).astype(np.int32)))
+        buf = torch.full((q.numel() + 512,), 7.0, dtype=q.dtype, device="cuda")
+        out = buf[256:-256].view(q.shape)
+        hb.hidet_cache_attention(b.cache, q, out, b.starts, 4, workspace=ws)
+        torch.cuda.synchronize()
+        assert bool((buf[:256] == 7.0).all()) and bool((buf[-256:] == 7.0).all())
+
+
 def test_at_most_max_new_tokens_of_a_sequence():
     b = Batch(6, "bf16", [40, 60], [9, 4], 2, 2, 64, 16)
     q, out, lse = b.run(max_new=5)
