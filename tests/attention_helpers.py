@@ -8,6 +8,7 @@ relatively.  fp16 operands below 2^-14 are rounded on a grid of 2^-24, 2^-25 off
   out   u |out| (its rounding) + (u + E) sum_j p |v|  (weights rounded for the product) + 2^-25 sum_j |v| (fp16; weights are at least
         relative to a maximum of 1)
   D     sum_d |g| (error of out) + 1e-6 sum_d |g out|
+        where no query of 128 rows sees more than 32 keys (`few`) it is sum_j p dP instead: 2 E sum_j p |dP| + 1e-6 sum_j p sum_d |g v|
   dS    |dS| (u + E) + p (error of D + 1e-6 sum_d |g v| + 2e-5 |dP - D| (1 + |x|) for the cap's derivative) + 2^-25 (fp16)
   dQ    u |dQ| + scale sum_j (error of dS) |k|;  dK the same with q, summed over the heads that share a key
   dV    u |dV| + sum_i (u + E) p |g| + 2^-35 sum_i |g| (fp16; weights are lifted by 2^10)
@@ -25,7 +26,7 @@ def f64(t):
     return t.detach().cpu().to(torch.float64).numpy()
 
 
-def bounds(dtype, q, k, v, see, scale, softcap=0.0, slopes=None, grad_out=None):
+def bounds(dtype, q, k, v, see, scale, softcap=0.0, slopes=None, grad_out=None, few=False):
     """(out, lse, their bounds) and, with grad_out, (dq, dk, dv) and theirs; everything float64."""
     u, small = U[dtype], (2.0 ** -25 if dtype == "f16" else 0.0)
     batch, heads, n, d = q.shape
@@ -52,6 +53,8 @@ def bounds(dtype, q, k, v, see, scale, softcap=0.0, slopes=None, grad_out=None):
             dp, delta = g @ vh.T, (g * out[b, h]).sum(1, keepdims=True)
             ds = np.abs(p * (dp - delta) * derivative)
             d_delta = (np.abs(g) * b_out[b, h]).sum(1, keepdims=True) + 1e-6 * np.abs(g * out[b, h]).sum(1, keepdims=True)
+            if few:
+                d_delta = 2 * e * (p * np.abs(dp)).sum(1, keepdims=True) + 1e-6 * (p * (np.abs(g) @ np.abs(vh).T)).sum(1, keepdims=True)
             d_ds = ds * (u + 2 * e) + p * (d_delta + 1e-6 * (np.abs(g) @ np.abs(vh).T) + 2e-5 * (1 + top) * np.abs(dp - delta) * (softcap > 0))
             d_ds = np.where(m, d_ds + small, 0.0)
             b_dq[b, h] = u * np.abs(grads[0][b, h]) + abs(scale) * (d_ds @ np.abs(kh)) + small

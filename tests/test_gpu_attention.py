@@ -206,6 +206,34 @@ def test_the_only_key_of_a_query_has_no_gradient_of_its_score(dtype, dim, softca
         assert bool((dv != 3.0).any())
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim,h,hk,softcap", [(64, 4, 2, 0.0), (128, 2, 1, 0.0), (40, 3, 3, 20.0)])
+def test_gradients_of_few_keys_do_not_carry_the_rounding_of_the_output(dtype, dim, h, hk, softcap):
+    """Large scores of which one key has nearly all the weight: dS is far smaller than dP and D, whose difference it is."""
+    g = np.random.Generator(np.random.PCG64(27))
+    documents = np.array([[i // 6 if i < 90 else i // 3 for i in range(200)]] * 2)
+    for n, window in ((5, 0), (32, 0), (300, 3), (200, None), (70, 32)):
+        q, dout = (_draw(g, (2, h, n, dim), dtype, "dense") for _ in range(2))
+        k, v = (_draw(g, (2, hk, n, dim), dtype, "dense") for _ in range(2))
+        q.mul_(4.0)
+        if window is None:
+            see = np.stack([(x[:, None] == x[None]) & np.tril(np.ones((n, n), bool)) for x in documents])
+            ranges = torch.empty(2, n, 2, dtype=torch.int32, device="cuda")
+            hb.hidet_attention_ranges(ranges, documents=torch.from_numpy(documents.astype(np.int32)).cuda(), causal=True)
+            opts = dict(softcap=softcap, ranges=ranges)
+        else:
+            see = np.stack([oa.sees(n, n, True, window)] * 2)
+            opts = dict(softcap=softcap, causal=True, window=window)
+        out, dq, dk, dv = (torch.empty_like(t) for t in (q, q, k, v))
+        lse = torch.empty(2, h, n, device="cuda")
+        hb.hidet_attention(q, k, v, out, lse=lse, **opts)
+        ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+        hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, **opts)
+        want, bound = bounds(dtype, f64(q), f64(k), f64(v), see, dim ** -0.5, softcap, None, grad_out=f64(dout), few=True)
+        for name, t, x, e in zip(("dq", "dk", "dv"), (dq, dk, dv), want[2:], bound[2:]):
+            assert_within(t, x, e, "%s %d keys %s" % (dtype, n, name))
+
+
 def test_no_keys_and_no_queries():
     q = torch.randn(2, 4, 5, 64, device="cuda").half()
     k = torch.empty(2, 2, 0, 64, device="cuda", dtype=torch.float16)
