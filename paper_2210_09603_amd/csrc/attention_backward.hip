@@ -877,16 +877,15 @@ hipError_t dispatch(int form, const BackArgs& b, hipStream_t stream) {
 }
 
 long long row_groups_of(long long rows) { return (rows + 31) / 32; }
-// (of all forms: with a bias twice the fields)
 long long order_bytes(long long batch, long long key_tiles) { return (batch * key_tiles * 4 + 15) / 16 * 16; }
+// (of all forms: with a bias twice the fields)
 long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
 
 // How the two kernels' work is cut.
 //   dQ: tiles of 128 rows, in pairs of wavefronts as in the forward pass while the device takes all of them at once, and then as many
-//   splits of at least 4 tiles of 128 keys as find a compute unit each.  A whole pass (forward, dQ, dK and dV) without and with pairs, us: 6 entries of
-//   3146 rows of 96 dimensions 170 and 152, 9 of 3332 at 128 470 and 429, 36 of 1021 at 64 125 and 122; 36 of 1024 at 128, 288 tiles,
-//   202 and 227, and so without; one fits worse, 4 entries of 1472
-//   rows over 184 keys 47 and 50.
+//   splits of at least 4 tiles of 128 keys as find a compute unit each.  A whole pass (forward, dQ, dK and dV) without and with pairs, us:
+//   6 entries of 3146 rows of 96 dimensions 170 and 152, 9 of 3332 at 128 470 and 429, 36 of 1021 at 64 125 and 122; 36 of 1024 at
+//   128, 288 tiles, 202 and 227, and so without; one fits worse, 4 entries of 1472 rows over 184 keys 47 and 50.
 //   dK and dV: tiles of 64 keys, and where they leave compute units without work splits of at least 2 tiles of 128 rows: 256 workgroups
 //   (512 at 64 dimensions: 24 heads over 1449 keys 199 us for 211).  With 512 of at least 4 everywhere: the first of the passes above 220 for 190,
 //   the second 486 for 449, and 285 for 271 of 2 entries of 6599 rows.
