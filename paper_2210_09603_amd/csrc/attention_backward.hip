@@ -620,7 +620,11 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
     return int4{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z),
                 __builtin_amdgcn_readfirstlane(v.w)};
   };
-  int4 next0 = seen[min(4 * t0 + part, groups - 1)], next1 = seen[min(4 * t0 + part + GROUPS - 1, groups - 1)];
+  int4 next0 = {0, 0, 0, 0}, next1 = next0;
+  if (t0 < t1) {  // (without queries there is no list of them)
+    next0 = seen[min(4 * t0 + part, groups - 1)];
+    next1 = seen[min(4 * t0 + part + GROUPS - 1, groups - 1)];
+  }
   settle();
   if (t0 < t1) request(t0);
   for (int t = t0; t < t1; ++t) {

@@ -251,6 +251,21 @@ def test_no_keys_and_no_queries():
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [24, 64, 128])
+@pytest.mark.parametrize("form", [dict(), dict(causal=True), dict(softcap=20.0), dict(slopes=True), dict(softcap=5.0, slopes=True, window=3)], ids=str)
+def test_keys_without_queries_have_gradients_of_zero(form, dim, dtype):
+    """There is nothing then that says which rows see a key: no list of them is read."""
+    form = dict(form)
+    none = torch.empty(2, 4, 0, dim, device="cuda", dtype=TYPES[dtype])
+    k = torch.randn(2, 2, 150, dim, device="cuda").to(TYPES[dtype])
+    dk, dv = torch.full_like(k, 3.0), torch.full_like(k, 3.0)
+    if form.pop("slopes", False):
+        form["slopes"] = torch.ones(4, device="cuda")
+    hb.hidet_attention_backward(none, none, k, k, none, torch.empty(2, 4, 0, device="cuda"), none, dk, dv, None, **form)
+    assert not dk.any() and not dv.any()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("dim", [64, 104])
 def test_what_nobody_sees_and_what_others_see_has_no_influence(dtype, dim):
     def padding(q, k, v, g, see):  # keys and queries that take no part, and the gradients of the latter
