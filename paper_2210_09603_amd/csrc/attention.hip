@@ -128,7 +128,7 @@ extern "C" {
 int64_t hidet_attention_workspace_bytes(int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k, int64_t head_dim) {
   if (batch <= 0 || kv_heads <= 0 || heads <= 0 || heads % kv_heads != 0 || seq_q <= 0 || seq_k <= 0 || head_dim <= 0 || head_dim > 128) return 0;
   const long long group = heads / kv_heads;
-  if (group > kMaxRows || seq_q >= kMaxRows || seq_q * group >= kMaxRows || batch > kMaxBlocks || kv_heads > kMaxBlocks) return 0;
+  if (group >= kMaxRows || seq_q >= kMaxRows || seq_k >= kMaxRows || !fits_cut(batch, kv_heads, seq_q * group, seq_k)) return 0;
   const int dp = padded_dim(head_dim);
   const Cut c = cut_work(batch * kv_heads, seq_q * group, seq_k, dp, 1LL << 62, false);
   return c.splits > 1 ? c.splits * split_bytes(batch * kv_heads, seq_q * group, dp) : 0;
@@ -155,7 +155,7 @@ hidet_status_t hidet_attention(int32_t dtype, int64_t batch, int64_t heads, int6
       if (t->stride_row >= kMaxStride) return HIDET_ERR_UNSUPPORTED;
     }
   if (!is_aligned(lse, 4) || !is_aligned(workspace, 16)) return HIDET_ERR_ALIGNMENT;
-  if (batch > kMaxBlocks || kv_heads > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
+  if (!fits_cut(batch, kv_heads, seq_q * group, seq_k)) return HIDET_ERR_UNSUPPORTED;
   Args p{};
   p.q = q->data;
   p.k = seq_k > 0 ? k->data : nullptr;

@@ -928,8 +928,7 @@ int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, i
                                                  int64_t head_dim) {
   if (batch <= 0 || kv_heads <= 0 || heads <= 0 || heads % kv_heads != 0 || seq_q <= 0 || seq_k < 0 || head_dim <= 0 || head_dim > 128) return 0;
   const long long group = heads / kv_heads;
-  if (group >= kMaxRows || seq_q >= kMaxRows || seq_q * group >= kMaxRows || seq_k >= kMaxRows || batch > kMaxBlocks || kv_heads > kMaxBlocks)
-    return 0;
+  if (group >= kMaxRows || seq_q >= kMaxRows || seq_k >= kMaxRows || !fits_cut(batch, kv_heads, seq_q * group, seq_k)) return 0;
   const BackCut c = cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim));
   return info_bytes(batch * kv_heads, seq_q * group) + batch * row_groups_of(seq_q * group) * 16 + order_bytes(batch, c.key_tiles) + c.part_bytes;
 }
@@ -948,7 +947,7 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
   if (head_dim > 128 || head_dim % 8 != 0) return HIDET_ERR_UNSUPPORTED;
   const long long group = heads / kv_heads;
   if (group >= kMaxRows || seq_q >= kMaxRows || seq_k >= kMaxRows || seq_q * group >= kMaxRows) return HIDET_ERR_UNSUPPORTED;
-  if (batch > kMaxBlocks || kv_heads > kMaxBlocks) return HIDET_ERR_UNSUPPORTED;
+  if (!fits_cut(batch, kv_heads, seq_q * group, seq_k)) return HIDET_ERR_UNSUPPORTED;
   if (seq_q > 0) {
     for (const hidet_heads_t* t : {grad_out, q, out})
       if (hidet_status_t st = check_heads(t, batch, heads, seq_q, head_dim, false); st != HIDET_OK) return st;

@@ -66,6 +66,11 @@ struct Cut {
   bool pairs;   // that of many with two wavefronts for 32 rows
   int row_tiles, splits, share;
 };
+// What cut_work and its like may be asked: with 2^24 entries of 2^29 rows the bytes of a partial result, 520 a row at most, stay
+// below 2^63.  (More entries are more workgroups than a launch has.)
+inline bool fits_cut(long long outer, long long kv_heads, long long rows, long long keys) {
+  return outer <= kMaxBlocks && kv_heads <= kMaxBlocks && outer * kv_heads <= kMaxBlocks && rows < kMaxRows && keys < (1LL << 31);
+}
 inline long long split_bytes(long long entries, long long rows, int dp) { return entries * rows * (dp + 2) * 4; }
 Cut cut_work(long long entries, long long rows, long long keys, int dp, long long room, bool ragged);
 

@@ -136,6 +136,7 @@ long long keys_at_most(const hidet_cache_t* c, long long max_new, long long wind
 // the pieces' second kernel, and the ends of two sequences one after the other.
 int flat_pieces(const hidet_cache_t* c, long long rows, long long keys) {
   if (rows > 32 || c->seqs > kFlatSeqs || c->seqs * c->heads < 256 || keys < 16384 || (keys / kStreamKeys + 1) * c->seqs >= (1LL << 30)) return 0;
+  if (c->seqs * c->heads * rows > kMaxBlocks) return 0;  // (the second kernel has a workgroup for each)
   return (int)std::max(1LL, 512 / (long long)c->heads);
 }
 long long flat_bytes(const hidet_cache_t* c, long long rows, int pieces, int dp) {
@@ -206,10 +207,11 @@ int64_t hidet_cache_attention_workspace_bytes(const hidet_cache_t* cache, int64_
       cache->head_dim > 128 || window < 0)
     return 0;
   const long long group = heads / cache->heads;
-  if (max_new >= kMaxRows || group >= kMaxRows || max_new * group >= kMaxRows) return 0;
+  if (max_new >= kMaxRows || group >= kMaxRows) return 0;
   const int dp = padded_dim(cache->head_dim);
   const long long entries = cache->seqs * cache->heads, rows = max_new * group;
   const long long keys = keys_at_most(cache, max_new, window);
+  if (!fits_cut(cache->seqs, cache->heads, rows, keys)) return 0;
   if (const int pieces = flat_pieces(cache, rows, keys)) return flat_bytes(cache, rows, pieces, dp);
   const Cut c = cut_work(entries, rows, keys, dp, 1LL << 62, true);
   return c.splits > 1 ? c.splits * split_bytes(entries, rows, dp) : 0;
@@ -264,6 +266,7 @@ hidet_status_t hidet_cache_attention(const hidet_cache_t* cache, int64_t heads, 
   p.softcap = options->softcap;
   const long long entries = cache->seqs * cache->heads, rows = max_new * group;
   const long long keys = keys_at_most(cache, max_new, options->window);
+  if (!fits_cut(cache->seqs, cache->heads, rows, keys)) return HIDET_ERR_UNSUPPORTED;
   const int dp = padded_dim(cache->head_dim), pieces = flat_pieces(cache, rows, keys);
   if (pieces && workspace && workspace_bytes >= flat_bytes(cache, rows, pieces, dp)) p.flat = pieces;
   const Cut c = cut_work(entries, rows, keys, dp, workspace ? workspace_bytes : 0, true);

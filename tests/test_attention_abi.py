@@ -217,3 +217,31 @@ def test_workspaces_that_are_not_dense_are_refused():
                         (hb.hidet_cache_attention, (cache, rows, rows, i32(2), 3))):
             with pytest.raises(ValueError, match="dense"):
                 f(*args, workspace=ws)
+
+
+def test_sizes_at_and_beyond_the_limits_are_answered():
+    """Each size within its own limit, their product far beyond: a query of a workspace answers 0, a call refuses; sizes that a call
+    takes have workspaces that are counted in 64 bits."""
+    L = hb.lib()
+    big = [(1 << 24, 1 << 20, 1 << 20, 1 << 20, 4096, 64), (1 << 24, 1 << 24, 1 << 24, 1 << 13, 1, 64), (1 << 24, 1 << 24, 1 << 24, 1 << 28, 1, 128),
+           (1 << 24, 2, 2, 5, 1 << 28, 64), (1, 1 << 28, 1, 2, 4096, 64), (2, 4, 2, 16, 1 << 62, 64), (1 << 62, 4, 2, 16, 16, 64), (1, 1 << 62, 1 << 62, 1, 1, 64),
+           (1, 1 << 62, 1, 1, 1, 64)]
+    for b, h, kv, n, m, d in big:
+        assert L.hidet_attention_workspace_bytes(b, h, kv, n, m, d) == 0, (b, h, kv, n, m, d)
+        assert L.hidet_attention_backward_workspace_bytes(b, h, kv, n, m, d) == 0, (b, h, kv, n, m, d)
+        near = heads(batch=128, head=128, row=128)
+        for call in (attention, backward):
+            kw = dict(q=near, k=near, v=near, out=heads(0x100000, 128, 128, 128), wb=1 << 62, ws=0x10000)
+            if call is backward:
+                kw.update(g=near, gq=heads(0x100000, 128, 128, 128), gk=near, gv=near)
+            assert call(batch=b, heads=h, kv=kv, sq=n, sk=m, dim=d, **kw) == UNSUPPORTED, (b, h, kv, n, m, d)
+    # rows and keys at their limits, for entries at theirs
+    most = L.hidet_attention_backward_workspace_bytes(1 << 12, 1 << 12, 1 << 12, (1 << 29) - 1, 1, 128)
+    assert most >= (1 << 24) * ((1 << 29) - 1) * 32
+    for seqs, kv, h, new in ((1 << 24, 1 << 20, 1 << 20, 1 << 13), (1 << 24, 1 << 24, 1 << 24, 1 << 13), (1 << 13, 1 << 12, 1 << 12, 4), (1 << 24, 2, 2, 1 << 28)):
+        c = cache(seqs=seqs, heads=kv, stride_head=64, stride_slot=64, stride_page=64)
+        assert L.hidet_cache_attention_workspace_bytes(c, h, new, 0) == 0
+        assert cache_attention(c, n_heads=h, max_new=new, q=heads(row=64, head=64), out=heads(0x90000, row=64, head=64)) == UNSUPPORTED
+    # (so many rows that the second kernel of equal pieces had no grid for them)
+    c = cache(seqs=1024, heads=1 << 14, stride_head=64, stride_slot=64, stride_page=64, table_width=4096, table_stride=4096)
+    assert L.hidet_cache_attention_workspace_bytes(c, 1 << 19, 1, 0) == 0
