@@ -332,6 +332,17 @@ __device__ __forceinline__ long long lse_offset(const Args& p, const Entry& e, c
     return ((long long)e.b * p.heads + w.head) * p.seq_q + w.token;
 }
 
+// Tiles of TILE keys from `begin` on: how many there are up to `end`, and key i of tile t, `end` at the farthest.  A cache's keys may
+// end at 2^31 - 1, and what lies a tile behind them passes 32 bits with a sign.
+template <int TILE>
+__device__ __forceinline__ int tiles_of(int begin, int end) {
+  return (int)(((unsigned)(end - begin) + TILE - 1) / TILE);
+}
+template <int TILE>
+__device__ __forceinline__ int key_at(int begin, int t, int i, int end) {
+  return (int)min((unsigned)begin + (unsigned)t * TILE + (unsigned)i, (unsigned)end);
+}
+
 // Where a key is.  What is asked of the table and what is made of it are apart: a loop asks one tile ahead of the keys' own loads, and
 // using the answer at once would wait for every load in flight.
 struct KeyPlace {
@@ -429,7 +440,7 @@ __device__ __forceinline__ void softmax_tile(State<T, DP>& st, f32x16 (&s)[KT], 
       for (int r = 0; r < 16; ++r) s[t][r] = score(s[t][r], distance - (float)(32 * t + 8 * (r >> 2) + (r & 3)));
   }
   if (masked) {
-    const int from = lo - first - 4 * half;
+    const unsigned from = (unsigned)lo - (unsigned)first - 4u * half;
     const unsigned count = (unsigned)(hi - lo);
     const unsigned long long mine = there >> (4 * half);
 #pragma unroll
@@ -437,7 +448,7 @@ __device__ __forceinline__ void softmax_tile(State<T, DP>& st, f32x16 (&s)[KT], 
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = 32 * t + 8 * (r >> 2) + (r & 3);
-        s[t][r] = (unsigned)(j - from) < count && ((mine >> j) & 1) ? s[t][r] : kNoMax;
+        s[t][r] = (unsigned)j - from < count && ((mine >> j) & 1) ? s[t][r] : kNoMax;
       }
   }
   float top = s[0][0];
@@ -667,7 +678,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
   }
   if (begin >= end) begin = end = 0;
   // this split's share of the tiles, the first of which begins with the first key that anyone sees
-  const int all = (end - begin + TILE - 1) / TILE;
+  const int all = tiles_of<TILE>(begin, end);
   const int t0 = min(all, z * p.share), t1 = z + 1 < p.splits ? min(all, t0 + p.share) : all;
 
   const T* kbase = keys_of<T, PAGED>(p, e, p.k, p.ks);
@@ -687,7 +698,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
   KeyPlace next = {0, 0};  // paged: where lane l's key of the tile after the next is
   unsigned long long there = ~0ull, there_next = ~0ull;
   auto look_up = [&](int t) {
-    if constexpr (PAGED) next = find_key<PAGED>(p, e, min(begin + t * TILE + lane, end - 1));
+    if constexpr (PAGED) next = find_key<PAGED>(p, e, key_at<TILE>(begin, t, lane, end - 1));
   };
   auto request = [&](int t) {
     const unsigned to = lds + (t & 1) * STAGE;
@@ -742,7 +753,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
     there = there_next;
     if (t + 1 < t1) request(t + 1);
     const int first = begin + t * TILE + own;
-    if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
+    if (first >= mine.hi || first <= mine.lo - kTileKeys) continue;
     const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
     f32x16 s[2];
 #pragma unroll
@@ -752,7 +763,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) s[i] = mfma_op(row_frag<T, DP>(map, keys, i * 32, ks), st.q[ks], s[i]);
     }
-    const bool masked = first < mine.full_lo || first + kTileKeys > mine.full_hi || (PAGED && ~there != 0);
+    const bool masked = first < mine.full_lo || first > mine.full_hi - kTileKeys || (PAGED && ~there != 0);
     Frag pf[4];
     softmax_tile<T, DP, FORM, 2>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
 #pragma unroll
@@ -783,7 +794,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
     st.sum = st.sum * by + meet[(DT * 16 + 1) * 64] * by_other;
     st.shift = level;
   }
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * TILE, min(end, begin + t1 * TILE),
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, key_at<TILE>(begin, t0, 0, end), key_at<TILE>(begin, t1, 0, end),
                                 part_of<DP>(p, e.b, e.kv, z, 0), p.splits > 1);
 }
 
@@ -817,7 +828,7 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
   const int at = w.token + e.shift;
   const Seen seen = seen_by<PAGED>(p, e, w, r0, min(r0 + 31, rows - 1));
   const int end = seen.hi, begin = min(seen.lo, end);
-  const int all = (end - begin + kStreamKeys - 1) / kStreamKeys;
+  const int all = tiles_of<kStreamKeys>(begin, end);
   t0 = min(t0, all);
   t1 = min(t1, all);
   const T* kbase = keys_of<T, PAGED>(p, e, p.k, p.ks);
@@ -830,7 +841,7 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
   u32x4 kr[NL], vr[NL];
   KeyPlace next = {0, 0};  // of lane's key, lane % 32 of the tile after the next
   unsigned long long there_next = ~0ull;
-  auto look_up = [&](int t) { next = find_key<PAGED>(p, e, min(begin + t * kStreamKeys + (lane & 31), end - 1)); };
+  auto look_up = [&](int t) { next = find_key<PAGED>(p, e, key_at<kStreamKeys>(begin, t, lane & 31, end - 1)); };
   auto from_lane = [&](long long v, int lane_of_row) {
     const unsigned low = __shfl((int)(unsigned)v, lane_of_row), high = __shfl((int)(unsigned)(v >> 32), lane_of_row);
     return (long long)(((unsigned long long)high << 32) | low) + load_chunk * 8;
@@ -876,7 +887,7 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
     for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) s[0] = mfma_op(row_frag<T, DP>(map, keys, 0, ks), st.q[ks], s[0]);
-    const bool masked = first < seen.full_lo || first + kStreamKeys > seen.full_hi || (PAGED && there != 0xffffffffull);
+    const bool masked = first < seen.full_lo || first > seen.full_hi - kStreamKeys || (PAGED && there != 0xffffffffull);
     Frag pf[2];
     softmax_tile<T, DP, FORM, 1>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
 #pragma unroll
@@ -936,7 +947,8 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
   st.top = top;
   st.shift = level;
   st.sum = half == 0 ? sum : 0.0f;
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, begin + t0 * kStreamKeys, min(end, begin + t1 * kStreamKeys), to_rows, partial);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, key_at<kStreamKeys>(begin, t0, 0, end), key_at<kStreamKeys>(begin, t1, 0, end), to_rows,
+                              partial);
 }
 
 template <typename T, int DP, bool PAGED, int FORM>
@@ -968,7 +980,7 @@ __device__ __forceinline__ int flat_tiles(const Args& p, int s) {
   int lo, first_hi, last_lo, hi;
   seen_from<true>(p, e, e.shift, lo, first_hi);
   seen_from<true>(p, e, e.tokens - 1 + e.shift, last_lo, hi);
-  return max((hi - min(lo, hi) + kStreamKeys - 1) / kStreamKeys, 1);
+  return max(tiles_of<kStreamKeys>(min(lo, hi), hi), 1);
 }
 __device__ __forceinline__ int flat_share(const Args& p, int total) { return max((total + p.flat - 1) / p.flat, 1); }
 // sums of a piece's part of a sequence: `begins` if the sequence begins in it

@@ -394,3 +394,51 @@ def test_a_serving_step_captured_and_replayed():
     hb.hidet_cache_attention(eager[0], eager[1][:, :8], out, starts, 1, workspace=eager[3], stream=side)
     side.synchronize()
     assert torch.equal(out, eager[2])
+
+
+LAST = 2 ** 31 - 1  # the longest sequence that a length can state
+
+
+def _one_page_everywhere(new, values):
+    """A sequence of 2^31 - 1 tokens of 8 dimensions whose pages are all the same one, of 2^20 slots that hold `values`."""
+    page = 1 << 20
+    k, v = (torch.from_numpy(x).to(torch.float16).cuda().view(1, page, 1, 8) for x in values)
+    cache = hb.make_cache(k, v, torch.zeros(1, 2048, dtype=torch.int32, device="cuda"), _ints([LAST]))
+    return cache, k, v, _ints([0, new])
+
+
+@pytest.mark.parametrize("new,window", [(1, 3000), (1, 33), (3, 50), (2000, 3000)])
+def test_windows_at_the_last_positions_that_a_length_can_state(new, window):
+    """Tiles of keys that end behind 2^31 - 1 (few rows, and 2000 in tiles of 128): the keys that the queries see are the last ones."""
+    g = np.random.Generator(np.random.PCG64(41))
+    cache, k, v, starts = _one_page_everywhere(new, [g.standard_normal((1 << 20, 8)).astype(np.float32) for _ in range(2)])
+    q = torch.from_numpy(g.standard_normal((new, 2, 8)).astype(np.float32)).half().cuda()
+    out, lse = torch.full_like(q, 7.0), torch.full((new, 2), 7.0, device="cuda")
+    size = hb.hidet_cache_attention_workspace_bytes(cache, q, new, window)
+    ws = torch.full((size // 4 + 4,), float("nan"), device="cuda")
+    hb.hidet_cache_attention(cache, q, out, starts, new, lse=lse, window=window, workspace=ws)
+    keys = new + window
+    slots = (LAST - keys + torch.arange(keys)) % (1 << 20)
+    kk, vv = (f64(x[0, :, 0].cpu()[slots])[None, None] for x in (k, v))
+    see = oa.sees(new, keys, causal=True, window=window)[None]
+    want, bound = bounds("f16", f64(q).transpose(1, 0, 2)[None], kk, vv, see, 8 ** -0.5)
+    assert_within(f64(out).transpose(1, 0, 2)[None], want[0], bound[0], "out")
+    assert_within(f64(lse).T[None], want[1], bound[1], "lse")
+
+
+def test_every_key_up_to_the_last_position_that_a_length_can_state():
+    """Scores of 0 and values of -1, 0 and 1: weights are 1 and all partial sums whole numbers of fp32, so that the mean is off by the
+    divisions and roundings of its end alone (2^-11, and a few of 2^-24)."""
+    g = np.random.Generator(np.random.PCG64(42))
+    v = g.integers(-1, 2, (1 << 20, 8)).astype(np.float32)
+    v[:, 0] = 1.0
+    cache, _, _, starts = _one_page_everywhere(1, [np.ones((1 << 20, 8), np.float32), v])
+    q = torch.zeros(1, 1, 8, dtype=torch.float16, device="cuda")
+    out, lse = torch.full_like(q, 7.0), torch.full((1, 1), 7.0, device="cuda")
+    size = hb.hidet_cache_attention_workspace_bytes(cache, q, 1)
+    assert size > 0
+    ws = torch.full((size // 4,), float("nan"), device="cuda")
+    hb.hidet_cache_attention(cache, q, out, starts, 1, lse=lse, workspace=ws)
+    want = (2048 * v.astype(np.float64).sum(0) - v[-1]) / LAST
+    assert np.all(np.abs(f64(out)[0, 0] - want) <= (2.0 ** -11 + 2.0 ** -20) * np.abs(want) + 2.0 ** -25), (f64(out), want)
+    assert abs(float(lse[0, 0]) - np.log(LAST)) <= 1e-5
