@@ -501,17 +501,17 @@ hidet_status_t hidet_rope_frequencies(int64_t rotary_dim, double base, int32_t s
  * A cache of keys and values in pages, shared by the sequences of a batch: element d of head h of the token at position t of
  * sequence s lies at  page * stride_page + (t % page_size) * stride_slot + h * stride_head + d  of k and of v, with
  * page = tables[s * table_stride + t / page_size].  lengths[s] is the number of tokens that the sequence has in the cache, the
- * new ones of a call among them (cut to table_width * page_size).  A page number outside 0 .. num_pages - 1 stands for no page:
- * nothing is written there and its keys are not seen.  Page sizes need not be powers of two, strides are free (both tensors
+ * new ones of a call among them.  A page number outside 0 .. num_pages - 1 stands for no page, and so does a position of
+ * table_width * page_size or more: nothing is written there and its keys are not seen.  Page sizes need not be powers of two, strides are free (both tensors
  * share them; the head_dim elements are contiguous), offsets are 64 bits wide.  All but the structure itself is DEVICE memory.
  *
  * A call serves a ragged batch: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of `tokens` rows (starts:
- * DEVICE, ascending, [seqs + 1]; cut to 0 .. tokens), and they are the sequence's last positions: its i-th new token stands at
- * position lengths[s] - (starts[s + 1] - starts[s]) + i.  Rows of no sequence are left as they are.  max_new bounds the new
+ * DEVICE, ascending, [seqs + 1]; cut to 0 .. tokens before anything else), and they are the sequence's last positions: its i-th new
+ * token stands at position lengths[s] - (starts[s + 1] - starts[s]) + i.  Rows of no sequence are left as they are.  max_new bounds the new
  * tokens of a sequence (it sizes the grid); of a sequence with more only the first max_new are worked on.
  *
  * hidet_cache_append writes k and v [tokens][heads][head_dim] of the cache's dtype (any of the three) into the pages.  Two tokens
- * for the same place (a page that two sequences share): one of them is kept, which one is not defined.
+ * for the same place (a page that two sequences share): every 16 bytes of it are those of one of them, which one is not defined.
  * hidet_cache_attention is hidet_attention (its options with causal = 1 and no ranges; q, out: [tokens][heads][head_dim], dtypes
  * F16 and BF16) of every new token over its sequence's keys up to its own position.  lse (may be NULL) is [tokens][heads].  The
  * workspace is as there; hidet_cache_attention_workspace_bytes gives its size.

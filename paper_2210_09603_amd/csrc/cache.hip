@@ -41,7 +41,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs p) {
   if (tid == 0) before = 0;
   __syncthreads();
   int ended = 0;
-  for (int s = tid; s < p.seqs; s += kThreads) ended += p.starts[s + 1] <= token0;
+  // (starts are cut to the rows that there are, as the attention cuts them: a sequence's new tokens are those that are left)
+  const auto start = [&](int s) { return min(max(p.starts[s], 0), p.tokens); };
+  for (int s = tid; s < p.seqs; s += kThreads) ended += start(s + 1) <= token0;
 #pragma unroll
   for (int m = 32; m; m >>= 1) ended += __shfl_xor(ended, m);
   if ((tid & 63) == 0 && ended) atomicAdd(&before, ended);  // (whole numbers: the order changes nothing)
@@ -49,10 +51,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(const AppendArgs p) {
   if (tid < tokens) {
     const int token = token0 + tid;
     int s = before;
-    while (s < p.seqs && p.starts[s + 1] <= token) ++s;
+    while (s < p.seqs && start(s + 1) <= token) ++s;
     long long at = -1;
     if (s < p.seqs) {
-      const int first = p.starts[s], count = p.starts[s + 1] - first, i = token - first;
+      const int first = start(s), count = start(s + 1) - first, i = token - first;
       const long long position = (long long)p.lengths[s] - count + i;
       if (i >= 0 && i < p.max_new && position >= 0 && position < (long long)p.table_width * p.page_size) {
         const int page_at = p.d_page.div((int)position);

@@ -442,3 +442,40 @@ def test_every_key_up_to_the_last_position_that_a_length_can_state():
     want = (2048 * v.astype(np.float64).sum(0) - v[-1]) / LAST
     assert np.all(np.abs(f64(out)[0, 0] - want) <= (2.0 ** -11 + 2.0 ** -20) * np.abs(want) + 2.0 ** -25), (f64(out), want)
     assert abs(float(lse[0, 0]) - np.log(LAST)) <= 1e-5
+
+
+@pytest.mark.parametrize("starts", [[0, 9], [-4, 5], [-4, 9, 2 ** 31 - 1], [0, 3, 9], [-2 ** 31, 2, 2 ** 31 - 1], [1, 4, 70]])
+@pytest.mark.parametrize("max_new", [9, 2])
+def test_starts_that_leave_the_batch_are_cut_to_it(starts, max_new):
+    """5 rows of tokens: append writes those of a sequence to its last positions, counted from the cut starts, where the attention that
+    follows looks for them."""
+    tokens, seqs, page = 5, len(starts) - 1, 16
+    b = Batch(43, "f16", [40, 33][:seqs], [1] * seqs, 2, 1, 64, page)
+    b.tokens = tokens
+    k, v, q = b.rows(1), b.rows(1), b.rows(2)
+    b.starts.copy_(_ints([max(min(x, 2 ** 31 - 1), -2 ** 31) for x in starts]))
+    cut = [min(max(x, 0), tokens) for x in starts]
+    want = [b.k_pages.clone(), b.v_pages.clone()]
+    for s in range(seqs):
+        n = cut[s + 1] - cut[s]
+        for i in range(min(n, max_new)):
+            at = b.lengths[s] - n + i
+            for x, new in zip(want, (k, v)):
+                x[int(b.table[s, at // page]), at % page] = new[cut[s] + i]
+    hb.hidet_cache_append(b.cache, k, v, b.starts, max_new)
+    assert torch.equal(b.k_pages, want[0]) and torch.equal(b.v_pages, want[1])
+    out, lse = torch.full_like(q, 7.0), torch.full((tokens, 2), 7.0, device="cuda")
+    hb.hidet_cache_attention(b.cache, q, out, b.starts, max_new, lse=lse)
+    for s in range(seqs):
+        n = cut[s + 1] - cut[s]
+        rows = slice(cut[s], cut[s] + min(n, max_new))
+        kk, vv = (oa.cache_rows(f64(x), b.table[s], b.lengths[s])[0] for x in want)
+        see = oa.sees(n, b.lengths[s], causal=True)[:min(n, max_new)]
+        if not len(see):
+            continue
+        w, e = bounds("f16", f64(q[rows]).transpose(1, 0, 2)[None], kk[None], vv[None], see[None], 64 ** -0.5)
+        assert_within(f64(out[rows]).transpose(1, 0, 2)[None], w[0], e[0], "sequence %d" % s)
+    written = np.zeros(tokens, bool)
+    for s in range(seqs):
+        written[cut[s]:cut[s] + min(cut[s + 1] - cut[s], max_new)] = True
+    assert bool((out[torch.from_numpy(~written).cuda()] == 7.0).all())
