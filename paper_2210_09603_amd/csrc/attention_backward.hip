@@ -44,6 +44,7 @@ struct BackArgs {
 // rows at once, and padded to whole tiles by rows that nobody is seen by.
 //   0  lse to base 2, less the lift     1  D, divided by the lift     2, 3  first key seen, their number
 //   4  position, 5  slope to base 2 (with a bias only: 8 fields, else 4)
+// (positions are whole numbers, as their differences to a key's are taken: from 2^24 on fp32 does not hold them)
 template <int FORM>
 __device__ __forceinline__ float* row_info(const BackArgs& b, const Entry& e, int r, int field) {
   constexpr int FIELDS = FORM & FORM_BIAS ? 8 : 4;
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
     *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 2)) = w.lo;
     *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 3)) = is ? w.hi - w.lo : 0;
     if constexpr (FORM & FORM_BIAS) {
-      *row_info<FORM>(b, e, r, 4) = (float)at;
+      *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 4)) = at;
       *row_info<FORM>(b, e, r, 5) = p.slopes ? p.slopes[w.head] * kLog2e : 0.0f;
     }
   }
@@ -613,7 +614,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
   const Score<FORM> all_scores(p, 0.0f);
-  const float at_key = (float)key;
   // (which groups of 32 rows take part: asked for a tile ahead, and in scalar registers before the next tile's loads are under way, for
   // which the compiler would otherwise wait)
   const auto in_scalars = [](const int4& v) {
@@ -682,11 +682,13 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
       for (int g = 0; g < 4; ++g) {  // P
         const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
         const f32x4 lse = *reinterpret_cast<const f32x4*>(quad);
-        f32x4 at = {0, 0, 0, 0}, slope = {0, 0, 0, 0};
+        f32x4 slope = {0, 0, 0, 0};
+        int4 at = {0, 0, 0, 0};
         if constexpr (FORM & FORM_BIAS) {
-          at = *reinterpret_cast<const f32x4*>(quad + 16);
+          at = *reinterpret_cast<const int4*>(quad + 16);
           slope = *reinterpret_cast<const f32x4*>(quad + 20);
         }
+        const int at4[4] = {at.x, at.y, at.z, at.w};
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int r = 4 * g + u;
@@ -694,7 +696,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
             s[r] = exp2_fast(__builtin_fmaf(s[r], score.factor, -lse[u]));
           } else {
             score.slope = slope[u];
-            s[r] = exp2_fast(score(s[r], at[u] - at_key, derivative[r]) - lse[u]);
+            s[r] = exp2_fast(score(s[r], (float)(at4[u] - key), derivative[r]) - lse[u]);
           }
         }
       }

@@ -567,6 +567,36 @@ def test_strides_beyond_32_bits(group):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim,softcap", [(64, 0.0), (128, 0.0), (40, 8.0)])
+def test_gradients_under_slopes_at_positions_beyond_2_to_24(dtype, dim, softcap):
+    """The distance of a query to a key is exact wherever both are: one query, and windows of several, at the end of 2^25 + 2^24 keys."""
+    g = np.random.Generator(np.random.PCG64(31))
+    m, h, hk = 2 ** 25 + 2 ** 24, 4, 2
+    slopes = torch.tensor([0.5, 0.25, 1.0, 0.125], device="cuda")
+    for n, width in ((1, 7), (40, 33), (200, 90)):
+        q, dout = (_draw(g, (1, h, n, dim), dtype, "dense") for _ in range(2))
+        near = n + width - 1  # keys that a query sees one of
+        k, v = (_draw(g, (1, hk, near, dim), dtype, "dense") for _ in range(2))
+        lo = torch.arange(n, dtype=torch.int32) + (m - near)
+        ranges = torch.stack([lo, lo + width], 1)[None].contiguous().cuda()
+        keys, values = (torch.zeros(1, hk, m, dim, dtype=TYPES[dtype], device="cuda") for _ in range(2))
+        keys[:, :, m - near:], values[:, :, m - near:] = k, v
+        out, dq = torch.empty_like(q), torch.empty_like(q)
+        lse = torch.empty(1, h, n, device="cuda")
+        dk, dv = (torch.full_like(keys, 3.0) for _ in range(2))
+        opts = dict(slopes=slopes, ranges=ranges, softcap=softcap)
+        hb.hidet_attention(q, keys, values, out, lse=lse, **opts)
+        ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, keys) // 4, device="cuda")
+        hb.hidet_attention_backward(dout, q, keys, values, out, lse, dq, dk, dv, ws, **opts)
+        see = np.stack([oa.in_ranges(ranges[0].cpu().numpy() - (m - near), near)])
+        want, bound = bounds(dtype, f64(q), f64(k), f64(v), see, dim ** -0.5, softcap, f64(slopes), grad_out=f64(dout))
+        got = (out, lse, dq, dk[:, :, m - near:], dv[:, :, m - near:])
+        for name, t, w, e in zip(("out", "lse", "dq", "dk", "dv"), got, want, bound):
+            assert_within(t, w, e, "%s %d %s" % (dtype, n, name))
+        assert not dk[:, :, :m - near].any() and not dv[:, :, :m - near].any()
+
+
 def test_a_training_step_from_tokens_to_gradients():
     """rope -> attention -> backward -> rope backward, as a step runs them, against the oracle's chain of the same."""
     g = np.random.Generator(np.random.PCG64(23))
