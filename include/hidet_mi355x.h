@@ -428,7 +428,7 @@ typedef struct {
 typedef struct {
   uint32_t struct_size; /* sizeof(hidet_attention_options_t) */
   int32_t causal;
-  float scale;          /* finite */
+  float scale;          /* finite, and so in fp32 are 2 log2(e) scale and, with a cap, 2 log2(e) scale / softcap */
   float softcap;        /* 0: none */
   int64_t window;       /* 0: none */
   const float* slopes;  /* DEVICE, [heads]; NULL: none */

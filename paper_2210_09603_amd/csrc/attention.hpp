@@ -194,21 +194,30 @@ __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_ex
 // ---- scores -----------------------------------------------------------------------------------------------------------
 // What a score is besides scale * q.k, a template parameter of the kernels: an exponential and a reciprocal an element for the cap
 // (half of such a kernel's vector time), two instructions for the bias.
-enum : int { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2 };  // PLAIN: scale > 0 and nothing else
+enum : int { FORM_PLAIN = 0, FORM_BIAS = 1, FORM_CAP = 2, FORM_WIDE = 7 };  // PLAIN: scale > 0 and nothing else; WIDE: both, see Score
 
 // The score to base 2 of a product: scale and cap as they stand in Args, slope for the query's head.
+//
+// cap tanh(y) = cap - 2 cap / (e^2y + 1) is off by some 2^-23 of the cap (2^-22 if every rounding falls the same way), whatever the
+// score is: up to kWideCap that is 8e-6, as much as scores of the cap's size are off anyhow.  Under larger caps (WIDE) scores below a
+// quarter of them are taken by tanh(y) = y (1 - y^2/3 + 2 y^4/15 - 17 y^6/315 + 62 y^8/2835 - ...), off by 4e-8 of itself at y = 1/4,
+// times cap / y, so that a cap that no score comes near leaves them as they are.  (A cap of 1e4, scores of 1 to 3: off by 1e-3 in the
+// first form.)  A form of its own: as a branch in the kernels of usual caps it took 25 registers of theirs.
+constexpr float kWideCap = 64.0f;
 template <int FORM>
 struct Score {
   float factor;  // to base 2; with a cap: 2 log2(e) scale / cap, so that exp2 of it is e^2y
   float cap;     // cap * log2(e)
   float slope;   // slope * log2(e)
+  float small, ratio;  // WIDE: without the cap, to base 2; y of a product
   __device__ __forceinline__ Score(const Args& p, float slope_of_head) {
     factor = FORM & FORM_CAP ? 2.0f * kLog2e * p.scale / p.softcap : p.scale * kLog2e;
     cap = p.softcap * kLog2e;
     slope = slope_of_head * kLog2e;
+    small = p.scale * kLog2e;
+    ratio = p.scale / p.softcap;
   }
-  // 1 / (e^2y + 1), of which tanh(y) is 1 - 2 r and its derivative 4 r (1 - r): off by some 2^-23, which is what the score's own
-  // rounding to fp32 is off for scores near the cap
+  // 1 / (e^2y + 1), of which tanh(y) is 1 - 2 r and its derivative 4 r (1 - r)
   __device__ __forceinline__ float share(float dot) const { return __builtin_amdgcn_rcpf(exp2_fast(dot * factor) + 1.0f); }
   // (distances beyond 2^24 are rounded to fp32, 2^-24 of themselves)
   __device__ __forceinline__ float biased(float x, float distance) const {
@@ -216,17 +225,25 @@ struct Score {
     return x;
   }
   __device__ __forceinline__ float operator()(float dot, float distance) const {
-    return biased(FORM & FORM_CAP ? __builtin_fmaf(-2.0f * cap, share(dot), cap) : dot * factor, distance);
+    float derivative;
+    return (*this)(dot, distance, derivative);
   }
   // the same with its derivative to the uncapped score
   __device__ __forceinline__ float operator()(float dot, float distance, float& derivative) const {
-    if constexpr (FORM & FORM_CAP) {
-      const float r = share(dot);
-      derivative = 4.0f * r * (1.0f - r);
-      return biased(__builtin_fmaf(-2.0f * cap, r, cap), distance);
-    }
     derivative = 1.0f;
-    return biased(dot * factor, distance);
+    if constexpr (!(FORM & FORM_CAP)) return biased(dot * factor, distance);
+    const float r = share(dot);
+    float x = __builtin_fmaf(-2.0f * cap, r, cap);
+    derivative = 4.0f * r * (1.0f - r);
+    if constexpr (FORM == FORM_WIDE) {
+      const float y = dot * ratio, y2 = y * y;
+      const float to_y = __builtin_fmaf(
+          y2, __builtin_fmaf(y2, __builtin_fmaf(y2, __builtin_fmaf(y2, 62.0f / 2835.0f, -17.0f / 315.0f), 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+      const bool flat = __builtin_fabsf(y) < 0.25f;
+      x = flat ? dot * small * to_y : x;
+      derivative = flat ? __builtin_fmaf(-(y * to_y), y * to_y, 1.0f) : derivative;
+    }
+    return biased(x, distance);
   }
 };
 

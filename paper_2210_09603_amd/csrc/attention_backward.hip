@@ -874,6 +874,7 @@ hipError_t dispatch_form(int form, const BackArgs& b, hipStream_t stream) {
     case FORM_PLAIN: return launch<T, DP, FORM_PLAIN>(b, stream);
     case FORM_BIAS: return launch<T, DP, FORM_BIAS>(b, stream);
     case FORM_CAP: return launch<T, DP, FORM_CAP>(b, stream);
+    case FORM_WIDE: return launch<T, DP, FORM_WIDE>(b, stream);
     default: return launch<T, DP, FORM_CAP | FORM_BIAS>(b, stream);
   }
 }

@@ -50,6 +50,8 @@ inline hidet_status_t check_options(const hidet_attention_options_t* o) {
   if (!std::isfinite(o->scale) || !std::isfinite(o->softcap) || o->softcap < 0 || o->window < 0 || o->causal < 0 || o->causal > 1)
     return HIDET_ERR_INVALID_ARG;
   if (o->ranges && (o->causal || o->window)) return HIDET_ERR_INVALID_ARG;
+  // (factors of a product, as Score takes them)
+  if (!std::isfinite(2.0f * kLog2e * o->scale) || (o->softcap > 0 && !std::isfinite(2.0f * kLog2e * o->scale / o->softcap))) return HIDET_ERR_UNSUPPORTED;
   if (!is_aligned(o->slopes, 4) || !is_aligned(o->ranges, 4)) return HIDET_ERR_ALIGNMENT;
   return HIDET_OK;
 }
@@ -57,6 +59,7 @@ inline hidet_status_t check_options(const hidet_attention_options_t* o) {
 inline int window_of(long long window) { return window >= (1LL << 30) ? 0 : (int)window; }
 // (scores that are no positive multiple of the products take the form with a score of their own: a slope of 0 where there is none)
 inline int form_of(const hidet_attention_options_t* o) {
+  if (o->softcap > kWideCap) return FORM_WIDE;
   return (o->softcap > 0 ? FORM_CAP : 0) | (o->slopes || (o->softcap == 0 && !(o->scale > 0)) ? FORM_BIAS : 0);
 }
 
@@ -106,6 +109,7 @@ hipError_t dispatch_form(int form, const Args& p, const Cut& c, hipStream_t stre
     case FORM_PLAIN: return launch_forward<T, DP, PAGED, FORM_PLAIN>(p, c, stream);
     case FORM_BIAS: return launch_forward<T, DP, PAGED, FORM_BIAS>(p, c, stream);
     case FORM_CAP: return launch_forward<T, DP, PAGED, FORM_CAP>(p, c, stream);
+    case FORM_WIDE: return launch_forward<T, DP, PAGED, FORM_WIDE>(p, c, stream);
     default: return launch_forward<T, DP, PAGED, FORM_CAP | FORM_BIAS>(p, c, stream);
   }
 }

@@ -245,3 +245,9 @@ def test_sizes_at_and_beyond_the_limits_are_answered():
     # (so many rows that the second kernel of equal pieces had no grid for them)
     c = cache(seqs=1024, heads=1 << 14, stride_head=64, stride_slot=64, stride_page=64, table_width=4096, table_stride=4096)
     assert L.hidet_cache_attention_workspace_bytes(c, 1 << 19, 1, 0) == 0
+
+
+@pytest.mark.parametrize("call", [attention, backward])
+def test_factors_that_pass_fp32_are_refused(call):
+    for o in (dict(softcap=1e-39), dict(scale=2e38), dict(scale=-2e38), dict(scale=1e20, softcap=1e-19), dict(scale=1e38, softcap=0.5)):
+        assert call(o=options(**o)) == UNSUPPORTED, o

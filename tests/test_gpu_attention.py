@@ -159,6 +159,36 @@ def test_cap_and_slopes(dtype, dim):
         _run(3000 + 7 * i + dim, dtype, 1, 6, 2, 70, 100, dim, causal=i % 2 == 0, softcap=softcap, slopes=slopes)
 
 
+@pytest.mark.parametrize("softcap", [2.0, 20.0, 50.0, 64.0, 65.0, 300.0, 1e4, 1e6, 1e12, 3e38])
+@pytest.mark.parametrize("scale", [0.35, -0.35, 40.0])
+def test_a_capped_score_is_as_good_as_an_uncapped_one(softcap, scale):
+    """The log-sum of a query's only key is its score.  Off by at most: 16 * 2^-24 of the products' sum of absolute values (8 exact
+    products, added in fp32, times scale), 16 * 2^-23 of itself (tanh, 4 * 2^-22 where the cap is no more than 4 of it, and steps of
+    fp32 on the way), and up to a cap of 64 2^-22 of the cap (1.5e-5 at most, whatever the score)."""
+    g = np.random.Generator(np.random.PCG64(61))
+    n, d = 3000, 8
+    q, k, v = (torch.from_numpy(g.standard_normal((1, 1, n, d)).astype(np.float32)).half().cuda() for _ in range(3))
+    q.mul_(torch.from_numpy(np.exp2(g.integers(-8, 5, (1, 1, n, 1))).astype(np.float32)).cuda())
+    out, lse = torch.empty_like(q), torch.empty(1, 1, n, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse, scale=scale, softcap=softcap, window=1)
+    products = f64(q)[0, 0] * f64(k)[0, 0]
+    scale, softcap = float(np.float32(scale)), float(np.float32(softcap))
+    x = softcap * np.tanh(scale * products.sum(1) / softcap)
+    bound = 16 * 2.0 ** -24 * abs(scale) * np.abs(products).sum(1) + 16 * 2.0 ** -23 * np.abs(x) + (2.0 ** -22 * softcap if softcap <= 64 else 0.0)
+    assert_within(f64(lse)[0, 0], x, bound, "cap %g scale %g" % (softcap, scale))
+    assert torch.equal(out, v)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128, 24])
+@pytest.mark.parametrize("softcap", [100.0, 1e4, 1e7, 1e30])
+def test_large_caps(softcap, dim, dtype):
+    _run(3500 + dim, dtype, 2, 6, 2, 140, 190, dim, softcap=softcap, causal=True)
+    _run(3510 + dim, dtype, 1, 4, 4, 200, 260, dim, softcap=softcap, slopes=True, layout="tokens")
+    _run(3520 + dim, dtype, 1, 8, 2, 3, 70, dim, softcap=softcap, scale=0.9)
+    _run(3530 + dim, dtype, 1, 2, 1, 2, 9000, dim, softcap=softcap, split=True, back=False)
+
+
 def test_scales_of_any_sign():
     for i, scale in enumerate((0.0, -0.2, 1.0)):
         _run(3100 + i, "f16", 1, 2, 1, 40, 70, 64, scale=scale)

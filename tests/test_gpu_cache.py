@@ -479,3 +479,17 @@ def test_starts_that_leave_the_batch_are_cut_to_it(starts, max_new):
     for s in range(seqs):
         written[cut[s]:cut[s] + min(cut[s + 1] - cut[s], max_new)] = True
     assert bool((out[torch.from_numpy(~written).cuda()] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("softcap", [64.0, 1e4, 1e30])
+def test_large_caps(softcap, dtype):
+    slopes = torch.tensor([0.5, 0.25, 0.125, 1.0], device="cuda")
+    for new, dim in (([1, 1, 1], 64), ([200, 3, 77], 128)):
+        b = Batch(44, dtype, [300, 1000, 77], new, 4, 2, dim, 16, pad=1)
+        for sl in (None, slopes):
+            q, out, lse = b.run(softcap=softcap, slopes=sl)
+            b.check(q, out, lse, softcap=softcap, slopes=None if sl is None else f64(sl))
+    b = _ragged(64, dtype, 64)
+    q, out, lse = b.run(softcap=softcap)
+    b.check(q, out, lse, softcap=softcap)
