@@ -455,8 +455,8 @@ hidet_status_t hidet_attention_ranges(int64_t batch, int64_t seq_q, int64_t seq_
  * The backward pass of hidet_attention, with the same options: the gradients of q, k and v from that of out (grad_out), given out
  * and lse of the forward call.  With P = exp(x - lse) and D_i = grad_out_i . out_i,
  *   dS = P (grad_out . V^T - D) dx/d(scale q.k);  grad_q = scale dS K;  grad_k = scale dS^T Q;  grad_v = P^T grad_out,
- * summed over the query heads that share a key head.  P and dS are rounded to dtype as operands of these products; sums are
- * fp32, in an order that depends on the sizes alone: no atomics, the same arguments give the same bits.  Slopes have no gradient.
+ * summed over the query heads that share a key head.  P and dS are rounded to dtype as operands of these products, in fp16 times a
+ * power of two that follows the size of grad_out, so that gradients of any size keep their bits; sums are fp32, in an order that depends on the sizes alone: no atomics, the same arguments give the same bits.  Slopes have no gradient.
  * D is grad_out . out with the rounded out, or, where no query of a tile of rows sees more than 32 keys, sum P (grad_out . v).
  * All three gradients are written whole (zeros where nothing was seen), in their own strides; infinities and NaN in what a query
  * does not see have no influence, as in the forward pass.  The workspace is needed: HIDET_ERR_INVALID_ARG if it is smaller than

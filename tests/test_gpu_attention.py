@@ -264,6 +264,35 @@ def test_gradients_of_few_keys_do_not_carry_the_rounding_of_the_output(dtype, di
             assert_within(t, x, e, "%s %d keys %s" % (dtype, n, name))
 
 
+@pytest.mark.parametrize("size", [(1, 2, 1, 300, 4096, 64), (1, 2, 2, 130, 4096, 128), (2, 4, 2, 70, 900, 40), (1, 2, 1, 3, 12, 64)], ids=str)
+@pytest.mark.parametrize("twos,opts", [(-10, dict()), (-10, dict(causal=True, softcap=20.0)), (11, dict(causal=True)), (-16, dict(window=40))], ids=str)
+def test_fp16_gradients_of_any_size(size, twos, opts):
+    """Gradients are linear in that of the output, and powers of two are exact: dQ, dK and dV of 2^twos times the gradient are 2^twos times
+    dQ, dK and dV, but for the two roundings of what is stored -- 2^-11 of each, or 2^-25 where fp16 is subnormal -- as dS keeps its bits
+    whatever its size.  (Elements of the gradient are at least 2^-4, or multiples of 2^-8, so that fp16 holds what they are scaled to.)"""
+    b, h, hk, n, m, d = size
+    g = np.random.Generator(np.random.PCG64(71))
+    q, dout, out = (_draw(g, (b, h, n, d), "f16", "dense") for _ in range(3))
+    k, v = (_draw(g, (b, hk, m, d), "f16", "dense") for _ in range(2))
+    dout = torch.where(dout.abs() < 2.0 ** -4, torch.zeros_like(dout), dout)
+    if twos < -10:  # (multiples of 2^-8)
+        dout = (dout * 256).round() / 256
+    lse = torch.empty(b, h, n, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse, **opts)
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+    got = []
+    for factor in (1.0, 2.0 ** twos):
+        scaled = dout * factor
+        assert torch.equal(scaled.double(), dout.double() * factor)
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        hb.hidet_attention_backward(scaled, q, k, v, out, lse, *grads, ws, **opts)
+        got.append([f64(t) for t in grads])
+    u, small = 2.0 ** -11, 2.0 ** -25
+    for name, one, other in zip(("dq", "dk", "dv"), *got):
+        value = (np.abs(one) + small) / (1 - u)
+        assert_within(other * 2.0 ** -twos, one, 2 * u * value + small + small * 2.0 ** -twos, "%s %s" % (size, name))
+
+
 def test_no_keys_and_no_queries():
     q = torch.randn(2, 4, 5, 64, device="cuda").half()
     k = torch.empty(2, 2, 0, 64, device="cuda", dtype=torch.float16)
