@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   constexpr int CPR = DP / 8, STAGE = TILE * CPR * 16, NL = TILE * CPR / THREADS, RPP = THREADS / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * STAGE];
-  __shared__ int bounds[4][2], most[4];
+  __shared__ int bounds[4][2], few_bounds[4][2];
   __shared__ float halves[8][32];
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -278,8 +278,13 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   const Row w = make_row<false>(p, e, min(r0 + (lane & 31), rows - 1));
   const int at = w.token + e.shift;
   const Seen mine = seen_by<false>(p, e, w, min(r0, rows - 1), min(r0 + 31, rows - 1));
-  const int most_of_wave = wave_max(w.hi - w.lo);
-  if (lane == 0 && wave < 4) most[wave] = most_of_wave;
+  // the keys that rows of few keys see
+  const bool few = w.hi - w.lo > 1 && w.hi - w.lo <= kFewKeys;
+  const int few_lo = wave_min(few ? w.lo : 0x7fffffff), few_hi = wave_max(few ? w.hi : 0);
+  if (lane == 0 && wave < 4) {
+    few_bounds[wave][0] = few_lo;
+    few_bounds[wave][1] = few_hi;
+  }
   int begin, end;  // of the workgroup
   if (p.ranges) {
     if (lane == 0 && wave < 4) {
@@ -353,7 +358,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   const bool loads = load_chunk * 8 < p.dim;
   const unsigned lds0 = lds_address(smem), lds = lds0 + wave * 1024;
   const ReadMap<DP> map(lane);
-  auto request = [&](int t) {
+  auto request = [&](int begin, int end, int t) {  // tile t of the keys begin..end - 1
     const unsigned to = lds + (t & 1) * STAGE;
     const int first = begin + t * TILE, last = end - 1 - first;
     const T* kt = kbase + (long long)first * p.ks.row;
@@ -369,18 +374,24 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
       }
     }
   };
+  int few_begin = min(min(few_bounds[0][0], few_bounds[1][0]), min(few_bounds[2][0], few_bounds[3][0]));
+  int few_end = max(max(few_bounds[0][1], few_bounds[1][1]), max(few_bounds[2][1], few_bounds[3][1]));
+  few_begin = __builtin_amdgcn_readfirstlane(few_begin);
+  few_end = __builtin_amdgcn_readfirstlane(few_end);
   settle();
-  // D from what was seen, where that is little: D = sum P dP, of which dout . out has the rounding of out.  That is half a step of D, and
-  // dS = P (dP - D) may be far smaller than D where a few keys have all the weight; among many it is not.  (Scores of 5 keys that spread
-  // by 4: dQ in bf16 13 times as far off without.  Windows of 32 keys over 4096 positions, 36 heads: a pass 154 us, 146 without.)
-  if (max(max(most[0], most[1]), max(most[2], most[3])) <= kFewKeys && all <= b.dq_share) {
+  // D of a query that sees few keys, from what it sees: D = sum P dP, of which dout . out has the rounding of out.  That is half a step of
+  // D, and dS = P (dP - D) may be far smaller than D where a few keys have all the weight; among many it is not.  (Scores of 5 keys that
+  // spread by 4: dQ in bf16 13 times as far off without.  Windows of 32 keys over 4096 positions, 36 heads: a pass 154 us, 146 without.)
+  // Every split of the tile works it out, over the tiles that such rows see.
+  if (few_begin < few_end) {
+    const int tiles = tiles_of<TILE>(few_begin, few_end);
     float rest = 0.0f;
-    if (t0 < t1) request(t0);
-    for (int t = t0; t < t1; ++t) {
+    request(few_begin, few_end, 0);
+    for (int t = 0; t < tiles; ++t) {
       wait_all_and_meet();
-      if (t + 1 < t1) request(t + 1);
-      const int first = begin + t * TILE + own;
-      if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
+      if (t + 1 < tiles) request(few_begin, few_end, t + 1);
+      const int first = few_begin + t * TILE + own;
+      if (first >= few_hi || first + kTileKeys <= few_lo) continue;
       const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
 #pragma unroll 1
       for (int c = 0; c < 2; ++c) {
@@ -408,7 +419,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
       rest += halves[wave ^ 4][lane & 31];
     }
     // (a row that comes out not finite is worked out again, with the D that it had)
-    if (__builtin_fabsf(rest) < __builtin_huge_valf()) delta += rest;
+    if (few && __builtin_fabsf(rest) < __builtin_huge_valf()) delta += rest;
     __syncthreads();
   }
   if (half == 0 && wave < 4 && z == 0) *row_info<FORM>(b, e, r0 + lane, 1) = r0 + lane < rows ? delta * (1.0f / kLift) : 0.0f;
@@ -418,10 +429,10 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
-  if (t0 < t1) request(t0);
+  if (t0 < t1) request(begin, end, t0);
   for (int t = t0; t < t1; ++t) {
     wait_all_and_meet();
-    if (t + 1 < t1) request(t + 1);
+    if (t + 1 < t1) request(begin, end, t + 1);
     const int first = begin + t * TILE + own;
     if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
     const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;

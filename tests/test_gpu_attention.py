@@ -264,6 +264,40 @@ def test_gradients_of_few_keys_do_not_carry_the_rounding_of_the_output(dtype, di
             assert_within(t, x, e, "%s %d keys %s" % (dtype, n, name))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dim,h,hk,softcap", [(64, 4, 2, 0.0), (128, 2, 1, 0.0), (40, 3, 3, 20.0)])
+@pytest.mark.parametrize("mask", ["causal", "documents", "alternating", "alternating in splits"])
+def test_gradients_of_few_keys_beside_queries_that_see_many(mask, dtype, dim, h, hk, softcap):
+    """The first rows of a causal sequence, short documents beside long ones, every other row: the same bounds as where all see few.
+    Gradients of rows that see more than 32 keys are zeros, so that dK and dV are those of the others alone."""
+    g = np.random.Generator(np.random.PCG64(28))
+    n, m = (200, 200) if mask != "alternating in splits" else (90, 3000)
+    q, dout = (_draw(g, (2, h, n, dim), dtype, "dense") for _ in range(2))
+    k, v = (_draw(g, (2, hk, m, dim), dtype, "dense") for _ in range(2))
+    q.mul_(4.0)
+    at = np.arange(n)
+    if mask == "causal":
+        r = np.stack([0 * at, at + 1], 1)
+    elif mask == "documents":  # 5, 60, 7, 100 and 28 tokens, causal
+        first = np.repeat([0, 5, 65, 72, 172], [5, 60, 7, 100, 28])
+        r = np.stack([first, at + 1], 1)
+    else:
+        few = (at * 37) % (m - 32)
+        r = np.where((at % 2 == 0)[:, None], np.stack([few, few + 2 + at % 31], 1), np.stack([0 * at, 0 * at + m], 1))
+    ranges = torch.from_numpy(np.stack([r, r]).astype(np.int32)).cuda()
+    see = np.stack([oa.in_ranges(r, m)] * 2)
+    opts = dict(softcap=softcap, causal=True) if mask == "causal" else dict(softcap=softcap, ranges=ranges)
+    dout[:, :, torch.from_numpy(r[:, 1] - r[:, 0] > 32).cuda()] = 0.0
+    out, dq, dk, dv = (torch.empty_like(t) for t in (q, q, k, v))
+    lse = torch.empty(2, h, n, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse, **opts)
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+    hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, **opts)
+    want, bound = bounds(dtype, f64(q), f64(k), f64(v), see, dim ** -0.5, softcap, None, grad_out=f64(dout), few=True)
+    for name, t, x, e in zip(("dq", "dk", "dv"), (dq, dk, dv), want[2:], bound[2:]):
+        assert_within(t, x, e, "%s %s %s" % (mask, dtype, name))
+
+
 @pytest.mark.parametrize("size", [(1, 2, 1, 300, 4096, 64), (1, 2, 2, 130, 4096, 128), (2, 4, 2, 70, 900, 40), (1, 2, 1, 3, 12, 64)], ids=str)
 @pytest.mark.parametrize("twos,opts", [(-10, dict()), (-10, dict(causal=True, softcap=20.0)), (11, dict(causal=True)), (-16, dict(window=40))], ids=str)
 def test_fp16_gradients_of_any_size(size, twos, opts):
