@@ -29,6 +29,10 @@ constexpr int kTileKeys = 64;
 // A running maximum is replaced only by one that is 2^8 times as large: P then stays below 2^8, which both storage types
 // hold, and most tiles leave the output's registers alone.
 constexpr float kSlack = 8.0f;
+// bf16 holds values as large as fp32: P is kept below 1 by taking 2^8 more from every score, which costs it nothing.  (fp16 has bits for
+// neither.)
+template <typename T>
+constexpr float kAbove = std::is_same<T, bf16>::value ? kSlack : 0.0f;
 
 struct Strides {
   long long batch, head, row;  // elements
@@ -298,11 +302,13 @@ __device__ __forceinline__ void seen_from(const Args& p, const Entry& e, int at,
     hi = p.window && p.window < e.keys - at ? at + p.window : e.keys;  // (at + window may pass 32 bits)
   hi = min(hi, e.keys);
 }
+__device__ __forceinline__ Row place_of_row(const Args& p, const Entry& e, int r) {
+  const int token = p.d_group.div(r);
+  return Row{token, e.kv * p.group + (r - token * p.group), 0, 0};
+}
 template <bool PAGED>
 __device__ __forceinline__ Row make_row(const Args& p, const Entry& e, int r) {
-  Row w;
-  w.token = p.d_group.div(r);
-  w.head = e.kv * p.group + (r - w.token * p.group);
+  Row w = place_of_row(p, e, r);
   if (!PAGED && p.ranges) {
     const int* range = p.ranges + ((long long)e.b * p.seq_q + w.token) * 2;
     w.lo = max(range[0], 0);
@@ -431,7 +437,7 @@ struct State {
   // A larger maximum: what was summed so far shrinks.
   __device__ __forceinline__ void raise(float tile_top, float factor) {
     const float now = fmaxf(top, tile_top);
-    const float next = now == kNoMax ? 0.0f : now * factor;
+    const float next = now == kNoMax ? 0.0f : now * factor + kAbove<T>;
     const float shrink = top == kNoMax ? 0.0f : exp2_fast(shift - next);  // (nothing was summed: 0 stays 0)
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -502,93 +508,187 @@ __device__ __forceinline__ Part part_of(const Args& p, int b, int kv, int z, int
   return Part{p.part + row * DP, p.part + p.splits * per_split * DP + row * 2};
 }
 
-// One query again, by all lanes of a wavefront: only the keys that it sees take part, each with its own multiplication.  Where
-// a masked key or value is infinite or NaN the tiled products multiply it by a zero and their sums become NaN; the rows that
-// come out not finite are computed by this definition instead.  Rare, and slow: a few hundred cycles a key.
-template <typename T, int DP, bool PAGED, int FORM>
-__device__ __forceinline__ void row_by_definition(const Args& p, const Entry& e, int r, int from, int to, const Part& rows, bool partial) {
-  constexpr int E = DP / 64;
-  const int lane = threadIdx.x & 63;
-  const Row w = make_row<PAGED>(p, e, r);
-  const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
-  const T* q = reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w);
-  const T* k = keys_of<T, PAGED>(p, e, p.k, p.ks);
-  const T* v = keys_of<T, PAGED>(p, e, p.v, p.vs);
-  float mine[E], acc[E], top = kNoMax, sum = 0.0f;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int d = lane * E + i;
-    mine[i] = d < p.dim ? to_f32(q[d]) : 0.0f;
-    acc[i] = 0.0f;
-  }
-  from = max(from, w.lo);
-  to = min(to, w.hi);
-  for (int j = from; j < to; ++j) {
-    const KeyPlace place = find_key<PAGED>(p, e, j);
-    if (!is_there<PAGED>(p, place)) continue;
-    const long long ko = key_offset<PAGED>(p, p.ks, place), vo = key_offset<PAGED>(p, p.vs, place);
-    float dot = 0.0f;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (lane * E + i < p.dim) dot = __builtin_fmaf(mine[i], to_f32(k[ko + lane * E + i]), dot);
-    const float x = score(wave_sum(dot), (float)(w.token + e.shift - j));
-    if (x == kNoMax) continue;  // (weight 0: as a masked key)
-    if (!(x <= top)) {
-      const float shrink = top == kNoMax ? 0.0f : exp2_fast(top - x);
-      sum *= shrink;
-#pragma unroll
-      for (int i = 0; i < E; ++i) acc[i] = top == kNoMax ? 0.0f : acc[i] * shrink;
-      top = x;
-    }
-    const float weight = exp2_fast(x - top);
-    sum += weight;
-#pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (lane * E + i < p.dim) acc[i] += weight * to_f32(v[vo + lane * E + i]);
-    if (sum != sum) break;  // (NaN stays NaN)
-  }
-  const bool none = top == kNoMax;
-  if (sum != sum) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) acc[i] = sum;
-    top = sum;
-  }
-  if (partial) {
-    const Part part = {rows.sums + (long long)r * DP, rows.stat + r * 2LL};
-#pragma unroll
-    for (int i = 0; i < E; ++i) part.sums[lane * E + i] = acc[i];
-    if (lane == 0) {
-      part.stat[0] = top;
-      part.stat[1] = sum;
-    }
-    return;
-  }
-  T* out = reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w);
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (lane * E + i < p.dim) out[lane * E + i] = from_f32<T>(none ? 0.0f : acc[i] / sum);
-  if (lane == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (top + __builtin_log2f(sum)) * kLn2;
+// ---- what comes out not finite -------------------------------------------------------------------------------------------------
+// A tile multiplies the values of keys that a query does not see by weights of 0, and where such a value is infinite or NaN the sum
+// becomes NaN.  What comes out finite was not touched by any.  Of the rest:
+//   - A score that is NaN or +inf makes the row's sum of weights NaN, and the row is NaN, whatever else it saw.
+//   - Otherwise the workgroup goes over its keys a second time, with 0 for what is not finite of the values: that gives every row what it
+//     would have been without (the same bits).  One pass over the values of keys that are seen then finds those that are not finite: in a
+//     dimension in which a row sees one, that is its result -- infinite, or NaN if it sees both infinities or a NaN.
+// So infinities and NaN cost a call a few times its time, whichever they are, and what they do not reach keeps its bits.  (A causal prompt of
+// 4096, 16 heads of 128 dimensions, 120 us: with one infinite value 590, one in each key 1200, all of them NaN 260; of the last key alone
+// 38 ms when such rows were computed one by one.)
+
+// A lane's number that the compiler knows nothing of: what follows from it is worked out behind this, and not before the tiles, whose loop
+// has no registers to keep it in.
+__device__ __forceinline__ int worked_out_here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
-// Stores a wavefront's 32 rows: the finished output, or the sums of a split, from `to_rows` of row 0 on.  `r0`: its first row.
-template <typename T, int DP, bool PAGED, int FORM>
-__device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, DP>& st, int r0, int rows, const Row& w, int from, int to, const Part& to_rows,
-                                       bool partial) {
-  const int lane = threadIdx.x & 63, half = lane >> 5, r = r0 + (lane & 31);
-  const float sum = sum_of_halves(st.sum);
+// Sets of a vector's dimensions, as ballots of lanes that hold DP / 64 each give them: dimension (DP / 64) lane + u is bit `lane` of set u.
+template <int DP>
+struct Dims {
+  static constexpr int E = DP / 64;
+  unsigned long long of[E];
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int u = 0; u < E; ++u) of[u] = 0;
+  }
+  // A transposed accumulator has dimension 32 t + 8 g + 4 half + i in register 4 g + i of tile t: of set i % E the bit below, counted from
+  // the first of the half.
+  static __device__ __forceinline__ constexpr int bit(int t, int r) { return (32 * t + 8 * (r >> 2) + (r & 3)) / E; }
+  static __device__ __forceinline__ int first(int half) { return 4 / E * half; }
+};
+// Sums of what is not finite: which dimensions hold +inf, -inf, NaN.
+template <int DP>
+struct OddSums {
+  Dims<DP> plus, minus, nan;
+  __device__ __forceinline__ void clear() {
+    plus.clear();
+    minus.clear();
+    nan.clear();
+  }
+  // v: of a vector, dimensions (DP / 64) lane + u, the same vector in all lanes; adds it where `to` says so
+  __device__ __forceinline__ void add(const float (&v)[DP / 64], bool to) {
+#pragma unroll
+    for (int u = 0; u < DP / 64; ++u) {
+      const unsigned long long p = __ballot(v[u] == __builtin_huge_valf()), m = __ballot(v[u] == -__builtin_huge_valf()), n = __ballot(v[u] != v[u]);
+      plus.of[u] |= to ? p : 0;
+      minus.of[u] |= to ? m : 0;
+      nan.of[u] |= to ? n : 0;
+    }
+  }
+  __device__ __forceinline__ void add_nan() {
+#pragma unroll
+    for (int u = 0; u < DP / 64; ++u) nan.of[u] = ~0ull;
+  }
+};
+template <int DT>
+__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[DT]) {
   bool finite = true;
 #pragma unroll
-  for (int t = 0; t < State<T, DP>::DT; ++t)
+  for (int t = 0; t < DT; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) finite &= __builtin_fabsf(st.o[t][i]) < __builtin_huge_valf();
-  finite &= __builtin_fabsf(sum) < __builtin_huge_valf();
-  const unsigned long long odd = __ballot(!finite);
-  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
-  const bool mine = r < rows && !((again >> (lane & 31)) & 1);
+    for (int i = 0; i < 16; ++i) finite &= __builtin_fabsf(acc[t][i]) < __builtin_huge_valf();
+  return finite;
+}
+// Whether more of them may change anything.
+template <int DP>
+__device__ __forceinline__ bool any_but_nan(const OddSums<DP>& sums, int dim) {
+  bool any = false;
+#pragma unroll
+  for (int u = 0; u < DP / 64; ++u) any |= (~sums.nan.of[u] & ~0ull >> (64 - dim / (DP / 64))) != 0;
+  return any;
+}
+// Puts the sums in their places.
+template <int DP>
+__device__ __forceinline__ void settle_odd(f32x16 (&acc)[DP / 32], const OddSums<DP>& sums, int half) {
+  const float inf = __builtin_huge_valf();
+#pragma unroll
+  for (int u = 0; u < Dims<DP>::E; ++u) {
+    const unsigned long long plus = sums.plus.of[u] >> Dims<DP>::first(half), minus = sums.minus.of[u] >> Dims<DP>::first(half);
+    const unsigned long long nan = sums.nan.of[u] >> Dims<DP>::first(half) | (plus & minus);
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+      for (int r = u; r < 16; r += Dims<DP>::E) {
+        float x = acc[t][r];
+        const unsigned long long bit = 1ull << Dims<DP>::bit(t, r);
+        x = plus & bit ? inf : x;
+        x = minus & bit ? -inf : x;
+        x = nan & bit ? __builtin_nanf("") : x;
+        acc[t][r] = x;
+      }
+  }
+}
+
+// What lane's row sees of values that are not finite, of keys from `from` on and before `to`, which the workgroup went over.
+template <typename T, int DP, bool PAGED>
+__device__ __forceinline__ OddSums<DP> odd_values(const Args& p, const Entry& e, const Row& w, int from, int to, bool ask) {
+  constexpr int E = DP / 64, U = 8;
+  struct __attribute__((packed, aligned(2))) Own {
+    T x[E];
+  };
+  const int lane = worked_out_here(threadIdx.x & 63);
+  const bool has = lane * E < p.dim;
+  const T* k = keys_of<T, PAGED>(p, e, p.k, p.ks) + (has ? lane * E : 0);
+  const T* v = keys_of<T, PAGED>(p, e, p.v, p.vs) + (has ? lane * E : 0);
+  OddSums<DP> sums;
+  sums.clear();
+  const int first = max(from, wave_min(ask ? w.lo : to)), last = min(to, wave_max(ask ? w.hi : from));
+  const unsigned count = last > first ? last - first : 0;
+#pragma unroll 1
+  for (unsigned i = 0; i < count; i += U) {
+    Own key[U], value[U];
+    bool there[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      KeyPlace place = find_key<PAGED>(p, e, first + (int)min(i + u, count - 1));
+      if constexpr (PAGED) place.page = __builtin_amdgcn_readfirstlane(place.page);
+      key[u] = *reinterpret_cast<const Own*>(k + key_offset<PAGED>(p, p.ks, place));
+      value[u] = *reinterpret_cast<const Own*>(v + key_offset<PAGED>(p, p.vs, place));
+      there[u] = is_there<PAGED>(p, place);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[E];
+      bool odd_key = false, odd = false;
+#pragma unroll
+      for (int c = 0; c < E; ++c) {
+        x[c] = has ? to_f32(value[u].x[c]) : 0.0f;
+        odd |= !(__builtin_fabsf(x[c]) < __builtin_huge_valf());
+        odd_key |= !(__builtin_fabsf(has ? to_f32(key[u].x[c]) : 0.0f) < __builtin_huge_valf());
+      }
+      // (a key that is not finite has a score of -inf here, and no weight: with any other the row were NaN)
+      if (__any(odd) && !__any(odd_key)) {
+        const int j = first + (int)min(i + u, count - 1);
+        sums.add(x, there[u] && j >= w.lo && j < w.hi);
+      }
+    }
+    if (!__any(ask && any_but_nan(sums, p.dim))) break;
+  }
+  return sums;
+}
+
+// 16-bit numbers, 8 of them, with 0 for what is not finite.
+template <typename T>
+__device__ __forceinline__ u32x4 finite_ones(u32x4 v) {
+  constexpr unsigned EXPONENT = std::is_same<T, bf16>::value ? 0x7f80 : 0x7c00;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((v[i] & EXPONENT) == EXPONENT) v[i] &= 0xffff0000u;
+    if ((v[i] & (EXPONENT << 16)) == EXPONENT << 16) v[i] &= 0xffffu;
+  }
+  return v;
+}
+// The chunks of a tile that this thread's loads filled, of N threads.
+template <typename T, int N, int NL>
+__device__ __forceinline__ void keep_finite(unsigned char* tile) {
+  const unsigned first = worked_out_here(threadIdx.x) * 16;
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    u32x4* at = reinterpret_cast<u32x4*>(tile + i * N * 16 + first);
+    *at = finite_ones<T>(*at);
+  }
+}
+
+// ---- results of a wavefront's 32 rows ---------------------------------------------------------------------------------------
+// Stores the finished output, or the sums of a split, from `to_rows` of row 0 on.  `r0`: the first row; `again`: the sums are those of
+// finite values alone, of keys from `from` on and before `to`.
+template <typename T, int DP, bool PAGED, int FORM>
+__device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, DP>& st, int r0, int rows, int from, int to, const Part& to_rows,
+                                       bool partial, bool again) {
+  const int lane = worked_out_here(threadIdx.x & 63), half = lane >> 5, r = r0 + (lane & 31);
+  const float sum = sum_of_halves(st.sum);
+  if (__builtin_expect(again, 0)) {
+    const Row w = make_row<PAGED>(p, e, min(r, rows - 1));
+    settle_odd<DP>(st.o, odd_values<T, DP, PAGED>(p, e, w, from, to, sum == sum), half);
+  }
+  if (r >= rows) return;
   if (partial) {
-    if (mine) {
-      const Part part = {to_rows.sums + (long long)r * DP, to_rows.stat + r * 2LL};
-      if (sum > 0.0f)  // (the sums of nothing are not read)
+    const Part part = {to_rows.sums + (long long)r * DP, to_rows.stat + r * 2LL};
+    if (sum > 0.0f)  // (the sums of nothing are not read)
 #pragma unroll
       for (int t = 0; t < State<T, DP>::DT; ++t)
 #pragma unroll
@@ -596,32 +696,26 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
           const f32x4 v = {st.o[t][4 * g], st.o[t][4 * g + 1], st.o[t][4 * g + 2], st.o[t][4 * g + 3]};
           *reinterpret_cast<f32x4*>(part.sums + 32 * t + 8 * g + 4 * half) = v;
         }
-      if (half == 0) {
-        part.stat[0] = sum > 0.0f ? st.shift : kNoMax;
-        part.stat[1] = sum;
-      }
+    if (half == 0) {
+      part.stat[0] = sum > 0.0f ? st.shift : sum == 0.0f ? kNoMax : sum;
+      part.stat[1] = sum;
     }
-  } else if (mine) {
-    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
-    T* out = reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w);
-#pragma unroll
-    for (int t = 0; t < State<T, DP>::DT; ++t)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * t + 8 * g + 4 * half;
-        T four[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) four[i] = from_f32<T>(st.o[t][4 * g + i] * by);
-        if (d < p.dim) __builtin_memcpy(reinterpret_cast<Chunk8*>(out + d), four, 8);
-      }
-    if (half == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = sum > 0.0f ? (st.shift + __builtin_log2f(sum)) * kLn2 : kNoMax;
+    return;
   }
-  again = __builtin_amdgcn_readfirstlane(again);
-  while (again) {
-    const int i = __builtin_ctz(again);
-    again &= again - 1;
-    if (r0 + i < rows) row_by_definition<T, DP, PAGED, FORM>(p, e, r0 + i, from, to, to_rows, partial);
-  }
+  const float by = sum > 0.0f ? 1.0f / sum : sum;  // (0: nothing was seen; NaN: so is the row)
+  const Row w = place_of_row(p, e, r);
+  T* out = reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w);
+#pragma unroll
+  for (int t = 0; t < State<T, DP>::DT; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = 32 * t + 8 * g + 4 * half;
+      T four[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) four[i] = from_f32<T>(st.o[t][4 * g + i] * by);
+      if (d < p.dim) __builtin_memcpy(reinterpret_cast<Chunk8*>(out + d), four, 8);
+    }
+  if (half == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = sum > 0.0f ? (st.shift + __builtin_log2f(sum)) * kLn2 : sum == 0.0f ? kNoMax : sum;
 }
 
 // ---- the kernel of many rows ------------------------------------------------------------------------------------------------
@@ -648,13 +742,13 @@ __device__ __forceinline__ Place place_of(int w, int entries, int pieces) {
 }
 
 template <typename T, int DP, bool PAGED, int FORM, int PAIRS>
-__global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
+__global__ __launch_bounds__(256 * PAIRS, DP == 128 ? 2 : FORM < 3 || (FORM == 3 && !PAGED) ? 4 : 3) void tile_kernel(const Args p) {
   static_assert(PAIRS == 1 || !PAGED, "a wavefront looks up 64 keys");
   constexpr int THREADS = 256 * PAIRS, TILE = kTileKeys * PAIRS;  // keys of a tile
   constexpr int CPR = DP / 8, STAGE = TILE * CPR * 16, NL = TILE * CPR / THREADS, RPP = THREADS / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * STAGE];  // keys of two stages, values of two
-  __shared__ int bounds[4][2];
+  __shared__ int bounds[4][2], spoilt;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int own = (wave >> 2) * kTileKeys;  // the first of its 64 keys of a tile
 
@@ -680,9 +774,9 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
     end = all.hi;
   }
   State<T, DP> st;
-  st.clear();
   load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w), half, p.dim, st.q);
   const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  if (tid == 0) spoilt = 0;
   const bool narrow = p.dim < DP;
   if (narrow)  // the chunks past the head's dimension, which no load fills
     for (int i = tid; i < 4 * STAGE / 16; i += THREADS) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
@@ -761,32 +855,45 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
   };
 
   settle();
-  if (t0 < t1) {
-    look_up(t0);
-    request(t0);
-  }
-  for (int t = t0; t < t1; ++t) {
-    wait_all_and_meet();
-    there = there_next;
-    if (t + 1 < t1) request(t + 1);
-    const int first = begin + t * TILE + own;
-    if (first >= mine.hi || first <= mine.lo - kTileKeys) continue;
-    const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
-    f32x16 s[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s[i] = mfma_op(row_frag<T, DP>(map, keys, i * 32, ks), st.q[ks], s[i]);
+  bool again = false;
+  for (;;) {
+    st.clear();
+    if (t0 < t1) {
+      look_up(t0);
+      request(t0);
     }
-    const bool masked = first < mine.full_lo || first > mine.full_hi - kTileKeys || (PAGED && ~there != 0);
-    Frag pf[4];
-    softmax_tile<T, DP, FORM, 2>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
+    for (int t = t0; t < t1; ++t) {
+      wait_all_and_meet();
+      if (__builtin_expect(again, 0)) {
+        keep_finite<T, THREADS, NL>(smem + 2 * STAGE + (t & 1) * STAGE);
+        __syncthreads();
+      }
+      there = there_next;
+      if (t + 1 < t1) request(t + 1);
+      const int first = begin + t * TILE + own;
+      if (first >= mine.hi || first <= mine.lo - kTileKeys) continue;
+      const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
+      f32x16 s[2];
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+      for (int i = 0; i < 2; ++i) {
 #pragma unroll
-      for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
+        for (int r = 0; r < 16; ++r) s[i][r] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s[i] = mfma_op(row_frag<T, DP>(map, keys, i * 32, ks), st.q[ks], s[i]);
+      }
+      const bool masked = first < mine.full_lo || first > mine.full_hi - kTileKeys || (PAGED && ~there != 0);
+      Frag pf[4];
+      softmax_tile<T, DP, FORM, 2>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
+    }
+    if (again) break;
+    if (__any(!all_finite(st.o) && st.sum < __builtin_huge_valf()) && lane == 0) spoilt = 1;
+    __syncthreads();
+    again = __builtin_amdgcn_readfirstlane(spoilt);
+    if (__builtin_expect(!again, 1)) break;
   }
   if constexpr (PAIRS == 2) {
     __syncthreads();
@@ -811,8 +918,8 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void tile_kernel(const Args p) {
     st.sum = st.sum * by + meet[(DT * 16 + 1) * 64] * by_other;
     st.shift = level;
   }
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, key_at<TILE>(begin, t0, 0, end), key_at<TILE>(begin, t1, 0, end),
-                                part_of<DP>(p, e.b, e.kv, z, 0), p.splits > 1);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, key_at<TILE>(begin, t0, 0, end), key_at<TILE>(begin, t1, 0, end),
+                                part_of<DP>(p, e.b, e.kv, z, 0), p.splits > 1, again);
 }
 
 // ---- the kernel of few rows ---------------------------------------------------------------------------------------------------
@@ -829,6 +936,7 @@ struct StreamLds {
   static constexpr int BYTES = kStreamWaves * 2 * TILE > kStreamWaves / 2 * JOIN ? kStreamWaves * 2 * TILE : kStreamWaves / 2 * JOIN;
   __attribute__((aligned(16))) unsigned char smem[BYTES];
   float stat[kStreamWaves][32][2];
+  int spoilt[kStreamWaves];
 };
 // Rows r0.. of an entry over tiles t0..t1 - 1 of the keys that they see.
 template <typename T, int DP, bool PAGED, int FORM>
@@ -884,43 +992,66 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
     request(t);
   }
   State<T, DP> st;
-  st.clear();
   load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<PAGED>(p, e, p.qs, w), half, p.dim, st.q);
   const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
   const ReadMap<DP> map(lane);
-  for (; t < t1; t += kStreamWaves) {
-    const int first = begin + t * kStreamKeys;
+  bool again = false;
+  for (;;) {
+    st.clear();
+    for (; t < t1; t += kStreamWaves) {
+      const int first = begin + t * kStreamKeys;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int row = i * RPP + load_row, to = (row * CPR + (load_chunk ^ swz<CPR>(row))) * 16;
-      *reinterpret_cast<u32x4*>(mine + to) = kr[i];
-      *reinterpret_cast<u32x4*>(mine + TILE + to) = vr[i];
+      for (int i = 0; i < NL; ++i) {
+        const int row = i * RPP + load_row, to = (row * CPR + (load_chunk ^ swz<CPR>(row))) * 16;
+        *reinterpret_cast<u32x4*>(mine + to) = kr[i];
+        *reinterpret_cast<u32x4*>(mine + TILE + to) = vr[i];
+      }
+      asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order: its writes, then its reads)
+      if (__builtin_expect(again, 0)) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          u32x4* at = reinterpret_cast<u32x4*>(mine + TILE + (i * 64 + lane) * 16);
+          *at = finite_ones<T>(*at);
+        }
+        asm volatile("" ::: "memory");
+      }
+      const unsigned long long there = there_next & 0xffffffffull;
+      if (t + kStreamWaves < t1) request(t + kStreamWaves);
+      f32x16 s[1];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) s[0] = mfma_op(row_frag<T, DP>(map, keys, 0, ks), st.q[ks], s[0]);
+      const bool masked = first < seen.full_lo || first > seen.full_hi - kStreamKeys || (PAGED && there != 0xffffffffull);
+      Frag pf[2];
+      softmax_tile<T, DP, FORM, 1>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
+      asm volatile("" ::: "memory");
     }
-    asm volatile("" ::: "memory");  // (a wavefront's LDS accesses run in order: its writes, then its reads)
-    const unsigned long long there = there_next & 0xffffffffull;
-    if (t + kStreamWaves < t1) request(t + kStreamWaves);
-    f32x16 s[1];
+    // the wavefronts' sums meet: all to one maximum, then halves of them into LDS and onto the others
+    const int spoilt = !again && __any(!all_finite(st.o) && st.sum < __builtin_huge_valf());
+    st.sum = sum_of_halves(st.sum);
+    if (half == 0) {
+      stat[wave][lane][0] = st.top == kNoMax ? kNoMax : st.shift;
+      stat[wave][lane][1] = st.sum;
+    }
+    if (lane == 0) lds.spoilt[wave] = spoilt;
+    __syncthreads();
+    int any = 0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[0][r] = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) s[0] = mfma_op(row_frag<T, DP>(map, keys, 0, ks), st.q[ks], s[0]);
-    const bool masked = first < seen.full_lo || first > seen.full_hi - kStreamKeys || (PAGED && there != 0xffffffffull);
-    Frag pf[2];
-    softmax_tile<T, DP, FORM, 1>(st, s, pf, score, first, w.lo, w.hi, at, half, masked, there);
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) st.o[d] = mfma_op(col_frag<T, DP>(map, values, c * 16, d), pf[c], st.o[d]);
-    asm volatile("" ::: "memory");
+    for (int i = 0; i < kStreamWaves; ++i) any |= lds.spoilt[i];
+    if (__builtin_expect(!__builtin_amdgcn_readfirstlane(any), 1)) break;
+    again = true;
+    __syncthreads();  // (what was read above is written again)
+    t = t0 + wave;
+    if (t < t1) {
+      look_up(t);
+      request(t);
+    }
   }
-
-  // the wavefronts' sums meet: all to one maximum, then halves of them into LDS and onto the others
-  st.sum = sum_of_halves(st.sum);
-  if (half == 0) {
-    stat[wave][lane][0] = st.top == kNoMax ? kNoMax : st.shift;
-    stat[wave][lane][1] = st.sum;
-  }
-  __syncthreads();
   float top = kNoMax;
 #pragma unroll
   for (int i = 0; i < kStreamWaves; ++i) top = fmaxf(top, stat[i][lane & 31][0]);
@@ -964,12 +1095,12 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
   st.top = top;
   st.shift = level;
   st.sum = half == 0 ? sum : 0.0f;
-  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, w, key_at<kStreamKeys>(begin, t0, 0, end), key_at<kStreamKeys>(begin, t1, 0, end), to_rows,
-                              partial);
+  finish<T, DP, PAGED, FORM>(p, e, st, r0, rows, key_at<kStreamKeys>(begin, t0, 0, end), key_at<kStreamKeys>(begin, t1, 0, end), to_rows,
+                              partial, again);
 }
 
 template <typename T, int DP, bool PAGED, int FORM>
-__global__ __launch_bounds__(64 * kStreamWaves, 2) void stream_kernel(const Args p) {
+__global__ __launch_bounds__(64 * kStreamWaves, DP == 128 ? 2 : 3) void stream_kernel(const Args p) {
   __shared__ StreamLds<DP> lds;
   // (workgroups share no keys; dealt to the XCDs in turn by kv head and sequence, so that each gets its part of every sequence, the first
   // splits of all before the second ones, which only long sequences have)
@@ -1009,7 +1140,7 @@ __device__ __forceinline__ Part flat_part(const Args& p, int piece, bool begins,
 }
 
 template <typename T, int DP, int FORM>
-__global__ __launch_bounds__(64 * kStreamWaves, 2) void flat_kernel(const Args p) {
+__global__ __launch_bounds__(64 * kStreamWaves, DP == 128 ? 2 : 3) void flat_kernel(const Args p) {
   constexpr int THREADS = 64 * kStreamWaves;
   __shared__ StreamLds<DP> lds;
   __shared__ int begins[kFlatSeqs + 1], sums[kStreamWaves], found;

@@ -183,16 +183,6 @@ __device__ __forceinline__ void store_columns(T* to, const f32x16 (&acc)[DT], in
     }
 }
 template <int DT>
-__device__ __forceinline__ bool all_finite(const f32x16 (&acc)[DT]) {
-  bool finite = true;
-#pragma unroll
-  for (int t = 0; t < DT; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) finite &= __builtin_fabsf(acc[t][i]) < __builtin_huge_valf();
-  return finite;
-}
-
-template <int DT>
 __device__ __forceinline__ void store_part(float* to, const f32x16 (&acc)[DT], int half) {
 #pragma unroll
   for (int t = 0; t < DT; ++t)

@@ -411,6 +411,117 @@ def test_a_poisoned_key_reaches_only_the_queries_that_see_it():
         assert bool(torch.isnan(dk[:, 1]).all()) and bool(torch.isnan(dv[:, 1]).all())
 
 
+def _scatter(g, shape, count):
+    """`count` places of a tensor of that shape with an infinity of either sign or NaN for each."""
+    return [(tuple(int(g.integers(n)) for n in shape), (np.inf, -np.inf, np.nan)[int(g.integers(3))]) for _ in range(count)]
+
+
+def _sums_of_odd(see, places, shape):
+    """What sums over the seen keys come to in the dimensions where a key holds something that is not finite: 0 where none does.
+    see [batch, n, m], places of [batch, heads, m, dim] -> [batch, heads, n, dim]."""
+    out = np.zeros((shape[0], shape[1], see.shape[1], shape[3]))
+    with np.errstate(invalid="ignore"):
+        for (b, h, j, d), x in dict(places).items():
+            out[b, h, see[b, :, j], d] += x
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [(1, 4, 2, 300, 300, 64), (2, 2, 1, 200, 260, 128), (86, 12, 6, 19, 193, 112), (1, 2, 1, 3, 700, 40), (1, 4, 2, 1, 9000, 128),
+                                  (1, 4, 2, 90, 3000, 64), (2, 3, 3, 130, 130, 24)], ids=str)
+@pytest.mark.parametrize("mask", ["causal", "window", "ranges"])
+def test_values_that_are_not_finite_reach_the_queries_that_see_them_alone(mask, size, dtype):
+    """In every kernel and cut: a dimension in which a query sees infinities or a NaN is their sum, and every other result has the bits
+    that it has without them."""
+    b, h, hk, n, m, d = size
+    g = np.random.Generator(np.random.PCG64(81))
+    q, k, v = _draw(g, (b, h, n, d), dtype, "dense"), _draw(g, (b, hk, m, d), dtype, "tokens"), _draw(g, (b, hk, m, d), dtype, "tokens")
+    if mask == "ranges":
+        lo = g.integers(0, m, (b, n))
+        r = np.stack([lo, np.minimum(m, lo + g.integers(0, m, (b, n)))], 2).astype(np.int32)
+        see, opts = np.stack([oa.in_ranges(x, m) for x in r]), dict(ranges=torch.from_numpy(r).cuda())
+    else:
+        opts = dict(causal=True, window=60 if mask == "window" else 0)
+        see = np.stack([oa.sees(n, m, **opts)] * b)
+    size = hb.hidet_attention_workspace_bytes(q, k)
+    for count in (1, 7, 60):
+        places = _scatter(g, v.shape, count)
+        # (one in the last key that is seen, which stands for those behind it in its tile)
+        places.append(((0, 0, m - 1, d - 1), np.inf))
+        odd = v.clone()
+        for at, x in places:
+            odd[at] = x
+        for ws in ([None, torch.empty(size // 4, device="cuda")] if size else [None]):
+            results = []
+            for values in (v, odd):
+                out, lse = torch.full_like(q, 7.0), torch.empty(b, h, n, device="cuda")
+                hb.hidet_attention(q, k, values, out, lse=lse, workspace=ws, **opts)
+                results.append((out, lse))
+            (clean, lse_clean), (out, lse) = results
+            sums = np.repeat(_sums_of_odd(see, places, tuple(v.shape)), h // hk, 1)
+            reached = torch.from_numpy(sums != 0.0).cuda()
+            want = torch.where(reached, torch.from_numpy(sums).cuda().to(out.dtype), clean)
+            assert torch.equal(lse, lse_clean)
+            assert torch.equal(torch.nan_to_num(out, 11.0, 12.0, 13.0), torch.nan_to_num(want, 11.0, 12.0, 13.0)), (count, ws is None)
+
+
+def test_scores_that_are_not_finite_and_values_beside_them():
+    """A row of which a score is NaN or +inf is NaN, one whose scores are all -inf is 0, whatever values are beside; keys of score -inf
+    count as masked, and so do their values."""
+    for dtype in ("f16", "bf16"):
+        for n in (1, 70, 200):
+            g = np.random.Generator(np.random.PCG64(82))
+            q, k, v = (_draw(g, (1, 2, 200, 64), dtype, "dense") for _ in range(3))
+            q = q[:, :, :n].abs() + 0.1
+            k[0, 0, 5:9] = -np.inf  # (scores of -inf, and values that nobody sees for it)
+            v[0, 0, 5:9] = np.nan
+            k[0, 1, 150, 3] = np.nan
+            v[0, 1, 20, 7] = np.inf
+            plain = [t.clone() for t in (k, v)]
+            see = np.ones((1, n, 200), bool)
+            see[0, :, 5:9] = False
+            out, lse = torch.empty_like(q), torch.empty(1, 2, n, device="cuda")
+            hb.hidet_attention(q, k, v, out, lse=lse)
+            assert bool(torch.isnan(out[0, 1]).all()) and bool(torch.isnan(lse[0, 1]).all())
+            plain[0][0, 0, 5:9] = 0.0
+            plain[1][0, 0, 5:9] = 0.0
+            want, bound = bounds(dtype, f64(q)[:, :1], f64(plain[0])[:, :1], f64(plain[1])[:, :1], see, 64 ** -0.5)
+            assert_within(out[:, :1], want[0], bound[0], "%s %d out" % (dtype, n))
+            assert_within(lse[:, :1], want[1], bound[1], "%s %d lse" % (dtype, n))
+            k[0, 0] = -np.inf
+            hb.hidet_attention(q, k, v, out, lse=lse)
+            assert not out[0, 0].any() and bool((lse[0, 0] == -np.inf).all())
+
+
+def _time(f):
+    f()
+    times = []
+    for _ in range(5):
+        e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        e[0].record()
+        f()
+        e[1].record()
+        torch.cuda.synchronize()
+        times.append(e[0].elapsed_time(e[1]))
+    return sorted(times)[2]
+
+
+@pytest.mark.parametrize("dtype,dim", [("f16", 64), ("bf16", 128)])
+def test_what_is_not_finite_costs_a_few_times_the_time(dtype, dim):
+    """Of a causal prompt of 2048: one value, the last, one in every key, all of them; measured 2 to 12 times the time, here up to 40."""
+    q = torch.randn(1, 8, 2048, dim, device="cuda").to(TYPES[dtype])
+    k, v = (torch.randn(1, 4, 2048, dim, device="cuda").to(TYPES[dtype]) for _ in range(2))
+    out, lse = torch.empty_like(q), torch.empty(1, 8, 2048, device="cuda")
+    clean = _time(lambda: hb.hidet_attention(q, k, v, out, lse=lse, causal=True))
+    for name, at in (("one", (0, 1, 100, 5)), ("the last", (0, 1, 2047, 5)), ("in every key", (slice(None), slice(None), slice(None), 5)), ("all", Ellipsis)):
+        for x in (np.inf, np.nan):
+            odd = v.clone()
+            odd[at] = x
+            took = _time(lambda: hb.hidet_attention(q, k, odd, out, lse=lse, causal=True))
+            print("%s %s: %.1f times" % (name, x, took / clean), flush=True)
+            assert took <= 40 * clean, name
+
+
 def test_large_scores_and_flat_ones():
     def grow(q, k, v, g, see):  # maxima that grow from tile to tile by far more than the slack before a rescale
         q.copy_(torch.ones_like(q))

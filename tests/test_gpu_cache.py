@@ -493,3 +493,42 @@ def test_large_caps(softcap, dtype):
     b = _ragged(64, dtype, 64)
     q, out, lse = b.run(softcap=softcap)
     b.check(q, out, lse, softcap=softcap)
+
+
+@pytest.mark.parametrize("dtype,dim", [("f16", 64), ("bf16", 128), ("bf16", 40)])
+@pytest.mark.parametrize("kind", ["single tokens", "chunks", "pieces"])
+def test_values_that_are_not_finite_reach_the_queries_that_see_them_alone(kind, dtype, dim):
+    """A dimension in which a query sees infinities or a NaN is their sum, and every other result has the bits that it has without them --
+    wherever the pages lie, the one that stands for no page among them."""
+    g = np.random.Generator(np.random.PCG64(45))
+    if kind == "pieces":
+        b = _ragged(45, dtype, dim)
+    else:
+        new = [1, 1, 1, 1] if kind == "single tokens" else [200, 3, 77, 40]
+        b = Batch(45, dtype, [300, 1000, 77, 500], new, 4, 2, dim, 24, pad=1)
+        b.table[1, 2] = -1
+        b.tables.copy_(torch.from_numpy(b.table))
+    before = b.v_pages.clone()
+    state = b.g.bit_generator.state
+    _, clean, lse_clean = b.run()
+    places = [tuple(int(g.integers(n)) for n in before.shape) + ((np.inf, -np.inf, np.nan)[int(g.integers(3))],) for _ in range(200)]
+    places += [(0, 1, 0, 3, np.inf), (0, 2, 1, 5, np.nan)]  # (of page 0)
+    for p, slot, h, d, x in places:
+        b.v_pages[p, slot, h, d] = x
+    b.g.bit_generator.state = state
+    _, out, lse = b.run()
+    assert torch.equal(lse, lse_clean)
+    want, group, first = clean.clone(), b.heads // b.kv_heads, 0
+    values = f64(b.v_pages)
+    for s, (length, n) in enumerate(zip(b.lengths, b.new)):
+        vv, there = oa.cache_rows(values, b.table[s], length)
+        see = oa.sees(n, length, causal=True) & there[None, :]
+        for h in range(b.heads):
+            v = np.where(there[:, None], vv[h // group], 0.0)
+            for j, d in zip(*np.nonzero(~np.isfinite(v))):
+                for i in np.flatnonzero(see[:, j]):
+                    old = want[first + i, h, d]
+                    want[first + i, h, d] = float(v[j, d]) if bool(torch.isfinite(old)) else old + float(v[j, d])
+        first += n
+    assert torch.equal(torch.nan_to_num(out, 11.0, 12.0, 13.0), torch.nan_to_num(want, 11.0, 12.0, 13.0))
+    assert not torch.equal(torch.nan_to_num(out, 11.0, 12.0, 13.0), clean)
