@@ -456,7 +456,7 @@ hidet_status_t hidet_attention_ranges(int64_t batch, int64_t seq_q, int64_t seq_
  * and lse of the forward call.  With P = exp(x - lse) and D_i = grad_out_i . out_i,
  *   dS = P (grad_out . V^T - D) dx/d(scale q.k);  grad_q = scale dS K;  grad_k = scale dS^T Q;  grad_v = P^T grad_out,
  * summed over the query heads that share a key head.  P and dS are rounded to dtype as operands of these products, in fp16 times a
- * power of two that follows the size of grad_out, so that gradients of any size keep their bits; sums are fp32, in an order that
+ * power of two that follows its size, so that gradients of any size keep their bits; sums are fp32, in an order that
  * depends on the sizes alone: no atomics, the same arguments give the same bits.  Slopes have no gradient.
  * D is grad_out . out with the rounded out, or, for a query that sees 32 keys at most, sum P (grad_out . v): what the rounding of
  * out leaves in dS = P (dP - D) is half a step of dtype of D, which is little beside dS unless a few keys have all the weight.

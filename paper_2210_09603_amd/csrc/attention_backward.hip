@@ -11,10 +11,9 @@
 // K^T by dS^T, the second S and dP (lane = key) and multiplies dout^T by P and Q^T by dS.
 //
 // P is at most 1 and mostly far below; as an operand it is taken times 2^10, which keeps it out of fp16's subnormals down to
-// 2^-24, and divided out at the end.  dS follows the caller's gradients in size: an fp16 operand takes it times the power of two that
-// brings the largest |dout| (of a row for dQ, of the rows that a block of keys is seen by for dK) to between 8 and 16.  Steps of
-// fp16's subnormals are then 2^-27 of that |dout|, and |dP - D| P may be 4096 times as large.  (As it is, dS of gradients of 1e-3 over 4096
-// keys is four such steps.)  bf16 has the range of fp32.
+// 2^-24, and divided out at the end.  dS follows the caller's gradients and values in size: an fp16 operand takes it times a power of
+// two that follows dS itself, see Lift.  (As it is, dS of gradients of 1e-3 over 4096 keys is four steps of fp16's subnormals.)  bf16 has
+// the range of fp32.
 #include "attention_host.hpp"
 
 using namespace hidet;
@@ -32,7 +31,6 @@ struct BackArgs {
   void* dv;
   Strides dos, dqs, dks, dvs;
   float* info;    // of every row of a kv head, see row_info
-  float* peak;    // [entry][row_groups]: the largest finite |dout| of 32 rows (fp16)
   int4* seen;     // [batch][row_groups]: of 32 rows, the first and last + 1 of the keys that any of them sees; that all of them see
   int* order;     // [batch][key_tiles]: the blocks of keys, the longest first; null: as they lie
   float* part;    // partial sums of the splits: dQ's [split][kv row][DP], then dK's and dV's [split][entry][key][2][DP]
@@ -62,8 +60,33 @@ __device__ __forceinline__ float unless_alone(int keys) { return keys == 1 ? 0.0
 
 __device__ __forceinline__ float lse_to_base_2(float lse) { return lse == kNoMax ? __builtin_huge_valf() : lse * kLog2e; }
 
-// Twos by which dS is lifted as an fp16 operand, for the largest |dout|
-__device__ __forceinline__ int lift_of(float peak) { return peak > 0.0f ? 4 - __builtin_amdgcn_frexp_expf(peak) : 0; }
+// The power of two by which dS is taken as an fp16 operand, for each sum of its own (a lane's and its partner's): the first numbers bring
+// their largest to between 2^9 and 2^10, and larger ones lower it before they leave fp16.  Smaller ones lose what is 2^-34 of the
+// largest.  (2^40 at most: what that leaves small is far below the steps of an fp16 result, and nothing that fp16 tensors give, 2^39,
+// leaves fp32.)
+struct Lift {
+  float by = 1.0f;
+  float most = 0.0f;  // 2^15 from the first numbers on
+  // ds: the numbers of a tile, already times `by`; acc: the sum so far
+  template <int DT>
+  __device__ __forceinline__ void fit(f32x16& ds, f32x16 (&acc)[DT]) {
+    float top = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, __builtin_fabsf(ds[r]));
+    top = max_of_halves(top);
+    if (!__any(top > most)) return;
+    const bool is = top > most && top < __builtin_huge_valf();
+    const float f = is ? __builtin_ldexpf(1.0f, min(10 - __builtin_amdgcn_frexp_expf(top), 40)) : 1.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] *= f;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[t][r] *= f;
+    by *= f;
+    most = is ? 32768.0f : most;
+  }
+};
 
 // Rows that come out not finite, again: only what a query sees takes part (see the forward pass).
 template <typename T, int DP, int FORM>
@@ -300,21 +323,6 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
       for (int i = 0; i < 8; ++i) delta = __builtin_fmaf(to_f32(g[ks][i]), to_f32(o[ks][i]), delta);
   }
   delta = sum_of_halves(delta);
-  int lift = 0;
-  if constexpr (!std::is_same<T, bf16>::value) {
-    float peak = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float a = __builtin_fabsf(to_f32(g[ks][i]));
-        peak = fmaxf(peak, a < __builtin_huge_valf() ? a : 0.0f);
-      }
-    peak = max_of_halves(peak);
-    lift = lift_of(peak);
-    const float of_rows = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(int, peak)));  // (of floats that are not negative: as whole numbers)
-    if (lane == 0 && wave < 4 && z == 0 && r0 < rows) b.peak[((long long)e.b * p.kv_heads + e.kv) * b.row_groups + (r0 >> 5)] = of_rows;
-  }
   const long long stat = lse_offset<false>(p, e, w);
   const float lse = lse_to_base_2(p.lse[stat]);
   if (half == 0 && wave < 4 && z == 0) {
@@ -413,7 +421,8 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
     __syncthreads();
   }
   if (half == 0 && wave < 4 && z == 0) *row_info<FORM>(b, e, r0 + lane, 1) = r0 + lane < rows ? delta * (1.0f / kLift) : 0.0f;
-  const float up = __builtin_ldexpf(1.0f, lift), lifted_delta = delta * up;
+  constexpr bool LIFTS = !std::is_same<T, bf16>::value;
+  Lift lift;
   f32x16 acc[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -447,9 +456,17 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
           x = __builtin_fmaf(s[r], score.factor, -lse);
         else
           x = score(s[r], distance - (float)(8 * (r >> 2) + (r & 3)), derivative) - lse;
-        float d = exp2_fast(x) * __builtin_fmaf(dp[r], up, -lifted_delta) * derivative;
+        float d = exp2_fast(x) * (LIFTS ? __builtin_fmaf(dp[r], lift.by, -delta * lift.by) : dp[r] - delta) * derivative;
         if (masked) d = (unsigned)(j - w.lo) < (unsigned)(w.hi - w.lo) ? d : 0.0f;
-        ds[r >> 3][r & 7] = from_f32<T>(d);
+        if constexpr (LIFTS)
+          s[r] = d;
+        else
+          ds[r >> 3][r & 7] = from_f32<T>(d);
+      }
+      if constexpr (LIFTS) {
+        lift.fit(s, acc);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) ds[r >> 3][r & 7] = from_f32<T>(s[r]);
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -457,7 +474,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
         for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, DP>(map, keys, c * 32 + h * 16, d), ds[h], acc[d]);
     }
   }
-  const float by = unless_alone(w.hi - w.lo) * __builtin_ldexpf(1.0f, -lift);
+  const float by = unless_alone(w.hi - w.lo) / lift.by;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -547,7 +564,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * STAGE];  // q of two stages, dout of two
   __shared__ __attribute__((aligned(16))) unsigned char info[2 * INFO];
-  __shared__ int bounds[8][3];
+  __shared__ int bounds[8][2];
   constexpr bool LIFTS = !std::is_same<T, bf16>::value;
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -562,24 +579,20 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   const int block_key = tile * kBlockKeys, key0 = block_key + (wave & 1) * 32, key = key0 + (lane & 31);
   const int block_end = min(block_key + kBlockKeys, e.keys);
 
-  // the first and last groups of 32 rows that see a key of the block, and the largest |dout| of such groups (as a whole number)
+  // the first and last groups of 32 rows that see a key of the block
   const int groups = (rows + 31) >> 5;
   const int4* seen = b.seen + (long long)e.b * b.row_groups;
-  const float* peaks = b.peak + ((long long)e.b * p.kv_heads + e.kv) * b.row_groups;
-  int from = 0x7fffffff, to = 0, peak = 0;
+  int from = 0x7fffffff, to = 0;
   for (int i = tid; i < groups; i += kDkvThreads)
     if (seen[i].x < block_end && seen[i].y > block_key) {
       from = min(from, i);
       to = i + 1;
-      if constexpr (LIFTS) peak = max(peak, __builtin_bit_cast(int, peaks[i]));
     }
   from = wave_min(from);
   to = wave_max(to);
-  if constexpr (LIFTS) peak = wave_max(peak);
   if (lane == 0) {
     bounds[wave][0] = from;
     bounds[wave][1] = to;
-    bounds[wave][2] = peak;
   }
   Frag kf[KS], vf[KS];
   const int mine = min(key, e.keys - 1);
@@ -592,10 +605,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   for (int i = 0; i < 8; ++i) {
     from = min(from, bounds[i][0]);
     to = max(to, bounds[i][1]);
-    if constexpr (LIFTS) peak = max(peak, bounds[i][2]);
   }
-  const int twos = LIFTS ? lift_of(__builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(peak))) : 0;
-  const float lift = __builtin_ldexpf(1.0f, twos);
   from = __builtin_amdgcn_readfirstlane(from);
   to = __builtin_amdgcn_readfirstlane(to);
   const int first_tile = from < to ? from >> 2 : 0, last_tile = from < to ? (to + 3) >> 2 : 0;
@@ -645,6 +655,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
+  Lift lift;
   const Score<FORM> all_scores(p, 0.0f);
   // (which groups of 32 rows take part: asked for a tile ahead, and in scalar registers before the next tile's loads are under way, for
   // which the compiler would otherwise wait)
@@ -740,7 +751,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
           for (int u = 0; u < 4; ++u) {
             const int r = 4 * g + u;
             dp[r] = __builtin_fmaf(dp[r], 1.0f / kLift, -delta[u]);
-            if constexpr (LIFTS) dp[r] *= lift;
+            if constexpr (LIFTS) dp[r] *= lift.by;
             dp[r] *= s[r];
             if constexpr (FORM & FORM_CAP) dp[r] *= derivative[r];
           }
@@ -763,6 +774,8 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
           }
         }
       }
+      if constexpr (LIFTS)
+        if (!for_dv) lift.fit(BOTH ? dp : s, acc[0]);
       Frag w[SUMS][2];  // both: dS, P
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -782,6 +795,13 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
           }
         }
     }
+  }
+  if (LIFTS && !for_dv) {
+    const float by = 1.0f / lift.by;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[0][d][r] *= by;
   }
   // the wavefronts of a sum meet: four (two of them onto two, one onto one), or two
   const int lead = BOTH ? 0 : wave & 4;  // the first wavefront of the kind
@@ -817,12 +837,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
 #pragma unroll
   for (int i = 0; i < SUMS; ++i) {
     const bool is_dv = for_dv || i == 1;
-    if (LIFTS && !is_dv) {
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][d][r] *= __builtin_ldexpf(1.0f, -twos);
-    }
     if (b.dkv_splits > 1) {
       if (key < e.keys) store_part<DT>(dkv_part<DP>(b, z, e, key) + (is_dv ? DP : 0), acc[i], half);
       continue;
@@ -925,8 +939,6 @@ hipError_t dispatch(int form, const BackArgs& b, hipStream_t stream) {
 
 long long row_groups_of(long long rows) { return (rows + 31) / 32; }
 long long order_bytes(long long batch, long long key_tiles) { return (batch * key_tiles * 4 + 15) / 16 * 16; }
-// (of both types)
-long long peak_bytes(long long entries, long long row_groups) { return (entries * row_groups * 4 + 15) / 16 * 16; }
 // (of all forms: with a bias twice the fields)
 long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
 
@@ -976,8 +988,7 @@ int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, i
   if (group >= kMaxRows || seq_q >= kMaxRows || seq_k >= kMaxRows || !fits_cut(batch, kv_heads, seq_q * group, seq_k)) return 0;
   const BackCut c = cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim));
   const long long row_groups = row_groups_of(seq_q * group);
-  return info_bytes(batch * kv_heads, seq_q * group) + peak_bytes(batch * kv_heads, row_groups) + batch * row_groups * 16 +
-         order_bytes(batch, c.key_tiles) + c.part_bytes;
+  return info_bytes(batch * kv_heads, seq_q * group) + batch * row_groups * 16 + order_bytes(batch, c.key_tiles) + c.part_bytes;
 }
 
 hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
@@ -1024,9 +1035,7 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
     b.dq = grad_q->data;
     b.dqs = strides_of(grad_q);
     b.info = static_cast<float*>(workspace);
-    char* peak = static_cast<char*>(workspace) + info_bytes(batch * kv_heads, seq_q * group);
-    b.peak = reinterpret_cast<float*>(peak);
-    b.seen = reinterpret_cast<int4*>(peak + peak_bytes(batch * kv_heads, row_groups_of(seq_q * group)));
+    b.seen = reinterpret_cast<int4*>(static_cast<char*>(workspace) + info_bytes(batch * kv_heads, seq_q * group));
   }
   if (seq_k > 0) {
     p.k = k->data;

@@ -327,6 +327,34 @@ def test_fp16_gradients_of_any_size(size, twos, opts):
         assert_within(other * 2.0 ** -twos, one, 2 * u * value + small + small * 2.0 ** -twos, "%s %s" % (size, name))
 
 
+@pytest.mark.parametrize("size", [(1, 2, 1, 300, 4096, 64), (1, 2, 2, 130, 1500, 128), (2, 4, 2, 70, 900, 40)], ids=str)
+@pytest.mark.parametrize("twos", [-8, 7, 12])
+def test_fp16_gradients_under_values_of_any_size(size, twos):
+    """dQ and dK are linear in the values (and the output with them) as well, and dV has nothing to do with them."""
+    b, h, hk, n, m, d = size
+    g = np.random.Generator(np.random.PCG64(72))
+    q, dout, out = (_draw(g, (b, h, n, d), "f16", "dense") for _ in range(3))
+    k, v = (_draw(g, (b, hk, m, d), "f16", "dense") for _ in range(2))
+    v = torch.where(v.abs() < 2.0 ** -4, torch.zeros_like(v), v)
+    lse = torch.empty(b, h, n, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse)
+    out = (out.float() * 2048).round().half() / 2048
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+    got = []
+    for factor in (1.0, 2.0 ** twos):
+        values, result = v * factor, out * factor
+        assert torch.equal(values.double(), v.double() * factor) and torch.equal(result.double(), out.double() * factor)
+        grads = [torch.empty_like(t) for t in (q, k, v)]
+        hb.hidet_attention_backward(dout, q, k, values, result, lse, *grads, ws)
+        assert all(bool(torch.isfinite(t).all()) for t in grads)
+        got.append([f64(t) for t in grads])
+    u, small = 2.0 ** -11, 2.0 ** -25
+    for name, one, other in zip(("dq", "dk"), *got):
+        value = (np.abs(one) + small) / (1 - u)
+        assert_within(other * 2.0 ** -twos, one, 2 * u * value + small + small * 2.0 ** -twos, "%s %s" % (size, name))
+    assert np.array_equal(got[0][2], got[1][2])
+
+
 def test_no_keys_and_no_queries():
     q = torch.randn(2, 4, 5, 64, device="cuda").half()
     k = torch.empty(2, 2, 0, 64, device="cuda", dtype=torch.float16)
