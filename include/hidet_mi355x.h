@@ -461,7 +461,8 @@ hidet_status_t hidet_attention_ranges(int64_t batch, int64_t seq_q, int64_t seq_
  * D is grad_out . out with the rounded out, or, for a query that sees 32 keys at most, sum P (grad_out . v): what the rounding of
  * out leaves in dS = P (dP - D) is half a step of dtype of D, which is little beside dS unless a few keys have all the weight.
  * All three gradients are written whole (zeros where nothing was seen), in their own strides; infinities and NaN in what a query
- * does not see have no influence, as in the forward pass.  The workspace is needed: HIDET_ERR_INVALID_ARG if it is smaller than
+ * does not see have no influence, as in the forward pass; a query that has or sees one has a grad_q that is not finite, as have grad_k
+ * of the keys that it sees, and grad_v where grad_out has it.  The workspace is needed: HIDET_ERR_INVALID_ARG if it is smaller than
  * hidet_attention_backward_workspace_bytes.  Limits and no-ops as for hidet_attention.
  */
 hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
@@ -504,13 +505,14 @@ hidet_status_t hidet_rope_frequencies(int64_t rotary_dim, double base, int32_t s
  * sequence s lies at  page * stride_page + (t % page_size) * stride_slot + h * stride_head + d  of k and of v, with
  * page = tables[s * table_stride + t / page_size].  lengths[s] is the number of tokens that the sequence has in the cache, the
  * new ones of a call among them.  A page number outside 0 .. num_pages - 1 stands for no page, and so does a position of
- * table_width * page_size or more: nothing is written there and its keys are not seen.  Page sizes need not be powers of two, strides are free (both tensors
- * share them; the head_dim elements are contiguous), offsets are 64 bits wide.  All but the structure itself is DEVICE memory.
+ * table_width * page_size or more: nothing is written there and its keys are not seen.  Page sizes need not be powers of two, strides
+ * are free (both tensors share them; the head_dim elements are contiguous), offsets are 64 bits wide.  All but the structure itself is
+ * DEVICE memory.
  *
  * A call serves a ragged batch: the new tokens of sequence s are rows starts[s] .. starts[s + 1] - 1 of `tokens` rows (starts:
  * DEVICE, ascending, [seqs + 1]; cut to 0 .. tokens before anything else), and they are the sequence's last positions: its i-th new
- * token stands at position lengths[s] - (starts[s + 1] - starts[s]) + i.  Rows of no sequence are left as they are.  max_new bounds the new
- * tokens of a sequence (it sizes the grid); of a sequence with more only the first max_new are worked on.
+ * token stands at position lengths[s] - (starts[s + 1] - starts[s]) + i.  Rows of no sequence are left as they are.  max_new bounds
+ * the new tokens of a sequence (it sizes the grid); of a sequence with more only the first max_new are worked on.
  *
  * hidet_cache_append writes k and v [tokens][heads][head_dim] of the cache's dtype (any of the three) into the pages.  Two tokens
  * for the same place (a page that two sequences share): every 16 bytes of it are those of one of them, which one is not defined.

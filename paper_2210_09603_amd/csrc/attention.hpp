@@ -129,6 +129,12 @@ __device__ __forceinline__ typename Frag8<T>::type col_frag(const ReadMap<DP>& m
 // register, so that nothing has to stay reserved while they run; they are waited for by wait_all_and_meet or wait_loads.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
+// (the same in all lanes, which the compiler does not always see)
+__device__ __forceinline__ unsigned in_scalar(unsigned v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const void* in_scalar(const void* v) {
+  const unsigned long long bits = (unsigned long long)v;
+  return (const void*)(((unsigned long long)in_scalar((unsigned)(bits >> 32)) << 32) | in_scalar((unsigned)bits));
+}
 struct DirectLoad {
   // from `offset` bytes behind `base`, which the scalar unit copies (a load may read a scalar register that a vector instruction has
   // written five wait states later at the earliest)
@@ -139,7 +145,7 @@ struct DirectLoad {
         "s_mov_b64 %0, %2\n\t"
         "global_load_lds_dwordx4 %1, %0"
         : "=&s"(copy)
-        : "v"(offset), "s"(base), "s"(lds)
+        : "v"(offset), "s"(in_scalar(base)), "s"(in_scalar(lds))
         : "memory", "m0");
   }
   // from an address of the lane's own
@@ -149,7 +155,7 @@ struct DirectLoad {
         "s_nop 3\n\t"
         "global_load_lds_dwordx4 %0, off"
         :
-        : "v"(address), "s"(lds)
+        : "v"(address), "s"(in_scalar(lds))
         : "memory", "m0");
   }
 };
@@ -1035,7 +1041,7 @@ __device__ __forceinline__ void stream_tiles(const Args& p, StreamLds<DP>& lds, 
     const int spoilt = !again && __any(!all_finite(st.o) && st.sum < __builtin_huge_valf());
     st.sum = sum_of_halves(st.sum);
     if (half == 0) {
-      stat[wave][lane][0] = st.top == kNoMax ? kNoMax : st.shift;
+      stat[wave][lane][0] = st.sum == 0.0f ? kNoMax : st.shift;  // (a sum that is NaN counts, though its scores make no maximum)
       stat[wave][lane][1] = st.sum;
     }
     if (lane == 0) lds.spoilt[wave] = spoilt;

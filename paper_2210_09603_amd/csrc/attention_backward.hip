@@ -12,7 +12,7 @@
 //
 // P is at most 1 and mostly far below; as an operand it is taken times 2^10, which keeps it out of fp16's subnormals down to
 // 2^-24, and divided out at the end.  dS follows the caller's gradients and values in size: an fp16 operand takes it times a power of
-// two that follows dS itself, see Lift.  (As it is, dS of gradients of 1e-3 over 4096 keys is four steps of fp16's subnormals.)  bf16 has
+// two that follows it, see Lift.  (As it is, dS of gradients of 1e-3 over 4096 keys is four steps of fp16's subnormals.)  bf16 has
 // the range of fp32.
 #include "attention_host.hpp"
 
@@ -31,6 +31,7 @@ struct BackArgs {
   void* dv;
   Strides dos, dqs, dks, dvs;
   float* info;    // of every row of a kv head, see row_info
+  float* peak;    // [entry][row_groups]: of 32 rows, the largest of what their dS are likely to be, see Lift (fp16)
   int4* seen;     // [batch][row_groups]: of 32 rows, the first and last + 1 of the keys that any of them sees; that all of them see
   int* order;     // [batch][key_tiles]: the blocks of keys, the longest first; null: as they lie
   float* part;    // partial sums of the splits: dQ's [split][kv row][DP], then dK's and dV's [split][entry][key][2][DP]
@@ -60,23 +61,25 @@ __device__ __forceinline__ float unless_alone(int keys) { return keys == 1 ? 0.0
 
 __device__ __forceinline__ float lse_to_base_2(float lse) { return lse == kNoMax ? __builtin_huge_valf() : lse * kLog2e; }
 
-// The power of two by which dS is taken as an fp16 operand, for each sum of its own (a lane's and its partner's): the first numbers bring
-// their largest to between 2^9 and 2^10, and larger ones lower it before they leave fp16.  Smaller ones lose what is 2^-34 of the
-// largest.  (2^40 at most: what that leaves small is far below the steps of an fp16 result, and nothing that fp16 tensors give, 2^39,
-// leaves fp32.)
+// The power of two by which dS is taken as an fp16 operand.  A query's dS = P (dP - D) are about as large as the product of its largest
+// |dout| and its largest |out| (`peak`), times the root of the dimensions: out is the sum of P v, and P v alone is not much larger.  For
+// dK it is the largest of the rows that see a block of keys.  `by` brings that to between 2^4 and 2^5: dS may be 2^11 times as large, and
+// steps of fp16's subnormals are 2^-29 of it.  Where dS passes fp16 all the same (large values that cancel in out) the sums come out not
+// finite, and are taken again: dQ with 2^-12 of it as often as that takes, dK with a look at every tile.
 struct Lift {
-  float by = 1.0f;
-  float most = 0.0f;  // 2^15 from the first numbers on
-  // ds: the numbers of a tile, already times `by`; acc: the sum so far
+  float by;
+  __device__ __forceinline__ explicit Lift(float peak) {
+    by = peak > 0.0f ? __builtin_ldexpf(1.0f, 5 - __builtin_amdgcn_frexp_expf(peak)) : 1.0f;
+  }
+  // ds: the numbers of a tile, already times `by`, acc: the sum so far, both of them lowered where ds would pass fp16
   template <int DT>
   __device__ __forceinline__ void fit(f32x16& ds, f32x16 (&acc)[DT]) {
     float top = 0.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) top = fmaxf(top, __builtin_fabsf(ds[r]));
     top = max_of_halves(top);
-    if (!__any(top > most)) return;
-    const bool is = top > most && top < __builtin_huge_valf();
-    const float f = is ? __builtin_ldexpf(1.0f, min(10 - __builtin_amdgcn_frexp_expf(top), 40)) : 1.0f;
+    if (!__any(top > 32768.0f)) return;
+    const float f = top > 32768.0f && top < __builtin_huge_valf() ? __builtin_ldexpf(1.0f, 10 - __builtin_amdgcn_frexp_expf(top)) : 1.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) ds[r] *= f;
 #pragma unroll
@@ -84,13 +87,20 @@ struct Lift {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[t][r] *= f;
     by *= f;
-    most = is ? 32768.0f : most;
   }
 };
 
-// Rows that come out not finite, again: only what a query sees takes part (see the forward pass).
+// What comes out not finite, as in the forward pass: a second walk without what is not finite of the operands of the last products -- zeros
+// for such keys for dQ, for such elements of q and dout for dK and dV --, which gives the bits that there are without.  A query whose
+// log-sum or D is not finite has dS that are not, in its own row and for all keys that it sees, from those two numbers alone; and where a
+// key is seen by a gradient of the output that is not finite, one pass over such rows puts it into dV.  (4096 rows and keys, 16 heads of 128
+// dimensions, causal, 570 us: with one infinite gradient 1170, one in every row 4400; 620 ms when such rows were computed one by one.)
+
+// dQ of a query that sees keys that are not finite and has a finite log-sum all the same (their scores are -inf, their weights 0), where zeros
+// in their place have weights that pass fp32: a log-sum below -88.  Over its keys from `from` on and before `to`; by all lanes of a
+// wavefront.
 template <typename T, int DP, int FORM>
-__device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry& e, int r, float delta) {
+__device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry& e, int r, int from, int to, float delta, float (&acc)[DP / 64]) {
   constexpr int E = DP / 64;
   const Args& p = b.f;
   const int lane = threadIdx.x & 63;
@@ -101,7 +111,7 @@ __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry&
   const T* k = keys_of<T, false>(p, e, p.k, p.ks);
   const T* v = keys_of<T, false>(p, e, p.v, p.vs);
   const float lse = lse_to_base_2(p.lse[lse_offset<false>(p, e, w)]);
-  float mq[E], mg[E], acc[E];
+  float mq[E], mg[E];
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     const int d = lane * E + i;
@@ -109,7 +119,9 @@ __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry&
     mg[i] = d < p.dim ? to_f32(g[d]) : 0.0f;
     acc[i] = 0.0f;
   }
-  for (int j = w.lo; j < w.hi; ++j) {
+  from = max(from, w.lo);
+  to = min(to, w.hi);
+  for (int j = from; j < to; ++j) {
     float dot = 0.0f, dp = 0.0f, mk[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -125,70 +137,54 @@ __device__ __forceinline__ void dq_by_definition(const BackArgs& b, const Entry&
     const float prob = exp2_fast(score(dot, (float)(w.token + e.shift - j), derivative) - lse);
     if (prob == 0.0f) continue;
     const float ds = prob * (dp - delta) * derivative * unless_alone(w.hi - w.lo);
-    bool finite = false;
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      acc[i] += ds * mk[i];
-      finite |= acc[i] == acc[i];
-    }
-    if (!__any(finite)) break;
+    for (int i = 0; i < E; ++i) acc[i] += ds * mk[i];
   }
-  T* to = reinterpret_cast<T*>(b.dq) + query_offset<false>(p, e, b.dqs, w);
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (lane * E + i < p.dim) to[lane * E + i] = from_f32<T>(acc[i] * p.scale);
 }
 
+// What is not finite of the gradients of the output of rows from `from` on and before `to`, for the lane's key: the sum of those that see it.
 template <typename T, int DP, int FORM>
-__device__ __forceinline__ void dkv_by_definition(const BackArgs& b, const Entry& e, int j, bool for_dv) {
-  constexpr int E = DP / 64;
+__device__ __forceinline__ OddSums<DP> odd_gradients(const BackArgs& b, const Entry& e, int key, int from, int to, bool ask) {
+  constexpr int E = DP / 64, U = 8;
+  struct __attribute__((packed, aligned(2))) Own {
+    T x[E];
+  };
   const Args& p = b.f;
-  const int lane = threadIdx.x & 63;
-  const T* k = keys_of<T, false>(p, e, p.k, p.ks) + (long long)j * p.ks.row;
-  const T* v = keys_of<T, false>(p, e, p.v, p.vs) + (long long)j * p.vs.row;
-  float mk[E], mv[E], acc[E];
+  const int lane = worked_out_here(threadIdx.x & 63);
+  const bool has = lane * E < p.dim;
+  const T* base = reinterpret_cast<const T*>(b.dout) + (long long)e.b * b.dos.batch + (long long)e.kv * p.group * b.dos.head + (has ? lane * E : 0);
+  OddSums<DP> sums;
+  sums.clear();
+#pragma unroll 1
+  for (int r0 = from; r0 < to; r0 += 64) {
+    // (a row whose own log-sum is not finite has weights that are 0 or NaN already)
+    const int r = min(r0 + lane, to - 1);
+    const bool odd = r0 + lane < to && !(__builtin_fabsf(*row_info<FORM>(b, e, r, 1)) < __builtin_huge_valf()) &&
+                     __builtin_fabsf(*row_info<FORM>(b, e, r, 0)) < __builtin_huge_valf();
+    const unsigned long long rows = __ballot(odd);
+    if (!rows) continue;
+    const int lo = *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 2)), count = *reinterpret_cast<int*>(row_info<FORM>(b, e, r, 3));
+#pragma unroll 1
+    for (int c = 0; c < 64; c += U) {
+      if (!((rows >> c) & ((1u << U) - 1))) continue;
+      Own g[U];
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int d = lane * E + i;
-    mk[i] = d < p.dim ? to_f32(k[d]) : 0.0f;
-    mv[i] = d < p.dim ? to_f32(v[d]) : 0.0f;
-    acc[i] = 0.0f;
-  }
-  for (int r = 0; r < e.tokens * p.group; ++r) {
-    const Row w = make_row<false>(p, e, r);
-    if (j < w.lo || j >= w.hi) continue;
-    const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
-    const T* q = reinterpret_cast<const T*>(p.q) + query_offset<false>(p, e, p.qs, w);
-    const T* g = reinterpret_cast<const T*>(b.dout) + query_offset<false>(p, e, b.dos, w);
-    float dot = 0.0f, dp = 0.0f, mq[E], mg[E];
+      for (int u = 0; u < U; ++u) {
+        const int row = min(r0 + c + u, to - 1), token = p.d_group.div(row), head = row - token * p.group;
+        g[u] = *reinterpret_cast<const Own*>(base + (long long)head * b.dos.head + (long long)token * b.dos.row);
+      }
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const int d = lane * E + i;
-      mq[i] = d < p.dim ? to_f32(q[d]) : 0.0f;
-      mg[i] = d < p.dim ? to_f32(g[d]) : 0.0f;
-      dot = __builtin_fmaf(mq[i], mk[i], dot);
-      dp = __builtin_fmaf(mg[i], mv[i], dp);
+      for (int u = 0; u < U; ++u)
+        if ((rows >> (c + u)) & 1) {
+          float x[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) x[i] = has ? to_f32(g[u].x[i]) : 0.0f;
+          sums.add(x, ask && (unsigned)(key - __builtin_amdgcn_readlane(lo, c + u)) < (unsigned)__builtin_amdgcn_readlane(count, c + u));
+        }
+      if (!__any(ask && any_but_nan(sums, p.dim))) return sums;
     }
-    dot = wave_sum(dot);
-    dp = wave_sum(dp);
-    const long long at = lse_offset<false>(p, e, w);
-    float derivative;
-    const float prob = exp2_fast(score(dot, (float)(w.token + e.shift - j), derivative) - lse_to_base_2(p.lse[at]));
-    if (prob == 0.0f) continue;
-    const float ds = prob * (dp - kLift * *row_info<FORM>(b, e, r, 1)) * derivative * unless_alone(w.hi - w.lo);
-    bool finite = false;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      acc[i] += for_dv ? prob * mg[i] : ds * mq[i];
-      finite |= acc[i] == acc[i];
-    }
-    if (!__any(finite)) break;
   }
-  const Strides& s = for_dv ? b.dvs : b.dks;
-  T* to = reinterpret_cast<T*>(for_dv ? b.dv : b.dk) + (long long)e.b * s.batch + (long long)e.kv * s.head + (long long)j * s.row;
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (lane * E + i < p.dim) to[lane * E + i] = from_f32<T>(for_dv ? acc[i] : acc[i] * p.scale);
+  return sums;
 }
 
 // A transposed accumulator (lane = vector, registers = its dimensions) to the vector's memory, times `by`.
@@ -275,7 +271,8 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   constexpr int CPR = DP / 8, STAGE = TILE * CPR * 16, NL = TILE * CPR / THREADS, RPP = THREADS / CPR, KS = DP / 16, DT = DP / 32;
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(16))) unsigned char smem[4 * STAGE];
-  __shared__ int bounds[4][2], few_bounds[4][2];
+  __shared__ int bounds[4][2], few_bounds[4][2], spoilt;
+  __shared__ unsigned odd_keys[TILE / 32];
   __shared__ float halves[8][32];
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -313,14 +310,30 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
   Frag q[KS], g[KS];
   load_row_frags<T, DP>(reinterpret_cast<const T*>(p.q) + query_offset<false>(p, e, p.qs, w), half, p.dim, q);
   load_row_frags<T, DP>(reinterpret_cast<const T*>(b.dout) + query_offset<false>(p, e, b.dos, w), half, p.dim, g);
-  float delta = 0.0f;
+  constexpr bool LIFTS = !std::is_same<T, bf16>::value;
+  float delta = 0.0f, peak = 0.0f;
   {
     Frag o[KS];
+    float g_peak = 0.0f, o_peak = 0.0f;
     load_row_frags<T, DP>(reinterpret_cast<const T*>(p.out) + query_offset<false>(p, e, p.os, w), half, p.dim, o);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) delta = __builtin_fmaf(to_f32(g[ks][i]), to_f32(o[ks][i]), delta);
+      for (int i = 0; i < 8; ++i) {
+        const float its = to_f32(g[ks][i]), out = to_f32(o[ks][i]);
+        delta = __builtin_fmaf(its, out, delta);
+        if constexpr (LIFTS) {
+          g_peak = fmaxf(g_peak, __builtin_fabsf(its) < __builtin_huge_valf() ? __builtin_fabsf(its) : 0.0f);
+          o_peak = fmaxf(o_peak, __builtin_fabsf(out) < __builtin_huge_valf() ? __builtin_fabsf(out) : 0.0f);
+        }
+      }
+    if constexpr (LIFTS) {
+      peak = max_of_halves(g_peak) * max_of_halves(o_peak);
+      // (numbers that are not negative compare as whole numbers)
+      const int of_rows = wave_max(__builtin_bit_cast(int, peak));
+      if (lane == 0 && wave < 4 && z == 0 && r0 < rows)
+        b.peak[((long long)e.b * p.kv_heads + e.kv) * b.row_groups + (r0 >> 5)] = __builtin_bit_cast(float, of_rows);
+    }
   }
   delta = sum_of_halves(delta);
   const long long stat = lse_offset<false>(p, e, w);
@@ -337,6 +350,7 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
     }
   }
   const Score<FORM> score(p, p.slopes ? p.slopes[w.head] : 0.0f);
+  if (tid == 0) spoilt = 0;
   if (p.dim < DP)
     for (int i = tid; i < 4 * STAGE / 16; i += THREADS) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
@@ -416,63 +430,110 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
       __syncthreads();
       rest += halves[wave ^ 4][lane & 31];
     }
-    // (a row that comes out not finite is worked out again, with the D that it had)
+    // (D that is not finite says so already)
     if (few && __builtin_fabsf(rest) < __builtin_huge_valf()) delta += rest;
     __syncthreads();
   }
   if (half == 0 && wave < 4 && z == 0) *row_info<FORM>(b, e, r0 + lane, 1) = r0 + lane < rows ? delta * (1.0f / kLift) : 0.0f;
-  constexpr bool LIFTS = !std::is_same<T, bf16>::value;
-  Lift lift;
-  f32x16 acc[DT];
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
-  if (t0 < t1) request(begin, end, t0);
-  for (int t = t0; t < t1; ++t) {
-    wait_all_and_meet();
-    if (t + 1 < t1) request(begin, end, t + 1);
-    const int first = begin + t * TILE + own;
-    if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
-    const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
-    const bool masked = first < mine.full_lo || first + kTileKeys > mine.full_hi;
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      f32x16 s, dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, keys, c * 32, ks), q[ks], s);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, values, c * 32, ks), g[ks], dp);
-      const int base = first + c * 32 + 4 * half;
-      const float distance = (float)(at - base);
-      Frag ds[2];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int j = base + 8 * (r >> 2) + (r & 3);
-        float derivative = 1.0f, x;
-        if constexpr (FORM == FORM_PLAIN)
-          x = __builtin_fmaf(s[r], score.factor, -lse);
-        else
-          x = score(s[r], distance - (float)(8 * (r >> 2) + (r & 3)), derivative) - lse;
-        float d = exp2_fast(x) * (LIFTS ? __builtin_fmaf(dp[r], lift.by, -delta * lift.by) : dp[r] - delta) * derivative;
-        if (masked) d = (unsigned)(j - w.lo) < (unsigned)(w.hi - w.lo) ? d : 0.0f;
-        if constexpr (LIFTS)
-          s[r] = d;
-        else
-          ds[r >> 3][r & 7] = from_f32<T>(d);
+  // Zeros for the keys of tile t that are not finite.  A row that sees such a one, and has a finite log-sum all the same, has a score of -inf
+  // for it and no weight: with a key of zeros its weight is another, but what it adds is 0.
+  auto drop_odd_keys = [&](int t) {
+    const int thread = worked_out_here(threadIdx.x);
+    if (thread < TILE / 32) odd_keys[thread] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {
+#pragma unroll 1
+      for (int i = 0; i < NL; ++i) {
+        u32x4* at = reinterpret_cast<u32x4*>(smem + (t & 1) * STAGE + (i * THREADS + thread) * 16);
+        const u32x4 was = *at, is = finite_ones<T>(was);
+        const int row = i * RPP + thread / CPR;
+        if (turn) {
+          if ((odd_keys[row / 32] >> (row % 32)) & 1) *at = u32x4{0, 0, 0, 0};
+        } else if (was[0] != is[0] || was[1] != is[1] || was[2] != is[2] || was[3] != is[3]) {
+          atomicOr(&odd_keys[row / 32], 1u << (row % 32));
+        }
       }
-      if constexpr (LIFTS) {
-        lift.fit(s, acc);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) ds[r >> 3][r & 7] = from_f32<T>(s[r]);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, DP>(map, keys, c * 32 + h * 16, d), ds[h], acc[d]);
+      __syncthreads();
     }
+  };
+  auto sees_one_of = [&](int t) {
+    const Row seen = make_row<false>(p, e, worked_out_here(min(r0 + (lane & 31), rows - 1)));
+    bool sees = false;
+#pragma unroll 1
+    for (int i = 0; i < TILE; ++i) {
+      const int j = begin + t * TILE + i;
+      sees |= ((odd_keys[i / 32] >> (i % 32)) & 1) && j >= seen.lo && j < seen.hi;
+    }
+    return sees;
+  };
+  f32x16 acc[DT];
+  Lift lift(peak);
+  bool sees_odd = false, odd = false;
+  int pass = 0;  // from 1 on without keys that are not finite
+  for (;; ++pass) {
+    const float lifted = delta * lift.by;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
+    if (t0 < t1) request(begin, end, t0);
+    for (int t = t0; t < t1; ++t) {
+      wait_all_and_meet();
+      if (__builtin_expect(pass != 0, 0)) {
+        drop_odd_keys(t);
+        sees_odd |= sees_one_of(t);
+      }
+      if (t + 1 < t1) request(begin, end, t + 1);
+      const int first = begin + t * TILE + own;
+      if (first >= mine.hi || first + kTileKeys <= mine.lo) continue;
+      const unsigned keys = lds0 + (t & 1) * STAGE + own * (DP * 2), values = keys + 2 * STAGE;
+      const bool masked = first < mine.full_lo || first + kTileKeys > mine.full_hi;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        f32x16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, keys, c * 32, ks), q[ks], s);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, values, c * 32, ks), g[ks], dp);
+        const int base = first + c * 32 + 4 * half;
+        const float distance = (float)(at - base);
+        Frag ds[2];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int j = base + 8 * (r >> 2) + (r & 3);
+          float derivative = 1.0f, x;
+          if constexpr (FORM == FORM_PLAIN)
+            x = __builtin_fmaf(s[r], score.factor, -lse);
+          else
+            x = score(s[r], distance - (float)(8 * (r >> 2) + (r & 3)), derivative) - lse;
+          float d = exp2_fast(x) * (LIFTS ? __builtin_fmaf(dp[r], lift.by, -lifted) : dp[r] - delta) * derivative;
+          if (masked) d = (unsigned)(j - w.lo) < (unsigned)(w.hi - w.lo) ? d : 0.0f;
+          ds[r >> 3][r & 7] = from_f32<T>(d);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) acc[d] = mfma_op(col_frag<T, DP>(map, keys, c * 32 + h * 16, d), ds[h], acc[d]);
+      }
+    }
+    odd = !all_finite(acc) && __builtin_fabsf(delta) < __builtin_huge_valf() && __builtin_fabsf(lse) < __builtin_huge_valf();
+    if (__any(odd) && lane == 0) spoilt = pass + 1;
+    __syncthreads();
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(spoilt) <= pass, 1) || pass == (LIFTS ? 6 : 1)) break;
+    if (pass > 0) {  // (finite numbers whose dS fp16 does not hold)
+      const unsigned long long lanes = __ballot(odd);
+      if ((((unsigned)lanes | (unsigned)(lanes >> 32)) >> (lane & 31)) & 1) lift.by *= 0x1p-12f;
+    }
+  }
+  const bool again = pass != 0;
+  if (lse == __builtin_huge_valf()) {  // (nothing was seen, or scores of -inf alone)
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[d][r] = 0.0f;
   }
   const float by = unless_alone(w.hi - w.lo) / lift.by;
 #pragma unroll
@@ -495,25 +556,40 @@ __global__ __launch_bounds__(256 * PAIRS, 2) void dq_kernel(const BackArgs b) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[d][r] += meet[(d * 16 + r) * 64];
   }
-  if (b.dq_splits > 1) {
-    if (r0 + (lane & 31) < rows) store_part<DT>(dq_part<DP>(b, z, e, r0 + (lane & 31)), acc, half);
-    return;
+  const unsigned long long lanes = __ballot(odd && sees_odd);
+  const bool alone_again = again && ((((unsigned)lanes | (unsigned)(lanes >> 32)) >> (lane & 31)) & 1);
+  const bool real = r0 + (lane & 31) < rows;
+  if (real && !alone_again) {
+    if (b.dq_splits > 1)
+      store_part<DT>(dq_part<DP>(b, z, e, r0 + (lane & 31)), acc, half);
+    else
+      store_columns<T, DT>(reinterpret_cast<T*>(b.dq) + query_offset<false>(p, e, b.dqs, place_of_row(p, e, worked_out_here(r0 + (lane & 31)))), acc, half,
+                           p.dim, p.scale);
   }
-  const unsigned long long odd = __ballot(!all_finite(acc));
-  unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
-  if (r0 + (lane & 31) < rows && !((again >> (lane & 31)) & 1))
-    store_columns<T, DT>(reinterpret_cast<T*>(b.dq) + query_offset<false>(p, e, b.dqs, w), acc, half, p.dim, p.scale);
-  again = __builtin_amdgcn_readfirstlane(again);
-  while (again) {
-    const int i = __builtin_ctz(again);
-    again &= again - 1;
-    const float its = __shfl(delta, i);
-    if (r0 + i < rows) dq_by_definition<T, DP, FORM>(b, e, r0 + i, its);
+  if (__builtin_expect(!again, 1)) return;
+  unsigned left = __builtin_amdgcn_readfirstlane((unsigned)__ballot(real && alone_again));  // (the same in both halves)
+  while (left) {
+    constexpr int E = DP / 64;
+    const int i = __builtin_ctz(left);
+    left &= left - 1;
+    float row[E];
+    dq_by_definition<T, DP, FORM>(b, e, r0 + i, key_at<TILE>(begin, t0, 0, end), key_at<TILE>(begin, t1, 0, end), __shfl(delta, i), row);
+    const Row its = make_row<false>(p, e, r0 + i);
+    T* to = reinterpret_cast<T*>(b.dq) + query_offset<false>(p, e, b.dqs, its);
+    float* part = b.dq_splits > 1 ? dq_part<DP>(b, z, e, r0 + i) : nullptr;
+#pragma unroll
+    for (int u = 0; u < E; ++u) {
+      const int d = lane * E + u;
+      if (part)
+        part[d] = row[u];
+      else if (d < p.dim)
+        to[d] = from_f32<T>(row[u] * p.scale);
+    }
   }
 }
 
 // The splits of a query's sum, in ascending order; one wavefront a query.
-template <typename T, int DP, int FORM>
+template <typename T, int DP>
 __global__ __launch_bounds__(256) void dq_join_kernel(const BackArgs b) {
   constexpr int E = DP / 64;
   const Args& p = b.f;
@@ -531,14 +607,7 @@ __global__ __launch_bounds__(256) void dq_join_kernel(const BackArgs b) {
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] += from[i];
   }
-  bool finite = true;
-#pragma unroll
-  for (int i = 0; i < E; ++i) finite &= __builtin_fabsf(acc[i]) < __builtin_huge_valf();
-  const Row w = make_row<false>(p, e, r);
-  if (!__all(finite)) {
-    dq_by_definition<T, DP, FORM>(b, e, r, kLift * *row_info<FORM>(b, e, r, 1));
-    return;
-  }
+  const Row w = place_of_row(p, e, r);
   T* to = reinterpret_cast<T*>(b.dq) + query_offset<false>(p, e, b.dqs, w);
 #pragma unroll
   for (int i = 0; i < E; ++i)
@@ -564,7 +633,7 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   using Frag = typename Frag8<T>::type;
   __shared__ __attribute__((aligned(256))) unsigned char smem[4 * STAGE];  // q of two stages, dout of two
   __shared__ __attribute__((aligned(16))) unsigned char info[2 * INFO];
-  __shared__ int bounds[8][2];
+  __shared__ int bounds[8][3], spoilt;
   constexpr bool LIFTS = !std::is_same<T, bf16>::value;
   const Args& p = b.f;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -579,25 +648,30 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   const int block_key = tile * kBlockKeys, key0 = block_key + (wave & 1) * 32, key = key0 + (lane & 31);
   const int block_end = min(block_key + kBlockKeys, e.keys);
 
-  // the first and last groups of 32 rows that see a key of the block
+  // the first and last groups of 32 rows that see a key of the block, and the largest peak of such groups (as a whole number)
   const int groups = (rows + 31) >> 5;
   const int4* seen = b.seen + (long long)e.b * b.row_groups;
-  int from = 0x7fffffff, to = 0;
+  const float* peaks = b.peak + ((long long)e.b * p.kv_heads + e.kv) * b.row_groups;
+  int from = 0x7fffffff, to = 0, peak = 0;
   for (int i = tid; i < groups; i += kDkvThreads)
     if (seen[i].x < block_end && seen[i].y > block_key) {
       from = min(from, i);
       to = i + 1;
+      if constexpr (LIFTS) peak = max(peak, __builtin_bit_cast(int, peaks[i]));
     }
   from = wave_min(from);
   to = wave_max(to);
+  if constexpr (LIFTS) peak = wave_max(peak);
   if (lane == 0) {
     bounds[wave][0] = from;
     bounds[wave][1] = to;
+    bounds[wave][2] = peak;
   }
   Frag kf[KS], vf[KS];
   const int mine = min(key, e.keys - 1);
   load_row_frags<T, DP>(keys_of<T, false>(p, e, p.k, p.ks) + (long long)mine * p.ks.row, half, p.dim, kf);
   load_row_frags<T, DP>(keys_of<T, false>(p, e, p.v, p.vs) + (long long)mine * p.vs.row, half, p.dim, vf);
+  if (tid == 0) spoilt = 0;
   if (p.dim < DP)
     for (int i = tid; i < 4 * STAGE / 16; i += kDkvThreads) reinterpret_cast<u32x4*>(smem)[i] = u32x4{0, 0, 0, 0};
   __syncthreads();
@@ -605,7 +679,9 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
   for (int i = 0; i < 8; ++i) {
     from = min(from, bounds[i][0]);
     to = max(to, bounds[i][1]);
+    if constexpr (LIFTS) peak = max(peak, bounds[i][2]);
   }
+  Lift lift(LIFTS ? __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(peak)) : 0.0f);
   from = __builtin_amdgcn_readfirstlane(from);
   to = __builtin_amdgcn_readfirstlane(to);
   const int first_tile = from < to ? from >> 2 : 0, last_tile = from < to ? (to + 3) >> 2 : 0;
@@ -648,14 +724,6 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
     }
   };
 
-  f32x16 acc[SUMS][DT];  // dK, dV or both, transposed: lane = key
-#pragma unroll
-  for (int i = 0; i < SUMS; ++i)
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
-  Lift lift;
   const Score<FORM> all_scores(p, 0.0f);
   // (which groups of 32 rows take part: asked for a tile ahead, and in scalar registers before the next tile's loads are under way, for
   // which the compiler would otherwise wait)
@@ -663,138 +731,160 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
     return int4{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z),
                 __builtin_amdgcn_readfirstlane(v.w)};
   };
-  int4 next0 = {0, 0, 0, 0}, next1 = next0;
-  if (t0 < t1) {  // (without queries there is no list of them)
-    next0 = seen[min(4 * t0 + part, groups - 1)];
-    next1 = seen[min(4 * t0 + part + GROUPS - 1, groups - 1)];
-  }
-  settle();
-  if (t0 < t1) request(t0);
-  for (int t = t0; t < t1; ++t) {
-    wait_all_and_meet();
-    const int4 seen0 = in_scalars(next0), seen1 = in_scalars(next1);
-    if (t + 1 < t1) {
-      request(t + 1);
-      next0 = seen[min(4 * t + 4 + part, groups - 1)];
-      next1 = seen[min(4 * t + 4 + part + GROUPS - 1, groups - 1)];
+  f32x16 acc[SUMS][DT];  // dK, dV or both, transposed: lane = key
+  bool again = false;
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < SUMS; ++i)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][d][r] = 0.0f;
+    int4 next0 = {0, 0, 0, 0}, next1 = next0;
+    if (t0 < t1) {  // (without queries there is no list of them)
+      next0 = seen[min(4 * t0 + part, groups - 1)];
+      next1 = seen[min(4 * t0 + part + GROUPS - 1, groups - 1)];
     }
-    const unsigned qs = lds0 + (t & 1) * STAGE, gs = qs + 2 * STAGE;
-    const float* of_rows = reinterpret_cast<const float*>(info + (t & 1) * INFO);
-#pragma unroll 1
-    for (int c = 0; c < GROUPS; ++c) {
-      const int row = (part + c) * 32, behind = t * kTileRows + row + 32;
-      if ((c ? seen1.x : seen0.x) >= key0 + 32 || (c ? seen1.y : seen0.y) <= key0 || behind - 32 >= rows) continue;
-      const bool masked = (c ? seen1.z : seen0.z) > key0 || (c ? seen1.w : seen0.w) < key0 + 32 || behind > rows;
-      f32x16 s, dp;
-      Frag gcol[BOTH ? 4 : 1], qcol[BOTH ? 4 : 1];
-      if constexpr (BOTH) {
-        // (one workgroup to a compute unit: what a wavefront reads from LDS is asked for well before its products, which the scheduler
-        // does not do of itself; 24 heads over 1449 keys 89 to 84 us)
-        Frag a[KS], g[KS];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) a[ks] = row_frag<T, DP>(map, qs, row, ks);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) g[ks] = row_frag<T, DP>(map, gs, row, ks);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma_op(a[ks], kf[ks], s);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) dp = mfma_op(g[ks], vf[ks], dp);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) qcol[i] = col_frag<T, DP>(map, qs, row + (i / DT) * 16, i % DT);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) gcol[i] = col_frag<T, DP>(map, gs, row + (i / DT) * 16, i % DT);
-        __builtin_amdgcn_sched_barrier(0);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.0f;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, qs, row, ks), kf[ks], s);
-        if (!for_dv) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, gs, row, ks), vf[ks], dp);
-        }
+    settle();
+    if (t0 < t1) request(t0);
+    for (int t = t0; t < t1; ++t) {
+      wait_all_and_meet();
+      if (__builtin_expect(again, 0)) {
+        keep_finite<T, kDkvThreads, NL>(smem + (t & 1) * STAGE);
+        keep_finite<T, kDkvThreads, NL>(smem + (t & 1) * STAGE + 2 * STAGE);
+        __syncthreads();
       }
-      Score<FORM> score = all_scores;
-      float derivative[16];
+      const int4 seen0 = in_scalars(next0), seen1 = in_scalars(next1);
+      if (t + 1 < t1) {
+        request(t + 1);
+        next0 = seen[min(4 * t + 4 + part, groups - 1)];
+        next1 = seen[min(4 * t + 4 + part + GROUPS - 1, groups - 1)];
+      }
+      const unsigned qs = lds0 + (t & 1) * STAGE, gs = qs + 2 * STAGE;
+      const float* of_rows = reinterpret_cast<const float*>(info + (t & 1) * INFO);
+#pragma unroll 1
+      for (int c = 0; c < GROUPS; ++c) {
+        const int row = (part + c) * 32, behind = t * kTileRows + row + 32;
+        if ((c ? seen1.x : seen0.x) >= key0 + 32 || (c ? seen1.y : seen0.y) <= key0 || behind - 32 >= rows) continue;
+        const bool masked = (c ? seen1.z : seen0.z) > key0 || (c ? seen1.w : seen0.w) < key0 + 32 || behind > rows;
+        f32x16 s, dp;
+        Frag gcol[BOTH ? 4 : 1], qcol[BOTH ? 4 : 1];
+        if constexpr (BOTH) {
+          // (one workgroup to a compute unit: what a wavefront reads from LDS is asked for well before its products, which the scheduler
+          // does not do of itself; 24 heads over 1449 keys 89 to 84 us)
+          Frag a[KS], g[KS];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {  // P
-        const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
-        const f32x4 lse = *reinterpret_cast<const f32x4*>(quad);
-        f32x4 slope = {0, 0, 0, 0};
-        int4 at = {0, 0, 0, 0};
-        if constexpr (FORM & FORM_BIAS) {
-          at = *reinterpret_cast<const int4*>(quad + 16);
-          slope = *reinterpret_cast<const f32x4*>(quad + 20);
-        }
-        const int at4[4] = {at.x, at.y, at.z, at.w};
+          for (int ks = 0; ks < KS; ++ks) a[ks] = row_frag<T, DP>(map, qs, row, ks);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int r = 4 * g + u;
-          if constexpr (FORM == FORM_PLAIN) {
-            s[r] = exp2_fast(__builtin_fmaf(s[r], score.factor, -lse[u]));
-          } else {
-            score.slope = slope[u];
-            s[r] = exp2_fast(score(s[r], (float)(at4[u] - key), derivative[r]) - lse[u]);
+          for (int ks = 0; ks < KS; ++ks) g[ks] = row_frag<T, DP>(map, gs, row, ks);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) s = mfma_op(a[ks], kf[ks], s);
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) dp = mfma_op(g[ks], vf[ks], dp);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qcol[i] = col_frag<T, DP>(map, qs, row + (i / DT) * 16, i % DT);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) gcol[i] = col_frag<T, DP>(map, gs, row + (i / DT) * 16, i % DT);
+          __builtin_amdgcn_sched_barrier(0);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) s = mfma_op(row_frag<T, DP>(map, qs, row, ks), kf[ks], s);
+          if (!for_dv) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) dp = mfma_op(row_frag<T, DP>(map, gs, row, ks), vf[ks], dp);
           }
         }
-      }
-      if (!for_dv) {
+        Score<FORM> score = all_scores;
+        float derivative[16];
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {  // dS
-          const f32x4 delta = *reinterpret_cast<const f32x4*>(of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4) + 4);
+        for (int g = 0; g < 4; ++g) {  // P
+          const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
+          const f32x4 lse = *reinterpret_cast<const f32x4*>(quad);
+          f32x4 slope = {0, 0, 0, 0};
+          int4 at = {0, 0, 0, 0};
+          if constexpr (FORM & FORM_BIAS) {
+            at = *reinterpret_cast<const int4*>(quad + 16);
+            slope = *reinterpret_cast<const f32x4*>(quad + 20);
+          }
+          const int at4[4] = {at.x, at.y, at.z, at.w};
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int r = 4 * g + u;
-            dp[r] = __builtin_fmaf(dp[r], 1.0f / kLift, -delta[u]);
-            if constexpr (LIFTS) dp[r] *= lift.by;
-            dp[r] *= s[r];
-            if constexpr (FORM & FORM_CAP) dp[r] *= derivative[r];
+            if constexpr (FORM == FORM_PLAIN) {
+              s[r] = exp2_fast(__builtin_fmaf(s[r], score.factor, -lse[u]));
+            } else {
+              score.slope = slope[u];
+              s[r] = exp2_fast(score(s[r], (float)(at4[u] - key), derivative[r]) - lse[u]);
+            }
           }
         }
-      }
-      if (!BOTH && !for_dv) s = dp;
-      if (masked) {
+        if (!for_dv) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
-          const int4 first = *reinterpret_cast<const int4*>(quad + 8), count = *reinterpret_cast<const int4*>(quad + 12);
-          const int f4[4] = {first.x, first.y, first.z, first.w}, c4[4] = {count.x, count.y, count.z, count.w};
+          for (int g = 0; g < 4; ++g) {  // dS
+            const f32x4 delta = *reinterpret_cast<const f32x4*>(of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4) + 4);
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const bool in = (unsigned)(key - f4[u]) < (unsigned)c4[u];
-            // (a row that sees one key has no whole tile, and comes by here)
-            const float by = for_dv ? 1.0f : unless_alone(c4[u]);
-            s[4 * g + u] = in ? (BOTH ? s[4 * g + u] : s[4 * g + u] * by) : 0.0f;
-            if constexpr (BOTH) dp[4 * g + u] = in ? dp[4 * g + u] * by : 0.0f;
+            for (int u = 0; u < 4; ++u) {
+              const int r = 4 * g + u;
+              dp[r] = __builtin_fmaf(dp[r], 1.0f / kLift, -delta[u]);
+              if constexpr (LIFTS) dp[r] *= lift.by;
+              dp[r] *= s[r];
+              if constexpr (FORM & FORM_CAP) dp[r] *= derivative[r];
+            }
           }
         }
-      }
-      if constexpr (LIFTS)
-        if (!for_dv) lift.fit(BOTH ? dp : s, acc[0]);
-      Frag w[SUMS][2];  // both: dS, P
+        if (!BOTH && !for_dv) s = dp;
+        if (masked) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        w[0][r >> 3][r & 7] = from_f32<T>(BOTH ? dp[r] : s[r]);
-        if constexpr (BOTH) w[SUMS - 1][r >> 3][r & 7] = from_f32<T>(s[r]);
-      }
-      const unsigned from_rows = for_dv ? gs : qs;
+          for (int g = 0; g < 4; ++g) {
+            const float* quad = of_rows + (row / 4 + 2 * g + half) * (FIELDS * 4);
+            const int4 first = *reinterpret_cast<const int4*>(quad + 8), count = *reinterpret_cast<const int4*>(quad + 12);
+            const int f4[4] = {first.x, first.y, first.z, first.w}, c4[4] = {count.x, count.y, count.z, count.w};
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          if constexpr (BOTH) {
-            acc[0][d] = mfma_op(qcol[h * DT + d], w[0][h], acc[0][d]);
-            acc[SUMS - 1][d] = mfma_op(gcol[h * DT + d], w[SUMS - 1][h], acc[SUMS - 1][d]);
-          } else {
-            acc[0][d] = mfma_op(col_frag<T, DP>(map, from_rows, row + h * 16, d), w[0][h], acc[0][d]);
+            for (int u = 0; u < 4; ++u) {
+              const bool in = (unsigned)(key - f4[u]) < (unsigned)c4[u];
+              // (a row that sees one key has no whole tile, and comes by here)
+              const float by = for_dv ? 1.0f : unless_alone(c4[u]);
+              s[4 * g + u] = in ? (BOTH ? s[4 * g + u] : s[4 * g + u] * by) : 0.0f;
+              if constexpr (BOTH) dp[4 * g + u] = in ? dp[4 * g + u] * by : 0.0f;
+            }
           }
         }
+        if constexpr (LIFTS)
+          if (__builtin_expect(again, 0) && !for_dv) lift.fit(BOTH ? dp : s, acc[0]);
+        Frag w[SUMS][2];  // both: dS, P
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          w[0][r >> 3][r & 7] = from_f32<T>(BOTH ? dp[r] : s[r]);
+          if constexpr (BOTH) w[SUMS - 1][r >> 3][r & 7] = from_f32<T>(s[r]);
+        }
+        const unsigned from_rows = for_dv ? gs : qs;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            if constexpr (BOTH) {
+              acc[0][d] = mfma_op(qcol[h * DT + d], w[0][h], acc[0][d]);
+              acc[SUMS - 1][d] = mfma_op(gcol[h * DT + d], w[SUMS - 1][h], acc[SUMS - 1][d]);
+            } else {
+              acc[0][d] = mfma_op(col_frag<T, DP>(map, from_rows, row + h * 16, d), w[0][h], acc[0][d]);
+            }
+          }
+      }
     }
+    if (again) break;
+    bool finite = all_finite(acc[0]);
+    if constexpr (BOTH) finite &= all_finite(acc[SUMS - 1]);
+    if (!__all(finite) && lane == 0) spoilt = 1;
+    __syncthreads();
+    again = __builtin_amdgcn_readfirstlane(spoilt);
+    if (__builtin_expect(!again, 1)) break;
   }
   if (LIFTS && !for_dv) {
     const float by = 1.0f / lift.by;
@@ -837,26 +927,29 @@ __global__ __launch_bounds__(kDkvThreads, 2) void dkv_kernel(const BackArgs b) {
 #pragma unroll
   for (int i = 0; i < SUMS; ++i) {
     const bool is_dv = for_dv || i == 1;
-    if (b.dkv_splits > 1) {
-      if (key < e.keys) store_part<DT>(dkv_part<DP>(b, z, e, key) + (is_dv ? DP : 0), acc[i], half);
-      continue;
+    if (__builtin_expect(again && is_dv, 0)) {
+      // (a key that is not finite has a weight of 0 here, or all its rows are NaN)
+      bool odd_key = false;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) odd_key |= !(__builtin_fabsf(to_f32(kf[ks][u])) < __builtin_huge_valf());
+      odd_key |= __shfl_xor((int)odd_key, 32);
+      settle_odd<DP>(acc[i], odd_gradients<T, DP, FORM>(b, e, key, t0 * kTileRows, min(t1 * kTileRows, rows), key < e.keys && !odd_key), half);
     }
-    const unsigned long long odd = __ballot(!all_finite(acc[i]));
-    unsigned again = (unsigned)odd | (unsigned)(odd >> 32);
-    const Strides& to_s = is_dv ? b.dvs : b.dks;
-    T* out = reinterpret_cast<T*>(is_dv ? b.dv : b.dk) + (long long)e.b * to_s.batch + (long long)e.kv * to_s.head + (long long)key * to_s.row;
-    if (key < e.keys && !((again >> (lane & 31)) & 1)) store_columns<T, DT>(out, acc[i], half, p.dim, is_dv ? 1.0f / kLift : p.scale);
-    again = __builtin_amdgcn_readfirstlane(again);
-    while (again) {
-      const int at = __builtin_ctz(again);
-      again &= again - 1;
-      if (key0 + at < e.keys) dkv_by_definition<T, DP, FORM>(b, e, key0 + at, is_dv);
+    if (key >= e.keys) continue;
+    if (b.dkv_splits > 1) {
+      store_part<DT>(dkv_part<DP>(b, z, e, key) + (is_dv ? DP : 0), acc[i], half);
+    } else {
+      const Strides& to_s = is_dv ? b.dvs : b.dks;
+      T* out = reinterpret_cast<T*>(is_dv ? b.dv : b.dk) + (long long)e.b * to_s.batch + (long long)e.kv * to_s.head + (long long)key * to_s.row;
+      store_columns<T, DT>(out, acc[i], half, p.dim, is_dv ? 1.0f / kLift : p.scale);
     }
   }
 }
 
 // The splits of a key's two sums, in ascending order; one wavefront a key.
-template <typename T, int DP, int FORM>
+template <typename T, int DP>
 __global__ __launch_bounds__(256) void dkv_join_kernel(const BackArgs b) {
   constexpr int E = DP / 64;
   const Args& p = b.f;
@@ -876,14 +969,6 @@ __global__ __launch_bounds__(256) void dkv_join_kernel(const BackArgs b) {
       dk[i] += from[i];
       dv[i] += from[DP + i];
     }
-  }
-  bool finite = true;
-#pragma unroll
-  for (int i = 0; i < E; ++i) finite &= __builtin_fabsf(dk[i]) < __builtin_huge_valf() && __builtin_fabsf(dv[i]) < __builtin_huge_valf();
-  if (!__all(finite)) {
-    dkv_by_definition<T, DP, FORM>(b, e, key, false);
-    dkv_by_definition<T, DP, FORM>(b, e, key, true);
-    return;
   }
   T* to_k = reinterpret_cast<T*>(b.dk) + (long long)e.b * b.dks.batch + (long long)e.kv * b.dks.head + (long long)key * b.dks.row;
   T* to_v = reinterpret_cast<T*>(b.dv) + (long long)e.b * b.dvs.batch + (long long)e.kv * b.dvs.head + (long long)key * b.dvs.row;
@@ -908,7 +993,7 @@ hipError_t launch(const BackArgs& b, hipStream_t stream) {
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (b.dq_splits > 1) {
       const long long rows = entries * p.seq_q * p.group;
-      hipLaunchKernelGGL((dq_join_kernel<T, DP, FORM>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, b);
+      hipLaunchKernelGGL((dq_join_kernel<T, DP>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, b);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
   }
@@ -916,7 +1001,7 @@ hipError_t launch(const BackArgs& b, hipStream_t stream) {
     hipLaunchKernelGGL((dkv_kernel<T, DP, FORM>), dim3((unsigned)(entries * b.key_tiles * b.dkv_splits)), dim3(kDkvThreads), 0, stream, b);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (b.dkv_splits > 1) {
-      hipLaunchKernelGGL((dkv_join_kernel<T, DP, FORM>), dim3((unsigned)((entries * p.seq_k + 3) / 4)), dim3(256), 0, stream, b);
+      hipLaunchKernelGGL((dkv_join_kernel<T, DP>), dim3((unsigned)((entries * p.seq_k + 3) / 4)), dim3(256), 0, stream, b);
       return hipGetLastError();
     }
   }
@@ -939,6 +1024,7 @@ hipError_t dispatch(int form, const BackArgs& b, hipStream_t stream) {
 
 long long row_groups_of(long long rows) { return (rows + 31) / 32; }
 long long order_bytes(long long batch, long long key_tiles) { return (batch * key_tiles * 4 + 15) / 16 * 16; }
+long long peak_bytes(long long entries, long long row_groups) { return (entries * row_groups * 4 + 15) / 16 * 16; }
 // (of all forms: with a bias twice the fields)
 long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
 
@@ -988,7 +1074,8 @@ int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, i
   if (group >= kMaxRows || seq_q >= kMaxRows || seq_k >= kMaxRows || !fits_cut(batch, kv_heads, seq_q * group, seq_k)) return 0;
   const BackCut c = cut_backward(batch * kv_heads, seq_q * group, seq_k, padded_dim(head_dim));
   const long long row_groups = row_groups_of(seq_q * group);
-  return info_bytes(batch * kv_heads, seq_q * group) + batch * row_groups * 16 + order_bytes(batch, c.key_tiles) + c.part_bytes;
+  return info_bytes(batch * kv_heads, seq_q * group) + peak_bytes(batch * kv_heads, row_groups) + batch * row_groups * 16 +
+         order_bytes(batch, c.key_tiles) + c.part_bytes;
 }
 
 hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t heads, int64_t kv_heads, int64_t seq_q, int64_t seq_k,
@@ -1035,7 +1122,9 @@ hidet_status_t hidet_attention_backward(int32_t dtype, int64_t batch, int64_t he
     b.dq = grad_q->data;
     b.dqs = strides_of(grad_q);
     b.info = static_cast<float*>(workspace);
-    b.seen = reinterpret_cast<int4*>(static_cast<char*>(workspace) + info_bytes(batch * kv_heads, seq_q * group));
+    char* peak = static_cast<char*>(workspace) + info_bytes(batch * kv_heads, seq_q * group);
+    b.peak = reinterpret_cast<float*>(peak);
+    b.seen = reinterpret_cast<int4*>(peak + peak_bytes(batch * kv_heads, row_groups_of(seq_q * group)));
   }
   if (seq_k > 0) {
     p.k = k->data;

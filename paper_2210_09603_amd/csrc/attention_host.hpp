@@ -51,7 +51,8 @@ inline hidet_status_t check_options(const hidet_attention_options_t* o) {
     return HIDET_ERR_INVALID_ARG;
   if (o->ranges && (o->causal || o->window)) return HIDET_ERR_INVALID_ARG;
   // (factors of a product, as Score takes them)
-  if (!std::isfinite(2.0f * kLog2e * o->scale) || (o->softcap > 0 && !std::isfinite(2.0f * kLog2e * o->scale / o->softcap))) return HIDET_ERR_UNSUPPORTED;
+  const float factor = 2.0f * kLog2e * o->scale;
+  if (!std::isfinite(factor) || (o->softcap > 0 && !std::isfinite(factor / o->softcap))) return HIDET_ERR_UNSUPPORTED;
   if (!is_aligned(o->slopes, 4) || !is_aligned(o->ranges, 4)) return HIDET_ERR_ALIGNMENT;
   return HIDET_OK;
 }

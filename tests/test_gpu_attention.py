@@ -519,6 +519,139 @@ def test_scores_that_are_not_finite_and_values_beside_them():
             k[0, 0] = -np.inf
             hb.hidet_attention(q, k, v, out, lse=lse)
             assert not out[0, 0].any() and bool((lse[0, 0] == -np.inf).all())
+            q[0, 1, n // 2] = np.nan  # (all scores NaN, none of which makes a maximum)
+            k[0, 1] = plain[0][0, 0]
+            hb.hidet_attention(q, k, v, out, lse=lse)
+            assert bool(torch.isnan(out[0, 1, n // 2]).all()) and bool(torch.isnan(lse[0, 1, n // 2]))
+            assert bool(torch.isfinite(lse[0, 1, torch.arange(n) != n // 2]).all())
+
+
+BACK_SIZES = [(1, 4, 2, 300, 300, 64), (2, 2, 1, 200, 260, 128), (1, 3, 1, 70, 700, 40), (1, 2, 1, 90, 3000, 128), (1, 4, 2, 900, 70, 64), (86, 12, 6, 19, 193, 112)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("size", BACK_SIZES, ids=str)
+@pytest.mark.parametrize("mask", ["causal", "window", "ranges"])
+def test_gradients_of_what_is_not_finite_spoil_what_it_reaches_alone(mask, size, dtype):
+    """Infinities and NaN in the gradient of the output, queries, keys, values: a query that has or sees one has a gradient that is not finite,
+    and so have the keys that it sees; dV where the gradient of the output has it is the sum of those (NaN where a weight is).  All
+    else has the bits that it has without them (dK in fp16 two roundings, as the scale of dS in a block of keys may be another)."""
+    b, h, hk, n, m, d = size
+    g = np.random.Generator(np.random.PCG64(83))
+    q, dout = (_draw(g, (b, h, n, d), dtype, "dense") for _ in range(2))
+    k, v = (_draw(g, (b, hk, m, d), dtype, "tokens") for _ in range(2))
+    if mask == "ranges":
+        lo = g.integers(0, m, (b, n))
+        r = np.stack([lo, np.minimum(m, lo + g.integers(0, m, (b, n)))], 2).astype(np.int32)
+        see, opts = np.stack([oa.in_ranges(x, m) for x in r]), dict(ranges=torch.from_numpy(r).cuda())
+    else:
+        opts = dict(causal=True, window=60 if mask == "window" else 0)
+        see = np.stack([oa.sees(n, m, **opts)] * b)
+    see = np.repeat(see[:, None], h, 1)  # [b, h, n, m]
+    group = h // hk
+
+    def forward(q, k, v):
+        out, lse = torch.full_like(q, 7.0), torch.empty(b, h, n, device="cuda")
+        hb.hidet_attention(q, k, v, out, lse=lse, **opts)
+        return out, lse
+
+    def run(q, k, v, dout, out, lse):
+        dq, dk, dv = (torch.full_like(t, 7.0) for t in (q, k, v))
+        ws = torch.full((hb.hidet_attention_backward_workspace_bytes(q, k) // 4,), float("nan"), device="cuda")
+        hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, **opts)
+        return dq, dk, dv
+
+    out, lse = forward(q, k, v)
+    clean = run(q, k, v, dout, out, lse)
+    for which in range(4):
+        for count in (1, 5):
+            x = [t.clone() for t in (q, k, v, dout)]
+            places = _scatter(g, x[which].shape, count)
+            if which < 2:  # (an infinite query or key may leave scores of -inf, and no weight)
+                places = [(at, np.nan) for at, _ in places]
+            for at, value in places:
+                x[which][at] = value
+            row = np.zeros((b, h, n), bool)  # (rows of which the log-sum or D is not finite)
+            for (bb, hh, i, _), _ in places:
+                if which in (0, 3):
+                    row[bb, hh, i] |= see[bb, hh, i].any()
+                else:
+                    row[bb, hh * group:(hh + 1) * group] |= see[bb, hh * group:(hh + 1) * group, :, i]
+            key = np.einsum("bhn,bhnm->bhm", row, see).reshape(b, hk, group, m).any(2)
+            row, key = (torch.from_numpy(t).cuda()[..., None] for t in (row, key))
+            # (outputs of the other rows as they are without: maxima are replaced for 32 rows at a time, which moves their last bits)
+            odd_out, odd_lse = forward(*x[:3])
+            dq, dk, dv = run(*x, torch.where(row, odd_out, out), torch.where(row[..., 0], odd_lse, lse))
+            bits = lambda t: torch.nan_to_num(t, 11.0, 12.0, 13.0)
+            what = "%s %s" % (("q", "k", "v", "grad_out")[which], count)
+            assert not bool((torch.isfinite(dq) & row).any()) and not bool((torch.isfinite(dk) & key).any()), what
+            assert torch.equal(torch.where(row, clean[0], dq), clean[0]), what + " dq"
+            rest = torch.where(key, clean[1], dk)
+            if dtype == "bf16":
+                assert torch.equal(rest, clean[1]), what + " dk"
+            else:
+                assert_within(rest, f64(clean[1]), 2.0 ** -10 * np.abs(f64(clean[1])) * 1.01 + 2.0 ** -24, what + " dk")
+            if which < 2:
+                assert bool((torch.isnan(dv) | ~key).all()) and torch.equal(torch.where(key, clean[2], dv), clean[2]), what + " dv"
+            elif which == 2:
+                assert torch.equal(dv, clean[2]), what + " dv"
+            else:
+                sums = np.zeros((b, hk, m, d))
+                with np.errstate(invalid="ignore"):
+                    for (bb, hh, i, dd), value in dict(places).items():
+                        sums[bb, hh // group, see[bb, hh, i], dd] += value
+                want = torch.where(torch.from_numpy(sums != 0.0).cuda(), torch.from_numpy(sums).cuda().to(dv.dtype), clean[2])
+                assert torch.equal(bits(dv), bits(want)), what + " dv"
+
+
+def test_gradients_of_keys_of_score_minus_infinity():
+    """Keys of -inf under queries that are positive have no weight, and neither they nor their values reach a gradient; their own are 0."""
+    for dtype in ("f16", "bf16"):
+        for n, d, level in ((70, 64, 0.0), (200, 128, 0.0), (40, 24, 0.0), (90, 64, -30.0), (700, 128, -30.0)):  # (scores of -200)
+            g = np.random.Generator(np.random.PCG64(84))
+            q, dout = (_draw(g, (1, 2, n, d), dtype, "dense") for _ in range(2))
+            k, v = (_draw(g, (1, 1, 3 * n, d), dtype, "dense") for _ in range(2))
+            q = q.abs() + 0.1
+            k = k + level
+            masked = torch.zeros(3 * n, dtype=torch.bool)
+            masked[::7] = True
+            kk = k.clone()
+            kk[:, :, masked.cuda()] = -np.inf
+            out, dq, dk, dv = (torch.full_like(t, 7.0) for t in (q, q, k, v))
+            lse = torch.empty(1, 2, n, device="cuda")
+            hb.hidet_attention(q, kk, v, out, lse=lse, causal=True)
+            ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+            hb.hidet_attention_backward(dout, q, kk, v, out, lse, dq, dk, dv, ws, causal=True)
+            see = (oa.sees(n, 3 * n, True) & ~masked.numpy()[None])[None]
+            want, bound = bounds(dtype, f64(q), f64(k), f64(v), see, d ** -0.5, grad_out=f64(dout))
+            for name, t, x, e in zip(("out", "lse", "dq", "dk", "dv"), (out, lse, dq, dk, dv), want, bound):
+                assert_within(t, x, e, "%s %d %s" % (dtype, n, name))
+            assert not dk[:, :, masked.cuda()].any() and not dv[:, :, masked.cuda()].any()
+
+
+@pytest.mark.parametrize("dim", [64, 128, 40])
+@pytest.mark.parametrize("h,n,m", [(2, 40, 40), (4, 300, 300), (2, 70, 2000)])
+def test_fp16_gradients_of_values_that_cancel_in_the_output(h, n, m, dim):
+    """Large values of either sign, with nearly equal weights: the output says nothing of how large dS is, which passes fp16 (some 1e6)."""
+    g = np.random.Generator(np.random.PCG64(85))
+    q, dout = (_draw(g, (1, h, n, dim), "f16", "dense") for _ in range(2))
+    k, v = (_draw(g, (1, h // 2, m, dim), "f16", "dense") for _ in range(2))
+    q.mul_(0.01)
+    dout.mul_(100.0)
+    v = (30000.0 + 0 * v) * torch.where(torch.arange(m, device="cuda") % 2 == 0, 1.0, -1.0).half()[None, None, :, None]
+    ranges = torch.tensor([[2 * (i % (m // 2)), 2 * (i % (m // 2)) + 2] for i in range(n)], dtype=torch.int32, device="cuda")[None]
+    out, dq, dk, dv = (torch.full_like(t, 7.0) for t in (q, q, k, v))
+    lse = torch.empty(1, h, n, device="cuda")
+    hb.hidet_attention(q, k, v, out, lse=lse, ranges=ranges)
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(q, k) // 4, device="cuda")
+    hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, ranges=ranges, scale=None)
+    see = np.stack([oa.in_ranges(ranges[0].cpu().numpy(), m)])
+    want, bound = bounds("f16", f64(q), f64(k), f64(v), see, dim ** -0.5, grad_out=f64(dout), few=True)
+    for name, t, x, e in zip(("dq", "dk", "dv"), (dq, dk, dv), want[2:], bound[2:]):
+        fits = np.abs(x) < 60000.0
+        got = f64(t)
+        assert np.all(np.isinf(got[np.abs(x) > 66000.0]))
+        assert_within(np.where(fits, got, 0.0), np.where(fits, x, 0.0), e + 1e-30, name)
 
 
 def _time(f):
@@ -548,6 +681,29 @@ def test_what_is_not_finite_costs_a_few_times_the_time(dtype, dim):
             took = _time(lambda: hb.hidet_attention(q, k, odd, out, lse=lse, causal=True))
             print("%s %s: %.1f times" % (name, x, took / clean), flush=True)
             assert took <= 40 * clean, name
+
+
+@pytest.mark.parametrize("dtype,dim", [("f16", 64), ("bf16", 128)])
+def test_gradients_of_what_is_not_finite_cost_a_few_times_the_time(dtype, dim):
+    """Of a causal prompt of 2048: one element of a tensor, one in every vector, all of them; measured 1 to 6 times the time, here up to 30."""
+    n = 2048
+    x = [torch.randn(1, heads, n, dim, device="cuda").to(TYPES[dtype]) for heads in (8, 4, 4, 8)]
+    out, dq, dk, dv = (torch.empty_like(x[i]) for i in (0, 0, 1, 2))
+    lse = torch.empty(1, 8, n, device="cuda")
+    ws = torch.empty(hb.hidet_attention_backward_workspace_bytes(x[0], x[1]) // 4, device="cuda")
+
+    def run(q, k, v, dout):
+        hb.hidet_attention(q, k, v, out, lse=lse, causal=True)
+        return _time(lambda: hb.hidet_attention_backward(dout, q, k, v, out, lse, dq, dk, dv, ws, causal=True))
+
+    clean = run(*x)
+    for i, name in enumerate(("q", "k", "v", "grad_out")):
+        for at in ((0, 1, 100, 5), (0, 1, n - 1, 5), (slice(None), slice(None), slice(None), 5), Ellipsis):
+            odd = [t.clone() for t in x]
+            odd[i][at] = np.inf
+            took = run(*odd)
+            print("%s %s: %.1f times" % (name, at, took / clean), flush=True)
+            assert took <= 30 * clean, name
 
 
 def test_large_scores_and_flat_ones():
