@@ -478,10 +478,10 @@ int64_t hidet_attention_backward_workspace_bytes(int64_t batch, int64_t heads, i
  *   (a, b) -> amplitude * (a cos t - b sin t, b cos t + a sin t),   t = position * frequencies[j], negated if inverse,
  * where pair j is elements (j, j + rotary_dim / 2), or (2 j, 2 j + 1) if interleaved; the rest of a vector is copied.  inverse is
  * the backward pass: the gradient of x from that of y, with the same amplitude.
- * x and y are [batch][heads][seq][head_dim] of dtype (any of the three), given as for hidet_attention; y may be x itself (the same
- * strides), no other overlap.  frequencies: DEVICE, fp64 [rotary_dim / 2].  Position of token s of batch entry b:
- * positions[b * positions_stride + s] (DEVICE, int32), or first_position + s if positions is NULL.  Angles are reduced in fp64:
- * positions up to 2^31 keep theirs to 2^-22 of a turn.
+ * x and y are [batch][heads][seq][head_dim] of dtype (any of the three), given as for hidet_attention; y may be x itself (with
+ * the same strides, else HIDET_ERR_INVALID_ARG), no other overlap.  frequencies: DEVICE, fp64 [rotary_dim / 2].  Position of token s of
+ * batch entry b: positions[b * positions_stride + s] (DEVICE, int32), or first_position + s if positions is NULL.  Angles are reduced
+ * in fp64: positions up to 2^31 keep theirs to 2^-22 of a turn.
  * batch, heads or seq of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: head_dim above 4096, 2^29 tokens, 2^20 heads.
  */
 hidet_status_t hidet_rope(int32_t dtype, int64_t batch, int64_t heads, int64_t seq, int64_t head_dim, int64_t rotary_dim,

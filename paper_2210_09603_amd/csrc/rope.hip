@@ -179,6 +179,10 @@ hidet_status_t hidet_rope(int32_t dtype, int64_t batch, int64_t heads, int64_t s
   if (hidet_status_t st = check_heads(x, batch, heads, seq, head_dim, false); st != HIDET_OK) return st;
   if (hidet_status_t st = check_heads(y, batch, heads, seq, head_dim, true); st != HIDET_OK) return st;
   if (!is_aligned(x->data, es) || !is_aligned(y->data, es) || !is_aligned(frequencies, 8) || !is_aligned(positions, 4)) return HIDET_ERR_ALIGNMENT;
+  const bool in_place = x->data == y->data;
+  if (in_place)  // (every element is written where it was read, and what is not turned is left)
+    if ((batch > 1 && x->stride_batch != y->stride_batch) || (heads > 1 && x->stride_head != y->stride_head) || (seq > 1 && x->stride_row != y->stride_row))
+      return HIDET_ERR_INVALID_ARG;
   RopeArgs p{};
   p.x = x->data;
   p.y = y->data;
@@ -195,7 +199,6 @@ hidet_status_t hidet_rope(int32_t dtype, int64_t batch, int64_t heads, int64_t s
   p.tokens = (int)(batch * seq);
   const int vec = 16 / (int)es, pairs = p.rotary / 2;
   p.turn_items = ((interleaved ? p.rotary : pairs) + vec - 1) / vec;
-  const bool in_place = x->data == y->data;
   p.copy_items = in_place ? 0 : (p.dim - p.rotary + vec - 1) / vec;
   p.inverse = inverse;
   p.amplitude = amplitude;

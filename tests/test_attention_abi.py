@@ -251,3 +251,12 @@ def test_sizes_at_and_beyond_the_limits_are_answered():
 def test_factors_that_pass_fp32_are_refused(call):
     for o in (dict(softcap=1e-39), dict(scale=2e38), dict(scale=-2e38), dict(scale=1e20, softcap=1e-19), dict(scale=1e38, softcap=0.5)):
         assert call(o=options(**o)) == UNSUPPORTED, o
+
+
+def test_rope_in_place_under_other_strides_is_refused():
+    """(It would read what it has written, and leave what it had to move.)"""
+    here = heads(0x100000)
+    for other in (heads(0x100000, row=128), heads(0x100000, head=1 << 15), heads(0x100000, batch=1 << 21), heads(0x100000, batch=0)):
+        assert rope(x=other, y=here) == INVALID
+    # (strides of dimensions that have one entry do not count: what is left to refuse is the alignment)
+    assert rope(batch=1, heads=1, x=heads(0x100000, batch=5, head=7), y=here, f=0x1004) == ALIGN
