@@ -704,7 +704,7 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
         }
     if (half == 0) {
       part.stat[0] = sum > 0.0f ? st.shift : sum == 0.0f ? kNoMax : sum;
-      part.stat[1] = sum;
+      part.stat[1] = again ? -sum : sum;  // (see Joined)
     }
     return;
   }
@@ -1195,6 +1195,27 @@ __global__ __launch_bounds__(64 * kStreamWaves, DP == 128 ? 2 : 3) void flat_ker
   }
 }
 
+// A row's sums, of parts that are added to them.  Where fp32 has no weight for a part or for the sums before it, it is 2^-149 if they may not
+// be finite, so that they stay so; such a part has left a sum of its weights that is negative.
+struct Joined {
+  float top = kNoMax, sum = 0.0f;
+  f32x4 acc = {0, 0, 0, 0};
+  bool odd = false;
+  static __device__ __forceinline__ float weight(float x, bool odd) {
+    const float w = exp2_fast(x);
+    return odd && w == 0.0f ? __builtin_bit_cast(float, 1u) : w;
+  }
+  __device__ __forceinline__ void add(float m, float its, const f32x4& v) {
+    const float next = m > top || m != m ? m : top;
+    const float old = top == kNoMax ? 0.0f : weight(top - next, odd), now = weight(m - next, its < 0.0f);
+    sum = sum * old + now * __builtin_fabsf(its);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] = acc[c] * old + now * v[c];
+    top = next;
+    odd |= its < 0.0f;
+  }
+};
+
 // One row of a sequence that lies in several pieces, by groups of lanes that take a piece each in turn.
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void join_flat_kernel(const Args p) {
@@ -1210,39 +1231,30 @@ __global__ __launch_bounds__(256) void join_flat_kernel(const Args p) {
   const Entry e = make_entry<true>(p, s, kv);
   if (r >= e.tokens * p.group) return;
   const int group = threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
-  float top = kNoMax, sum = 0.0f;
-  f32x4 acc = {0, 0, 0, 0};
-  auto add = [&](float m, float its, const f32x4& v) {
-    const float next = m > top || m != m ? m : top;
-    const float old = top == kNoMax ? 0.0f : exp2_fast(top - next), now = exp2_fast(m - next);
-    sum = sum * old + now * its;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] = acc[c] * old + now * v[c];
-    top = next;
-  };
+  Joined all;
   for (int piece = from + group; piece <= to; piece += GROUPS) {
     const Part part = flat_part<DP>(p, piece, piece == from, kv);
     const float m = part.stat[r * 2];
-    if (m != kNoMax) add(m, part.stat[r * 2 + 1], *reinterpret_cast<const f32x4*>(part.sums + (long long)r * DP + d));
+    if (m != kNoMax) all.add(m, part.stat[r * 2 + 1], *reinterpret_cast<const f32x4*>(part.sums + (long long)r * DP + d));
   }
-  *reinterpret_cast<f32x4*>(&meet[group][d]) = acc;
+  *reinterpret_cast<f32x4*>(&meet[group][d]) = all.acc;
   if (d == 0) {
-    stat[group][0] = top;
-    stat[group][1] = sum;
+    stat[group][0] = all.top;
+    stat[group][1] = all.odd ? -all.sum : all.sum;
   }
   __syncthreads();
   if (group != 0) return;
   for (int g = 1; g < GROUPS; ++g)
-    if (stat[g][0] != kNoMax) add(stat[g][0], stat[g][1], *reinterpret_cast<const f32x4*>(&meet[g][d]));
-  const Row w = make_row<true>(p, e, r);
-  const bool none = top == kNoMax;
+    if (stat[g][0] != kNoMax) all.add(stat[g][0], stat[g][1], *reinterpret_cast<const f32x4*>(&meet[g][d]));
+  const Row w = place_of_row(p, e, r);
+  const bool none = all.top == kNoMax;
   if (d < p.dim) {
     T four[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : acc[c] / sum);
+    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : all.acc[c] / all.sum);
     __builtin_memcpy(reinterpret_cast<Chunk8*>(reinterpret_cast<T*>(p.out) + query_offset<true>(p, e, p.os, w) + d), four, 8);
   }
-  if (d == 0 && p.lse) p.lse[lse_offset<true>(p, e, w)] = none ? kNoMax : (top + __builtin_log2f(sum)) * kLn2;
+  if (d == 0 && p.lse) p.lse[lse_offset<true>(p, e, w)] = none ? kNoMax : (all.top + __builtin_log2f(all.sum)) * kLn2;
 }
 
 // ---- joining the splits -----------------------------------------------------------------------------------------------------
@@ -1257,8 +1269,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Args p) {
   const int entry = (int)(row / per_entry), r = (int)(row - (long long)entry * per_entry);
   const Entry e = make_entry<PAGED>(p, entry / p.kv_heads, entry % p.kv_heads);
   if (r >= e.tokens * p.group) return;
-  float top = kNoMax, sum = 0.0f;
-  f32x4 acc = {0, 0, 0, 0};
+  Joined all;
   for (int z0 = 0; z0 < p.splits; z0 += U) {
     f32x4 v[U];
     float m[U], s[U];
@@ -1270,112 +1281,95 @@ __global__ __launch_bounds__(256) void join_kernel(const Args p) {
       v[u] = *reinterpret_cast<const f32x4*>(part.sums + d);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (m[u] == kNoMax) continue;  // (nothing was seen, and no sums were written)
-      const float next = m[u] > top || m[u] != m[u] ? m[u] : top;
-      const float old = top == kNoMax ? 0.0f : exp2_fast(top - next), now = exp2_fast(m[u] - next);
-      sum = sum * old + now * s[u];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] = acc[c] * old + now * v[u][c];
-      top = next;
-    }
+    for (int u = 0; u < U; ++u)
+      if (m[u] != kNoMax) all.add(m[u], s[u], v[u]);  // (nothing was seen otherwise, and no sums were written)
   }
-  const Row w = make_row<PAGED>(p, e, r);
-  const bool none = top == kNoMax;
+  const Row w = place_of_row(p, e, r);
+  const bool none = all.top == kNoMax;
   if (d < p.dim) {
     T four[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : acc[c] / sum);
+    for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : all.acc[c] / all.sum);
     __builtin_memcpy(reinterpret_cast<Chunk8*>(reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w) + d), four, 8);
   }
-  if (d == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (top + __builtin_log2f(sum)) * kLn2;
+  if (d == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (all.top + __builtin_log2f(all.sum)) * kLn2;
 }
 // Many: a workgroup a row, four splits of it in flight in each half or quarter of a wavefront.
 template <typename T, int DP, bool PAGED>
 __global__ __launch_bounds__(256) void join_many_kernel(const Args p) {
-  constexpr int WAVES = 4;
-  constexpr int LANES = DP / 4, GROUPS = 64 / LANES, ROWS = 1;
-  __shared__ __attribute__((aligned(16))) float meet[4][DP + 4];
+  constexpr int WAVES = 4, LANES = DP / 4, GROUPS = 64 / LANES;
+  __shared__ __attribute__((aligned(16))) float meet[WAVES][DP + 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_entry = p.seq_q * p.group;
-  const long long row = (long long)blockIdx.x * ROWS + wave / WAVES;
-  const int part_of_row = wave % WAVES;
-  const bool exists = row < (long long)p.batch * p.kv_heads * per_entry;
-  const int entry = exists ? (int)(row / per_entry) : 0, r = exists ? (int)(row - (long long)entry * per_entry) : 0;
+  const int entry = blockIdx.x / per_entry, r = blockIdx.x - entry * per_entry;
   const Entry e = make_entry<PAGED>(p, entry / p.kv_heads, entry % p.kv_heads);
-  const bool mine = exists && r < e.tokens * p.group;
   const int d = (lane % LANES) * 4, group = lane / LANES;
   float top = kNoMax, sum = 0.0f;
   f32x4 acc = {0, 0, 0, 0};
   bool nan = false;
-  if (mine) {
-    // (the maximum over all splits, by every wavefront of the row)
-    for (int z = lane; z < p.splits; z += 64) {
-      const float m = part_of<DP>(p, e.b, e.kv, z, r).stat[0];
-      nan |= m != m;
-      top = fmaxf(top, m);
-    }
+  // (the maximum over all splits, by every wavefront)
+  for (int z = lane; z < p.splits; z += 64) {
+    const float m = part_of<DP>(p, e.b, e.kv, z, r).stat[0];
+    nan |= m != m;
+    top = fmaxf(top, m);
+  }
 #pragma unroll
-    for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-    nan = __any(nan);
-    const float next = top == kNoMax ? 0.0f : top;
-    for (int z0 = part_of_row * 64; z0 < p.splits; z0 += WAVES * 64) {
-      float weight = 0.0f;
-      if (z0 + lane < p.splits) {
-        const Part part = part_of<DP>(p, e.b, e.kv, z0 + lane, r);
-        if (part.stat[0] != kNoMax) {
-          weight = exp2_fast(part.stat[0] - next);
-          sum += weight * part.stat[1];
-        }
-      }
-      const int count = min(64, p.splits - z0);
-      for (int i = 0; i < count; i += 4 * GROUPS) {
-        f32x4 v[4];
-        float w[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int z = i + u * GROUPS + group;
-          w[u] = __shfl(weight, z & 63);
-          v[u] = f32x4{0, 0, 0, 0};
-          if (z >= count) w[u] = 0.0f;
-          if (w[u] != 0.0f) v[u] = *reinterpret_cast<const f32x4*>(part_of<DP>(p, e.b, e.kv, z0 + z, r).sums + d);
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(w[u], v[u][c], acc[c]);
+  for (int m = 32; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+  nan = __any(nan);
+  if (r >= e.tokens * p.group) return;  // (asked behind the first loads: it takes loads of its own)
+  const float level = top == kNoMax ? 0.0f : top;
+  for (int z0 = wave * 64; z0 < p.splits; z0 += WAVES * 64) {
+    float weight = 0.0f;  // (of a split in which nothing was seen, whose sums were not written)
+    if (z0 + lane < p.splits) {
+      const Part part = part_of<DP>(p, e.b, e.kv, z0 + lane, r);
+      if (part.stat[0] != kNoMax) {
+        weight = Joined::weight(part.stat[0] - level, part.stat[1] < 0.0f);
+        sum += weight * __builtin_fabsf(part.stat[1]);
       }
     }
-    sum = wave_sum(sum);
+    const int count = min(64, p.splits - z0);
+    for (int i = 0; i < count; i += 4 * GROUPS) {
+      f32x4 v[4];
+      float w[4];
 #pragma unroll
-    for (int m = 32; m >= LANES; m >>= 1)
+      for (int u = 0; u < 4; ++u) {
+        const int z = i + u * GROUPS + group;
+        w[u] = __shfl(weight, z & 63);
+        v[u] = f32x4{0, 0, 0, 0};
+        if (z >= count) w[u] = 0.0f;
+        if (w[u] != 0.0f) v[u] = *reinterpret_cast<const f32x4*>(part_of<DP>(p, e.b, e.kv, z0 + z, r).sums + d);
+      }
 #pragma unroll
-      for (int c = 0; c < 4; ++c) acc[c] += __shfl_xor(acc[c], m);
-  }
-  {
-    if (group == 0) *reinterpret_cast<f32x4*>(&meet[wave][d]) = acc;
-    if (lane == 0) meet[wave][DP] = sum;
-    __syncthreads();
-    if (part_of_row != 0) return;
-    acc = f32x4{0, 0, 0, 0};
-    sum = 0.0f;
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-      acc += *reinterpret_cast<const f32x4*>(&meet[wave + i][d]);
-      sum += meet[wave + i][DP];
+        for (int c = 0; c < 4; ++c) acc[c] = __builtin_fmaf(w[u], v[u][c], acc[c]);
     }
   }
-  if (!mine) return;
+  sum = wave_sum(sum);
+#pragma unroll
+  for (int m = 32; m >= LANES; m >>= 1)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] += __shfl_xor(acc[c], m);
+  if (group == 0) *reinterpret_cast<f32x4*>(&meet[wave][d]) = acc;
+  if (lane == 0) meet[wave][DP] = sum;
+  __syncthreads();
+  if (wave != 0) return;
+  acc = f32x4{0, 0, 0, 0};
+  sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    acc += *reinterpret_cast<const f32x4*>(&meet[i][d]);
+    sum += meet[i][DP];
+  }
   if (nan) sum = __builtin_nanf("");
-  const Row w = make_row<PAGED>(p, e, r);
+  const Row w = place_of_row(p, e, r);
   const bool none = top == kNoMax && !nan;
-  const float next = top == kNoMax ? 0.0f : top;
   if (group == 0 && d < p.dim) {
     T four[4];
 #pragma unroll
     for (int c = 0; c < 4; ++c) four[c] = from_f32<T>(none ? 0.0f : acc[c] / sum);
     __builtin_memcpy(reinterpret_cast<Chunk8*>(reinterpret_cast<T*>(p.out) + query_offset<PAGED>(p, e, p.os, w) + d), four, 8);
   }
-  if (lane == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (next + __builtin_log2f(sum)) * kLn2;
+  if (lane == 0 && p.lse) p.lse[lse_offset<PAGED>(p, e, w)] = none ? kNoMax : (level + __builtin_log2f(sum)) * kLn2;
 }
 
 }  // namespace attn

@@ -654,6 +654,27 @@ def test_fp16_gradients_of_values_that_cancel_in_the_output(h, n, m, dim):
         assert_within(np.where(fits, got, 0.0), np.where(fits, x, 0.0), e + 1e-30, name)
 
 
+@pytest.mark.parametrize("n,m,splits", [(3, 600, 2), (90, 3000, 2), (1, 9000, 17)])
+def test_an_infinite_value_of_a_key_of_little_weight(n, m, splits):
+    """Its weight, 2^-288, is not a number of fp32 beside the others', nor is that of its split; times infinity it is infinite all the same."""
+    for dtype in ("f16", "bf16"):
+        q = torch.ones(1, 2, n, 64, device="cuda").to(TYPES[dtype])
+        k, v = (torch.ones(1, 1, m, 64, device="cuda").to(TYPES[dtype]) for _ in range(2))
+        k[:, :, :m // 2] = -24.0  # (scores of -192 and 8)
+        for at in (5, m // 2 - 1):
+            v[0, 0, at, 9] = np.inf
+        out, lse = torch.empty_like(q), torch.empty(1, 2, n, device="cuda")
+        size = hb.hidet_attention_workspace_bytes(q, k)
+        rows, width = (n * 2), 66
+        assert size // (rows * width * 4) >= splits, "this size is not split enough"
+        want = torch.ones_like(q)
+        want[..., 9] = np.inf
+        for ws in (None, torch.full((size // 4,), float("nan"), device="cuda")):
+            hb.hidet_attention(q, k, v, out, lse=lse, workspace=ws)
+            assert torch.equal(out, want), (dtype, ws is None)
+            assert float((lse - 8.0 - np.log(m - m // 2)).abs().max()) <= 1e-4
+
+
 def _time(f):
     f()
     times = []
