@@ -91,8 +91,9 @@ EXPORTS = (
     "hidet_batched_gemm_splitk_static", "hidet_conv2d_pack_weights", "hidet_conv2d_implicit_gemm_packed",
     "hidet_tune_conv2d_packed", "hidet_row_schedule", "hidet_conv2d_untuned_config",
     "hidet_gemm_untuned_config", "hidet_conv2d_patch_rows", "hidet_conv2d_untuned_form", "hidet_attention",
-    "hidet_attention_workspace_bytes", "hidet_attention_backward", "hidet_attention_backward_workspace_bytes", "hidet_attention_ranges", "hidet_rope", "hidet_rope_frequencies", "hidet_cache_append",
-    "hidet_cache_attention", "hidet_cache_attention_workspace_bytes",
+    "hidet_attention_workspace_bytes", "hidet_attention_backward", "hidet_attention_backward_workspace_bytes",
+    "hidet_attention_ranges", "hidet_rope", "hidet_rope_frequencies", "hidet_cache_append", "hidet_cache_attention",
+    "hidet_cache_attention_workspace_bytes",
 )
 
 _lib = None

@@ -1029,10 +1029,11 @@ long long peak_bytes(long long entries, long long row_groups) { return (entries 
 long long info_bytes(long long entries, long long rows) { return entries * ((rows + 127) / 128 * 128) * 8 * 4; }
 
 // How the two kernels' work is cut.
-//   dQ: tiles of 128 rows, in pairs of wavefronts as in the forward pass while the device takes all of them at once, and then as many
-//   splits of at least 4 tiles of 128 keys as find a compute unit each.  A whole pass (forward, dQ, dK and dV) without and with pairs, us:
-//   6 entries of 3146 rows of 96 dimensions 170 and 152, 9 of 3332 at 128 470 and 429, 36 of 1021 at 64 125 and 122; 36 of 1024 at
-//   128, 288 tiles, 202 and 227, and so without; one fits worse, 4 entries of 1472 rows over 184 keys 47 and 50.
+//   dQ: tiles of 128 rows, in pairs of wavefronts while a compute unit each takes them (its registers leave room for one such workgroup, at 64
+//   dimensions too, where the tail of up to 320 is short enough: heads of 1021 rows, pairs and without, us: 288 tiles 46 and 47, 320 47 and
+//   48, 416 56 and 49, 496 57 and 49), and then as many splits of at least 4 tiles of 128 keys as find a compute unit each.  A whole pass
+//   (forward, dQ, dK and dV) without and with pairs, us: 6 entries of 3146 rows of 96 dimensions 170 and 152, 9 of 3332 at 128 470 and 429;
+//   36 of 1024 at 128, 288 tiles, 202 and 227, and so without; one fits worse, 4 entries of 1472 rows over 184 keys 47 and 50.
 //   dK and dV: tiles of 64 keys, and where they leave compute units without work splits of at least 2 tiles of 128 rows: 256 workgroups
 //   (512 at 64 dimensions: 24 heads over 1449 keys 199 us for 211).  With 512 of at least 4 everywhere: the first of the passes above 220 for 190,
 //   the second 486 for 449, and 285 for 271 of 2 entries of 6599 rows.
@@ -1051,7 +1052,7 @@ BackCut cut_backward(long long entries, long long rows, long long keys, int dp) 
   c.row_tiles = (int)((rows + 127) / 128);
   c.key_tiles = (int)((keys + kBlockKeys - 1) / kBlockKeys);
   const long long row_blocks = std::max(1LL, entries * c.row_tiles), key_blocks = std::max(1LL, entries * c.key_tiles);
-  c.dq_pairs = (dp == 64 ? row_blocks < 512 : row_blocks <= 256) && keys > kTileKeys;
+  c.dq_pairs = row_blocks <= (dp == 64 ? 320 : 256) && keys > kTileKeys;
   const long long tile_keys = c.dq_pairs ? 2 * kTileKeys : kTileKeys;
   const long long tiles = std::max(1LL, (keys + tile_keys - 1) / tile_keys), row_tiles = std::max(1LL, (rows + kTileRows - 1) / kTileRows);
   split(tiles, c.dq_pairs ? std::min(256 / row_blocks, tiles / 4) : 1, c.dq_splits, c.dq_share);
