@@ -609,7 +609,7 @@ __device__ __forceinline__ void settle_odd(f32x16 (&acc)[DP / 32], const OddSums
   }
 }
 
-// What lane's row sees of values that are not finite, of keys from `from` on and before `to`, which the workgroup went over.
+// What lane's row, if it asks, sees of values that are not finite, of keys from `from` on and before `to`, which the workgroup went over.
 template <typename T, int DP, bool PAGED>
 __device__ __forceinline__ OddSums<DP> odd_values(const Args& p, const Entry& e, const Row& w, int from, int to, bool ask) {
   constexpr int E = DP / 64, U = 8;
@@ -649,7 +649,7 @@ __device__ __forceinline__ OddSums<DP> odd_values(const Args& p, const Entry& e,
       // (a key that is not finite has a score of -inf here, and no weight: with any other the row were NaN)
       if (__any(odd) && !__any(odd_key)) {
         const int j = first + (int)min(i + u, count - 1);
-        sums.add(x, there[u] && j >= w.lo && j < w.hi);
+        sums.add(x, ask && there[u] && j >= w.lo && j < w.hi);
       }
     }
     if (!__any(ask && any_but_nan(sums, p.dim))) break;
@@ -689,7 +689,7 @@ __device__ __forceinline__ void finish(const Args& p, const Entry& e, State<T, D
   const float sum = sum_of_halves(st.sum);
   if (__builtin_expect(again, 0)) {
     const Row w = make_row<PAGED>(p, e, min(r, rows - 1));
-    settle_odd<DP>(st.o, odd_values<T, DP, PAGED>(p, e, w, from, to, sum == sum), half);
+    settle_odd<DP>(st.o, odd_values<T, DP, PAGED>(p, e, w, from, to, sum > 0.0f), half);
   }
   if (r >= rows) return;
   if (partial) {

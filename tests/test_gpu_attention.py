@@ -524,6 +524,12 @@ def test_scores_that_are_not_finite_and_values_beside_them():
             hb.hidet_attention(q, k, v, out, lse=lse)
             assert bool(torch.isnan(out[0, 1, n // 2]).all()) and bool(torch.isnan(lse[0, 1, n // 2]))
             assert bool(torch.isfinite(lse[0, 1, torch.arange(n) != n // 2]).all())
+            k[0, 1] = k[0, 1].abs() + 0.1
+            q[0, 1, n // 2] = -np.inf  # (all scores -inf, beside an infinite value that the others see)
+            hb.hidet_attention(q, k, v, out, lse=lse)
+            others = torch.arange(n) != n // 2
+            assert not out[0, 1, n // 2].any() and float(lse[0, 1, n // 2]) == -np.inf
+            assert bool((out[0, 1, others, 7] == np.inf).all()) and bool(torch.isfinite(out[0, 1, others, :7]).all())
 
 
 BACK_SIZES = [(1, 4, 2, 300, 300, 64), (2, 2, 1, 200, 260, 128), (1, 3, 1, 70, 700, 40), (1, 2, 1, 90, 3000, 128), (1, 4, 2, 900, 70, 64), (86, 12, 6, 19, 193, 112)]
