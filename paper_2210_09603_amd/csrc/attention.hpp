@@ -747,6 +747,7 @@ __device__ __forceinline__ Place place_of(int w, int entries, int pieces) {
   return Place{(entries & ~7) + turn, at - turn * pieces};
 }
 
+// (wavefronts to a SIMD: 64 dimensions fit 128 registers, but for a bias and a cap over pages, and caps of the WIDE form)
 template <typename T, int DP, bool PAGED, int FORM, int PAIRS>
 __global__ __launch_bounds__(256 * PAIRS, DP == 128 ? 2 : FORM < 3 || (FORM == 3 && !PAGED) ? 4 : 3) void tile_kernel(const Args p) {
   static_assert(PAIRS == 1 || !PAGED, "a wavefront looks up 64 keys");
