@@ -135,7 +135,10 @@ long long keys_at_most(const hidet_cache_t* c, long long max_new, long long wind
 // tables have room for: where that is far more than the sequences hold, one split has all of a sequence.  64 sequences, 8 kv heads,
 // splits and pieces, us: room for 131000, lengths 100 to 8000 244 and 204, 100 to 163 27.6 and 23.1, one of 120000 beside 63 of 200 546
 // and 154; room for 8000 and lengths 100 to 8000 222 and 217; room for 2000 and lengths 100 to 163 12.3 and 23, where splits stay:
-// the pieces' second kernel, and the ends of two sequences one after the other.
+// the pieces' second kernel, and the ends of two sequences one after the other.  Fewer than 256 entries (sequences x kv heads) keep splits,
+// though pieces would be the faster in most tables that are too wide.  Room for 131000, 8 kv heads, splits and pieces, us: one sequence
+// of 2000 tokens 34.6 and 19.5, of 120000 102 and 104; 8 of 2000 34.7 and 27.2, of 8000 57.5 and 55.1; 16 of 8000 126 and 108; 31 of 8000
+// 184 and 192, of 100 to 7600 124 and 102.
 int flat_pieces(const hidet_cache_t* c, long long rows, long long keys) {
   if (rows > 32 || c->seqs > kFlatSeqs || c->seqs * c->heads < 256 || keys < 16384 || (keys / kStreamKeys + 1) * c->seqs >= (1LL << 30)) return 0;
   if (c->seqs * c->heads * rows > kMaxBlocks) return 0;  // (the second kernel has a workgroup for each)
