@@ -456,7 +456,8 @@ def _sums_of_odd(see, places, shape):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("size", [(1, 4, 2, 300, 300, 64), (2, 2, 1, 200, 260, 128), (86, 12, 6, 19, 193, 112), (1, 2, 1, 3, 700, 40), (1, 4, 2, 1, 9000, 128),
-                                  (1, 4, 2, 90, 3000, 64), (2, 3, 3, 130, 130, 24)], ids=str)
+                                  (1, 4, 2, 90, 3000, 64), (2, 3, 3, 130, 130, 24), (1, 4, 2, 1500, 1500, 64), (1, 2, 1, 1300, 2100, 128), (1, 9, 9, 2000, 1100, 104),
+                                  (1, 40, 40, 1000, 1000, 64)], ids=str)
 @pytest.mark.parametrize("mask", ["causal", "window", "ranges"])
 def test_values_that_are_not_finite_reach_the_queries_that_see_them_alone(mask, size, dtype):
     """In every kernel and cut: a dimension in which a query sees infinities or a NaN is their sum, and every other result has the bits
@@ -491,6 +492,31 @@ def test_values_that_are_not_finite_reach_the_queries_that_see_them_alone(mask, 
             want = torch.where(reached, torch.from_numpy(sums).cuda().to(out.dtype), clean)
             assert torch.equal(lse, lse_clean)
             assert torch.equal(torch.nan_to_num(out, 11.0, 12.0, 13.0), torch.nan_to_num(want, 11.0, 12.0, 13.0)), (count, ws is None)
+
+
+@pytest.mark.parametrize("size", [(1, 4, 2, 1500, 1500, 64), (1, 2, 1, 1300, 2100, 128), (1, 40, 40, 1000, 1000, 64), (1, 2, 1, 2, 9000, 64)], ids=str)
+def test_queries_that_are_not_finite_are_so_alone(size):
+    b, h, hk, n, m, d = size
+    for dtype in ("f16", "bf16"):
+        g = np.random.Generator(np.random.PCG64(86))
+        q, k, v = _draw(g, (b, h, n, d), dtype, "dense"), _draw(g, (b, hk, m, d), dtype, "dense"), _draw(g, (b, hk, m, d), dtype, "dense")
+        odd, rows = q.clone(), torch.zeros(b, h, n, dtype=torch.bool, device="cuda")
+        for (bb, hh, i, dd), _ in _scatter(g, q.shape, 9):
+            odd[bb, hh, i, dd] = np.nan
+            rows[bb, hh, i] = True
+        size = hb.hidet_attention_workspace_bytes(q, k)
+        for ws in (None, torch.full((size // 4 + 4,), float("nan"), device="cuda")):
+            results = []
+            for queries in (q, odd):
+                out, lse = torch.full_like(q, 7.0), torch.empty(b, h, n, device="cuda")
+                hb.hidet_attention(queries, k, v, out, lse=lse, workspace=ws)
+                results.append((out, lse))
+            (clean, lse_clean), (out, lse) = results
+            assert bool((torch.isnan(lse) == rows).all()) and bool((torch.isnan(out) == rows[..., None]).all())
+            # (maxima are replaced for 32 rows at a time, which moves the others' last bits: two roundings of weights and of the result)
+            u = {"f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
+            off = torch.where(rows[..., None], torch.zeros_like(out), (out - clean).abs()).float()
+            assert float(off.max()) <= 4 * u * float(v.abs().max()) and float(torch.where(rows, 0.0, lse - lse_clean).abs().max()) <= 1e-5
 
 
 def test_scores_that_are_not_finite_and_values_beside_them():

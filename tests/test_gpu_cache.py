@@ -496,7 +496,7 @@ def test_large_caps(softcap, dtype):
 
 
 @pytest.mark.parametrize("dtype,dim", [("f16", 64), ("bf16", 128), ("bf16", 40)])
-@pytest.mark.parametrize("kind", ["single tokens", "chunks", "pieces"])
+@pytest.mark.parametrize("kind", ["single tokens", "chunks", "long chunks", "pieces"])
 def test_values_that_are_not_finite_reach_the_queries_that_see_them_alone(kind, dtype, dim):
     """A dimension in which a query sees infinities or a NaN is their sum, and every other result has the bits that it has without them --
     wherever the pages lie, the one that stands for no page among them."""
@@ -504,8 +504,8 @@ def test_values_that_are_not_finite_reach_the_queries_that_see_them_alone(kind, 
     if kind == "pieces":
         b = _ragged(45, dtype, dim)
     else:
-        new = [1, 1, 1, 1] if kind == "single tokens" else [200, 3, 77, 40]
-        b = Batch(45, dtype, [300, 1000, 77, 500], new, 4, 2, dim, 24, pad=1)
+        new = {"single tokens": [1, 1, 1, 1], "chunks": [200, 3, 77, 40], "long chunks": [300, 3, 77, 500]}[kind]
+        b = Batch(45, dtype, [300, 1700, 77, 500], new, 4, 2, dim, 24, pad=1)
         b.table[1, 2] = -1
         b.tables.copy_(torch.from_numpy(b.table))
     before = b.v_pages.clone()
