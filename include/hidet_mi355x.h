@@ -542,6 +542,79 @@ hidet_status_t hidet_cache_attention(const hidet_cache_t* cache, int64_t heads, 
 int64_t hidet_cache_attention_workspace_bytes(const hidet_cache_t* cache, int64_t heads, int64_t max_new, int64_t window);
 
 /*
+ * Matrices in 8 and 4 bits: every 32 elements of a row share a scale, a power of two.  Element k of row i stands for
+ *   value(i, k) * 2^(scales[(k / 32) * stride_scales + i] - 127),     scale code 255: NaN.
+ * Row i of the values begins at values + i * stride_values (bytes) and holds whole blocks: ceil(cols / 32) of 32 bytes, or, in
+ * HIDET_MX_E2M1, of 16, the element of the even index in the low half of a byte; what fills the last one is 0.  The scales of
+ * a block of columns lie side by side, row after row: as the matrix cores take them.
+ *   HIDET_MX_E4M3   sign, 4 bits of exponent, 3 of mantissa, up to 448;   HIDET_MX_E5M2   5 and 2, up to 57344;
+ *   HIDET_MX_E2M1   2 and 1: 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ * values are aligned to 16 bytes, stride_values is a multiple of 16 below 2^23; scales are aligned to 4 bytes, stride_scales is a
+ * multiple of 4 below 2^29 and at least the rows rounded up to 4, and all those bytes may be read.  Rows a multiple of 4 apart are
+ * matrices of their own.  DEVICE memory, but for the structure itself.
+ */
+typedef enum { HIDET_MX_E4M3 = 0, HIDET_MX_E5M2 = 1, HIDET_MX_E2M1 = 2 } hidet_mx_format_t;
+typedef struct {
+  uint32_t struct_size; /* sizeof(hidet_mx_t) */
+  int32_t format;       /* hidet_mx_format_t */
+  void* values;
+  void* scales;
+  int64_t stride_values, stride_scales; /* bytes */
+} hidet_mx_t;
+/*
+ * x [rows][cols] of dtype (any of the three; ldx >= cols elements) in such blocks: of its rows (by_rows, [rows][cols]), of its columns
+ * (by_columns: x transposed, [cols][rows]), or both from one reading of x; either may be NULL.  The scale of a block is
+ * 2^(floor(log2 m) - e), m its largest magnitude and 2^e the largest power of two of the format (2^8, 2^15, 2^2), 2^-127 at least;
+ * elements are x / scale, rounded to nearest even and cut to the largest value of the format.  A block that holds a NaN or an
+ * infinity has the scale NaN and elements 0.
+ * hidet_mx_dequantize: y [rows][cols] of dtype, rounded once.
+ * rows or cols of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: rows or cols of 2^29 or more, rows * ld beyond 2^47 elements.
+ */
+hidet_status_t hidet_mx_quantize(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const hidet_mx_t* by_rows,
+                                 const hidet_mx_t* by_columns, void* stream);
+hidet_status_t hidet_mx_dequantize(int64_t rows, int64_t cols, const hidet_mx_t* x, int32_t dtype, void* y, int64_t ldy, void* stream);
+/*
+ * C [M][N] = epilogue(A . B^T) for A [M][K] and B [N][K] in such blocks, each in a format of its own; C, bias and residual are of dtype
+ * `out` (any of the three).  alpha, bias, residual and ReLU as for hidet_gemm; C may be the residual (same ld), no other overlap.
+ * Products are exact and accumulated in fp32.  Where an operand has 8 bits the matrix cores align the products of 8 neighbouring k
+ * to 13 bits below the largest of them before they add them: about 1.5e-5 of the result's size for normally distributed operands.
+ * Work that is too small for the device otherwise is cut along K into slices, whose fp32 sums meet in the workspace (DEVICE, 16-byte
+ * aligned, hidet_mx_gemm_workspace_bytes() for as many as the library would like; with less, or NULL, it cuts into fewer) in ascending
+ * order.  Calls that share a workspace must be ordered on one stream.
+ * M or N of 0 is an OK no-op; K == 0 writes epilogue(0).  HIDET_ERR_UNSUPPORTED: M, N or K of 2^29 or more, ldc or ld_residual of 2^32
+ * or more, a head-split output map, an input prologue.
+ */
+hidet_status_t hidet_mx_gemm(int32_t out, int64_t M, int64_t N, int64_t K, const hidet_mx_t* A, const hidet_mx_t* B, void* C, int64_t ldc,
+                             const hidet_epilogue_t* epi, void* workspace, int64_t workspace_bytes, void* stream);
+int64_t hidet_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t format_a, int32_t format_b);
+
+/*
+ * Root-mean-square norm of rows, with the addition of a residual before it:
+ *   h = x + residual (rounded to dtype; x if residual is NULL);   rstd = 1 / sqrt(mean(h^2) + eps);   y = h * rstd * (offset + weight)
+ * x, residual, sum, y: [rows][cols] of dtype (any of the three), each with a leading dimension >= cols; weight [cols] of weight_dtype,
+ * which is dtype or HIDET_F32.  Any of these may be NULL: residual; sum (receives h); y; quantized (receives y in blocks of its rows, as
+ * hidet_mx_quantize of the unrounded y); rstd (receives fp32 [rows], which the backward pass takes); y or quantized is needed.
+ * Squares are added in fp64, the rest is fp32.  sum and y may each be x or residual (the same ld), no other overlap.
+ *
+ * hidet_rms_norm_backward: with g = grad_y * (offset + weight) and xhat = h * rstd,
+ *   grad_h = rstd * (g - xhat * mean(g * xhat)) + grad_sum;     grad_weight = sum over the rows of grad_y * xhat
+ * given h (sum of the forward call, or its x) and rstd.  grad_h is the gradient of x and of residual alike; grad_sum (may be NULL) is what
+ * comes down the residual stream.  grad_h may be grad_y or grad_sum (the same ld).  grad_weight [cols] of weight_dtype; NULL: not
+ * wanted, and no workspace is.  Sums over rows are fp32, in an order that depends on the sizes alone: no atomics.  The workspace:
+ * 16-byte aligned, HIDET_ERR_INVALID_ARG if it is smaller than hidet_rms_norm_backward_workspace_bytes.
+ * Both: rows or cols of 0 is an OK no-op, but for grad_weight of no rows, which is 0.  HIDET_ERR_UNSUPPORTED: cols above 32768, rows of 2^29 or
+ * more, rows * ld beyond 2^47 elements.
+ */
+hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                              const void* residual, int64_t ld_residual, const void* weight, float eps, float offset, void* sum,
+                              int64_t ld_sum, void* y, int64_t ldy, const hidet_mx_t* quantized, float* rstd, void* stream);
+hidet_status_t hidet_rms_norm_backward(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* grad_y, int64_t ld_grad_y,
+                                       const void* h, int64_t ldh, const float* rstd, const void* weight, float offset,
+                                       const void* grad_sum, int64_t ld_grad_sum, void* grad_h, int64_t ld_grad_h, void* grad_weight,
+                                       void* workspace, int64_t workspace_bytes, void* stream);
+int64_t hidet_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+
+/*
  * Task mappings (Section 5.1): the compile-time mappings the kernels are built from, plus the
  * paper's worked examples, evaluated on the host so that tests can compare them with the
  * definitions.  `expr` receives a string such as "repeat(4,1)*spatial(16,8)".  hidet_taskmap_tasks

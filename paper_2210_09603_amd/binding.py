@@ -24,6 +24,7 @@ HIDET_ACT_NONE, HIDET_ACT_RELU = 0, 1
 HIDET_MAP_PLAIN, HIDET_MAP_HEAD_SPLIT = 0, 1
 HIDET_PROLOGUE_NONE, HIDET_PROLOGUE_RELU = 0, 1
 HIDET_REDUCE_SUM, HIDET_REDUCE_MAX, HIDET_REDUCE_MEAN = 0, 1, 2
+HIDET_MX_E4M3, HIDET_MX_E5M2, HIDET_MX_E2M1 = 0, 1, 2
 HIDET_ROPE_PLAIN, HIDET_ROPE_LINEAR, HIDET_ROPE_BASE, HIDET_ROPE_BANDS = 0, 1, 2, 3
 
 _DTYPES = {torch.float32: HIDET_F32, torch.float16: HIDET_F16, torch.bfloat16: HIDET_BF16}
@@ -73,6 +74,11 @@ class hidet_cache_t(ctypes.Structure):
         ("tables", _vp), ("table_width", _i64), ("table_stride", _i64), ("lengths", _vp), ("seqs", _i64)]
 
 
+class hidet_mx_t(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("format", _i32), ("values", _vp), ("scales", _vp), ("stride_values", _i64),
+                ("stride_scales", _i64)]
+
+
 class HidetError(RuntimeError):
     def __init__(self, status, where):
         self.status = status
@@ -93,7 +99,8 @@ EXPORTS = (
     "hidet_gemm_untuned_config", "hidet_conv2d_patch_rows", "hidet_conv2d_untuned_form", "hidet_attention",
     "hidet_attention_workspace_bytes", "hidet_attention_backward", "hidet_attention_backward_workspace_bytes",
     "hidet_attention_ranges", "hidet_rope", "hidet_rope_frequencies", "hidet_cache_append", "hidet_cache_attention",
-    "hidet_cache_attention_workspace_bytes",
+    "hidet_cache_attention_workspace_bytes", "hidet_mx_quantize", "hidet_mx_dequantize", "hidet_mx_gemm",
+    "hidet_mx_gemm_workspace_bytes", "hidet_rms_norm", "hidet_rms_norm_backward", "hidet_rms_norm_backward_workspace_bytes",
 )
 
 _lib = None
@@ -171,6 +178,17 @@ def lib():
         L.hidet_cache_attention.argtypes = [cp, _i64, _i64, _i64, hp, hp, _vp, _vp, op, _vp, _i64, _vp]
         L.hidet_cache_attention_workspace_bytes.argtypes = [cp, _i64, _i64, _i64]
         L.hidet_cache_attention_workspace_bytes.restype = _i64
+        mp, f32 = ctypes.POINTER(hidet_mx_t), ctypes.c_float
+        L.hidet_mx_quantize.argtypes = [_i32, _i64, _i64, _vp, _i64, mp, mp, _vp]
+        L.hidet_mx_dequantize.argtypes = [_i64, _i64, mp, _i32, _vp, _i64, _vp]
+        L.hidet_mx_gemm.argtypes = [_i32, _i64, _i64, _i64, mp, mp, _vp, _i64, ep, _vp, _i64, _vp]
+        L.hidet_mx_gemm_workspace_bytes.argtypes = [_i64, _i64, _i64, _i32, _i32]
+        L.hidet_mx_gemm_workspace_bytes.restype = _i64
+        L.hidet_rms_norm.argtypes = [_i32, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, f32, f32, _vp, _i64, _vp, _i64, mp, _vp, _vp]
+        L.hidet_rms_norm_backward.argtypes = [_i32, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _vp, f32, _vp, _i64, _vp, _i64, _vp, _vp,
+                                              _i64, _vp]
+        L.hidet_rms_norm_backward_workspace_bytes.argtypes = [_i64, _i64]
+        L.hidet_rms_norm_backward_workspace_bytes.restype = _i64
         L.hidet_status_string.argtypes = [_i32]
         L.hidet_status_string.restype = ctypes.c_char_p
         L.hidet_version.restype = ctypes.c_char_p
@@ -894,6 +912,142 @@ def _cache_attention(cache, q, out, starts, max_new, scale, window, softcap, slo
 def hidet_cache_attention_workspace_bytes(cache, q, max_new, window=0):
     """Workspace bytes of hidet_cache_attention for queries like q (0: none is wanted)."""
     return lib().hidet_cache_attention_workspace_bytes(cache, q.shape[1], max_new, window)
+
+
+# ---- norms, matrices in 8 and 4 bits, and their products --------------------------------------------------------------------
+def make_mx(rows, cols, format, values=None, scales=None, device=None):
+    """hidet_mx_t of a [rows, cols] matrix in blocks of 32 along its rows.  values: a tensor of 1-byte elements, [rows, at least the bytes of
+    the blocks], scales: [blocks, rows], rows of either contiguous and their distances multiples of 16 and 4; both are allocated on
+    `device` where they are not given.  It holds their addresses; `tensors` are the two."""
+    blocks = (cols + 31) // 32
+    width = blocks * (16 if format == HIDET_MX_E2M1 else 32)
+    if (values is None) != (scales is None):
+        raise ValueError("need values and scales, or neither")
+    if values is None:
+        values = torch.empty((rows, width), dtype=torch.uint8, device=device)
+        scales = torch.empty((blocks, (rows + 3) // 4 * 4), dtype=torch.uint8, device=device)[:, :rows]
+    for t, n, m, what in ((values, rows, width, "values"), (scales, blocks, rows, "scales")):
+        if t.dim() != 2 or t.element_size() != 1 or t.shape[0] != n or t.shape[1] < m or (t.stride(1) != 1 and t.shape[1] > 1):
+            raise ValueError("%s must be [%d, %d] of 1-byte elements with contiguous rows" % (what, n, m))
+    if values.device != scales.device:
+        raise ValueError("tensors are on different devices")
+    if blocks and rows:  # (the words of scales at the end of a row are read whole)
+        stride = scales.stride(0) if blocks > 1 else 0
+        if scales.storage_offset() + (blocks - 1) * stride + (rows + 3) // 4 * 4 > scales.untyped_storage().nbytes():
+            raise ValueError("scales need memory up to a multiple of 4 rows")
+    m = hidet_mx_t()
+    m.struct_size = ctypes.sizeof(hidet_mx_t)
+    m.format, m.values, m.scales = format, values.data_ptr(), scales.data_ptr()
+    m.stride_values = values.stride(0) if rows > 1 else (width + 15) // 16 * 16
+    m.stride_scales = scales.stride(0) if blocks > 1 else (rows + 3) // 4 * 4
+    m.tensors = m._keep = (values, scales)  # (the structure holds raw addresses)
+    m.shape = (rows, cols)
+    m._device = values.device.index if values.is_cuda else -1
+    return m
+
+
+def _mx(m, shape):
+    """The tensors of a hidet_mx_t that has that shape."""
+    if m is None:
+        return ()
+    if m.shape != tuple(shape):
+        raise ValueError("expected blocks of a %s matrix, got %s" % (tuple(shape), m.shape))
+    return m.tensors
+
+
+def _norm_rows(x, *others):
+    """(rows, cols, leading dimensions) of tensors of one shape and dtype; None counts as fine."""
+    rows, cols, ld = _rows_view(x)
+    lds = [ld]
+    for t in others:
+        if t is None:
+            lds.append(0)
+            continue
+        if t.shape != x.shape or t.dtype != x.dtype:
+            raise ValueError("tensors must agree in shape and dtype")
+        lds.append(_rows_view(t)[2])
+    return rows, cols, lds
+
+
+def _weight(w, cols):
+    if w.dim() != 1 or w.shape[0] != cols or not w.is_contiguous():
+        raise ValueError("the weight must be a dense vector of %d elements" % cols)
+    return w.data_ptr()
+
+
+def hidet_rms_norm(x, weight, y=None, residual=None, sum=None, quantized=None, rstd=None, eps=1e-6, offset=0.0, stream=None):
+    """y = h * rstd * (offset + weight) with h = x + residual and rstd = 1 / sqrt(mean(h^2) + eps), over the last axis of x; y (like x),
+    quantized (make_mx) or both are written, and sum (h, like x) and rstd (float32, one a row) where given."""
+    rows, cols, (ldx, ldr, lds, ldy) = _norm_rows(x, residual, sum, y)
+    device, handle = _on((x, weight, y, residual, sum, rstd) + _mx(quantized, (rows, cols)), stream)
+    if rstd is not None and (rstd.dtype != torch.float32 or rstd.numel() != rows or not rstd.is_contiguous()):
+        raise ValueError("rstd must be a dense float32 tensor of %d elements" % rows)
+    with device:
+        st = lib().hidet_rms_norm(_dtype(x), _dtype(weight), rows, cols, _ptr(x), ldx, _ptr(residual), ldr, _weight(weight, cols), eps,
+                                  offset, _ptr(sum), lds, _ptr(y), ldy, quantized, _ptr(rstd), handle)
+    _check(st, "hidet_rms_norm")
+
+
+def hidet_rms_norm_backward(grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum=None, offset=0.0, stream=None):
+    """Writes grad_h (like h), and grad_weight (like weight) unless it is None, from grad_y and what comes down the residual stream
+    (grad_sum); h and rstd are those of the forward call (its sum, or its x)."""
+    rows, cols, (ldh, ldg, lds, ldo) = _norm_rows(h, grad_y, grad_sum, grad_h)
+    if rstd.dtype != torch.float32 or rstd.numel() != rows or not rstd.is_contiguous():
+        raise ValueError("rstd must be a dense float32 tensor of %d elements" % rows)
+    if grad_weight is not None and grad_weight.dtype != weight.dtype:
+        raise ValueError("grad_weight must have the weight's dtype")
+    wp, wb = _dense_ws(workspace)
+    device, handle = _on((grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum), stream)
+    with device:
+        st = lib().hidet_rms_norm_backward(_dtype(h), _dtype(weight), rows, cols, _ptr(grad_y), ldg, _ptr(h), ldh, _ptr(rstd),
+                                           _weight(weight, cols), offset, _ptr(grad_sum), lds, _ptr(grad_h), ldo,
+                                           None if grad_weight is None else _weight(grad_weight, cols), wp, wb, handle)
+    _check(st, "hidet_rms_norm_backward")
+
+
+def hidet_rms_norm_backward_workspace_bytes(rows, cols):
+    """Workspace bytes of hidet_rms_norm_backward with a gradient of the weight."""
+    return lib().hidet_rms_norm_backward_workspace_bytes(rows, cols)
+
+
+def hidet_mx_quantize(x, by_rows=None, by_columns=None, stream=None):
+    """x [rows, cols] into blocks of 32 along its rows (by_rows, make_mx(rows, cols, ...)), along its columns (by_columns, make_mx(cols, rows,
+    ...): x transposed), or both."""
+    if x.dim() != 2:
+        raise ValueError("x must be [rows, cols]")
+    rows, cols = x.shape
+    device, handle = _on((x,) + _mx(by_rows, (rows, cols)) + _mx(by_columns, (cols, rows)), stream)
+    with device:
+        st = lib().hidet_mx_quantize(_dtype(x), rows, cols, _ptr(x), _ld(x), by_rows, by_columns, handle)
+    _check(st, "hidet_mx_quantize")
+
+
+def hidet_mx_dequantize(x, y, stream=None):
+    """y [rows, cols] = the numbers that x (make_mx) stands for."""
+    device, handle = _on((y,) + _mx(x, y.shape), stream)
+    with device:
+        st = lib().hidet_mx_dequantize(y.shape[0], y.shape[1], x, _dtype(y), _ptr(y), _ld(y), handle)
+    _check(st, "hidet_mx_dequantize")
+
+
+def hidet_mx_gemm(A, B, C, epilogue=None, workspace=None, stream=None):
+    """C [M, N] = epilogue(A . B^T); A and B are make_mx(M, K, ...) and make_mx(N, K, ...), in any of the formats."""
+    (M, K), (N, _) = A.shape, B.shape
+    if C.dim() != 2:
+        raise ValueError("C must be [M, N]")
+    if tuple(C.shape) != (M, N):
+        raise ValueError("expected C of shape %s, got %s" % ((M, N), tuple(C.shape)))
+    wp, wb = _dense_ws(workspace)
+    kept = tuple(epilogue._keep) if epilogue is not None else ()
+    device, handle = _on((C, workspace) + _mx(A, (M, K)) + _mx(B, (N, K)) + kept, stream)
+    with device:
+        st = lib().hidet_mx_gemm(_dtype(C), M, N, K, A, B, _ptr(C), _ld(C), epilogue, wp, wb, handle)
+    _check(st, "hidet_mx_gemm")
+
+
+def hidet_mx_gemm_workspace_bytes(A, B):
+    """Workspace bytes of hidet_mx_gemm on these operands (0: none is wanted)."""
+    return lib().hidet_mx_gemm_workspace_bytes(A.shape[0], B.shape[0], A.shape[1], A.format, B.format)
 
 
 def hidet_conv2d_untuned_config(dtype, x_shape, w_shape, stride=(1, 1), pad=(0, 0), packed=False):

@@ -127,11 +127,16 @@ def build(force=False, jobs=None, verbose=True):
             objs.append(obj)
             if not os.path.exists(obj):
                 tasks.append((os.path.join(CSRC, "instances.hip"), obj, ["-DHIDET_TU=%d" % idx, "-DHIDET_TYPE=%d" % t]))
-    for name in ("api", "attention", "attention_backward", "cache", "conv_patch", "probe", "reduce", "rope"):
+    for name in ("api", "attention", "attention_backward", "cache", "conv_patch", "mx_convert", "mx_gemm", "norm", "probe", "reduce", "rope"):
         obj = os.path.join(BUILD, name + ".o")
         objs.append(obj)
         if not os.path.exists(obj):
             tasks.append((os.path.join(CSRC, name + ".hip"), obj, []))
+    for fmt in range(3):  # (HIDET_MX_E4M3, E5M2, E2M1)
+        obj = os.path.join(BUILD, "mx_kernels_%d.o" % fmt)
+        objs.append(obj)
+        if not os.path.exists(obj):
+            tasks.append((os.path.join(CSRC, "mx_kernels.hip"), obj, ["-DHIDET_MX_A=%d" % fmt]))
     jobs = jobs or min(8, os.cpu_count() or 1)
     failed = False
     with concurrent.futures.ThreadPoolExecutor(max_workers=jobs) as ex:

@@ -1,0 +1,521 @@
+// Root-mean-square norm of rows, y = h / sqrt(mean(h^2) + eps) * (offset + weight) with h = x + residual, and its gradients.
+//
+// Memory bound: a row is read once, stays in the registers of the lanes that share it -- in its storage type, as it was rounded for the
+// residual stream -- and leaves them normalised, in its type or in blocks of 32 with a scale.  The scale of a block is the maximum over 4 (16-bit
+// types) or 8 neighbouring lanes.  Scales lie [block][row]: a workgroup takes 4 rows or more where it can, collects theirs in LDS and
+// writes words of 4.
+//
+// Squares are added in fp64, whose rate here is that of fp32: 1 / sqrt(mean) is the nearest fp32 however long the row and large its values, and
+// the elements of y are then rounded to 8 bits on the same side by whoever works them out in this order.
+#include <math.h>
+
+#include <algorithm>
+
+#include "mx.hpp"
+
+using namespace hidet;
+using namespace hidet::mx;
+
+namespace {
+
+constexpr long long kMaxCols = 32768;
+
+struct NormArgs {
+  const void* x;
+  const void* residual;  // may be null, as all below but the weight
+  const void* weight;
+  void* sum;
+  void* y;
+  unsigned char* values;
+  unsigned char* scales;
+  float* rstd;
+  long long ldx, ldr, lds, ldy, stride_values, stride_scales;
+  int rows, cols;
+  int format;
+  float eps, offset;
+};
+
+// N weights from column `col` on, offset added; 0 beyond the row
+template <typename TW, int N>
+__device__ __forceinline__ void load_weights(const TW* w, int col, int cols, float offset, float (&v)[N]) {
+  constexpr int PER = Chunk<TW>::N;
+  if constexpr (PER == N) {
+    float t[PER];
+    unpack<TW>(load_chunk(w + col, cols - col), t);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = t[e] + offset;
+  } else {  // (fp32 weights of a row in 16 bits: two chunks)
+#pragma unroll
+    for (int i = 0; i < N / PER; ++i) {
+      float t[PER];
+      unpack<TW>(load_chunk(w + col + i * PER, cols - col - i * PER), t);
+#pragma unroll
+      for (int e = 0; e < PER; ++e) v[i * PER + e] = t[e] + offset;
+    }
+  }
+}
+
+// Sum over the LANES threads of a row, the same bits in all of them.  LANES > 64: `room` holds a sum of every wavefront of the row; contains
+// a barrier.
+template <int LANES>
+__device__ __forceinline__ double row_sum(double v, double* room) {
+#pragma unroll
+  for (int m = LANES < 64 ? LANES / 2 : 32; m; m >>= 1) v += __shfl_xor(v, m);
+  if constexpr (LANES > 64) {
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = room[0];
+#pragma unroll
+    for (int i = 1; i < LANES / 64; ++i) v += room[i];
+  }
+  return v;
+}
+
+// LANES threads a row, CHUNKS chunks of 16 bytes a thread; 256 threads, or as many as a row has.  STREAM: x, residual and what is written pass
+// the caches by.
+template <typename T, typename TW, int LANES, int CHUNKS, bool STREAM>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(const NormArgs p) {
+  constexpr int N = Chunk<T>::N, ROWS = LANES > 256 ? 1 : 256 / LANES, BLOCKS = LANES * CHUNKS * N / kBlock;
+  __shared__ double room[LANES > 64 ? LANES / 64 : 1];
+  __shared__ __attribute__((aligned(16))) unsigned char codes[ROWS > 1 ? BLOCKS * ROWS : 4];
+  const int tid = threadIdx.x, lane = tid % LANES, mine = tid / LANES;
+  const int row0 = blockIdx.x * ROWS, row = row0 + mine;
+  const bool active = row < p.rows;
+  const long long at = active ? row : p.rows - 1;  // (a thread without a row reads the last one and writes nothing)
+  const T* x = reinterpret_cast<const T*>(p.x) + at * p.ldx;
+
+  u32x4 h[CHUNKS];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int col = (i * LANES + lane) * N;
+    h[i] = load_chunk<T, STREAM>(x + col, p.cols - col);
+  }
+  if (p.residual) {
+    const T* r = reinterpret_cast<const T*>(p.residual) + at * p.ldr;
+    u32x4 other[CHUNKS];
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int col = (i * LANES + lane) * N;
+      other[i] = load_chunk<T, STREAM>(r + col, p.cols - col);
+    }
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      float a[N], b[N];
+      unpack<T>(h[i], a);
+      unpack<T>(other[i], b);
+#pragma unroll
+      for (int e = 0; e < N; ++e) a[e] += b[e];
+      h[i] = pack<T>(a);
+    }
+  }
+  if (p.sum && active) {
+    T* s = reinterpret_cast<T*>(p.sum) + at * p.lds;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int col = (i * LANES + lane) * N;
+      store_chunk<T, STREAM>(s + col, p.cols - col, h[i]);
+    }
+  }
+  double squares = 0.0;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    float v[N];
+    unpack<T>(h[i], v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) squares = __builtin_fma((double)v[e], (double)v[e], squares);
+  }
+  squares = row_sum<LANES>(squares, room);
+  const float rstd = (float)(1.0 / sqrt(squares / p.cols + (double)p.eps));
+  if (p.rstd && active && lane == 0) p.rstd[row] = rstd;
+
+  const TW* weight = reinterpret_cast<const TW*>(p.weight);
+  T* y = p.y ? reinterpret_cast<T*>(p.y) + at * p.ldy : nullptr;
+  unsigned char* values = p.values ? p.values + at * p.stride_values : nullptr;
+  const int filled = (p.cols + kBlock - 1) / kBlock * kBlock;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int col = (i * LANES + lane) * N;
+    float v[N], w[N];
+    unpack<T>(h[i], v);
+    load_weights<TW, N>(weight, col, p.cols, p.offset, w);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = v[e] * rstd * w[e];
+    if (y && active) store_chunk<T, STREAM>(y + col, p.cols - col, pack<T>(v));
+    if (values) {  // (the same for all lanes)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (col + e >= p.cols) v[e] = 0.0f;  // (0 * NaN of a row's statistics, were they left)
+      const int code = scale_code(largest_of_block<N>(v), p.format), block = col / kBlock;
+      if (col < filled) {
+        if (active) store_elements<N>(values, col, p.format, v, code);
+        if (col % kBlock == 0) {
+          if constexpr (ROWS > 1)
+            codes[block * ROWS + mine] = (unsigned char)code;
+          else
+            p.scales[(long long)block * p.stride_scales + row] = (unsigned char)code;
+        }
+      }
+    }
+  }
+  if constexpr (ROWS > 1) {
+    if (!p.values) return;
+    __syncthreads();
+    constexpr int WORDS = ROWS / 4;
+    for (int i = tid; i < filled / kBlock * WORDS; i += 256) {
+      const int block = i / WORDS, first = i % WORDS * 4;
+      unsigned char* to = p.scales + (long long)block * p.stride_scales + row0 + first;
+      const unsigned char* from = codes + block * ROWS + first;
+      if (row0 + first + 4 <= p.rows)
+        *reinterpret_cast<unsigned*>(to) = *reinterpret_cast<const unsigned*>(from);
+      else
+        for (int r = 0; row0 + first + r < p.rows; ++r) to[r] = from[r];
+    }
+  }
+}
+
+template <typename T, typename TW, int LANES, int CHUNKS>
+hipError_t launch_norm(const NormArgs& p, bool far, hipStream_t stream) {
+  constexpr int ROWS = LANES > 256 ? 1 : 256 / LANES;
+  const dim3 grid((unsigned)((p.rows + ROWS - 1) / ROWS)), block(LANES > 256 ? LANES : 256);
+  if (far)
+    hipLaunchKernelGGL((norm_kernel<T, TW, LANES, CHUNKS, true>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((norm_kernel<T, TW, LANES, CHUNKS, false>), grid, block, 0, stream, p);
+  return hipGetLastError();
+}
+// How many lanes share a row.  Many rows: as few as hold it, since every row's lanes wait for one another once.  Few rows: more of them, with a
+// chunk or two each.
+template <typename T, typename TW>
+hipError_t dispatch_norm(const NormArgs& p, bool far, hipStream_t stream) {
+  const int chunks = (int)(blocks_of(p.cols) * kBlock / Chunk<T>::N);
+  const bool few = p.rows < 1024;
+  if (chunks <= 16) return launch_norm<T, TW, 16, 1>(p, far, stream);
+  if (chunks <= 64) return launch_norm<T, TW, 64, 1>(p, far, stream);
+  if (few) {
+    if (chunks <= 256) return launch_norm<T, TW, 256, 1>(p, far, stream);
+    if (chunks <= 512) return launch_norm<T, TW, 256, 2>(p, far, stream);
+  }
+  if (chunks <= 128) return launch_norm<T, TW, 64, 2>(p, far, stream);
+  if (chunks <= 256) return launch_norm<T, TW, 64, 4>(p, far, stream);
+  if (chunks <= 512) return launch_norm<T, TW, 64, 8>(p, far, stream);
+  if (chunks <= 1024) return launch_norm<T, TW, 256, 4>(p, far, stream);
+  if (chunks <= 2048) return launch_norm<T, TW, 256, 8>(p, far, stream);
+  if (chunks <= 4096) return launch_norm<T, TW, 1024, 4>(p, far, stream);
+  return launch_norm<T, TW, 1024, 8>(p, far, stream);
+}
+
+// ---- gradients ------------------------------------------------------------------------------------------------------------
+struct GradArgs {
+  const void* grad_y;
+  const void* h;
+  const float* rstd;
+  const void* weight;
+  const void* grad_sum;  // may be null
+  void* grad_h;
+  float* part;           // [workgroup][cols]; null: no gradient of the weight
+  long long ldg, ldh, lds, ldo;
+  int rows, cols;
+  float offset;
+};
+
+// A workgroup takes every gridDim-th group of rows and keeps its part of the weight's gradient in registers: lanes hold the same columns of
+// every row.  LANES > 64: one row at a time.
+template <typename T, typename TW, int LANES, int CHUNKS>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const GradArgs p) {
+  constexpr int N = Chunk<T>::N, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES, COLS = LANES * CHUNKS * N;
+  __shared__ double room[2][LANES > 64 ? LANES / 64 : 1];
+  __shared__ float meet[ROWS > 1 ? (ROWS - 1) * COLS : 1];
+  const int tid = threadIdx.x, lane = tid % LANES, mine = tid / LANES;
+  const TW* weight = reinterpret_cast<const TW*>(p.weight);
+  float w[CHUNKS][N], total[CHUNKS][N];
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    load_weights<TW, N>(weight, (i * LANES + lane) * N, p.cols, p.offset, w[i]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) total[i][e] = 0.0f;
+  }
+  const int groups = (p.rows + ROWS - 1) / ROWS;
+  int turn = 0;
+  for (int group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
+    const int row = group * ROWS + mine;
+    const bool active = row < p.rows;
+    const long long at = active ? row : p.rows - 1;
+    const T* gy = reinterpret_cast<const T*>(p.grad_y) + at * p.ldg;
+    const T* hh = reinterpret_cast<const T*>(p.h) + at * p.ldh;
+    u32x4 rg[CHUNKS], rh[CHUNKS], rs[CHUNKS];
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int col = (i * LANES + lane) * N;
+      rg[i] = load_chunk<T>(gy + col, p.cols - col);
+      rh[i] = load_chunk<T>(hh + col, p.cols - col);
+    }
+    if (p.grad_sum) {
+      const T* gs = reinterpret_cast<const T*>(p.grad_sum) + at * p.lds;
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) {
+        const int col = (i * LANES + lane) * N;
+        rs[i] = load_chunk<T>(gs + col, p.cols - col);
+      }
+    }
+    const float rstd = p.rstd[at];
+    double dot = 0.0;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      float g[N], h[N], s = 0.0f;
+      unpack<T>(rg[i], g);
+      unpack<T>(rh[i], h);
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float xhat = h[e] * rstd;
+        s += g[e] * w[i][e] * xhat;
+        if (active) total[i][e] += g[e] * xhat;
+      }
+      dot += (double)s;
+    }
+    // (two rooms in turn: a wavefront may be a row ahead of one that still reads)
+    const float mean = (float)(row_sum<LANES>(dot, room[turn]) / p.cols);
+    if (!active) continue;
+    T* out = reinterpret_cast<T*>(p.grad_h) + at * p.ldo;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      const int col = (i * LANES + lane) * N;
+      float g[N], h[N], s[N];
+      unpack<T>(rg[i], g);
+      unpack<T>(rh[i], h);
+      if (p.grad_sum) {
+        unpack<T>(rs[i], s);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) s[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) g[e] = rstd * (g[e] * w[i][e] - h[e] * rstd * mean) + s[e];
+      store_chunk<T>(out + col, p.cols - col, pack<T>(g));
+    }
+  }
+  if (!p.part) return;
+  if constexpr (ROWS > 1) {
+    if (mine > 0) {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) meet[(mine - 1) * COLS + (i * N + e) * LANES + lane] = total[i][e];
+    }
+    __syncthreads();
+    if (mine > 0) return;
+    for (int r = 0; r < ROWS - 1; ++r)
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) total[i][e] += meet[r * COLS + (i * N + e) * LANES + lane];
+  }
+  float* part = p.part + (long long)blockIdx.x * p.cols;
+#pragma unroll
+  for (int i = 0; i < CHUNKS; ++i) {
+    const int col = (i * LANES + lane) * N;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (col + e < p.cols) part[col + e] = total[i][e];
+  }
+}
+
+// The parts of 64 columns: 16 threads add every 16th of them, and one adds what they have, in order.
+template <typename TW>
+__global__ __launch_bounds__(1024) void join_kernel(const float* part, TW* out, int parts, int cols) {
+  __shared__ float meet[16][64];
+  const int lane = threadIdx.x % 64, mine = threadIdx.x / 64, col = blockIdx.x * 64 + lane;
+  float v = 0.0f;
+  if (col < cols) {
+#pragma unroll 8
+    for (int i = mine; i < parts; i += 16) v += part[(long long)i * cols + col];
+  }
+  meet[mine][lane] = v;
+  __syncthreads();
+  if (mine > 0 || col >= cols) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) v += meet[i][lane];
+  out[col] = from_f32<TW>(v);
+}
+
+// Lanes and chunks of a row's gradient; parts: workgroups, and with them rows of the workspace, by the sizes alone.
+struct GradCut {
+  int lanes, chunks, parts;
+};
+// (fp32 rows have twice the chunks: the workspace is sized for either)
+GradCut cut_grad(long long rows, long long cols, int per_chunk) {
+  GradCut c;
+  const long long chunks = (cols + per_chunk - 1) / per_chunk;
+  c.lanes = chunks <= 16 ? 16 : chunks <= 256 ? 64 : chunks <= 1024 ? 256 : 1024;
+  const long long each = (chunks + c.lanes - 1) / c.lanes;
+  c.chunks = each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
+  const long long groups = c.lanes >= 256 ? rows : (rows + 256 / c.lanes - 1) / (256 / c.lanes);
+  c.parts = (int)std::min<long long>(groups, 1024);
+  return c;
+}
+
+template <typename T, typename TW, int LANES, int CHUNKS>
+hipError_t launch_grad(const GradArgs& p, int parts, void* grad_weight, hipStream_t stream) {
+  hipLaunchKernelGGL((grad_kernel<T, TW, LANES, CHUNKS>), dim3((unsigned)parts), dim3(LANES > 256 ? LANES : 256), 0, stream, p);
+  if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.part) return e;
+  hipLaunchKernelGGL((join_kernel<TW>), dim3((unsigned)((p.cols + 63) / 64)), dim3(1024), 0, stream, (const float*)p.part,
+                     reinterpret_cast<TW*>(grad_weight), parts, p.cols);
+  return hipGetLastError();
+}
+template <typename T, typename TW>
+hipError_t dispatch_grad(const GradArgs& p, void* grad_weight, hipStream_t stream) {
+  const GradCut c = cut_grad(p.rows, p.cols, Chunk<T>::N);
+  if (c.lanes == 16) return launch_grad<T, TW, 16, 1>(p, c.parts, grad_weight, stream);
+  if (c.lanes == 64) {
+    if (c.chunks == 1) return launch_grad<T, TW, 64, 1>(p, c.parts, grad_weight, stream);
+    if (c.chunks == 2) return launch_grad<T, TW, 64, 2>(p, c.parts, grad_weight, stream);
+    return launch_grad<T, TW, 64, 4>(p, c.parts, grad_weight, stream);
+  }
+  if (c.lanes == 256) {
+    if (c.chunks <= 2) return launch_grad<T, TW, 256, 2>(p, c.parts, grad_weight, stream);
+    return launch_grad<T, TW, 256, 4>(p, c.parts, grad_weight, stream);
+  }
+  if (c.chunks <= 4) return launch_grad<T, TW, 1024, 4>(p, c.parts, grad_weight, stream);
+  return launch_grad<T, TW, 1024, 8>(p, c.parts, grad_weight, stream);
+}
+
+hidet_status_t check_norm(int dtype, int weight_dtype, long long rows, long long cols) {
+  if (dtype < 0 || dtype > 2 || weight_dtype < 0 || weight_dtype > 2 || rows < 0 || cols < 0) return HIDET_ERR_INVALID_ARG;
+  if (weight_dtype != dtype && weight_dtype != HIDET_F32) return HIDET_ERR_UNSUPPORTED;
+  if (rows >= kMaxSide || cols > kMaxCols) return HIDET_ERR_UNSUPPORTED;
+  return HIDET_OK;
+}
+// `out` may be `in` itself, with the same rows
+bool in_place_ok(const void* out, long long ld_out, const void* in, long long ld_in, long long rows) {
+  return !out || out != in || rows <= 1 || ld_out == ld_in;
+}
+
+template <template <typename, typename> class Call, class... A>
+hipError_t by_types(int dtype, int weight_dtype, A&&... a) {
+  if (dtype == HIDET_F32) return Call<float, float>::run(a...);
+  if (dtype == HIDET_F16) return weight_dtype == HIDET_F32 ? Call<f16, float>::run(a...) : Call<f16, f16>::run(a...);
+  return weight_dtype == HIDET_F32 ? Call<bf16, float>::run(a...) : Call<bf16, bf16>::run(a...);
+}
+template <typename T, typename TW>
+struct Norm {
+  static hipError_t run(const NormArgs& p, bool far, hipStream_t s) { return dispatch_norm<T, TW>(p, far, s); }
+};
+template <typename T, typename TW>
+struct Grad {
+  static hipError_t run(const GradArgs& p, void* grad_weight, hipStream_t s) { return dispatch_grad<T, TW>(p, grad_weight, s); }
+};
+
+template <typename TW>
+__global__ __launch_bounds__(256) void zero_kernel(TW* out, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) out[i] = TW(0.0f);
+}
+
+}  // namespace
+
+extern "C" {
+
+hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx,
+                              const void* residual, int64_t ld_residual, const void* weight, float eps, float offset, void* sum,
+                              int64_t ld_sum, void* y, int64_t ldy, const hidet_mx_t* quantized, float* rstd, void* stream) {
+  hidet_status_t st = check_norm(dtype, weight_dtype, rows, cols);
+  if (st != HIDET_OK) return st;
+  if (!(eps >= 0.0f) || !std::isfinite(eps) || !std::isfinite(offset)) return HIDET_ERR_INVALID_ARG;
+  if (!y && !quantized) return HIDET_ERR_INVALID_ARG;
+  if (quantized)
+    if (st = check_mx(quantized, rows, cols); st != HIDET_OK) return st;
+  if (rows == 0 || cols == 0) return HIDET_OK;
+  if (!weight) return HIDET_ERR_INVALID_ARG;
+  if (st = check_rows(x, dtype, rows, cols, ldx); st != HIDET_OK) return st;
+  if (residual)
+    if (st = check_rows(residual, dtype, rows, cols, ld_residual); st != HIDET_OK) return st;
+  if (sum)
+    if (st = check_rows(sum, dtype, rows, cols, ld_sum); st != HIDET_OK) return st;
+  if (y)
+    if (st = check_rows(y, dtype, rows, cols, ldy); st != HIDET_OK) return st;
+  if (!is_aligned(weight, size_of(weight_dtype)) || !is_aligned(rstd, 4)) return HIDET_ERR_ALIGNMENT;
+  if (!in_place_ok(sum, ld_sum, x, ldx, rows) || !in_place_ok(sum, ld_sum, residual, ld_residual, rows) ||
+      !in_place_ok(y, ldy, x, ldx, rows) || !in_place_ok(y, ldy, residual, ld_residual, rows) || (sum && sum == y))
+    return HIDET_ERR_INVALID_ARG;
+  NormArgs p{};
+  p.x = x;
+  p.residual = residual;
+  p.weight = weight;
+  p.sum = sum;
+  p.y = y;
+  p.rstd = rstd;
+  p.ldx = ldx;
+  p.ldr = ld_residual;
+  p.lds = ld_sum;
+  p.ldy = ldy;
+  p.rows = (int)rows;
+  p.cols = (int)cols;
+  p.eps = eps;
+  p.offset = offset;
+  if (quantized) {
+    p.values = reinterpret_cast<unsigned char*>(quantized->values);
+    p.scales = reinterpret_cast<unsigned char*>(quantized->scales);
+    p.stride_values = quantized->stride_values;
+    p.stride_scales = quantized->stride_scales;
+    p.format = quantized->format;
+  }
+  const hipError_t e = by_types<Norm>(dtype, weight_dtype, p, false, (hipStream_t)stream);
+  return e == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
+}
+
+int64_t hidet_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
+  if (rows <= 0 || cols <= 0 || rows >= kMaxSide || cols > kMaxCols) return 0;
+  return 4LL * cols * std::max(cut_grad(rows, cols, 4).parts, cut_grad(rows, cols, 8).parts);
+}
+
+hidet_status_t hidet_rms_norm_backward(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* grad_y, int64_t ld_grad_y,
+                                       const void* h, int64_t ldh, const float* rstd, const void* weight, float offset,
+                                       const void* grad_sum, int64_t ld_grad_sum, void* grad_h, int64_t ld_grad_h, void* grad_weight,
+                                       void* workspace, int64_t workspace_bytes, void* stream) {
+  hidet_status_t st = check_norm(dtype, weight_dtype, rows, cols);
+  if (st != HIDET_OK) return st;
+  if (!std::isfinite(offset) || workspace_bytes < 0) return HIDET_ERR_INVALID_ARG;
+  if (!is_aligned(grad_weight, size_of(weight_dtype))) return HIDET_ERR_ALIGNMENT;
+  const hipStream_t s = (hipStream_t)stream;
+  if (cols == 0) return HIDET_OK;
+  if (rows == 0) {
+    if (!grad_weight) return HIDET_OK;
+    const dim3 grid((unsigned)((cols + 255) / 256));
+    if (weight_dtype == HIDET_F32)
+      hipLaunchKernelGGL((zero_kernel<float>), grid, dim3(256), 0, s, reinterpret_cast<float*>(grad_weight), (int)cols);
+    else  // (the zeros of both types are alike)
+      hipLaunchKernelGGL((zero_kernel<f16>), grid, dim3(256), 0, s, reinterpret_cast<f16*>(grad_weight), (int)cols);
+    return hipGetLastError() == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
+  }
+  if (!weight || !rstd) return HIDET_ERR_INVALID_ARG;
+  if (st = check_rows(grad_y, dtype, rows, cols, ld_grad_y); st != HIDET_OK) return st;
+  if (st = check_rows(h, dtype, rows, cols, ldh); st != HIDET_OK) return st;
+  if (grad_sum)
+    if (st = check_rows(grad_sum, dtype, rows, cols, ld_grad_sum); st != HIDET_OK) return st;
+  if (st = check_rows(grad_h, dtype, rows, cols, ld_grad_h); st != HIDET_OK) return st;
+  if (!is_aligned(weight, size_of(weight_dtype)) || !is_aligned(rstd, 4)) return HIDET_ERR_ALIGNMENT;
+  if (!in_place_ok(grad_h, ld_grad_h, grad_y, ld_grad_y, rows) || !in_place_ok(grad_h, ld_grad_h, grad_sum, ld_grad_sum, rows) || grad_h == h)
+    return HIDET_ERR_INVALID_ARG;
+  if (grad_weight) {
+    if (!workspace || workspace_bytes < hidet_rms_norm_backward_workspace_bytes(rows, cols)) return HIDET_ERR_INVALID_ARG;
+    if (!is_aligned(workspace, 16)) return HIDET_ERR_ALIGNMENT;
+  }
+  GradArgs p{};
+  p.grad_y = grad_y;
+  p.h = h;
+  p.rstd = rstd;
+  p.weight = weight;
+  p.grad_sum = grad_sum;
+  p.grad_h = grad_h;
+  p.part = grad_weight ? reinterpret_cast<float*>(workspace) : nullptr;
+  p.ldg = ld_grad_y;
+  p.ldh = ldh;
+  p.lds = ld_grad_sum;
+  p.ldo = ld_grad_h;
+  p.rows = (int)rows;
+  p.cols = (int)cols;
+  p.offset = offset;
+  const hipError_t e = by_types<Grad>(dtype, weight_dtype, p, grad_weight, s);
+  return e == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
+}
+
+}  // extern "C"
