@@ -603,7 +603,7 @@ int64_t hidet_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t f
  * wanted, and no workspace is.  Sums over rows are fp32, in an order that depends on the sizes alone: no atomics.  The workspace:
  * 16-byte aligned, HIDET_ERR_INVALID_ARG if it is smaller than hidet_rms_norm_backward_workspace_bytes.
  * Both: rows or cols of 0 is an OK no-op, but for grad_weight of no rows, which is 0.  HIDET_ERR_UNSUPPORTED: cols above 32768, rows of 2^29 or
- * more, rows * ld beyond 2^47 elements.
+ * more, leading dimensions of 2^32 or more, rows * ld beyond 2^47 elements.
  */
 hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx,
                               const void* residual, int64_t ld_residual, const void* weight, float eps, float offset, void* sum,

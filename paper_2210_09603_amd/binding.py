@@ -256,6 +256,21 @@ def _attn():
     return _attention_calls
 
 
+def _load_mx_calls(L):
+    entry = (L.hidet_rms_norm, L.hidet_rms_norm_backward, L.hidet_mx_quantize, L.hidet_mx_dequantize, L.hidet_mx_gemm)
+    return _host_module().MxCalls(tuple(ctypes.cast(f, _vp).value for f in entry), hidet_mx_t, hidet_epilogue_t, *_of_the_process())
+
+
+_mx_calls = None
+
+
+def _mxc():
+    global _mx_calls
+    if _mx_calls is None:
+        _mx_calls = _load_mx_calls(lib())
+    return _mx_calls
+
+
 def _check(status, where):
     if status != 0:
         raise HidetError(status, where)
@@ -978,6 +993,14 @@ def _weight(w, cols):
 def hidet_rms_norm(x, weight, y=None, residual=None, sum=None, quantized=None, rstd=None, eps=1e-6, offset=0.0, stream=None):
     """y = h * rstd * (offset + weight) with h = x + residual and rstd = 1 / sqrt(mean(h^2) + eps), over the last axis of x; y (like x),
     quantized (make_mx) or both are written, and sum (h, like x) and rstd (float32, one a row) where given."""
+    st = (_mx_calls or _mxc()).rms_norm(x, weight, y, residual, sum, quantized, rstd, eps, offset, stream)
+    if st < 0:
+        _rms_norm(x, weight, y, residual, sum, quantized, rstd, eps, offset, stream)
+    else:
+        _check(st, "hidet_rms_norm")
+
+
+def _rms_norm(x, weight, y, residual, sum, quantized, rstd, eps, offset, stream):
     rows, cols, (ldx, ldr, lds, ldy) = _norm_rows(x, residual, sum, y)
     device, handle = _on((x, weight, y, residual, sum, rstd) + _mx(quantized, (rows, cols)), stream)
     if rstd is not None and (rstd.dtype != torch.float32 or rstd.numel() != rows or not rstd.is_contiguous()):
@@ -991,6 +1014,14 @@ def hidet_rms_norm(x, weight, y=None, residual=None, sum=None, quantized=None, r
 def hidet_rms_norm_backward(grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum=None, offset=0.0, stream=None):
     """Writes grad_h (like h), and grad_weight (like weight) unless it is None, from grad_y and what comes down the residual stream
     (grad_sum); h and rstd are those of the forward call (its sum, or its x)."""
+    st = (_mx_calls or _mxc()).rms_norm_backward(grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum, offset, stream)
+    if st < 0:
+        _rms_norm_backward(grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum, offset, stream)
+    else:
+        _check(st, "hidet_rms_norm_backward")
+
+
+def _rms_norm_backward(grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum, offset, stream):
     rows, cols, (ldh, ldg, lds, ldo) = _norm_rows(h, grad_y, grad_sum, grad_h)
     if rstd.dtype != torch.float32 or rstd.numel() != rows or not rstd.is_contiguous():
         raise ValueError("rstd must be a dense float32 tensor of %d elements" % rows)
@@ -1013,6 +1044,14 @@ def hidet_rms_norm_backward_workspace_bytes(rows, cols):
 def hidet_mx_quantize(x, by_rows=None, by_columns=None, stream=None):
     """x [rows, cols] into blocks of 32 along its rows (by_rows, make_mx(rows, cols, ...)), along its columns (by_columns, make_mx(cols, rows,
     ...): x transposed), or both."""
+    st = (_mx_calls or _mxc()).mx_quantize(x, by_rows, by_columns, stream)
+    if st < 0:
+        _mx_quantize(x, by_rows, by_columns, stream)
+    else:
+        _check(st, "hidet_mx_quantize")
+
+
+def _mx_quantize(x, by_rows, by_columns, stream):
     if x.dim() != 2:
         raise ValueError("x must be [rows, cols]")
     rows, cols = x.shape
@@ -1024,6 +1063,14 @@ def hidet_mx_quantize(x, by_rows=None, by_columns=None, stream=None):
 
 def hidet_mx_dequantize(x, y, stream=None):
     """y [rows, cols] = the numbers that x (make_mx) stands for."""
+    st = (_mx_calls or _mxc()).mx_dequantize(x, y, stream)
+    if st < 0:
+        _mx_dequantize(x, y, stream)
+    else:
+        _check(st, "hidet_mx_dequantize")
+
+
+def _mx_dequantize(x, y, stream):
     device, handle = _on((y,) + _mx(x, y.shape), stream)
     with device:
         st = lib().hidet_mx_dequantize(y.shape[0], y.shape[1], x, _dtype(y), _ptr(y), _ld(y), handle)
@@ -1032,6 +1079,14 @@ def hidet_mx_dequantize(x, y, stream=None):
 
 def hidet_mx_gemm(A, B, C, epilogue=None, workspace=None, stream=None):
     """C [M, N] = epilogue(A . B^T); A and B are make_mx(M, K, ...) and make_mx(N, K, ...), in any of the formats."""
+    st = (_mx_calls or _mxc()).mx_gemm(A, B, C, epilogue, workspace, stream)
+    if st < 0:
+        _mx_gemm(A, B, C, epilogue, workspace, stream)
+    else:
+        _check(st, "hidet_mx_gemm")
+
+
+def _mx_gemm(A, B, C, epilogue, workspace, stream):
     (M, K), (N, _) = A.shape, B.shape
     if C.dim() != 2:
         raise ValueError("C must be [M, N]")

@@ -109,7 +109,8 @@ bool whole32(PyObject* o, int32_t& v) {
 // The epilogue descriptor of a call, borrowed from the ctypes structure for as long as this lives.
 class Epilogue {
  public:
-  Epilogue(const Calls* c, PyObject* o) {
+  template <class C>
+  Epilogue(const C* c, PyObject* o) {
     if (o == Py_None) {
       ok_ = true;
     } else if ((PyObject*)Py_TYPE(o) == c->epilogue_type) {
@@ -408,7 +409,8 @@ P* address(const at::Tensor* x) {
 int64_t bytes_of(const at::Tensor* x) { return x ? x->numel() * (int64_t)x->element_size() : 0; }
 
 // The stream given, or the current one; the tensors' device has to be the current one.
-bool stream_on(const AttentionCalls* c, PyObject* o, const Tensors& t, void*& out) {
+template <class C>
+bool stream_on(const C* c, PyObject* o, const Tensors& t, void*& out) {
   bool ok = false;
   PyObject* bad = PyObject_CallNoArgs(c->in_bad_fork);
   if (bad == Py_False) {
@@ -672,6 +674,253 @@ void attention_calls_dealloc(PyObject* self) {
   Py_TYPE(self)->tp_free(self);
 }
 
+// ---- norms, matrices in 8 and 4 bits, and their products --------------------------------------------------------------------------
+struct MxCalls {
+  PyObject_HEAD
+  decltype(&hidet_rms_norm) norm;
+  decltype(&hidet_rms_norm_backward) norm_backward;
+  decltype(&hidet_mx_quantize) quantize;
+  decltype(&hidet_mx_dequantize) dequantize;
+  decltype(&hidet_mx_gemm) gemm;
+  PyObject *mx_type, *epilogue_type, *in_bad_fork, *get_device, *get_stream;
+};
+
+// The descriptor of a matrix in blocks, borrowed from the ctypes structure for as long as this lives; None: get() is null.
+class MxArg {
+ public:
+  MxArg(const MxCalls* c, PyObject* o, bool optional = false) {
+    if (o == Py_None) {
+      ok_ = optional;
+      return;
+    }
+    if ((PyObject*)Py_TYPE(o) != c->mx_type) return;
+    int64_t device = -1;
+    PyObject* d = PyObject_GetAttrString(o, "_device");
+    PyObject* s = PyObject_GetAttrString(o, "shape");
+    const bool known = d && s && whole(d, device) && pair(s, shape_) && device >= 0;
+    Py_XDECREF(d);
+    Py_XDECREF(s);
+    device_ = device;
+    if (!known || PyObject_GetBuffer(o, &view_, PyBUF_SIMPLE) != 0) {
+      PyErr_Clear();
+      return;
+    }
+    held_ = true;
+    ok_ = view_.len == (Py_ssize_t)sizeof(hidet_mx_t);
+  }
+  ~MxArg() {
+    if (held_) PyBuffer_Release(&view_);
+  }
+  MxArg(const MxArg&) = delete;
+  MxArg& operator=(const MxArg&) = delete;
+  const hidet_mx_t* get() const { return held_ ? static_cast<const hidet_mx_t*>(view_.buf) : nullptr; }
+  bool ok() const { return ok_; }
+  int64_t rows() const { return shape_[0]; }
+  int64_t cols() const { return shape_[1]; }
+  // none, or of that shape and beside those tensors
+  bool fits(const Tensors& t, int64_t rows, int64_t cols) const {
+    return ok_ && (!held_ || (t.on(device_) && shape_[0] == rows && shape_[1] == cols));
+  }
+
+ private:
+  Py_buffer view_;
+  int64_t shape_[2] = {0, 0}, device_ = -1;
+  bool held_ = false, ok_ = false;
+};
+
+// Rows of tensors of one shape and type; a missing one has a leading dimension of 0.
+struct RowArgs {
+  int64_t rows = 0, cols = 0;
+  int32_t dtype = -1;
+  bool add(Tensors& t, PyObject* o, bool optional, void*& at, int64_t& ld) {
+    at = nullptr;
+    ld = 0;
+    const at::Tensor* x = t.get(o, optional);
+    if (!t.ok) return false;
+    if (!x) return true;
+    const Arg a(o);
+    int64_t r, c;
+    if (!a || !a.rows(r, c, ld)) return false;
+    if (dtype < 0) {
+      dtype = a.dtype;
+      rows = r;
+      cols = c;
+      first_ = x;
+    } else if (a.dtype != dtype || x->sizes() != first_->sizes()) {
+      return false;
+    }
+    at = x->data_ptr();
+    return true;
+  }
+
+ private:
+  const at::Tensor* first_ = nullptr;
+};
+const at::Tensor* weight_of(Tensors& t, PyObject* o, int64_t cols, bool optional = false) {
+  const at::Tensor* w = t.get(o, optional);
+  if (w && (w->dim() != 1 || w->size(0) != cols || !w->is_contiguous() || type_of(w) < 0)) {
+    t.ok = false;
+    return nullptr;
+  }
+  return w;
+}
+// fp32, one a row, in any shape
+float* of_rows(Tensors& t, PyObject* o, int64_t rows, bool optional) {
+  const at::Tensor* x = t.get(o, optional);
+  if (x && (x->scalar_type() != at::kFloat || x->numel() != rows || !x->is_contiguous())) t.ok = false;
+  return t.ok ? address<float>(x) : nullptr;
+}
+
+// rms_norm(x, weight, y, residual, sum, quantized, rstd, eps, offset, stream)
+PyObject* call_rms_norm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 10)) return nullptr;
+  const MxCalls* c = reinterpret_cast<const MxCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    RowArgs r;
+    void *x, *y, *residual, *sum;
+    int64_t ldx, ldy, ldr, lds;
+    if (!r.add(t, a[0], false, x, ldx) || !r.add(t, a[2], true, y, ldy) || !r.add(t, a[3], true, residual, ldr) || !r.add(t, a[4], true, sum, lds))
+      return kGeneral;
+    const at::Tensor* w = weight_of(t, a[1], r.cols);
+    float* rstd = t.ok ? of_rows(t, a[6], r.rows, true) : nullptr;
+    const MxArg q(c, a[5], true);
+    double eps, offset;
+    void* stream;
+    if (!t.ok || !q.fits(t, r.rows, r.cols) || !real(a[7], eps) || !real(a[8], offset) || !stream_on(c, a[9], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->norm(r.dtype, type_of(w), r.rows, r.cols, x, ldx, residual, ldr, w->data_ptr(), (float)eps, (float)offset, sum, lds, y, ldy, q.get(),
+                     rstd, stream);
+    });
+  });
+}
+
+// rms_norm_backward(grad_y, h, rstd, weight, grad_h, grad_weight, workspace, grad_sum, offset, stream)
+PyObject* call_rms_norm_backward(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 10)) return nullptr;
+  const MxCalls* c = reinterpret_cast<const MxCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    RowArgs r;
+    void *h, *gy, *gh, *gs;
+    int64_t ldh, ldg, ldo, lds;
+    if (!r.add(t, a[1], false, h, ldh) || !r.add(t, a[0], false, gy, ldg) || !r.add(t, a[4], false, gh, ldo) || !r.add(t, a[7], true, gs, lds))
+      return kGeneral;
+    const float* rstd = of_rows(t, a[2], r.rows, false);
+    const at::Tensor* w = t.ok ? weight_of(t, a[3], r.cols) : nullptr;
+    const at::Tensor* gw = t.ok ? weight_of(t, a[5], r.cols, true) : nullptr;
+    const at::Tensor* ws = t.ok ? t.workspace(a[6]) : nullptr;
+    double offset;
+    void* stream;
+    if (!t.ok || (gw && gw->scalar_type() != w->scalar_type()) || !real(a[8], offset) || !stream_on(c, a[9], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->norm_backward(r.dtype, type_of(w), r.rows, r.cols, gy, ldg, h, ldh, rstd, w->data_ptr(), (float)offset, gs, lds, gh, ldo,
+                              address<void>(gw), address<void>(ws), bytes_of(ws), stream);
+    });
+  });
+}
+
+// mx_quantize(x, by_rows, by_columns, stream)
+PyObject* call_mx_quantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 4)) return nullptr;
+  const MxCalls* c = reinterpret_cast<const MxCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    const at::Tensor* x = t.get(a[0]);
+    const Arg arg(a[0]);
+    int64_t ld;
+    if (!x || !arg || x->dim() != 2 || !arg.ld(ld)) return kGeneral;
+    const MxArg by_rows(c, a[1], true), by_columns(c, a[2], true);
+    void* stream;
+    if (!by_rows.fits(t, x->size(0), x->size(1)) || !by_columns.fits(t, x->size(1), x->size(0)) || !stream_on(c, a[3], t, stream)) return kGeneral;
+    return without_lock([&] { return c->quantize(arg.dtype, x->size(0), x->size(1), x->data_ptr(), ld, by_rows.get(), by_columns.get(), stream); });
+  });
+}
+
+// mx_dequantize(x, y, stream)
+PyObject* call_mx_dequantize(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 3)) return nullptr;
+  const MxCalls* c = reinterpret_cast<const MxCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    const MxArg x(c, a[0]);
+    const at::Tensor* y = t.get(a[1]);
+    const Arg arg(a[1]);
+    int64_t ld;
+    void* stream;
+    if (!y || !arg || y->dim() != 2 || !arg.ld(ld) || !x.fits(t, y->size(0), y->size(1)) || !stream_on(c, a[2], t, stream)) return kGeneral;
+    return without_lock([&] { return c->dequantize(y->size(0), y->size(1), x.get(), arg.dtype, y->data_ptr(), ld, stream); });
+  });
+}
+
+// mx_gemm(A, B, C, epilogue, workspace, stream)
+PyObject* call_mx_gemm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
+  if (!expect(n, 6)) return nullptr;
+  const MxCalls* c = reinterpret_cast<const MxCalls*>(self);
+  return guarded([&]() -> int {
+    Tensors t;
+    const MxArg x(c, a[0]), w(c, a[1]);
+    const at::Tensor* y = t.get(a[2]);
+    const Arg arg(a[2]);
+    int64_t ld;
+    if (!y || !arg || y->dim() != 2 || !arg.ld(ld) || !x.ok() || !w.ok()) return kGeneral;
+    const int64_t m = x.rows(), rows = w.rows(), k = x.cols();
+    if (!x.fits(t, m, k) || !w.fits(t, rows, k) || y->size(0) != m || y->size(1) != rows) return kGeneral;
+    const at::Tensor* ws = t.workspace(a[4]);
+    if (a[3] != Py_None) {  // (what the epilogue reads is beside the others)
+      PyObject* kept = PyObject_GetAttrString(a[3], "_keep");
+      if (kept && PyTuple_CheckExact(kept))
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(kept); ++i) t.get(PyTuple_GET_ITEM(kept, i), true);
+      else
+        t.ok = false;
+      Py_XDECREF(kept);
+      PyErr_Clear();
+    }
+    const Epilogue e(c, a[3]);
+    void* stream;
+    if (!t.ok || !e.plain() || !stream_on(c, a[5], t, stream)) return kGeneral;
+    return without_lock([&] {
+      return c->gemm(arg.dtype, m, rows, k, x.get(), w.get(), y->data_ptr(), ld, e.get(), address<void>(ws), bytes_of(ws), stream);
+    });
+  });
+}
+
+// MxCalls((addresses of the five entry points), matrix type, epilogue type, in_bad_fork, get_device, get_stream)
+PyObject* mx_calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
+  unsigned long long at[5];
+  PyObject *mx_type, *epilogue_type, *in_bad_fork, *get_device, *get_stream;
+  if (!PyArg_ParseTuple(args, "(KKKKK)OOOOO", &at[0], &at[1], &at[2], &at[3], &at[4], &mx_type, &epilogue_type, &in_bad_fork, &get_device, &get_stream))
+    return nullptr;
+  for (unsigned long long a : at) {
+    if (a == 0) {
+      PyErr_SetString(PyExc_ValueError, "null entry point");
+      return nullptr;
+    }
+  }
+  MxCalls* c = reinterpret_cast<MxCalls*>(type->tp_alloc(type, 0));
+  if (!c) return nullptr;
+  c->norm = reinterpret_cast<decltype(c->norm)>((uintptr_t)at[0]);
+  c->norm_backward = reinterpret_cast<decltype(c->norm_backward)>((uintptr_t)at[1]);
+  c->quantize = reinterpret_cast<decltype(c->quantize)>((uintptr_t)at[2]);
+  c->dequantize = reinterpret_cast<decltype(c->dequantize)>((uintptr_t)at[3]);
+  c->gemm = reinterpret_cast<decltype(c->gemm)>((uintptr_t)at[4]);
+  c->mx_type = Py_NewRef(mx_type);
+  c->epilogue_type = Py_NewRef(epilogue_type);
+  c->in_bad_fork = Py_NewRef(in_bad_fork);
+  c->get_device = Py_NewRef(get_device);
+  c->get_stream = Py_NewRef(get_stream);
+  return reinterpret_cast<PyObject*>(c);
+}
+void mx_calls_dealloc(PyObject* self) {
+  MxCalls* c = reinterpret_cast<MxCalls*>(self);
+  Py_XDECREF(c->mx_type);
+  Py_XDECREF(c->epilogue_type);
+  Py_XDECREF(c->in_bad_fork);
+  Py_XDECREF(c->get_device);
+  Py_XDECREF(c->get_stream);
+  Py_TYPE(self)->tp_free(self);
+}
+
 using Fast = PyObject* (*)(PyObject*, PyObject* const*, Py_ssize_t);
 PyMethodDef method(const char* name, Fast f) { return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}; }
 PyMethodDef g_methods[] = {method("gemm", call_gemm<2>),         method("batched_gemm", call_gemm<3>),
@@ -682,8 +931,12 @@ PyMethodDef g_attention_methods[] = {method("attention", call_attention),       
                                      method("rope", call_rope),                 method("attention_ranges", call_attention_ranges),
                                      method("cache_append", call_cache_append), method("cache_attention", call_cache_attention),
                                      {nullptr, nullptr, 0, nullptr}};
+PyMethodDef g_mx_methods[] = {method("rms_norm", call_rms_norm),       method("rms_norm_backward", call_rms_norm_backward),
+                              method("mx_quantize", call_mx_quantize), method("mx_dequantize", call_mx_dequantize),
+                              method("mx_gemm", call_mx_gemm),         {nullptr, nullptr, 0, nullptr}};
 PyTypeObject g_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyTypeObject g_attention_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+PyTypeObject g_mx_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_host_calls", nullptr, -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -701,12 +954,19 @@ PyMODINIT_FUNC PyInit__host_calls() {
   g_attention_type.tp_new = attention_calls_new;
   g_attention_type.tp_dealloc = attention_calls_dealloc;
   g_attention_type.tp_methods = g_attention_methods;
-  if (PyType_Ready(&g_type) < 0 || PyType_Ready(&g_attention_type) < 0) return nullptr;
+  g_mx_type.tp_name = "_host_calls.MxCalls";
+  g_mx_type.tp_basicsize = sizeof(MxCalls);
+  g_mx_type.tp_flags = Py_TPFLAGS_DEFAULT;
+  g_mx_type.tp_new = mx_calls_new;
+  g_mx_type.tp_dealloc = mx_calls_dealloc;
+  g_mx_type.tp_methods = g_mx_methods;
+  if (PyType_Ready(&g_type) < 0 || PyType_Ready(&g_attention_type) < 0 || PyType_Ready(&g_mx_type) < 0) return nullptr;
   PyObject* m = PyModule_Create(&g_module);
   if (!m) return nullptr;
   // (what this was compiled for: the binding refuses it under another torch or Python, whose tensors it would misread)
   if (PyModule_AddObjectRef(m, "Calls", reinterpret_cast<PyObject*>(&g_type)) < 0 ||
       PyModule_AddObjectRef(m, "AttentionCalls", reinterpret_cast<PyObject*>(&g_attention_type)) < 0 ||
+      PyModule_AddObjectRef(m, "MxCalls", reinterpret_cast<PyObject*>(&g_mx_type)) < 0 ||
       PyModule_AddStringConstant(m, "built_for", HIDET_BUILT_FOR) < 0) {
     Py_DECREF(m);
     return nullptr;

@@ -22,21 +22,69 @@ namespace {
 constexpr long long kMaxLd = 1LL << 32;          // of C and the residual
 constexpr long long kMaxGrid = (1LL << 22) - 1;  // workgroups of up to 512 threads: below 2^32 work items
 
+constexpr int kUnits = 256;                      // compute units
+
+// What a tile takes for a step of 128 k, in us: where each unit has one of them, and, by the unit's time, where there are more.  Both operands in 8
+// bits, one, none.  (K = 4096; 333 x 5120, 1024 x 1024, 4096 x 4096 and 8192 x 8192.)
+struct TileCost {
+  int kernel, rows, cols;
+  float alone[3], among[3], once;  // once: of a tile, its first loads and its stores
+};
+constexpr TileCost kTiles[] = {
+    {KERNEL_TILE_256, 256, 256, {1.60f, 1.45f, 1.05f}, {1.65f, 1.48f, 1.05f}, 5.0f},
+    {KERNEL_TILE_128, 128, 128, {0.57f, 0.50f, 0.34f}, {0.47f, 0.41f, 0.30f}, 2.0f},
+    {KERNEL_TILE_64X128, 64, 128, {0.42f, 0.34f, 0.27f}, {0.48f, 0.26f, 0.19f}, 2.0f},
+    {KERNEL_TILE_64, 64, 64, {0.28f, 0.24f, 0.18f}, {0.35f, 0.31f, 0.16f}, 2.0f},
+};
+constexpr float kJoin = 4.0f;  // us, of the second launch of a product in slices
+
+long long tiles_of(long long M, long long N, long long rows, long long cols) { return (M + rows - 1) / rows * ((N + cols - 1) / cols); }
+
 // `room`: bytes of workspace
-GemmCut cut_gemm(long long M, long long N, long long K, long long room) {
-  (void)K;
-  (void)room;
-  GemmCut c;
-  c.slices = 1;
+GemmCut cut_gemm(long long M, long long N, long long K, int format_a, int format_b, long long room) {
+  const long long steps = std::max(1LL, (K + 127) / 128);
+  const int kind = 2 - (int)is_wide(format_a) - (int)is_wide(format_b);
+  GemmCut c{KERNEL_STREAM_16, 1, 1 << 24, tiles_of(M, N, 16, 16)};
+  long long each = 1;  // steps that a slice is made of
+  float per = 0.0f;    // us that a slice of one step takes
   if (M <= 16) {
-    c.kernel = KERNEL_STREAM_16;
-    c.blocks = (M + 15) / 16 * ((N + 15) / 16);
-  } else if (M <= 64) {
-    c.kernel = KERNEL_STREAM_64;
-    c.blocks = (M + 63) / 64 * ((N + 63) / 64);
+    // (8 wavefronts of a workgroup take a step each: 0.5 us.)  4 x 8192 x 4096, 8 bits by 4: 7.0 us; 64 columns a workgroup 8.0, 64 x 64 tiles 13.8.
+    each = 8;
+    per = 0.06f;
+  } else if (M <= 64 && !is_wide(format_b)) {
+    // 64 x 4096 x 4096, 8 bits by 4 and 4 by 4: 9.6 and 9.2 us, 64 x 64 tiles 13.8 and 11.6.  (By 8 bits: 20.7 and 15.0.)
+    c.kernel = KERNEL_STREAM_16X64;
+    c.blocks = tiles_of(M, N, 16, 64);
+    each = 8;
+    per = 0.09f;
   } else {
-    c.kernel = KERNEL_TILE_128;
-    c.blocks = (M + 127) / 128 * ((N + 127) / 128);
+    float best = 0.0f;
+    for (const TileCost& t : kTiles) {
+      const long long tiles = tiles_of(M, N, t.rows, t.cols);
+      const float rounds = (float)((tiles + kUnits - 1) / kUnits);
+      const float us = rounds * ((float)steps * (tiles <= kUnits ? t.alone[kind] : t.among[kind]) + t.once);
+      if (best == 0.0f || us < best) {
+        best = us;
+        c.kernel = t.kernel;
+        c.blocks = tiles;
+        per = t.alone[kind];
+      }
+    }
+    each = 4;
+  }
+  // Slices of K where that leaves units without work, and saves more than the second launch takes.
+  if (c.blocks <= kUnits / 2) {
+    long long slices = std::min<long long>(kUnits / c.blocks, steps / (2 * each));
+    slices = std::min(slices, room / (4 * M * N));
+    if (slices > 1) {
+      const long long slice = ((steps + slices - 1) / slices + each - 1) / each * each;
+      slices = (steps + slice - 1) / slice;
+      if (slices > 1 && (float)(steps - slice) * per > kJoin) {
+        c.slices = (int)slices;
+        c.slice = (int)slice;
+        c.blocks *= slices;
+      }
+    }
   }
   return c;
 }
@@ -62,10 +110,9 @@ hidet_status_t check_epilogue(const hidet_epilogue_t* e, int out, long long M, l
 extern "C" {
 
 int64_t hidet_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t format_a, int32_t format_b) {
-  (void)format_a;
-  (void)format_b;
+  if (format_a < 0 || format_a > HIDET_MX_E2M1 || format_b < 0 || format_b > HIDET_MX_E2M1) return 0;
   if (M <= 0 || N <= 0 || K <= 0 || M >= kMaxSide || N >= kMaxSide || K >= kMaxSide) return 0;
-  const GemmCut c = cut_gemm(M, N, K, 1LL << 62);
+  const GemmCut c = cut_gemm(M, N, K, format_a, format_b, 1LL << 62);
   return c.slices > 1 ? 4LL * c.slices * M * N : 0;
 }
 
@@ -83,7 +130,7 @@ hidet_status_t hidet_mx_gemm(int32_t out, int64_t M, int64_t N, int64_t K, const
   if (ldc >= kMaxLd) return HIDET_ERR_UNSUPPORTED;
   if (epi && epi->residual == C && M > 1 && epi->ld_residual != ldc) return HIDET_ERR_INVALID_ARG;
 
-  const GemmCut c = cut_gemm(M, N, K, workspace ? workspace_bytes : 0);
+  const GemmCut c = cut_gemm(M, N, K, A->format, B->format, workspace ? workspace_bytes : 0);
   if (c.blocks > kMaxGrid) return HIDET_ERR_UNSUPPORTED;
   GemmArgs p{};
   p.a = reinterpret_cast<const unsigned char*>(A->values);
@@ -112,8 +159,7 @@ hidet_status_t hidet_mx_gemm(int32_t out, int64_t M, int64_t N, int64_t K, const
     if (epi->residual) quads = quads && is_aligned(epi->residual, four) && (M == 1 || epi->ld_residual % 4 == 0);
   }
   p.flags |= (quads ? 32u : 0u) | (unsigned)c.slices << 8;
-  const int steps = (p.blocks + 3) / 4;
-  p.slice = (steps + c.slices - 1) / c.slices;
+  p.slice = c.slice;
   if (c.slices > 1) p.c = workspace;
   const hipStream_t s = (hipStream_t)stream;
   hipError_t e = A->format == HIDET_MX_E4M3   ? launch_gemm<HIDET_MX_E4M3>(B->format, c, p, s)

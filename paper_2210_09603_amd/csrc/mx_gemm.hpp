@@ -183,81 +183,75 @@ __device__ __forceinline__ unsigned lds_address(const void* p) {
   return (unsigned)(size_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// One operand of a tile in LDS: ROWS rows of a step of 128 k, and their scales.  Row 64 g + 4 r + f lies in place 64 g + 16 f + r, so that a
-// fragment's rows are neighbours; the chunks of a place are permuted (swz_kc) so that the reads of a fragment spread over the banks.
-template <int FORMAT, int ROWS, int WAVES>
+// One operand of a tile in LDS: ROWS rows of STEPS steps of 128 k, and their scales.  Row 64 g + 4 r + f lies in place 64 g + 16 f + r, so that
+// a fragment's rows are neighbours; the chunks of a place are permuted (swz_kc) so that the reads of a fragment spread over the banks.
+template <int FORMAT, int ROWS, int STEPS, int WAVES>
 struct Panel {
-  static constexpr int CHUNKS = step_bytes(FORMAT) / 16, BYTES = ROWS * CHUNKS * 16, SCALE_BYTES = ROWS * 4;
+  static constexpr int CHUNKS = STEPS * step_bytes(FORMAT) / 16, BYTES = ROWS * CHUNKS * 16, SCALE_BYTES = ROWS * 4 * STEPS;
   static constexpr int LOADS = ROWS * CHUNKS / 64 / WAVES;  // 1 KB each, of a wavefront
-  static constexpr int SCALE_LOADS = ROWS / 64;             // 256 bytes each, of the workgroup
+  static constexpr int PARTS = ROWS / 64;                   // loads of scales a step, 256 bytes each, of the workgroup
   static_assert(LOADS * 64 * WAVES == ROWS * CHUNKS, "whole loads");
   const unsigned char* base;    // of the tile's first row
-  const unsigned char* scales;  // of block 0
+  const unsigned char* scales;  // of the tile's first row, block 0
   unsigned ld_scales;
-  int chunks, blocks;           // of a whole row
-  unsigned offset[LOADS];       // of the lane's chunk of every load
-  int chunk[LOADS];
-  unsigned scale_word;          // 4 times the word of scales that the lane loads, in its block
-  int scale_block;
+  int last_word;                // word of scales, from the tile's first row, that the matrix ends with
+  int blocks;                   // of a row
+  unsigned offset[LOADS];       // of the lane's chunk of every load, in bytes from the tile's first row: below 2^31
 
-  // `part`: which of the workgroup's loads of scales this wavefront makes (any number beyond SCALE_LOADS: none)
-  __device__ __forceinline__ void init(const unsigned char* values, const unsigned char* s, unsigned ld, unsigned ld_s, int row0, int rows,
-                                       int blocks_in_row, int wave, int lane, int part) {
-    base = values + (long long)row0 * ld;
-    scales = s;
-    ld_scales = ld_s;
-    blocks = blocks_in_row;
-    chunks = blocks_in_row * (is_wide(FORMAT) ? 2 : 1);
+  __device__ __forceinline__ Panel(const unsigned char* values, const unsigned char* s, unsigned ld, unsigned ld_s, int row0, int rows, int first_block,
+                                   int blocks_in_row, int wave, int lane)
+      : base(values + (long long)row0 * ld + (long long)first_block * (is_wide(FORMAT) ? 32 : 16)),
+        scales(s + (long long)first_block * ld_s + row0), ld_scales(ld_s), last_word((rows + 3) / 4 - 1 - row0 / 4), blocks(blocks_in_row) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int q = (wave * LOADS + i) * 64 + lane, place = q / CHUNKS;
-      const int row = (place & ~63) + 4 * (place & 15) + ((place >> 4) & 3);
-      chunk[i] = (q % CHUNKS) ^ swz_kc<CHUNKS, 16>(place);
-      offset[i] = (unsigned)min(row, rows - 1 - row0) * ld + chunk[i] * 16;
-    }
-    const int q = part * 64 + lane;
-    scale_block = q / (ROWS / 4);
-    scale_word = 4u * (unsigned)min(row0 / 4 + q % (ROWS / 4), (rows + 3) / 4 - 1);
-  }
-  // The loads of step `step` into a stage at `at` in LDS (scales at `scales_at`).
-  template <bool SCALES>
-  __device__ __forceinline__ void request(int step, unsigned at, unsigned scales_at, unsigned char* smem, int wave, int lane, int part) const {
-    const unsigned char* from = base + (long long)step * (CHUNKS * 16);
-    if ((step + 1) * CHUNKS <= chunks) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) DirectLoad::chunks(from, offset[i], at + (wave * LOADS + i) * 1024);
-    } else {  // the last step: what lies beyond K is 0
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        if (step * CHUNKS + chunk[i] < chunks)
-          DirectLoad::chunks(from, offset[i], at + (wave * LOADS + i) * 1024);
-        else
-          *reinterpret_cast<u32x4*>(smem + (wave * LOADS + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
-      }
-    }
-    if (SCALES && part < SCALE_LOADS) {
-      const int block = min(step * 4 + scale_block, blocks - 1);
-      DirectLoad::words(scales + (long long)step * 4 * ld_scales, (unsigned)(block - step * 4) * ld_scales + scale_word, scales_at + part * 256);
+      const int place = place_of(i, wave, lane), row = (place & ~63) + 4 * (place & 15) + ((place >> 4) & 3);
+      offset[i] = (unsigned)min(row, rows - 1 - row0) * ld + chunk_of(i, wave, lane) * 16;
     }
   }
-  // Fragment f of group g, and the word of scales of group g.
-  static __device__ __forceinline__ Fragment<FORMAT> fragment(const unsigned char* stage, int g, int f, int lane) {
+  static __device__ __forceinline__ int place_of(int load, int wave, int lane) { return ((wave * LOADS + load) * 64 + lane) / CHUNKS; }
+  static __device__ __forceinline__ int chunk_of(int load, int wave, int lane) { return lane % CHUNKS ^ swz_kc<CHUNKS, 16>(place_of(load, wave, lane)); }
+  // The loads of a whole stage to `at` in LDS.
+  __device__ __forceinline__ void request(int stage, unsigned at, int wave) const {
+    const unsigned char* from = base + (long long)stage * (CHUNKS * 16);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) DirectLoad::chunks(from, offset[i], at + (wave * LOADS + i) * 1024);
+  }
+  // The same of the last stage, which K ends in: what lies beyond is 0.  `smem`: `at` as an address.
+  __device__ __forceinline__ void request_end(int stage, unsigned at, unsigned char* smem, int wave, int lane) const {
+    const unsigned char* from = base + (long long)stage * (CHUNKS * 16);
+    const int left = blocks * (is_wide(FORMAT) ? 2 : 1) - stage * CHUNKS;  // chunks
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      if (chunk_of(i, wave, lane) < left)
+        DirectLoad::chunks(from, offset[i], at + (wave * LOADS + i) * 1024);
+      else
+        *reinterpret_cast<u32x4*>(smem + (wave * LOADS + i) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    }
+  }
+  // Part `part` of the scales of step s of a stage.  (Blocks beyond K: the last one.)
+  __device__ __forceinline__ void request_scales(int stage, int s, unsigned at, int part, int lane) const {
+    const int first = min((stage * STEPS + s) * 4, blocks - 1), q = part * 64 + lane;
+    const int block = min(q / (ROWS / 4), blocks - 1 - first), word = min(q % (ROWS / 4), last_word);
+    DirectLoad::words(scales + (long long)first * ld_scales, (unsigned)block * ld_scales + 4u * (unsigned)word, at + (s * PARTS + part) * 256);
+  }
+  // Fragment f of group g for step s of the stage, and the word of scales of group g.
+  static __device__ __forceinline__ Fragment<FORMAT> fragment(const unsigned char* stage, int s, int g, int f, int lane) {
     const int place = 64 * g + 16 * f + lane % 16, swz = swz_kc<CHUNKS, 16>(lane % 16);
     const unsigned char* row = stage + place * (CHUNKS * 16);
     Fragment<FORMAT> x;
-    x.v[0] = *reinterpret_cast<const u32x4*>(row + ((lane / 16) ^ swz) * 16);
-    if constexpr (is_wide(FORMAT)) x.v[1] = *reinterpret_cast<const u32x4*>(row + ((4 + lane / 16) ^ swz) * 16);
+    x.v[0] = *reinterpret_cast<const u32x4*>(row + ((s * (step_bytes(FORMAT) / 16) + lane / 16) ^ swz) * 16);
+    if constexpr (is_wide(FORMAT)) x.v[1] = *reinterpret_cast<const u32x4*>(row + ((s * 8 + 4 + lane / 16) ^ swz) * 16);
     return x;
   }
-  static __device__ __forceinline__ unsigned scale(const unsigned char* stage_scales, int g, int lane) {
-    return *reinterpret_cast<const unsigned*>(stage_scales + (lane / 16) * ROWS + 64 * g + 4 * (lane % 16));
+  static __device__ __forceinline__ unsigned scale(const unsigned char* stage_scales, int s, int g, int lane) {
+    return *reinterpret_cast<const unsigned*>(stage_scales + (s * 4 + lane / 16) * ROWS + 64 * g + 4 * (lane % 16));
   }
 };
 
 // Which tile a workgroup takes: workgroups are handed to the 8 dies in turn; each die, which has an L2 of its own, gets one run of tiles, walked
 // 4 tile rows at a time.
-__device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& i, int& j) {
-  const unsigned total = (unsigned)tiles_m * (unsigned)tiles_n, xcd = blockIdx.x % 8u, slot = blockIdx.x / 8u;
+__device__ __forceinline__ void tile_of(unsigned at, int tiles_m, int tiles_n, int& i, int& j) {
+  const unsigned total = (unsigned)tiles_m * (unsigned)tiles_n, xcd = at % 8u, slot = at / 8u;
   const unsigned each = total / 8u, extra = total % 8u;
   const unsigned w = xcd * each + (xcd < extra ? xcd : extra) + slot;
   const unsigned panel = w / (4u * tiles_n), first = panel * 4u, rows = min(4u, (unsigned)tiles_m - first), within = w - first * tiles_n;
@@ -265,68 +259,10 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& i, int& j
   j = (int)(within / rows);
 }
 
-// Tiles from LDS: WM x WN wavefronts of 64 GM x 64 GN each, two stages of 128 k.
-template <int FA, int FB, int GM, int GN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const GemmArgs p) {
-  constexpr int WAVES = WM * WN, BM = 64 * GM * WM, BN = 64 * GN * WN;
-  using A = Panel<FA, BM, WAVES>;
-  using B = Panel<FB, BN, WAVES>;
-  constexpr int VALUES = A::BYTES + B::BYTES, STAGE = VALUES + A::SCALE_BYTES + B::SCALE_BYTES;
-  static_assert(A::SCALE_LOADS + B::SCALE_LOADS <= WAVES, "a wavefront loads scales once a stage");
-  __shared__ __attribute__((aligned(16))) unsigned char smem[2 * STAGE];
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  int ti, tj;
-  tile_of((p.M + BM - 1) / BM, (p.N + BN - 1) / BN, ti, tj);
-  const int m0 = ti * BM, n0 = tj * BN, gm = wave / WN * GM, gn = wave % WN * GN;
-
-  A a;
-  B b;
-  const int part_b = wave < A::SCALE_LOADS ? WAVES : wave - A::SCALE_LOADS;
-  a.init(p.a, p.scales_a, p.lda, p.ld_scales_a, m0, p.M, p.blocks, wave, lane, wave);
-  b.init(p.b, p.scales_b, p.ldb, p.ld_scales_b, n0, p.N, p.blocks, wave, lane, part_b);
-  f32x4 acc[4 * GM][4 * GN];
-#pragma unroll
-  for (int i = 0; i < 4 * GM; ++i)
-#pragma unroll
-    for (int j = 0; j < 4 * GN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  const unsigned lds = lds_address(smem);
-  auto request = [&](int step) {
-    const unsigned at = (step & 1) * STAGE;
-    a.template request<true>(step, lds + at, lds + at + VALUES, smem + at, wave, lane, wave);
-    b.template request<true>(step, lds + at + A::BYTES, lds + at + VALUES + A::SCALE_BYTES, smem + at + A::BYTES, wave, lane, part_b);
-  };
-  const int steps = (p.blocks + 3) / 4;
-  if (steps > 0) request(0);
-  for (int step = 0; step < steps; ++step) {
-    wait_all_and_meet();  // (the stage has arrived, and nobody reads the other one any more)
-    if (step + 1 < steps) request(step + 1);
-    const unsigned char* stage = smem + (step & 1) * STAGE;
-    Fragment<FB> fb[4 * GN];
-    unsigned sb[GN];
-#pragma unroll
-    for (int g = 0; g < GN; ++g) {
-      sb[g] = B::scale(stage + VALUES + A::SCALE_BYTES, gn + g, lane);
-#pragma unroll
-      for (int f = 0; f < 4; ++f) fb[4 * g + f] = B::fragment(stage + A::BYTES, gn + g, f, lane);
-    }
-#pragma unroll
-    for (int g = 0; g < GM; ++g) {
-      const unsigned sa = A::scale(stage + VALUES, gm + g, lane);
-      each<4>([&](auto f) {
-        constexpr int F = decltype(f)::value;
-        const Fragment<FA> fa = A::fragment(stage, gm + g, F, lane);
-#pragma unroll
-        for (int h = 0; h < GN; ++h)
-          each<4>([&](auto e) {
-            constexpr int E = decltype(e)::value;
-            acc[4 * g + F][4 * h + E] = multiply<FA, FB, F, E>(fa, fb[4 * h + E], acc[4 * g + F][4 * h + E], sa, sb[h]);
-          });
-      });
-    }
-  }
-  with_out_type(p, [&](auto type) {
-    using TO = decltype(type);
+// What a wavefront has summed: 64 GM x 64 GN from row m and column n on.
+template <int GM, int GN>
+__device__ __forceinline__ void finish_tile(const GemmArgs& p, int slice, int m, int n, int lane, const f32x4 (&acc)[4 * GM][4 * GN]) {
+  auto quads = [&](auto done) {
 #pragma unroll
     for (int g = 0; g < GM; ++g)
 #pragma unroll
@@ -336,9 +272,165 @@ __global__ __launch_bounds__(64 * WM * WN) void tile_kernel(const GemmArgs p) {
 #pragma unroll
           for (int h = 0; h < GN; ++h) {
             const float v[4] = {acc[4 * g + f][4 * h][i], acc[4 * g + f][4 * h + 1][i], acc[4 * g + f][4 * h + 2][i], acc[4 * g + f][4 * h + 3][i]};
-            finish4<TO>(p, m0 + 64 * (gm + g) + 16 * (lane / 16) + 4 * i + f, n0 + 64 * (gn + h) + 4 * (lane % 16), v);
+            done(m + 64 * g + 16 * (lane / 16) + 4 * i + f, n + 64 * h + 4 * (lane % 16), v);
           }
-  });
+  };
+  if (slices_of(p) > 1)
+    quads([&](int row, int col, const float (&v)[4]) { keep4(p, slice, row, col, v); });
+  else
+    with_out_type(p, [&](auto type) { quads([&](int row, int col, const float (&v)[4]) { finish4<decltype(type)>(p, row, col, v); }); });
+}
+
+// Bytes of a stage, and of the LDS of tile_kernel.
+template <int FA, int FB, int GM, int GN, int WM, int WN, int GROUPS>
+struct TileShape {
+  // steps of 128 k: of a wavefront, and of a stage.  (Rows of 128 bytes, a line, in a stage: with 64 every line is fetched twice.)
+  static constexpr int EACH = !is_wide(FA) && !is_wide(FB) && GROUPS == 1 ? 2 : 1, STEPS = EACH * GROUPS;
+  static constexpr int WAVES = WM * WN * GROUPS, BM = 64 * GM * WM, BN = 64 * GN * WN;
+  using A = Panel<FA, BM, STEPS, WAVES>;
+  using B = Panel<FB, BN, STEPS, WAVES>;
+  static constexpr int VALUES = A::BYTES + B::BYTES, STAGE = VALUES + A::SCALE_BYTES + B::SCALE_BYTES;
+  static constexpr int SUMS = (GROUPS - 1) * WM * WN * GM * GN * 16384;
+  static constexpr int lds(int places) { return places * STAGE > SUMS ? places * STAGE : SUMS; }
+};
+
+// Tiles from LDS: WM x WN wavefronts of 64 GM x 64 GN each, PLACES stages, all but one of them on their way.  GROUPS such sets of wavefronts take
+// a part of every stage's k each, and add their sums in LDS, in order.
+template <int FA, int FB, int GM, int GN, int WM, int WN, int GROUPS, int PLACES>
+__global__ __launch_bounds__(64 * WM * WN * GROUPS) void tile_kernel(const GemmArgs p) {
+  using S = TileShape<FA, FB, GM, GN, WM, WN, GROUPS>;
+  using A = typename S::A;
+  using B = typename S::B;
+  constexpr int SET = WM * WN, PARTS = A::PARTS + B::PARTS, LOADS = A::LOADS + B::LOADS + S::STEPS;  // of a wavefront, a stage
+  static_assert(PARTS <= S::WAVES && (PLACES - 2) * LOADS < 64, "a load of scales a wavefront; loads in flight are counted in 6 bits");
+  // The loads of another stage are handed over behind a quarter of a wavefront's products, not before them: it is held up there for long
+  // enough that the matrix cores should have work by then.  (Two operands of 8 bits have no registers left for it.)
+  constexpr bool LATE = !(is_wide(FA) && is_wide(FB));
+  __shared__ __attribute__((aligned(16))) unsigned char smem[S::lds(PLACES)];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int group = wave / SET, member = wave % SET;
+  const int slices = slices_of(p), slice = blockIdx.x % slices, first_block = slice * p.slice * 4;
+  const int blocks = min(p.blocks - first_block, p.slice * 4);  // of this slice
+  int ti, tj;
+  tile_of(blockIdx.x / slices, (p.M + S::BM - 1) / S::BM, (p.N + S::BN - 1) / S::BN, ti, tj);
+  const int m0 = ti * S::BM, n0 = tj * S::BN, gm = member / WN * GM, gn = member % WN * GN;
+  const A a(p.a, p.scales_a, p.lda, p.ld_scales_a, m0, p.M, first_block, blocks, wave, lane);
+  const B b(p.b, p.scales_b, p.ldb, p.ld_scales_b, n0, p.N, first_block, blocks, wave, lane);
+  f32x4 acc[4 * GM][4 * GN];
+#pragma unroll
+  for (int i = 0; i < 4 * GM; ++i)
+#pragma unroll
+    for (int j = 0; j < 4 * GN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const unsigned lds = lds_address(smem);
+  // whole stages; what K ends in comes before them, in the first place
+  const int stages = blocks / (4 * S::STEPS), ahead = blocks % (4 * S::STEPS) != 0;
+  auto request_scales = [&](int s, unsigned at) {
+    const int part = wave % PARTS;  // (some may be loaded twice: all wavefronts have as many in flight)
+#pragma unroll
+    for (int u = 0; u < S::STEPS; ++u) {
+      if (part < A::PARTS)
+        a.request_scales(s, u, at + S::VALUES, part, lane);
+      else
+        b.request_scales(s, u, at + S::VALUES + A::SCALE_BYTES, part - A::PARTS, lane);
+    }
+  };
+  auto request = [&](int s, int place) {
+    const unsigned at = lds + place * S::STAGE;
+    a.request(s, at, wave);
+    b.request(s, at + A::BYTES, wave);
+    request_scales(s, at);
+  };
+  // `between`: called behind the first quarter of the products
+  auto work = [&](int place, auto between) {
+    const unsigned char* stage = smem + place * S::STAGE;
+#pragma unroll
+    for (int i = 0; i < S::EACH; ++i) {
+      const int u = group * S::EACH + i;
+      Fragment<FA> fa[4 * GM];
+      Fragment<FB> fb[4 * GN];
+      unsigned sa[GM], sb[GN];
+#pragma unroll
+      for (int g = 0; g < GN; ++g) {
+        sb[g] = B::scale(stage + S::VALUES + A::SCALE_BYTES, u, gn + g, lane);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) fb[4 * g + f] = B::fragment(stage + A::BYTES, u, gn + g, f, lane);
+      }
+#pragma unroll
+      for (int g = 0; g < GM; ++g) {
+        sa[g] = A::scale(stage + S::VALUES, u, gm + g, lane);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) fa[4 * g + f] = A::fragment(stage, u, gm + g, f, lane);
+      }
+#pragma unroll
+      for (int g = 0; g < GM; ++g)
+        each<4>([&](auto f) {
+          constexpr int F = decltype(f)::value;
+          if (i == 0 && g == 0 && F == 1) between();
+#pragma unroll
+          for (int h = 0; h < GN; ++h)
+            each<4>([&](auto e) {
+              constexpr int E = decltype(e)::value;
+              acc[4 * g + F][4 * h + E] = multiply<FA, FB, F, E>(fa[4 * g + F], fb[4 * h + E], acc[4 * g + F][4 * h + E], sa[g], sb[h]);
+            });
+        });
+    }
+  };
+  if (ahead) {
+    a.request_end(stages, lds, smem, wave, lane);
+    b.request_end(stages, lds + A::BYTES, smem + A::BYTES, wave, lane);
+    request_scales(stages, lds);
+  }
+#pragma unroll
+  for (int s = 0; s < PLACES - 1; ++s)
+    if (s < stages) request(s, (s + ahead) % PLACES);
+  if (ahead) {
+    wait_all_and_meet();
+    work(0, [] {});
+  }
+  int place = ahead, next = (PLACES - 1 + ahead) % PLACES;  // of this stage, and of the one that is requested
+  for (int s = 0; s < stages; ++s) {
+    __builtin_amdgcn_sched_barrier(0);
+    // the stage has arrived, and nobody reads the one before any more
+    if (PLACES > 2 && s + PLACES - 2 < stages) {
+      constexpr int YOUNGER = (PLACES - 2) * LOADS;
+      __builtin_amdgcn_s_waitcnt(0x0070 | (YOUNGER & 15) | ((YOUNGER >> 4) << 14));
+      __builtin_amdgcn_s_barrier();
+    } else {
+      wait_all_and_meet();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const bool more = s + PLACES - 1 < stages;
+    if (!LATE && more) request(s + PLACES - 1, next);
+    work(place, [&] {
+      if constexpr (LATE) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) request(s + PLACES - 1, next);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    place = place + 1 == PLACES ? 0 : place + 1;
+    next = next + 1 == PLACES ? 0 : next + 1;
+  }
+  if constexpr (GROUPS > 1) {
+    f32x4* meet = reinterpret_cast<f32x4*>(smem) + lane;
+    __syncthreads();  // (the stages are read)
+    if (group > 0) {
+#pragma unroll
+      for (int i = 0; i < 4 * GM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 * GN; ++j) meet[(((group - 1) * SET + member) * 16 * GM * GN + i * 4 * GN + j) * 64] = acc[i][j];
+    }
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int k = 0; k < GROUPS - 1; ++k)
+#pragma unroll
+      for (int i = 0; i < 4 * GM; ++i)
+#pragma unroll
+        for (int j = 0; j < 4 * GN; ++j) acc[i][j] += meet[((k * SET + member) * 16 * GM * GN + i * 4 * GN + j) * 64];
+  }
+  finish_tile<GM, GN>(p, slice, m0 + 64 * gm, n0 + 64 * gn, lane, acc);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------------
@@ -362,17 +454,25 @@ struct Rows {
     ld_scales = ld_s;
     blocks = blocks_in_row;
   }
+  // Whole steps, and one that K ends in.
   __device__ __forceinline__ void load(int step, int lane, Fragment<FORMAT> (&x)[F], unsigned& scale) const {
-    const int g = lane / 16, last = blocks - 1;
-    const int first = step * step_bytes(FORMAT) + g * 16;
-    const int end = blocks * (is_wide(FORMAT) ? 32 : 16);
+    const long long first = (long long)step * step_bytes(FORMAT) + lane / 16 * 16;
 #pragma unroll
     for (int f = 0; f < F; ++f) {
-      const u32x4 none = {0, 0, 0, 0};
+      x[f].v[0] = *reinterpret_cast<const u32x4*>(row[f] + first);
+      if constexpr (is_wide(FORMAT)) x[f].v[1] = *reinterpret_cast<const u32x4*>(row[f] + first + 64);
+    }
+    scale = *reinterpret_cast<const unsigned*>(scales + (long long)(step * 4 + lane / 16) * ld_scales) >> shift;
+  }
+  __device__ __forceinline__ void load_end(int step, int lane, Fragment<FORMAT> (&x)[F], unsigned& scale) const {
+    const int g = lane / 16, first = step * step_bytes(FORMAT) + g * 16, end = blocks * (is_wide(FORMAT) ? 32 : 16);
+    const u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
       x[f].v[0] = first < end ? *reinterpret_cast<const u32x4*>(row[f] + first) : none;
       if constexpr (is_wide(FORMAT)) x[f].v[1] = first + 64 < end ? *reinterpret_cast<const u32x4*>(row[f] + first + 64) : none;
     }
-    scale = *reinterpret_cast<const unsigned*>(scales + (long long)min(step * 4 + g, last) * ld_scales) >> shift;
+    scale = *reinterpret_cast<const unsigned*>(scales + (long long)min(step * 4 + g, blocks - 1) * ld_scales) >> shift;
   }
 };
 
@@ -380,6 +480,7 @@ struct Rows {
 template <int FA, int FB, bool GROUP_M, bool GROUP_N, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
   constexpr int FM = GROUP_M ? 4 : 1, FN = GROUP_N ? 4 : 1, BM = 16 * FM, BN = 16 * FN;
+  constexpr int AT_ONCE = FM * FN == 1 ? 4 : 2;  // steps whose loads are in flight
   __shared__ f32x4 meet[WAVES][FM * FN][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN, slices = slices_of(p);
@@ -395,20 +496,37 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
   for (int i = 0; i < FM; ++i)
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const int steps = min((p.blocks + 3) / 4, (slice + 1) * p.slice);
-#pragma unroll 4
-  for (int step = slice * p.slice + wave; step < steps; step += WAVES) {
-    Fragment<FA> fa[FM];
-    Fragment<FB> fb[FN];
-    unsigned sa, sb;
-    a.load(step, lane, fa, sa);
-    b.load(step, lane, fb, sb);
+  Fragment<FA> fa[AT_ONCE][FM];
+  Fragment<FB> fb[AT_ONCE][FN];
+  unsigned sa[AT_ONCE], sb[AT_ONCE];
+  auto product = [&](int u) {
     each<FM>([&](auto f) {
       each<FN>([&](auto e) {
         constexpr int F = decltype(f)::value, E = decltype(e)::value;
-        acc[F][E] = multiply<FA, FB, F, E>(fa[F], fb[E], acc[F][E], sa, sb);
+        acc[F][E] = multiply<FA, FB, F, E>(fa[u][F], fb[u][E], acc[F][E], sa[u], sb[u]);
       });
     });
+  };
+  const int end = (slice + 1) * p.slice, whole = min(p.blocks / 4, end);  // (p.slice is below 2^25)
+  int step = slice * p.slice + wave;
+  for (; step + (AT_ONCE - 1) * WAVES < whole; step += AT_ONCE * WAVES) {
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      a.load(step + u * WAVES, lane, fa[u], sa[u]);
+      b.load(step + u * WAVES, lane, fb[u], sb[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) product(u);
+  }
+  for (; step < whole; step += WAVES) {
+    a.load(step, lane, fa[0], sa[0]);
+    b.load(step, lane, fb[0], sb[0]);
+    product(0);
+  }
+  if (step * 4 < p.blocks && step < end) {
+    a.load_end(step, lane, fa[0], sa[0]);
+    b.load_end(step, lane, fb[0], sb[0]);
+    product(0);
   }
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -476,11 +594,11 @@ __global__ __launch_bounds__(256) void join_slices_kernel(const GemmArgs p, cons
 }
 
 // Which kernel serves a product, and how it is cut.
-enum : int { KERNEL_TILE_128 = 0, KERNEL_STREAM_16 = 1, KERNEL_STREAM_64 = 2 };
+enum : int { KERNEL_TILE_256 = 0, KERNEL_TILE_128, KERNEL_TILE_64X128, KERNEL_TILE_64, KERNEL_STREAM_16, KERNEL_STREAM_16X64 };
 struct GemmCut {
   int kernel;
-  int slices;
-  long long blocks;  // workgroups
+  int slices, slice;  // slice: steps of 128 k of each
+  long long blocks;   // workgroups
 };
 // the kernels of A's format (mx_kernels.hip, once for each)
 template <int FA>

@@ -19,6 +19,7 @@ using namespace hidet::mx;
 namespace {
 
 constexpr long long kMaxCols = 32768;
+constexpr long long kMaxLd = (1LL << 32) - 1;
 
 struct NormArgs {
   const void* x;
@@ -29,11 +30,13 @@ struct NormArgs {
   unsigned char* values;
   unsigned char* scales;
   float* rstd;
-  long long ldx, ldr, lds, ldy, stride_values, stride_scales;
+  unsigned ldx, ldr, lds, ldy;               // elements
+  unsigned stride_values, stride_scales;     // bytes
   int rows, cols;
   int format;
   float eps, offset;
 };
+static_assert(sizeof(NormArgs) <= 112, "a launch with more takes longer");
 
 // N weights from column `col` on, offset added; 0 beyond the row
 template <typename TW, int N>
@@ -213,10 +216,11 @@ struct GradArgs {
   const void* grad_sum;  // may be null
   void* grad_h;
   float* part;           // [workgroup][cols]; null: no gradient of the weight
-  long long ldg, ldh, lds, ldo;
+  unsigned ldg, ldh, lds, ldo;
   int rows, cols;
   float offset;
 };
+static_assert(sizeof(GradArgs) <= 112, "a launch with more takes longer");
 
 // A workgroup takes every gridDim-th group of rows and keeps its part of the weight's gradient in registers: lanes hold the same columns of
 // every row.  LANES > 64: one row at a time.
@@ -384,6 +388,11 @@ hidet_status_t check_norm(int dtype, int weight_dtype, long long rows, long long
   if (rows >= kMaxSide || cols > kMaxCols) return HIDET_ERR_UNSUPPORTED;
   return HIDET_OK;
 }
+// check_rows, and distances that the kernels hold in 32 bits
+hidet_status_t check_norm_rows(const void* data, int dtype, long long rows, long long cols, long long ld) {
+  if (hidet_status_t st = check_rows(data, dtype, rows, cols, ld); st != HIDET_OK) return st;
+  return ld > kMaxLd ? HIDET_ERR_UNSUPPORTED : HIDET_OK;
+}
 // `out` may be `in` itself, with the same rows
 bool in_place_ok(const void* out, long long ld_out, const void* in, long long ld_in, long long rows) {
   return !out || out != in || rows <= 1 || ld_out == ld_in;
@@ -425,13 +434,13 @@ hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows,
     if (st = check_mx(quantized, rows, cols); st != HIDET_OK) return st;
   if (rows == 0 || cols == 0) return HIDET_OK;
   if (!weight) return HIDET_ERR_INVALID_ARG;
-  if (st = check_rows(x, dtype, rows, cols, ldx); st != HIDET_OK) return st;
+  if (st = check_norm_rows(x, dtype, rows, cols, ldx); st != HIDET_OK) return st;
   if (residual)
-    if (st = check_rows(residual, dtype, rows, cols, ld_residual); st != HIDET_OK) return st;
+    if (st = check_norm_rows(residual, dtype, rows, cols, ld_residual); st != HIDET_OK) return st;
   if (sum)
-    if (st = check_rows(sum, dtype, rows, cols, ld_sum); st != HIDET_OK) return st;
+    if (st = check_norm_rows(sum, dtype, rows, cols, ld_sum); st != HIDET_OK) return st;
   if (y)
-    if (st = check_rows(y, dtype, rows, cols, ldy); st != HIDET_OK) return st;
+    if (st = check_norm_rows(y, dtype, rows, cols, ldy); st != HIDET_OK) return st;
   if (!is_aligned(weight, size_of(weight_dtype)) || !is_aligned(rstd, 4)) return HIDET_ERR_ALIGNMENT;
   if (!in_place_ok(sum, ld_sum, x, ldx, rows) || !in_place_ok(sum, ld_sum, residual, ld_residual, rows) ||
       !in_place_ok(y, ldy, x, ldx, rows) || !in_place_ok(y, ldy, residual, ld_residual, rows) || (sum && sum == y))
@@ -443,10 +452,10 @@ hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows,
   p.sum = sum;
   p.y = y;
   p.rstd = rstd;
-  p.ldx = ldx;
-  p.ldr = ld_residual;
-  p.lds = ld_sum;
-  p.ldy = ldy;
+  p.ldx = (unsigned)ldx;
+  p.ldr = residual ? (unsigned)ld_residual : 0;
+  p.lds = sum ? (unsigned)ld_sum : 0;
+  p.ldy = y ? (unsigned)ldy : 0;
   p.rows = (int)rows;
   p.cols = (int)cols;
   p.eps = eps;
@@ -454,8 +463,8 @@ hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows,
   if (quantized) {
     p.values = reinterpret_cast<unsigned char*>(quantized->values);
     p.scales = reinterpret_cast<unsigned char*>(quantized->scales);
-    p.stride_values = quantized->stride_values;
-    p.stride_scales = quantized->stride_scales;
+    p.stride_values = (unsigned)quantized->stride_values;
+    p.stride_scales = (unsigned)quantized->stride_scales;
     p.format = quantized->format;
   }
   const hipError_t e = by_types<Norm>(dtype, weight_dtype, p, false, (hipStream_t)stream);
@@ -487,11 +496,11 @@ hidet_status_t hidet_rms_norm_backward(int32_t dtype, int32_t weight_dtype, int6
     return hipGetLastError() == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
   }
   if (!weight || !rstd) return HIDET_ERR_INVALID_ARG;
-  if (st = check_rows(grad_y, dtype, rows, cols, ld_grad_y); st != HIDET_OK) return st;
-  if (st = check_rows(h, dtype, rows, cols, ldh); st != HIDET_OK) return st;
+  if (st = check_norm_rows(grad_y, dtype, rows, cols, ld_grad_y); st != HIDET_OK) return st;
+  if (st = check_norm_rows(h, dtype, rows, cols, ldh); st != HIDET_OK) return st;
   if (grad_sum)
-    if (st = check_rows(grad_sum, dtype, rows, cols, ld_grad_sum); st != HIDET_OK) return st;
-  if (st = check_rows(grad_h, dtype, rows, cols, ld_grad_h); st != HIDET_OK) return st;
+    if (st = check_norm_rows(grad_sum, dtype, rows, cols, ld_grad_sum); st != HIDET_OK) return st;
+  if (st = check_norm_rows(grad_h, dtype, rows, cols, ld_grad_h); st != HIDET_OK) return st;
   if (!is_aligned(weight, size_of(weight_dtype)) || !is_aligned(rstd, 4)) return HIDET_ERR_ALIGNMENT;
   if (!in_place_ok(grad_h, ld_grad_h, grad_y, ld_grad_y, rows) || !in_place_ok(grad_h, ld_grad_h, grad_sum, ld_grad_sum, rows) || grad_h == h)
     return HIDET_ERR_INVALID_ARG;
@@ -507,10 +516,10 @@ hidet_status_t hidet_rms_norm_backward(int32_t dtype, int32_t weight_dtype, int6
   p.grad_sum = grad_sum;
   p.grad_h = grad_h;
   p.part = grad_weight ? reinterpret_cast<float*>(workspace) : nullptr;
-  p.ldg = ld_grad_y;
-  p.ldh = ldh;
-  p.lds = ld_grad_sum;
-  p.ldo = ld_grad_h;
+  p.ldg = (unsigned)ld_grad_y;
+  p.ldh = (unsigned)ldh;
+  p.lds = grad_sum ? (unsigned)ld_grad_sum : 0;
+  p.ldo = (unsigned)ld_grad_h;
   p.rows = (int)rows;
   p.cols = (int)cols;
   p.offset = offset;

@@ -138,7 +138,8 @@ def _exact_case(m, n, k, fa, fb, out, seed, **epilogue):
 
 SIZES = [(1, 1, 1), (1, 16, 32), (2, 17, 33), (3, 64, 128), (5, 100, 200), (16, 48, 1000), (4, 300, 4096), (17, 64, 96), (33, 65, 160), (64, 64, 128),
          (64, 130, 2080), (65, 127, 31), (100, 200, 300), (128, 128, 256), (129, 257, 512), (200, 100, 1056), (256, 256, 384), (300, 520, 192),
-         (513, 260, 640), (1, 3000, 96), (2000, 3, 64), (260, 1030, 288)]
+         (513, 260, 640), (1, 3000, 96), (2000, 3, 64), (260, 1030, 288),
+         (7, 40, 20000), (70, 66, 9000), (2050, 2051, 130), (3000, 1500, 1000), (1100, 4200, 544)]
 
 
 @pytest.mark.parametrize("formats", [(a, b) for a in FORMATS for b in FORMATS], ids=str)
