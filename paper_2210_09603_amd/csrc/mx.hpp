@@ -20,6 +20,7 @@ constexpr int kBlock = 32;
 constexpr long long kMaxSide = 1LL << 29;          // rows and columns of a matrix
 constexpr long long kMaxSpan = 1LL << 47;          // elements that a matrix spans
 constexpr long long kMaxValueStride = 1LL << 23;   // bytes: 256 rows are reached by 32-bit offsets
+constexpr long long kFarBytes = 128LL << 20;       // matrices of more are streamed past the caches
 constexpr long long kMaxScaleStride = 1LL << 29;   // bytes: 8 blocks likewise
 
 inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -125,6 +126,21 @@ struct Chunk {
   };
   typedef u32x4 Streamed __attribute__((aligned(2)));  // (the same, for an access with a hint)
 };
+// STREAM: past the caches
+template <bool STREAM, typename W>
+__device__ __forceinline__ W load_word(const W* at) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(at);
+  else
+    return *at;
+}
+template <bool STREAM, typename W>
+__device__ __forceinline__ void store_word(W* at, W v) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, at);
+  else
+    *at = v;
+}
 // `left` elements are there, any number: the others are 0.  STREAM: passes the caches by.
 template <typename T, bool STREAM = false>
 __device__ __forceinline__ u32x4 load_chunk(const T* at, int left) {
@@ -185,20 +201,20 @@ __device__ __forceinline__ unsigned largest_of_block(const float (&v)[N]) {
   return m;
 }
 // Encodes and stores N values of which the first has index `at` in its row of values; the block's lanes hold the same code.
-template <int N>
+template <int N, bool STREAM = false>
 __device__ __forceinline__ void store_elements(unsigned char* row, int at, int format, const float (&v)[N], int code) {
   unsigned words[N / 4];
   encode<N>(v, scale_inverse(code), format, words);
   if (format == HIDET_MX_E2M1) {
     if constexpr (N == 8)
-      *reinterpret_cast<unsigned*>(row + at / 2) = words[0];
+      store_word<STREAM>(reinterpret_cast<unsigned*>(row + at / 2), words[0]);
     else
-      *reinterpret_cast<unsigned short*>(row + at / 2) = (unsigned short)words[0];
+      store_word<STREAM>(reinterpret_cast<unsigned short*>(row + at / 2), (unsigned short)words[0]);
   } else {
     if constexpr (N == 8)
-      *reinterpret_cast<u32x2*>(row + at) = u32x2{words[0], words[1]};
+      store_word<STREAM>(reinterpret_cast<u32x2*>(row + at), u32x2{words[0], words[1]});
     else
-      *reinterpret_cast<unsigned*>(row + at) = words[0];
+      store_word<STREAM>(reinterpret_cast<unsigned*>(row + at), words[0]);
   }
 }
 #endif

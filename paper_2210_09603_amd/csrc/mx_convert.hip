@@ -12,7 +12,6 @@ using namespace hidet::mx;
 
 namespace {
 
-constexpr int kCols = 128;                       // of a tile
 constexpr long long kMaxTiles = (1LL << 24) - 1; // of 256 threads: below 2^32 work items
 
 struct Side {
@@ -28,27 +27,27 @@ struct QuantizeArgs {
   Side by_rows, by_columns;
 };
 
-// What the threads of a tile share while they go through its rows: 16 of them (32 in fp32) hold 128 columns of a row.
-template <typename T>
+// How 256 threads go through a tile of COLS columns: LANES of them hold a row, ROWS rows are a pass.
+template <typename T, int COLS>
 struct Walk {
-  static constexpr int N = Chunk<T>::N, LANES = kCols / N, ROWS = 256 / LANES;  // rows a pass
+  static constexpr int N = Chunk<T>::N, LANES = COLS / N, ROWS = 256 / LANES;
 };
 
 // One pass of blocks along rows: row r of the tile, `v` its values from column `col` on.
-template <typename T, int TILE_ROWS>
+template <typename T, int COLS, int TILE_ROWS, bool STREAM>
 __device__ __forceinline__ void rows_pass(const QuantizeArgs& p, u32x4 raw, int row, int r, int col, int filled, unsigned char* codes) {
   constexpr int N = Chunk<T>::N;
   float v[N];
   unpack<T>(raw, v);
   const int code = scale_code(largest_of_block<N>(v), p.by_rows.format);
-  if (row < p.rows && col < filled) store_elements<N>(p.by_rows.values + (long long)row * p.by_rows.stride_values, col, p.by_rows.format, v, code);
-  if (col % kBlock == 0) codes[col % kCols / kBlock * TILE_ROWS + r] = (unsigned char)code;
+  if (row < p.rows && col < filled) store_elements<N, STREAM>(p.by_rows.values + (long long)row * p.by_rows.stride_values, col, p.by_rows.format, v, code);
+  if (col % kBlock == 0) codes[col % COLS / kBlock * TILE_ROWS + r] = (unsigned char)code;
 }
 // The codes [block][row] of a tile into the scales.
-template <int TILE_ROWS>
+template <int COLS, int TILE_ROWS>
 __device__ __forceinline__ void write_codes(const Side& s, const unsigned char* codes, int row0, int rows, int block0, int blocks) {
   constexpr int WORDS = TILE_ROWS / 4;
-  for (int i = threadIdx.x; i < kCols / kBlock * WORDS; i += 256) {
+  for (int i = threadIdx.x; i < COLS / kBlock * WORDS; i += 256) {
     const int b = i / WORDS, first = i % WORDS * 4;
     if (block0 + b >= blocks) continue;
     unsigned char* to = s.scales + (long long)(block0 + b) * s.stride_scales + row0 + first;
@@ -60,33 +59,32 @@ __device__ __forceinline__ void write_codes(const Side& s, const unsigned char* 
   }
 }
 
-template <typename T, int PASSES>
+template <typename T, int COLS, int PASSES, bool STREAM>
 __global__ __launch_bounds__(256) void rows_kernel(const QuantizeArgs p) {
-  using W = Walk<T>;
+  using W = Walk<T, COLS>;
   constexpr int TILE_ROWS = W::ROWS * PASSES;
-  __shared__ __attribute__((aligned(4))) unsigned char codes[kCols / kBlock * TILE_ROWS];
+  __shared__ __attribute__((aligned(4))) unsigned char codes[COLS / kBlock * TILE_ROWS];
   const int tile_row = blockIdx.x / p.col_tiles, tile_col = blockIdx.x - tile_row * p.col_tiles;
   const int row0 = tile_row * TILE_ROWS, lane = threadIdx.x % W::LANES, first = threadIdx.x / W::LANES;
-  const int col = tile_col * kCols + lane * W::N, filled = (p.cols + kBlock - 1) / kBlock * kBlock;
+  const int col = tile_col * COLS + lane * W::N, filled = (p.cols + kBlock - 1) / kBlock * kBlock;
   u32x4 raw[PASSES];
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const int row = row0 + i * W::ROWS + first;
-    raw[i] = load_chunk(reinterpret_cast<const T*>(p.x) + (long long)row * p.ldx + col, row < p.rows ? p.cols - col : 0);
+    raw[i] = load_chunk<T, STREAM>(reinterpret_cast<const T*>(p.x) + (long long)row * p.ldx + col, row < p.rows ? p.cols - col : 0);
   }
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i) rows_pass<T, TILE_ROWS>(p, raw[i], row0 + i * W::ROWS + first, i * W::ROWS + first, col, filled, codes);
+  for (int i = 0; i < PASSES; ++i) rows_pass<T, COLS, TILE_ROWS, STREAM>(p, raw[i], row0 + i * W::ROWS + first, i * W::ROWS + first, col, filled, codes);
   __syncthreads();
-  write_codes<TILE_ROWS>(p.by_rows, codes, row0, p.rows, tile_col * (kCols / kBlock), filled / kBlock);
+  write_codes<COLS, TILE_ROWS>(p.by_rows, codes, row0, p.rows, tile_col * (COLS / kBlock), filled / kBlock);
 }
 
 template <typename T>
 struct Two {
   T a, b;
 };
-// 32 values of a column into its row of the transposed matrix
-__device__ __forceinline__ void store_column(const Side& s, long long column, int block, const float (&v)[kBlock], int code) {
-  unsigned char* to = s.values + column * s.stride_values + (long long)block * (s.format == HIDET_MX_E2M1 ? 16 : 32);
+// The 32 elements of a block, 16 or 32 bytes of LDS
+__device__ __forceinline__ void put_block(unsigned char* to, int format, const float (&v)[kBlock], int code) {
   unsigned words[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -94,11 +92,11 @@ __device__ __forceinline__ void store_column(const Side& s, long long column, in
     unsigned two[2];
 #pragma unroll
     for (int e = 0; e < 8; ++e) part[e] = v[8 * i + e];
-    encode<8>(part, scale_inverse(code), s.format, two);
+    encode<8>(part, scale_inverse(code), format, two);
     words[2 * i] = two[0];
     words[2 * i + 1] = two[1];
   }
-  if (s.format == HIDET_MX_E2M1) {
+  if (format == HIDET_MX_E2M1) {
     *reinterpret_cast<u32x4*>(to) = u32x4{words[0], words[2], words[4], words[6]};
   } else {
     *reinterpret_cast<u32x4*>(to) = u32x4{words[0], words[1], words[2], words[3]};
@@ -106,68 +104,91 @@ __device__ __forceinline__ void store_column(const Side& s, long long column, in
   }
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void columns_kernel(const QuantizeArgs p) {
-  using W = Walk<T>;
-  constexpr int TILE_ROWS = 128, PASSES = TILE_ROWS / W::ROWS;
-  __shared__ __attribute__((aligned(16))) T tile[TILE_ROWS * kCols];
-  __shared__ __attribute__((aligned(4))) unsigned char codes[kCols / kBlock * TILE_ROWS];
+  constexpr int COLS = 128, TILE_ROWS = 128;
+  using W = Walk<T, COLS>;
+  constexpr int PASSES = TILE_ROWS / W::ROWS;
+  __shared__ __attribute__((aligned(16))) T tile[TILE_ROWS * COLS];
+  __shared__ __attribute__((aligned(4))) unsigned char codes[COLS / kBlock * TILE_ROWS];
   const int tile_row = blockIdx.x / p.col_tiles, tile_col = blockIdx.x - tile_row * p.col_tiles;
   const int row0 = tile_row * TILE_ROWS, lane = threadIdx.x % W::LANES, first = threadIdx.x / W::LANES;
-  const int col = tile_col * kCols + lane * W::N, filled = (p.cols + kBlock - 1) / kBlock * kBlock;
+  const int col = tile_col * COLS + lane * W::N, filled = (p.cols + kBlock - 1) / kBlock * kBlock;
   u32x4 raw[PASSES];
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const int row = row0 + i * W::ROWS + first;
-    raw[i] = load_chunk(reinterpret_cast<const T*>(p.x) + (long long)row * p.ldx + col, row < p.rows ? p.cols - col : 0);
+    raw[i] = load_chunk<T, STREAM>(reinterpret_cast<const T*>(p.x) + (long long)row * p.ldx + col, row < p.rows ? p.cols - col : 0);
   }
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i) *reinterpret_cast<u32x4*>(tile + (i * W::ROWS + first) * kCols + lane * W::N) = raw[i];
+  for (int i = 0; i < PASSES; ++i) *reinterpret_cast<u32x4*>(tile + (i * W::ROWS + first) * COLS + lane * W::N) = raw[i];
   if (p.by_rows.values) {
 #pragma unroll
-    for (int i = 0; i < PASSES; ++i) rows_pass<T, TILE_ROWS>(p, raw[i], row0 + i * W::ROWS + first, i * W::ROWS + first, col, filled, codes);
+    for (int i = 0; i < PASSES; ++i) rows_pass<T, COLS, TILE_ROWS, STREAM>(p, raw[i], row0 + i * W::ROWS + first, i * W::ROWS + first, col, filled, codes);
   }
   __syncthreads();
-  if (p.by_rows.values) write_codes<TILE_ROWS>(p.by_rows, codes, row0, p.rows, tile_col * (kCols / kBlock), filled / kBlock);
+  if (p.by_rows.values) write_codes<COLS, TILE_ROWS>(p.by_rows, codes, row0, p.rows, tile_col * (COLS / kBlock), filled / kBlock);
 
-  const int pair = threadIdx.x % 64 * 2, block = threadIdx.x / 64;
-  const long long column = (long long)tile_col * kCols + pair;
-  if (column >= p.cols || row0 + block * kBlock >= p.rows) return;
+  // columns: their elements back into LDS, from where they leave as whole rows of the transposed matrix
+  constexpr int PITCH = TILE_ROWS + 16;
+  static_assert(COLS * PITCH <= (int)sizeof(tile), "the elements take the tile's place");
+  const Side& s = p.by_columns;
+  const int pair = threadIdx.x % 64 * 2, block = threadIdx.x / 64, each = s.format == HIDET_MX_E2M1 ? 16 : 32;
+  const long long column = (long long)tile_col * COLS + pair;
   float a[kBlock], b[kBlock];
   unsigned top_a = 0, top_b = 0;
 #pragma unroll
   for (int r = 0; r < kBlock; ++r) {
-    const Two<T> two = *reinterpret_cast<const Two<T>*>(tile + (block * kBlock + r) * kCols + pair);
+    const Two<T> two = *reinterpret_cast<const Two<T>*>(tile + (block * kBlock + r) * COLS + pair);
     a[r] = to_f32(two.a);
     b[r] = to_f32(two.b);
     top_a = max(top_a, magnitude(a[r]));
     top_b = max(top_b, magnitude(b[r]));
   }
-  const Side& s = p.by_columns;
-  const int code_a = scale_code(top_a, s.format), code_b = scale_code(top_b, s.format), at = row0 / kBlock + block;
-  unsigned char* scales = s.scales + (long long)at * s.stride_scales + column;
-  store_column(s, column, at, a, code_a);
-  if (column + 1 < p.cols) {
-    store_column(s, column + 1, at, b, code_b);
-    *reinterpret_cast<unsigned short*>(scales) = (unsigned short)(code_a | code_b << 8);
-  } else {
-    *scales = (unsigned char)code_a;
+  const int code_a = scale_code(top_a, s.format), code_b = scale_code(top_b, s.format);
+  if (column < p.cols && row0 + block * kBlock < p.rows) {
+    unsigned char* scales = s.scales + (long long)(row0 / kBlock + block) * s.stride_scales + column;
+    if (column + 1 < p.cols)
+      *reinterpret_cast<unsigned short*>(scales) = (unsigned short)(code_a | code_b << 8);
+    else
+      *scales = (unsigned char)code_a;
+  }
+  __syncthreads();  // (the tile is read)
+  unsigned char* out = reinterpret_cast<unsigned char*>(tile);
+  put_block(out + pair * PITCH + block * each, s.format, a, code_a);
+  put_block(out + (pair + 1) * PITCH + block * each, s.format, b, code_b);
+  __syncthreads();
+  const int chunks = TILE_ROWS / kBlock * each / 16;  // of a row of the transposed matrix
+  for (int i = threadIdx.x; i < COLS * chunks; i += 256) {
+    const int r = i / chunks, c = i - r * chunks;
+    if (tile_col * COLS + r >= p.cols || row0 + c * 16 / each * kBlock >= p.rows) continue;
+    unsigned char* to = s.values + (long long)(tile_col * COLS + r) * s.stride_values + (long long)row0 / kBlock * each + c * 16;
+    *reinterpret_cast<u32x4*>(to) = *reinterpret_cast<const u32x4*>(out + r * PITCH + c * 16);
   }
 }
 
 template <typename T>
 hipError_t launch_quantize(QuantizeArgs p, hipStream_t stream) {
-  const long long col_tiles = (p.cols + kCols - 1) / kCols;
-  p.col_tiles = (int)col_tiles;
+  const bool far = (long long)p.rows * p.cols * (int)sizeof(T) >= kFarBytes;
+  auto grid = [&](int rows, int cols) {
+    const long long col_tiles = (p.cols + (long long)cols - 1) / cols, tiles = (p.rows + (long long)rows - 1) / rows * col_tiles;
+    p.col_tiles = (int)col_tiles;
+    return tiles;
+  };
   if (p.by_columns.values) {
-    const long long tiles = ((p.rows + 127LL) / 128) * col_tiles;
+    const long long tiles = grid(128, 128);
     if (tiles > kMaxTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((columns_kernel<T>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((far ? columns_kernel<T, true> : columns_kernel<T, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    return hipGetLastError();
+  }
+  // Rows of 1 KB or more of a tile, four loads a thread in flight: 16384 x 4096 in bf16 into 4 bits 28.8 us (5.8 TB/s); 128 columns 32.1, two
+  // loads 30.4, all through the caches 36.2.  Few tiles of these: smaller ones.
+  constexpr int FAR_ROWS = Walk<T, 512>::ROWS * 4, NEAR_ROWS = Walk<T, 128>::ROWS;
+  if (const long long tiles = grid(FAR_ROWS, 512); tiles >= 1024) {
+    if (tiles > kMaxTiles) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((far ? rows_kernel<T, 512, 4, true> : rows_kernel<T, 512, 4, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
   } else {
-    constexpr int PASSES = 4, TILE_ROWS = Walk<T>::ROWS * PASSES;
-    const long long tiles = ((p.rows + (long long)TILE_ROWS - 1) / TILE_ROWS) * col_tiles;
-    if (tiles > kMaxTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((rows_kernel<T, PASSES>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((rows_kernel<T, 128, 1, false>), dim3((unsigned)grid(NEAR_ROWS, 128)), dim3(256), 0, stream, p);
   }
   return hipGetLastError();
 }
@@ -179,56 +200,43 @@ struct DequantizeArgs {
   long long stride_values, stride_scales, ldy;
   int rows, cols, col_tiles, format;
 };
-// 16 threads hold 128 columns of a row, 8 each.
-template <typename T, int PASSES>
+// Tiles of 16 x 128: 16 threads hold the columns of a row, 8 each.
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs p) {
   const int tile_row = blockIdx.x / p.col_tiles, tile_col = blockIdx.x - tile_row * p.col_tiles;
-  const int row0 = tile_row * (16 * PASSES) + threadIdx.x / 16, col = tile_col * kCols + threadIdx.x % 16 * 8;
-  if (col >= p.cols) return;
-  const unsigned char* scales = p.scales + (long long)(col / kBlock) * p.stride_scales;
-  unsigned words[PASSES][2];
-  int codes[PASSES];
-#pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int row = min(row0 + i * 16, p.rows - 1);
-    const unsigned char* from = p.values + (long long)row * p.stride_values;
-    if (p.format == HIDET_MX_E2M1) {
-      words[i][0] = *reinterpret_cast<const unsigned*>(from + col / 2);
-      words[i][1] = 0;
-    } else {
-      const u32x2 two = *reinterpret_cast<const u32x2*>(from + col);
-      words[i][0] = two[0];
-      words[i][1] = two[1];
-    }
-    codes[i] = scales[row];
+  const int row = tile_row * 16 + threadIdx.x / 16, col = tile_col * 128 + threadIdx.x % 16 * 8;
+  if (col >= p.cols || row >= p.rows) return;
+  const unsigned char* from = p.values + (long long)row * p.stride_values;
+  unsigned words[2] = {0, 0};
+  if (p.format == HIDET_MX_E2M1) {
+    words[0] = load_word<STREAM>(reinterpret_cast<const unsigned*>(from + col / 2));
+  } else {
+    const u32x2 two = load_word<STREAM>(reinterpret_cast<const u32x2*>(from + col));
+    words[0] = two[0];
+    words[1] = two[1];
   }
+  const float scale = scale_value(p.scales[(long long)(col / kBlock) * p.stride_scales + row]);
+  float v[8];
+  decode(words, p.format, v);
+  T* y = reinterpret_cast<T*>(p.y) + (long long)row * p.ldy + col;
+  constexpr int N = Chunk<T>::N;
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int row = row0 + i * 16;
-    if (row >= p.rows) return;
-    float v[8];
-    decode(words[i], p.format, v);
-    const float scale = scale_value(codes[i]);
+  for (int c = 0; c < 8 / N; ++c) {
+    float part[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= scale;
-    T* y = reinterpret_cast<T*>(p.y) + (long long)row * p.ldy + col;
-    constexpr int N = Chunk<T>::N;
-#pragma unroll
-    for (int c = 0; c < 8 / N; ++c) {
-      float part[N];
-#pragma unroll
-      for (int e = 0; e < N; ++e) part[e] = v[c * N + e];
-      store_chunk<T>(y + c * N, p.cols - col - c * N, pack<T>(part));
-    }
+    for (int e = 0; e < N; ++e) part[e] = v[c * N + e] * scale;
+    store_chunk<T, STREAM>(y + c * N, p.cols - col - c * N, pack<T>(part));
   }
 }
 template <typename T>
 hipError_t launch_dequantize(DequantizeArgs p, hipStream_t stream) {
-  constexpr int PASSES = 4;
-  const long long col_tiles = (p.cols + kCols - 1) / kCols, tiles = ((p.rows + 16LL * PASSES - 1) / (16 * PASSES)) * col_tiles;
+  // (16384 x 4096 from 4 bits into bf16: 33.4 us, 5.0 TB/s, four fifths of it written; with two rows a thread 36.2, with four 39.7, all through the
+  // caches 40.8)
+  const long long col_tiles = (p.cols + 127LL) / 128, tiles = (p.rows + 15LL) / 16 * col_tiles;
   if (tiles > kMaxTiles) return hipErrorInvalidValue;
   p.col_tiles = (int)col_tiles;
-  hipLaunchKernelGGL((dequantize_kernel<T, PASSES>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+  const bool far = (long long)p.rows * p.cols * (int)sizeof(T) >= kFarBytes;
+  hipLaunchKernelGGL((far ? dequantize_kernel<T, true> : dequantize_kernel<T, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -2,8 +2,8 @@
 //
 // Memory bound: a row is read once, stays in the registers of the lanes that share it -- in its storage type, as it was rounded for the
 // residual stream -- and leaves them normalised, in its type or in blocks of 32 with a scale.  The scale of a block is the maximum over 4 (16-bit
-// types) or 8 neighbouring lanes.  Scales lie [block][row]: a workgroup takes 4 rows or more where it can, collects theirs in LDS and
-// writes words of 4.
+// types) or 8 neighbouring lanes.  Scales lie [block][row]: a workgroup that takes several rows collects theirs in LDS and writes
+// words of 4 or 2.
 //
 // Squares are added in fp64, whose rate here is that of fp32: 1 / sqrt(mean) is the nearest fp32 however long the row and large its values, and
 // the elements of y are then rounded to 8 bits on the same side by whoever works them out in this order.
@@ -58,14 +58,14 @@ __device__ __forceinline__ void load_weights(const TW* w, int col, int cols, flo
   }
 }
 
-// Sum over the LANES threads of a row, the same bits in all of them.  LANES > 64: `room` holds a sum of every wavefront of the row; contains
-// a barrier.
+// Sum over the LANES threads of a row, the same bits in all of them.  LANES > 64: `room`, the row's own, holds a sum of each of its wavefronts;
+// contains a barrier of the workgroup.
 template <int LANES>
 __device__ __forceinline__ double row_sum(double v, double* room) {
 #pragma unroll
   for (int m = LANES < 64 ? LANES / 2 : 32; m; m >>= 1) v += __shfl_xor(v, m);
   if constexpr (LANES > 64) {
-    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x % LANES >> 6] = v;
     __syncthreads();
     v = room[0];
 #pragma unroll
@@ -78,8 +78,9 @@ __device__ __forceinline__ double row_sum(double v, double* room) {
 // the caches by.
 template <typename T, typename TW, int LANES, int CHUNKS, bool STREAM>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(const NormArgs p) {
+  static_assert(LANES >= 256 || 256 % LANES == 0, "whole rows");
   constexpr int N = Chunk<T>::N, ROWS = LANES > 256 ? 1 : 256 / LANES, BLOCKS = LANES * CHUNKS * N / kBlock;
-  __shared__ double room[LANES > 64 ? LANES / 64 : 1];
+  __shared__ double room[LANES > 64 ? ROWS : 1][LANES > 64 ? LANES / 64 : 1];
   __shared__ __attribute__((aligned(16))) unsigned char codes[ROWS > 1 ? BLOCKS * ROWS : 4];
   const int tid = threadIdx.x, lane = tid % LANES, mine = tid / LANES;
   const int row0 = blockIdx.x * ROWS, row = row0 + mine;
@@ -127,7 +128,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(const N
 #pragma unroll
     for (int e = 0; e < N; ++e) squares = __builtin_fma((double)v[e], (double)v[e], squares);
   }
-  squares = row_sum<LANES>(squares, room);
+  squares = row_sum<LANES>(squares, room[LANES > 64 ? mine : 0]);
   const float rstd = (float)(1.0 / sqrt(squares / p.cols + (double)p.eps));
   if (p.rstd && active && lane == 0) p.rstd[row] = rstd;
 
@@ -150,7 +151,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(const N
         if (col + e >= p.cols) v[e] = 0.0f;  // (0 * NaN of a row's statistics, were they left)
       const int code = scale_code(largest_of_block<N>(v), p.format), block = col / kBlock;
       if (col < filled) {
-        if (active) store_elements<N>(values, col, p.format, v, code);
+        if (active) store_elements<N, STREAM>(values, col, p.format, v, code);
         if (col % kBlock == 0) {
           if constexpr (ROWS > 1)
             codes[block * ROWS + mine] = (unsigned char)code;
@@ -163,13 +164,14 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(const N
   if constexpr (ROWS > 1) {
     if (!p.values) return;
     __syncthreads();
-    constexpr int WORDS = ROWS / 4;
+    using Word = typename std::conditional<ROWS % 4 == 0, unsigned, unsigned short>::type;
+    constexpr int EACH = (int)sizeof(Word), WORDS = ROWS / EACH;
     for (int i = tid; i < filled / kBlock * WORDS; i += 256) {
-      const int block = i / WORDS, first = i % WORDS * 4;
+      const int block = i / WORDS, first = i % WORDS * EACH;
       unsigned char* to = p.scales + (long long)block * p.stride_scales + row0 + first;
       const unsigned char* from = codes + block * ROWS + first;
-      if (row0 + first + 4 <= p.rows)
-        *reinterpret_cast<unsigned*>(to) = *reinterpret_cast<const unsigned*>(from);
+      if (row0 + first + EACH <= p.rows)
+        *reinterpret_cast<Word*>(to) = *reinterpret_cast<const Word*>(from);
       else
         for (int r = 0; row0 + first + r < p.rows; ++r) to[r] = from[r];
     }
@@ -186,23 +188,28 @@ hipError_t launch_norm(const NormArgs& p, bool far, hipStream_t stream) {
     hipLaunchKernelGGL((norm_kernel<T, TW, LANES, CHUNKS, false>), grid, block, 0, stream, p);
   return hipGetLastError();
 }
-// How many lanes share a row.  Many rows: as few as hold it, since every row's lanes wait for one another once.  Few rows: more of them, with a
-// chunk or two each.
+// How many lanes share a row: two or three chunks each (bf16, x + residual into y and the stream: 16384 x 4096 by 256 lanes 87.7 us, 6.1 TB/s, by 128
+// 91.1, by 64 94.4; 32768 x 2048 by 128 88.3, by 64 91.0, by 512 111; 16384 x 8192 into 8 bits by 512 166 us, by 256 172, by 1024 191).  Few
+// rows: one chunk, since the row's latency is all there is.
 template <typename T, typename TW>
 hipError_t dispatch_norm(const NormArgs& p, bool far, hipStream_t stream) {
   const int chunks = (int)(blocks_of(p.cols) * kBlock / Chunk<T>::N);
-  const bool few = p.rows < 1024;
   if (chunks <= 16) return launch_norm<T, TW, 16, 1>(p, far, stream);
   if (chunks <= 64) return launch_norm<T, TW, 64, 1>(p, far, stream);
-  if (few) {
+  if (p.rows < 1024) {
     if (chunks <= 256) return launch_norm<T, TW, 256, 1>(p, far, stream);
-    if (chunks <= 512) return launch_norm<T, TW, 256, 2>(p, far, stream);
+    if (chunks <= 512) return launch_norm<T, TW, 512, 1>(p, far, stream);
+    if (chunks <= 1024) return launch_norm<T, TW, 1024, 1>(p, far, stream);
   }
   if (chunks <= 128) return launch_norm<T, TW, 64, 2>(p, far, stream);
-  if (chunks <= 256) return launch_norm<T, TW, 64, 4>(p, far, stream);
-  if (chunks <= 512) return launch_norm<T, TW, 64, 8>(p, far, stream);
-  if (chunks <= 1024) return launch_norm<T, TW, 256, 4>(p, far, stream);
-  if (chunks <= 2048) return launch_norm<T, TW, 256, 8>(p, far, stream);
+  if (chunks <= 192) return launch_norm<T, TW, 64, 3>(p, far, stream);
+  if (chunks <= 256) return launch_norm<T, TW, 128, 2>(p, far, stream);
+  if (chunks <= 384) return launch_norm<T, TW, 128, 3>(p, far, stream);
+  if (chunks <= 512) return launch_norm<T, TW, 256, 2>(p, far, stream);
+  if (chunks <= 768) return launch_norm<T, TW, 256, 3>(p, far, stream);
+  if (chunks <= 1024) return launch_norm<T, TW, 512, 2>(p, far, stream);
+  if (chunks <= 1536) return launch_norm<T, TW, 512, 3>(p, far, stream);
+  if (chunks <= 2048) return launch_norm<T, TW, 1024, 2>(p, far, stream);
   if (chunks <= 4096) return launch_norm<T, TW, 1024, 4>(p, far, stream);
   return launch_norm<T, TW, 1024, 8>(p, far, stream);
 }
@@ -223,11 +230,11 @@ struct GradArgs {
 static_assert(sizeof(GradArgs) <= 112, "a launch with more takes longer");
 
 // A workgroup takes every gridDim-th group of rows and keeps its part of the weight's gradient in registers: lanes hold the same columns of
-// every row.  LANES > 64: one row at a time.
-template <typename T, typename TW, int LANES, int CHUNKS>
+// every row.  AHEAD: the loads of the next rows are on their way while one group is worked on.
+template <typename T, typename TW, int LANES, int CHUNKS, bool AHEAD, bool STREAM>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const GradArgs p) {
   constexpr int N = Chunk<T>::N, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES, COLS = LANES * CHUNKS * N;
-  __shared__ double room[2][LANES > 64 ? LANES / 64 : 1];
+  __shared__ double room[2][ROWS][LANES > 64 ? LANES / 64 : 1];
   __shared__ float meet[ROWS > 1 ? (ROWS - 1) * COLS : 1];
   const int tid = threadIdx.x, lane = tid % LANES, mine = tid / LANES;
   const TW* weight = reinterpret_cast<const TW*>(p.weight);
@@ -239,29 +246,46 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
     for (int e = 0; e < N; ++e) total[i][e] = 0.0f;
   }
   const int groups = (p.rows + ROWS - 1) / ROWS;
-  int turn = 0;
-  for (int group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
-    const int row = group * ROWS + mine;
-    const bool active = row < p.rows;
-    const long long at = active ? row : p.rows - 1;
+  u32x4 next_g[CHUNKS], next_h[CHUNKS], next_s[CHUNKS];
+  float next_rstd;
+  auto load = [&](int group) {
+    const long long at = min(group * ROWS + mine, p.rows - 1);  // (a thread without a row reads the last one, and nothing comes of it)
     const T* gy = reinterpret_cast<const T*>(p.grad_y) + at * p.ldg;
     const T* hh = reinterpret_cast<const T*>(p.h) + at * p.ldh;
-    u32x4 rg[CHUNKS], rh[CHUNKS], rs[CHUNKS];
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int col = (i * LANES + lane) * N;
-      rg[i] = load_chunk<T>(gy + col, p.cols - col);
-      rh[i] = load_chunk<T>(hh + col, p.cols - col);
+      next_g[i] = load_chunk<T, STREAM>(gy + col, p.cols - col);
+      next_h[i] = load_chunk<T, STREAM>(hh + col, p.cols - col);
     }
     if (p.grad_sum) {
       const T* gs = reinterpret_cast<const T*>(p.grad_sum) + at * p.lds;
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
         const int col = (i * LANES + lane) * N;
-        rs[i] = load_chunk<T>(gs + col, p.cols - col);
+        next_s[i] = load_chunk<T, STREAM>(gs + col, p.cols - col);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < CHUNKS; ++i) next_s[i] = u32x4{0, 0, 0, 0};
     }
-    const float rstd = p.rstd[at];
+    next_rstd = p.rstd[at];
+  };
+  if (AHEAD) load(blockIdx.x);
+  int turn = 0;
+  for (int group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
+    const int row = group * ROWS + mine;
+    const bool active = row < p.rows;
+    if (!AHEAD) load(group);
+    u32x4 rg[CHUNKS], rh[CHUNKS], rs[CHUNKS];
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+      rg[i] = next_g[i];
+      rh[i] = next_h[i];
+      rs[i] = next_s[i];
+    }
+    const float rstd = next_rstd;
+    if (AHEAD && group + (int)gridDim.x < groups) load(group + gridDim.x);
     double dot = 0.0;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
@@ -277,24 +301,19 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
       dot += (double)s;
     }
     // (two rooms in turn: a wavefront may be a row ahead of one that still reads)
-    const float mean = (float)(row_sum<LANES>(dot, room[turn]) / p.cols);
+    const float mean = (float)(row_sum<LANES>(dot, room[turn][mine]) / p.cols);
     if (!active) continue;
-    T* out = reinterpret_cast<T*>(p.grad_h) + at * p.ldo;
+    T* out = reinterpret_cast<T*>(p.grad_h) + (long long)row * p.ldo;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       const int col = (i * LANES + lane) * N;
       float g[N], h[N], s[N];
       unpack<T>(rg[i], g);
       unpack<T>(rh[i], h);
-      if (p.grad_sum) {
-        unpack<T>(rs[i], s);
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) s[e] = 0.0f;
-      }
+      unpack<T>(rs[i], s);
 #pragma unroll
       for (int e = 0; e < N; ++e) g[e] = rstd * (g[e] * w[i][e] - h[e] * rstd * mean) + s[e];
-      store_chunk<T>(out + col, p.cols - col, pack<T>(g));
+      store_chunk<T, STREAM>(out + col, p.cols - col, pack<T>(g));
     }
   }
   if (!p.part) return;
@@ -341,45 +360,46 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, TW* out, 
   out[col] = from_f32<TW>(v);
 }
 
-// Lanes and chunks of a row's gradient; parts: workgroups, and with them rows of the workspace, by the sizes alone.
+// Lanes and chunks of a row's gradient, by its chunks; `most` workgroups, as many as the units hold at once by their registers (8192 x 5120 in bf16 with
+// the residual's gradient: 512 workgroups of 256 x 3 64 us, 768 80, 1024 69).  Workgroups are rows of the workspace: they follow from the
+// sizes alone.
 struct GradCut {
-  int lanes, chunks, parts;
+  int chunks, lanes, each, most;
 };
-// (fp32 rows have twice the chunks: the workspace is sized for either)
-GradCut cut_grad(long long rows, long long cols, int per_chunk) {
-  GradCut c;
+constexpr GradCut kGradCuts[] = {{16, 16, 1, 512},   {64, 64, 1, 512},    {128, 64, 2, 512},   {256, 256, 1, 1024}, {512, 256, 2, 512},
+                                 {768, 256, 3, 512}, {1024, 512, 2, 256}, {1536, 512, 3, 256}, {4096, 1024, 4, 256}, {8192, 1024, 8, 256}};
+int cut_of(long long cols, int per_chunk) {
   const long long chunks = (cols + per_chunk - 1) / per_chunk;
-  c.lanes = chunks <= 16 ? 16 : chunks <= 256 ? 64 : chunks <= 1024 ? 256 : 1024;
-  const long long each = (chunks + c.lanes - 1) / c.lanes;
-  c.chunks = each <= 1 ? 1 : each <= 2 ? 2 : each <= 4 ? 4 : 8;
-  const long long groups = c.lanes >= 256 ? rows : (rows + 256 / c.lanes - 1) / (256 / c.lanes);
-  c.parts = (int)std::min<long long>(groups, 1024);
-  return c;
+  int i = 0;
+  while (kGradCuts[i].chunks < chunks) ++i;  // (kMaxCols of 4 a chunk are 8192)
+  return i;
+}
+int parts_of(long long rows, long long cols, int per_chunk) {
+  const GradCut& c = kGradCuts[cut_of(cols, per_chunk)];
+  const int beside = c.lanes < 256 ? 256 / c.lanes : 1;
+  return (int)std::min<long long>((rows + beside - 1) / beside, c.most);
 }
 
-template <typename T, typename TW, int LANES, int CHUNKS>
-hipError_t launch_grad(const GradArgs& p, int parts, void* grad_weight, hipStream_t stream) {
-  hipLaunchKernelGGL((grad_kernel<T, TW, LANES, CHUNKS>), dim3((unsigned)parts), dim3(LANES > 256 ? LANES : 256), 0, stream, p);
+template <typename T, typename TW, int CUT>
+hipError_t launch_grad(const GradArgs& p, bool far, void* grad_weight, hipStream_t stream) {
+  constexpr GradCut c = kGradCuts[CUT];
+  constexpr bool AHEAD = c.lanes < 1024;  // (1024 lanes have 128 registers each)
+  const int parts = parts_of(p.rows, p.cols, Chunk<T>::N);
+  const dim3 grid((unsigned)parts), block(c.lanes > 256 ? c.lanes : 256);
+  if (far)
+    hipLaunchKernelGGL((grad_kernel<T, TW, c.lanes, c.each, AHEAD, true>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((grad_kernel<T, TW, c.lanes, c.each, AHEAD, false>), grid, block, 0, stream, p);
   if (hipError_t e = hipGetLastError(); e != hipSuccess || !p.part) return e;
   hipLaunchKernelGGL((join_kernel<TW>), dim3((unsigned)((p.cols + 63) / 64)), dim3(1024), 0, stream, (const float*)p.part,
                      reinterpret_cast<TW*>(grad_weight), parts, p.cols);
   return hipGetLastError();
 }
-template <typename T, typename TW>
-hipError_t dispatch_grad(const GradArgs& p, void* grad_weight, hipStream_t stream) {
-  const GradCut c = cut_grad(p.rows, p.cols, Chunk<T>::N);
-  if (c.lanes == 16) return launch_grad<T, TW, 16, 1>(p, c.parts, grad_weight, stream);
-  if (c.lanes == 64) {
-    if (c.chunks == 1) return launch_grad<T, TW, 64, 1>(p, c.parts, grad_weight, stream);
-    if (c.chunks == 2) return launch_grad<T, TW, 64, 2>(p, c.parts, grad_weight, stream);
-    return launch_grad<T, TW, 64, 4>(p, c.parts, grad_weight, stream);
-  }
-  if (c.lanes == 256) {
-    if (c.chunks <= 2) return launch_grad<T, TW, 256, 2>(p, c.parts, grad_weight, stream);
-    return launch_grad<T, TW, 256, 4>(p, c.parts, grad_weight, stream);
-  }
-  if (c.chunks <= 4) return launch_grad<T, TW, 1024, 4>(p, c.parts, grad_weight, stream);
-  return launch_grad<T, TW, 1024, 8>(p, c.parts, grad_weight, stream);
+template <typename T, typename TW, int CUT = 0>
+hipError_t dispatch_grad(int cut, const GradArgs& p, bool far, void* grad_weight, hipStream_t stream) {
+  if constexpr (CUT + 1 < (int)(sizeof(kGradCuts) / sizeof(kGradCuts[0])))
+    if (cut > CUT) return dispatch_grad<T, TW, CUT + 1>(cut, p, far, grad_weight, stream);
+  return launch_grad<T, TW, CUT>(p, far, grad_weight, stream);
 }
 
 hidet_status_t check_norm(int dtype, int weight_dtype, long long rows, long long cols) {
@@ -410,7 +430,9 @@ struct Norm {
 };
 template <typename T, typename TW>
 struct Grad {
-  static hipError_t run(const GradArgs& p, void* grad_weight, hipStream_t s) { return dispatch_grad<T, TW>(p, grad_weight, s); }
+  static hipError_t run(const GradArgs& p, bool far, void* grad_weight, hipStream_t s) {
+    return dispatch_grad<T, TW>(cut_of(p.cols, Chunk<T>::N), p, far, grad_weight, s);
+  }
 };
 
 template <typename TW>
@@ -467,13 +489,14 @@ hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows,
     p.stride_scales = (unsigned)quantized->stride_scales;
     p.format = quantized->format;
   }
-  const hipError_t e = by_types<Norm>(dtype, weight_dtype, p, false, (hipStream_t)stream);
+  const bool far = rows * cols * (long long)size_of(dtype) * (1 + (residual ? 1 : 0) + (sum ? 1 : 0) + (y ? 1 : 0)) > 2 * kFarBytes;
+  const hipError_t e = by_types<Norm>(dtype, weight_dtype, p, far, (hipStream_t)stream);
   return e == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }
 
 int64_t hidet_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0 || rows >= kMaxSide || cols > kMaxCols) return 0;
-  return 4LL * cols * std::max(cut_grad(rows, cols, 4).parts, cut_grad(rows, cols, 8).parts);
+  return 4LL * cols * std::max(parts_of(rows, cols, 4), parts_of(rows, cols, 8));  // (of rows in 32 bits, and in 16)
 }
 
 hidet_status_t hidet_rms_norm_backward(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* grad_y, int64_t ld_grad_y,
@@ -523,7 +546,8 @@ hidet_status_t hidet_rms_norm_backward(int32_t dtype, int32_t weight_dtype, int6
   p.rows = (int)rows;
   p.cols = (int)cols;
   p.offset = offset;
-  const hipError_t e = by_types<Grad>(dtype, weight_dtype, p, grad_weight, s);
+  const bool far = rows * cols * (long long)size_of(dtype) * (grad_sum ? 4 : 3) > 2 * kFarBytes;  // (more than the last cache holds)
+  const hipError_t e = by_types<Grad>(dtype, weight_dtype, p, far, grad_weight, s);
   return e == hipSuccess ? HIDET_OK : HIDET_ERR_LAUNCH;
 }
 
