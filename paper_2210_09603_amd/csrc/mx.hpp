@@ -64,10 +64,6 @@ __device__ __forceinline__ float scale_inverse(int code) { return __builtin_bit_
 __device__ __forceinline__ float scale_value(int code) {
   return __builtin_bit_cast(float, code == 0 ? 0x00400000u : code == 255 ? 0x7fc00000u : (unsigned)code << 23);
 }
-__device__ __forceinline__ float fit(float v, float inverse, float top) {
-  // (infinity times the 0 of its block is NaN, which the maximum drops)
-  return inverse == 0.0f ? 0.0f : fminf(fmaxf(v * inverse, -top), top);
-}
 
 // N (4 or 8) values of a block as elements of the format, first in the lowest bits: N / 4 words of 8 bits, one of 4
 template <int N>
@@ -76,9 +72,10 @@ __device__ __forceinline__ void encode(const float (&v)[N], float inverse, int f
   float q[N];
   const float top = largest_value(format);
 #pragma unroll
-  for (int e = 0; e < N; ++e) q[e] = fit(v[e], inverse, top);
-#pragma unroll
   for (int w = 0; w < N / 4; ++w) out[w] = 0;
+  if (inverse == 0.0f) return;  // (no finite scale)
+#pragma unroll
+  for (int e = 0; e < N; ++e) q[e] = __builtin_amdgcn_fmed3f(v[e] * inverse, -top, top);
   if (format == HIDET_MX_E4M3) {
 #pragma unroll
     for (int w = 0; w < N / 4; ++w) {
@@ -190,12 +187,41 @@ __device__ __forceinline__ u32x4 pack(const float (&v)[Chunk<T>::N]) {
   __builtin_memcpy(&raw, t, 16);
   return raw;
 }
-// The largest magnitude of a block that 32 / N consecutive lanes hold.
+// Magnitudes as whole numbers, two of a 16-bit type in a word: they are ordered as the numbers are, infinity and NaN above.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ unsigned larger_pair(unsigned a, unsigned b) {
+  return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b & 0x7fff7fffu)));
+}
+// The number that 16 bits of T are, as the bits of its magnitude in fp32.
+template <typename T>
+__device__ __forceinline__ unsigned widened(unsigned bits) {
+  return magnitude(to_f32(__builtin_bit_cast(T, (unsigned short)bits)));
+}
+// The largest magnitude of a chunk
+template <typename T>
+__device__ __forceinline__ unsigned largest_of_chunk(u32x4 raw) {
+  if constexpr (sizeof(T) == 4) {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = max(m, raw[i] & 0x7fffffffu);
+    return m;
+  } else {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = larger_pair(m, raw[i]);
+    return widened<T>(max(m & 0xffffu, m >> 16));
+  }
+}
 template <int N>
-__device__ __forceinline__ unsigned largest_of_block(const float (&v)[N]) {
+__device__ __forceinline__ unsigned largest_of(const float (&v)[N]) {
   unsigned m = 0;
 #pragma unroll
   for (int e = 0; e < N; ++e) m = max(m, magnitude(v[e]));
+  return m;
+}
+// The same of a block, from those of the 32 / N consecutive lanes that hold it.
+template <int N>
+__device__ __forceinline__ unsigned largest_of_block(unsigned m) {
 #pragma unroll
   for (int d = 1; d < kBlock / N; d <<= 1) m = max(m, (unsigned)__shfl_xor((int)m, d));
   return m;

@@ -27,10 +27,10 @@ struct QuantizeArgs {
   Side by_rows, by_columns;
 };
 
-// How 256 threads go through a tile of COLS columns: LANES of them hold a row, ROWS rows are a pass.
-template <typename T, int COLS>
+// How THREADS threads go through a tile of COLS columns: LANES of them hold a row, ROWS rows are a pass.
+template <typename T, int COLS, int THREADS = 256>
 struct Walk {
-  static constexpr int N = Chunk<T>::N, LANES = COLS / N, ROWS = 256 / LANES;
+  static constexpr int N = Chunk<T>::N, LANES = COLS / N, ROWS = THREADS / LANES;
 };
 
 // One pass of blocks along rows: row r of the tile, `v` its values from column `col` on.
@@ -39,7 +39,7 @@ __device__ __forceinline__ void rows_pass(const QuantizeArgs& p, u32x4 raw, int 
   constexpr int N = Chunk<T>::N;
   float v[N];
   unpack<T>(raw, v);
-  const int code = scale_code(largest_of_block<N>(v), p.by_rows.format);
+  const int code = scale_code(largest_of_block<N>(largest_of_chunk<T>(raw)), p.by_rows.format);
   if (row < p.rows && col < filled) store_elements<N, STREAM>(p.by_rows.values + (long long)row * p.by_rows.stride_values, col, p.by_rows.format, v, code);
   if (col % kBlock == 0) codes[col % COLS / kBlock * TILE_ROWS + r] = (unsigned char)code;
 }
@@ -47,7 +47,7 @@ __device__ __forceinline__ void rows_pass(const QuantizeArgs& p, u32x4 raw, int 
 template <int COLS, int TILE_ROWS>
 __device__ __forceinline__ void write_codes(const Side& s, const unsigned char* codes, int row0, int rows, int block0, int blocks) {
   constexpr int WORDS = TILE_ROWS / 4;
-  for (int i = threadIdx.x; i < COLS / kBlock * WORDS; i += 256) {
+  for (int i = threadIdx.x; i < COLS / kBlock * WORDS; i += blockDim.x) {
     const int b = i / WORDS, first = i % WORDS * 4;
     if (block0 + b >= blocks) continue;
     unsigned char* to = s.scales + (long long)(block0 + b) * s.stride_scales + row0 + first;
@@ -79,22 +79,44 @@ __global__ __launch_bounds__(256) void rows_kernel(const QuantizeArgs p) {
   write_codes<COLS, TILE_ROWS>(p.by_rows, codes, row0, p.rows, tile_col * (COLS / kBlock), filled / kBlock);
 }
 
+// 32 rows of two neighbouring columns of a tile in LDS.
 template <typename T>
-struct Two {
-  T a, b;
+struct Pair {
+  unsigned raw[kBlock * (int)sizeof(T) / 2];
+  // the larger magnitude of either column
+  __device__ __forceinline__ void largest(unsigned (&top)[2]) const {
+    if constexpr (sizeof(T) == 4) {
+      top[0] = top[1] = 0;
+#pragma unroll
+      for (int i = 0; i < 2 * kBlock; ++i) top[i & 1] = max(top[i & 1], raw[i] & 0x7fffffffu);
+    } else {
+      unsigned m = 0;
+#pragma unroll
+      for (int i = 0; i < kBlock; ++i) m = larger_pair(m, raw[i]);
+      top[0] = widened<T>(m & 0xffffu);
+      top[1] = widened<T>(m >> 16);
+    }
+  }
+  __device__ __forceinline__ float value(int row, int column) const {
+    if constexpr (sizeof(T) == 4)
+      return __builtin_bit_cast(float, raw[2 * row + column]);
+    else
+      return to_f32(__builtin_bit_cast(T, (unsigned short)(column ? raw[row] >> 16 : raw[row] & 0xffffu)));
+  }
 };
-// The 32 elements of a block, 16 or 32 bytes of LDS
-__device__ __forceinline__ void put_block(unsigned char* to, int format, const float (&v)[kBlock], int code) {
+// The elements of a column of them, 16 or 32 bytes of LDS
+template <typename T>
+__device__ __forceinline__ void put_block(unsigned char* to, int format, const Pair<T>& two, int column, int code) {
   unsigned words[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float part[8];
-    unsigned two[2];
+    unsigned out[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) part[e] = v[8 * i + e];
-    encode<8>(part, scale_inverse(code), format, two);
-    words[2 * i] = two[0];
-    words[2 * i + 1] = two[1];
+    for (int e = 0; e < 8; ++e) part[e] = two.value(8 * i + e, column);
+    encode<8>(part, scale_inverse(code), format, out);
+    words[2 * i] = out[0];
+    words[2 * i + 1] = out[1];
   }
   if (format == HIDET_MX_E2M1) {
     *reinterpret_cast<u32x4*>(to) = u32x4{words[0], words[2], words[4], words[6]};
@@ -104,10 +126,10 @@ __device__ __forceinline__ void put_block(unsigned char* to, int format, const f
   }
 }
 
-template <typename T, bool STREAM>
-__global__ __launch_bounds__(256) void columns_kernel(const QuantizeArgs p) {
-  constexpr int COLS = 128, TILE_ROWS = 128;
-  using W = Walk<T, COLS>;
+template <typename T, int TILE_ROWS, bool STREAM>
+__global__ __launch_bounds__(2 * TILE_ROWS) void columns_kernel(const QuantizeArgs p) {
+  constexpr int COLS = 128, THREADS = 2 * TILE_ROWS;  // (a thread for two columns of a block)
+  using W = Walk<T, COLS, THREADS>;
   constexpr int PASSES = TILE_ROWS / W::ROWS;
   __shared__ __attribute__((aligned(16))) T tile[TILE_ROWS * COLS];
   __shared__ __attribute__((aligned(4))) unsigned char codes[COLS / kBlock * TILE_ROWS];
@@ -135,17 +157,12 @@ __global__ __launch_bounds__(256) void columns_kernel(const QuantizeArgs p) {
   const Side& s = p.by_columns;
   const int pair = threadIdx.x % 64 * 2, block = threadIdx.x / 64, each = s.format == HIDET_MX_E2M1 ? 16 : 32;
   const long long column = (long long)tile_col * COLS + pair;
-  float a[kBlock], b[kBlock];
-  unsigned top_a = 0, top_b = 0;
+  Pair<T> two;
 #pragma unroll
-  for (int r = 0; r < kBlock; ++r) {
-    const Two<T> two = *reinterpret_cast<const Two<T>*>(tile + (block * kBlock + r) * COLS + pair);
-    a[r] = to_f32(two.a);
-    b[r] = to_f32(two.b);
-    top_a = max(top_a, magnitude(a[r]));
-    top_b = max(top_b, magnitude(b[r]));
-  }
-  const int code_a = scale_code(top_a, s.format), code_b = scale_code(top_b, s.format);
+  for (int r = 0; r < kBlock; ++r) __builtin_memcpy(two.raw + r * (int)sizeof(T) / 2, tile + (block * kBlock + r) * COLS + pair, 2 * sizeof(T));
+  unsigned top[2];
+  two.largest(top);
+  const int code_a = scale_code(top[0], s.format), code_b = scale_code(top[1], s.format);
   if (column < p.cols && row0 + block * kBlock < p.rows) {
     unsigned char* scales = s.scales + (long long)(row0 / kBlock + block) * s.stride_scales + column;
     if (column + 1 < p.cols)
@@ -155,11 +172,11 @@ __global__ __launch_bounds__(256) void columns_kernel(const QuantizeArgs p) {
   }
   __syncthreads();  // (the tile is read)
   unsigned char* out = reinterpret_cast<unsigned char*>(tile);
-  put_block(out + pair * PITCH + block * each, s.format, a, code_a);
-  put_block(out + (pair + 1) * PITCH + block * each, s.format, b, code_b);
+  put_block(out + pair * PITCH + block * each, s.format, two, 0, code_a);
+  put_block(out + (pair + 1) * PITCH + block * each, s.format, two, 1, code_b);
   __syncthreads();
   const int chunks = TILE_ROWS / kBlock * each / 16;  // of a row of the transposed matrix
-  for (int i = threadIdx.x; i < COLS * chunks; i += 256) {
+  for (int i = threadIdx.x; i < COLS * chunks; i += THREADS) {
     const int r = i / chunks, c = i - r * chunks;
     if (tile_col * COLS + r >= p.cols || row0 + c * 16 / each * kBlock >= p.rows) continue;
     unsigned char* to = s.values + (long long)(tile_col * COLS + r) * s.stride_values + (long long)row0 / kBlock * each + c * 16;
@@ -178,7 +195,7 @@ hipError_t launch_quantize(QuantizeArgs p, hipStream_t stream) {
   if (p.by_columns.values) {
     const long long tiles = grid(128, 128);
     if (tiles > kMaxTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((far ? columns_kernel<T, true> : columns_kernel<T, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((far ? columns_kernel<T, 128, true> : columns_kernel<T, 128, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
     return hipGetLastError();
   }
   // Rows of 1 KB or more of a tile, four loads a thread in flight: 16384 x 4096 in bf16 into 4 bits 28.8 us (5.8 TB/s); 128 columns 32.1, two

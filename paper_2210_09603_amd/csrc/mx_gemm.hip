@@ -147,8 +147,6 @@ hidet_status_t hidet_mx_gemm(int32_t out, int64_t M, int64_t N, int64_t K, const
   p.N = (int)N;
   p.blocks = (int)blocks_of(K);
   p.alpha = 1.0f;
-  const size_t four = 4 * size_of(out);
-  bool quads = is_aligned(C, four) && (M == 1 || ldc % 4 == 0);
   p.flags = (unsigned)out;
   if (epi) {
     p.alpha = epi->alpha;
@@ -156,9 +154,8 @@ hidet_status_t hidet_mx_gemm(int32_t out, int64_t M, int64_t N, int64_t K, const
     p.residual = epi->residual;
     p.ldr = epi->residual ? (unsigned)epi->ld_residual : 0;
     p.flags |= (unsigned)epi->bias_axis << 2 | (epi->act == HIDET_ACT_RELU ? 16u : 0u);
-    if (epi->residual) quads = quads && is_aligned(epi->residual, four) && (M == 1 || epi->ld_residual % 4 == 0);
   }
-  p.flags |= (quads ? 32u : 0u) | (unsigned)c.slices << 8;
+  p.flags |= (unsigned)c.slices << 8;
   p.slice = c.slice;
   if (c.slices > 1) p.c = workspace;
   const hipStream_t s = (hipStream_t)stream;

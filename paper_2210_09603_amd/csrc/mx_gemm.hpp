@@ -35,7 +35,7 @@ struct GemmArgs {
   unsigned ldc, ldr;                            // elements
   int M, N, blocks;                             // blocks: of K
   float alpha;
-  unsigned flags;  // bits 0-1 dtype of C, 2-3 bias axis, 4 ReLU, 5 rows of C and residual are aligned to 4 elements, 8.. slices
+  unsigned flags;  // bits 0-1 dtype of C, 2-3 bias axis, 4 ReLU, 8.. slices
   int slice;       // K steps of 128 of a slice
 };
 static_assert(sizeof(GemmArgs) <= 112, "a launch with more takes longer");
@@ -76,13 +76,13 @@ __device__ __forceinline__ f32x4 multiply(const Fragment<FA>& a, const Fragment<
 // Columns n .. n + 3 of row m, as the other products finish theirs: alpha, bias, residual, ReLU, one rounding.
 template <typename TO>
 __device__ __forceinline__ void finish4(const GemmArgs& p, int m, int n, const float (&sum)[4]) {
-  struct __attribute__((aligned(4 * sizeof(TO)))) Quad {
+  struct __attribute__((packed, aligned(sizeof(TO)))) Quad {  // (one access, at element alignment)
     TO e[4];
   };
   const int left = p.N - n;
   if (m >= p.M || left <= 0) return;
   const int axis = (p.flags >> 2) & 3;
-  const bool whole = (p.flags & 32) != 0 && left >= 4;
+  const bool whole = left >= 4;
   const TO* bias = reinterpret_cast<const TO*>(p.bias);
   float v[4];
 #pragma unroll
@@ -135,8 +135,11 @@ __device__ __forceinline__ void keep4(const GemmArgs& p, int slice, int m, int n
   const int left = p.N - n;
   if (m >= p.M || left <= 0) return;
   float* c = reinterpret_cast<float*>(p.c) + ((long long)slice * p.M + m) * p.N + n;
-  if (left >= 4 && p.N % 4 == 0) {
-    *reinterpret_cast<f32x4*>(c) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+  struct __attribute__((packed, aligned(4))) Quad {
+    f32x4 v;
+  };
+  if (left >= 4) {
+    reinterpret_cast<Quad*>(c)->v = f32x4{sum[0], sum[1], sum[2], sum[3]};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -491,6 +494,16 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
   Rows<FB, GROUP_N> b;
   a.init(p.a, p.scales_a, p.lda, p.ld_scales_a, m0, p.M, p.blocks, lane);
   b.init(p.b, p.scales_b, p.ldb, p.ld_scales_b, n0, p.N, p.blocks, lane);
+  // (the residual is asked for before all else, so that it is at hand when the sums are)
+  unsigned near = 0;
+  if (p.residual && slices == 1 && wave < FM) {
+    const int size = (p.flags & 3) == HIDET_F32 ? 4 : 2, col = n0 + (GROUP_N ? 4 : 1) * (lane % 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = m0 + (GROUP_M ? 16 * (lane / 16) + 4 * e + wave : 4 * (lane / 16) + e);
+      if (row < p.M && col < p.N) near |= *reinterpret_cast<const unsigned short*>(reinterpret_cast<const unsigned char*>(p.residual) + ((long long)row * p.ldr + col) * size);
+    }
+  }
   f32x4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -528,6 +541,7 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
     b.load_end(step, lane, fb[0], sb[0]);
     product(0);
   }
+  asm volatile("" ::"v"(near));
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -577,12 +591,15 @@ __global__ __launch_bounds__(256) void join_slices_kernel(const GemmArgs p, cons
   if (m >= p.M) return;
   const float* from = workspace + (long long)m * p.N + n;
   const long long each = (long long)p.M * p.N;
-  const bool whole = p.N % 4 == 0;
+  struct __attribute__((packed, aligned(4))) Quad {
+    f32x4 v;
+  };
+  const bool whole = n + 4 <= p.N;
   float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 4
   for (int s = 0; s < slices; ++s) {
     if (whole) {
-      const f32x4 t = *reinterpret_cast<const f32x4*>(from + s * each);
+      const f32x4 t = reinterpret_cast<const Quad*>(from + s * each)->v;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += t[e];
     } else {

@@ -149,7 +149,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(const N
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (col + e >= p.cols) v[e] = 0.0f;  // (0 * NaN of a row's statistics, were they left)
-      const int code = scale_code(largest_of_block<N>(v), p.format), block = col / kBlock;
+      const int code = scale_code(largest_of_block<N>(largest_of(v)), p.format), block = col / kBlock;
       if (col < filled) {
         if (active) store_elements<N, STREAM>(values, col, p.format, v, code);
         if (col % kBlock == 0) {
