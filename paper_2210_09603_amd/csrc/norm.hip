@@ -58,12 +58,63 @@ __device__ __forceinline__ void load_weights(const TW* w, int col, int cols, flo
   }
 }
 
+// A sum over 16 or 64 lanes, the same bits in all of them (a + b and b + a are), without the LDS that shuffles go through: neighbours, pairs, then the
+// lanes of 8 and of 16 mirrored, then rows of 16 and halves exchanged.
+template <int CONTROL>
+__device__ __forceinline__ unsigned lanes_moved(unsigned v) {
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CONTROL, 0xf, 0xf, true);
+}
+template <int CONTROL>
+__device__ __forceinline__ float moved(float v) {
+  return __builtin_bit_cast(float, lanes_moved<CONTROL>(__builtin_bit_cast(unsigned, v)));
+}
+template <int CONTROL>
+__device__ __forceinline__ double moved(double v) {
+  const u32x2 u = __builtin_bit_cast(u32x2, v);
+  return __builtin_bit_cast(double, u32x2{lanes_moved<CONTROL>(u[0]), lanes_moved<CONTROL>(u[1])});
+}
+template <bool HALVES>
+__device__ __forceinline__ void exchanged(unsigned u, unsigned& a, unsigned& b) {
+  if constexpr (HALVES) {
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    a = (unsigned)r[0], b = (unsigned)r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    a = (unsigned)r[0], b = (unsigned)r[1];
+  }
+}
+template <bool HALVES>
+__device__ __forceinline__ float sum_exchanged(float v) {
+  unsigned a, b;
+  exchanged<HALVES>(__builtin_bit_cast(unsigned, v), a, b);
+  return __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b);
+}
+template <bool HALVES>
+__device__ __forceinline__ double sum_exchanged(double v) {
+  const u32x2 u = __builtin_bit_cast(u32x2, v);
+  unsigned a[2], b[2];
+  exchanged<HALVES>(u[0], a[0], b[0]);
+  exchanged<HALVES>(u[1], a[1], b[1]);
+  return __builtin_bit_cast(double, u32x2{a[0], a[1]}) + __builtin_bit_cast(double, u32x2{b[0], b[1]});
+}
+template <int LANES, typename S>
+__device__ __forceinline__ S lane_sum(S v) {
+  static_assert(LANES == 16 || LANES >= 64, "a row of lanes, or whole wavefronts");
+  v += moved<0xb1>(v);   // quad_perm 1 0 3 2
+  v += moved<0x4e>(v);   // quad_perm 2 3 0 1
+  v += moved<0x141>(v);  // row_half_mirror
+  v += moved<0x140>(v);  // row_mirror
+  if constexpr (LANES >= 64) {
+    v = sum_exchanged<false>(v);
+    v = sum_exchanged<true>(v);
+  }
+  return v;
+}
 // Sum over the LANES threads of a row, the same bits in all of them.  LANES > 64: `room`, the row's own, holds a sum of each of its wavefronts;
 // contains a barrier of the workgroup.
-template <int LANES>
-__device__ __forceinline__ double row_sum(double v, double* room) {
-#pragma unroll
-  for (int m = LANES < 64 ? LANES / 2 : 32; m; m >>= 1) v += __shfl_xor(v, m);
+template <int LANES, typename S>
+__device__ __forceinline__ S row_sum(S v, S* room) {
+  v = lane_sum<LANES>(v);
   if constexpr (LANES > 64) {
     if ((threadIdx.x & 63) == 0) room[threadIdx.x % LANES >> 6] = v;
     __syncthreads();
@@ -234,7 +285,7 @@ static_assert(sizeof(GradArgs) <= 112, "a launch with more takes longer");
 template <typename T, typename TW, int LANES, int CHUNKS, bool AHEAD, bool STREAM>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const GradArgs p) {
   constexpr int N = Chunk<T>::N, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES, COLS = LANES * CHUNKS * N;
-  __shared__ double room[2][ROWS][LANES > 64 ? LANES / 64 : 1];
+  __shared__ float room[2][ROWS][LANES > 64 ? LANES / 64 : 1];
   __shared__ float meet[ROWS > 1 ? (ROWS - 1) * COLS : 1];
   const int tid = threadIdx.x, lane = tid % LANES, mine = tid / LANES;
   const TW* weight = reinterpret_cast<const TW*>(p.weight);
@@ -286,22 +337,21 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
     }
     const float rstd = next_rstd;
     if (AHEAD && group + (int)gridDim.x < groups) load(group + gridDim.x);
-    double dot = 0.0;
+    float dot = 0.0f;
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
-      float g[N], h[N], s = 0.0f;
+      float g[N], h[N];
       unpack<T>(rg[i], g);
       unpack<T>(rh[i], h);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float xhat = h[e] * rstd;
-        s += g[e] * w[i][e] * xhat;
+        dot += g[e] * w[i][e] * xhat;
         if (active) total[i][e] += g[e] * xhat;
       }
-      dot += (double)s;
     }
     // (two rooms in turn: a wavefront may be a row ahead of one that still reads)
-    const float mean = (float)(row_sum<LANES>(dot, room[turn][mine]) / p.cols);
+    const float mean = row_sum<LANES>(dot, room[turn][mine]) / (float)p.cols;
     if (!active) continue;
     T* out = reinterpret_cast<T*>(p.grad_h) + (long long)row * p.ldo;
 #pragma unroll
