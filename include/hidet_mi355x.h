@@ -568,7 +568,9 @@ typedef struct {
  * elements are x / scale, rounded to nearest even and cut to the largest value of the format.  A block that holds a NaN or an
  * infinity has the scale NaN and elements 0.
  * hidet_mx_dequantize: y [rows][cols] of dtype, rounded once.
- * rows or cols of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: rows or cols of 2^29 or more, rows * ld beyond 2^47 elements.
+ * Nothing that is written may overlap anything else.
+ * rows or cols of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: rows or cols of 2^29 or more, rows * ld beyond 2^47 elements, 2^24 tiles or more (of
+ * 16 x 128 elements at the smallest).
  */
 hidet_status_t hidet_mx_quantize(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const hidet_mx_t* by_rows,
                                  const hidet_mx_t* by_columns, void* stream);
@@ -582,7 +584,8 @@ hidet_status_t hidet_mx_dequantize(int64_t rows, int64_t cols, const hidet_mx_t*
  * aligned, hidet_mx_gemm_workspace_bytes() for as many as the library would like; with less, or NULL, it cuts into fewer) in ascending
  * order.  Calls that share a workspace must be ordered on one stream.
  * M or N of 0 is an OK no-op; K == 0 writes epilogue(0).  HIDET_ERR_UNSUPPORTED: M, N or K of 2^29 or more, ldc or ld_residual of 2^32
- * or more, a head-split output map, an input prologue.
+ * or more, 2^22 tiles or more (of 16 x 16 elements for M of up to 16, at least 64 x 64 or 16 x 64 otherwise), a head-split output map, an
+ * input prologue.
  */
 hidet_status_t hidet_mx_gemm(int32_t out, int64_t M, int64_t N, int64_t K, const hidet_mx_t* A, const hidet_mx_t* B, void* C, int64_t ldc,
                              const hidet_epilogue_t* epi, void* workspace, int64_t workspace_bytes, void* stream);
@@ -603,7 +606,8 @@ int64_t hidet_mx_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K, int32_t f
  * wanted, and no workspace is.  Sums over rows are fp32, in an order that depends on the sizes alone: no atomics.  The workspace:
  * 16-byte aligned, HIDET_ERR_INVALID_ARG if it is smaller than hidet_rms_norm_backward_workspace_bytes.
  * Both: rows or cols of 0 is an OK no-op, but for grad_weight of no rows, which is 0.  HIDET_ERR_UNSUPPORTED: cols above 32768, rows of 2^29 or
- * more, leading dimensions of 2^32 or more, rows * ld beyond 2^47 elements.
+ * more, leading dimensions of 2^32 or more, rows * ld beyond 2^47 elements; hidet_rms_norm: rows that take 2^32 threads or
+ * more (up to 1024 each: fewer than 2^22 rows are always served).
  */
 hidet_status_t hidet_rms_norm(int32_t dtype, int32_t weight_dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx,
                               const void* residual, int64_t ld_residual, const void* weight, float eps, float offset, void* sum,

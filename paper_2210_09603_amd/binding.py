@@ -1093,7 +1093,13 @@ def _mx_gemm(A, B, C, epilogue, workspace, stream):
     if tuple(C.shape) != (M, N):
         raise ValueError("expected C of shape %s, got %s" % ((M, N), tuple(C.shape)))
     wp, wb = _dense_ws(workspace)
-    kept = tuple(epilogue._keep) if epilogue is not None else ()
+    kept = bias, residual = epilogue._keep if epilogue is not None else (None, None)
+    if bias is not None and epilogue.bias_axis != HIDET_BIAS_NONE:
+        length = M if epilogue.bias_axis == HIDET_BIAS_PER_ROW else N
+        if bias.dtype != C.dtype or bias.numel() != length or not bias.is_contiguous():
+            raise ValueError("the bias must be a dense vector of %d elements of C's dtype" % length)
+    if residual is not None and epilogue.out_map == HIDET_MAP_PLAIN and (residual.dtype != C.dtype or residual.shape != C.shape):
+        raise ValueError("the residual must have C's shape and dtype")
     device, handle = _on((C, workspace) + _mx(A, (M, K)) + _mx(B, (N, K)) + kept, stream)
     with device:
         st = lib().hidet_mx_gemm(_dtype(C), M, N, K, A, B, _ptr(C), _ld(C), epilogue, wp, wb, handle)

@@ -866,19 +866,25 @@ PyObject* call_mx_gemm(PyObject* self, PyObject* const* a, Py_ssize_t n) {
     if (!y || !arg || y->dim() != 2 || !arg.ld(ld) || !x.ok() || !w.ok()) return kGeneral;
     const int64_t m = x.rows(), rows = w.rows(), k = x.cols();
     if (!x.fits(t, m, k) || !w.fits(t, rows, k) || y->size(0) != m || y->size(1) != rows) return kGeneral;
-    const at::Tensor* ws = t.workspace(a[4]);
+    const at::Tensor *ws = t.workspace(a[4]), *bias = nullptr, *residual = nullptr;
     if (a[3] != Py_None) {  // (what the epilogue reads is beside the others)
       PyObject* kept = PyObject_GetAttrString(a[3], "_keep");
-      if (kept && PyTuple_CheckExact(kept))
-        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(kept); ++i) t.get(PyTuple_GET_ITEM(kept, i), true);
-      else
+      if (kept && PyTuple_CheckExact(kept) && PyTuple_GET_SIZE(kept) == 2) {
+        bias = t.get(PyTuple_GET_ITEM(kept, 0), true);
+        residual = t.get(PyTuple_GET_ITEM(kept, 1), true);
+      } else {
         t.ok = false;
+      }
       Py_XDECREF(kept);
       PyErr_Clear();
     }
     const Epilogue e(c, a[3]);
     void* stream;
     if (!t.ok || !e.plain() || !stream_on(c, a[5], t, stream)) return kGeneral;
+    if (bias && e.get()->bias_axis != HIDET_BIAS_NONE &&
+        (bias->scalar_type() != y->scalar_type() || !bias->is_contiguous() || bias->numel() != (e.get()->bias_axis == HIDET_BIAS_PER_ROW ? m : rows)))
+      return kGeneral;
+    if (residual && (residual->scalar_type() != y->scalar_type() || residual->sizes() != y->sizes())) return kGeneral;
     return without_lock([&] {
       return c->gemm(arg.dtype, m, rows, k, x.get(), w.get(), y->data_ptr(), ld, e.get(), address<void>(ws), bytes_of(ws), stream);
     });

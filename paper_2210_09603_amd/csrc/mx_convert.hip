@@ -126,6 +126,8 @@ __device__ __forceinline__ void put_block(unsigned char* to, int format, const P
   }
 }
 
+// 4096 x 4096 in 16 bits into 8 along both axes: 17.9 us, 3.8 TB/s, and 4099 x 1003 11.2.  Neither memory nor the vector unit (30 % busy) nor LDS (9 %)
+// bounds it, but four phases with a barrier between them, and 4 workgroups a compute unit to hide one behind another's.
 template <typename T, int TILE_ROWS, bool STREAM>
 __global__ __launch_bounds__(2 * TILE_ROWS) void columns_kernel(const QuantizeArgs p) {
   constexpr int COLS = 128, THREADS = 2 * TILE_ROWS;  // (a thread for two columns of a block)
@@ -281,6 +283,7 @@ hidet_status_t hidet_mx_quantize(int32_t dtype, int64_t rows, int64_t cols, cons
   if (by_columns)
     if (st = check_mx(by_columns, cols, rows); st != HIDET_OK) return st;
   if (rows == 0 || cols == 0) return HIDET_OK;
+  if (by_rows && by_columns && (by_rows->values == by_columns->values || by_rows->scales == by_columns->scales)) return HIDET_ERR_INVALID_ARG;
   if (st = check_rows(x, dtype, rows, cols, ldx); st != HIDET_OK) return st;
   QuantizeArgs p{};
   p.x = x;

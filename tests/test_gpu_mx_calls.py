@@ -111,6 +111,10 @@ def test_gemm(monkeypatch):
         assert both(rec, "hidet_mx_gemm", args, True) is None
     # (another device's bias; a head-split map is the library's to refuse, through the general path)
     cpu = hb.make_epilogue(bias=t(9, device="cpu"), bias_axis=hb.HIDET_BIAS_PER_COL)
+    for x, axis in ((t(6), hb.HIDET_BIAS_PER_COL), (t(9), hb.HIDET_BIAS_PER_ROW), (t(9, dtype=F32), hb.HIDET_BIAS_PER_COL)):
+        assert both(rec, "hidet_mx_gemm", (a, b, t(6, 9), hb.make_epilogue(bias=x, bias_axis=axis), None, None), False) is not None
+    for r in (t(5, 9), t(6, 9, dtype=BF16)):
+        assert both(rec, "hidet_mx_gemm", (a, b, t(6, 9), hb.make_epilogue(residual=r), None, None), False) is not None
     for args in ((a, b, t(6, 8), None, None, None), (a, mx(9, 99), t(6, 9), None, None, None), (a, b, t(9, 6).t(), None, None, None), (a, b, t(54), None, None, None),
                  (a, b, t(6, 9), cpu, None, None), (a, b, t(6, 9), None, t(64, 4)[:, :2], None), (a, mx(9, 100, device="cpu"), t(6, 9), None, None, None)):
         assert both(rec, "hidet_mx_gemm", args, False) is not None

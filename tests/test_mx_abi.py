@@ -79,6 +79,22 @@ def test_quantize_needs_a_destination():
     assert quantize(rows=0) == OK and quantize(cols=0) == OK and dequantize(rows=0, x=None) == OK
 
 
+def test_quantize_needs_two_destinations_for_two():
+    one = blocks(stride_values=1 << 10, stride_scales=1 << 10)
+    assert quantize(by_rows=one, by_columns=one) == INVALID
+    assert quantize(by_rows=one, by_columns=blocks(values=0x8000, stride_scales=1 << 10)) == INVALID
+    assert quantize(by_rows=one, by_columns=blocks(scales=0x8000, stride_scales=1 << 10)) == INVALID
+
+
+def test_more_tiles_than_a_launch_has():
+    # 2^29 - 32 rows: a launch has fewer than 2^32 threads (nothing is launched)
+    rows = (1 << 29) - 32
+    wide = blocks(stride_values=32, stride_scales=rows)
+    assert quantize(rows=rows, cols=32, by_rows=wide) == UNSUPPORTED and dequantize(rows=rows, cols=32, by_rows=wide) == UNSUPPORTED
+    assert norm(rows=rows, cols=1024, ldx=1024, ldr=1024, lds=1024, ldy=1024, q=None) == UNSUPPORTED
+    assert gemm(M=16, N=rows, K=32, A=wide, B=wide, ldc=rows) == UNSUPPORTED
+
+
 def test_gemm():
     assert gemm(out=3) == INVALID and gemm(M=-1) == INVALID and gemm(K=-1) == INVALID and gemm(wb=-1) == INVALID
     for n in ("M", "N", "K"):
