@@ -73,51 +73,80 @@ __device__ __forceinline__ f32x4 multiply(const Fragment<FA>& a, const Fragment<
 }
 
 // ---- epilogue -----------------------------------------------------------------------------------------------------------
-// Columns n .. n + 3 of row m, as the other products finish theirs: alpha, bias, residual, ReLU, one rounding.
-template <typename TO>
-__device__ __forceinline__ void finish4(const GemmArgs& p, int m, int n, const float (&sum)[4]) {
+// R rows of H times four neighbouring columns, as the other products finish theirs: alpha, bias, residual, ReLU, one rounding.  All that is read
+// is asked for before anything is written, so that a thread waits once for all of it.
+template <typename TO, int H>
+struct ColumnBias {
+  float v[H][4];  // 0 if there is none
+  __device__ __forceinline__ ColumnBias(const GemmArgs& p, const int (&col)[H]) {
+    const bool any = ((p.flags >> 2) & 3) == HIDET_BIAS_PER_COL;
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[h][e] = any ? to_f32(reinterpret_cast<const TO*>(p.bias)[min(col[h] + e, p.N - 1)]) : 0.0f;
+  }
+};
+template <typename TO, int R, int H>
+__device__ __forceinline__ void finish(const GemmArgs& p, const int (&row)[R], const int (&col)[H], const ColumnBias<TO, H>& bias, const float (&sum)[R][H][4]) {
   struct __attribute__((packed, aligned(sizeof(TO)))) Quad {  // (one access, at element alignment)
     TO e[4];
   };
-  const int left = p.N - n;
-  if (m >= p.M || left <= 0) return;
-  const int axis = (p.flags >> 2) & 3;
-  const bool whole = left >= 4;
-  const TO* bias = reinterpret_cast<const TO*>(p.bias);
-  float v[4];
+  float of_row[R];
+  Quad other[R][H];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = p.alpha * sum[e];
-  if (axis == HIDET_BIAS_PER_ROW) {
-    const float b = to_f32(bias[m]);
+  for (int r = 0; r < R; ++r) {
+    of_row[r] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += b;
-  } else if (axis == HIDET_BIAS_PER_COL) {
+    for (int h = 0; h < H; ++h)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += to_f32(bias[n + (e < left ? e : 0)]);
+      for (int e = 0; e < 4; ++e) other[r][h].e[e] = TO(0.0f);
+  }
+  if (((p.flags >> 2) & 3) == HIDET_BIAS_PER_ROW) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) of_row[r] = to_f32(reinterpret_cast<const TO*>(p.bias)[min(row[r], p.M - 1)]);
   }
   if (p.residual) {
-    const TO* r = reinterpret_cast<const TO*>(p.residual) + (long long)m * p.ldr + n;
-    TO t[4];
-    if (whole) {
-      *reinterpret_cast<Quad*>(t) = *reinterpret_cast<const Quad*>(r);
-    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t[e] = r[e < left ? e : 0];
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        const int left = row[r] < p.M ? p.N - col[h] : 0;
+        const TO* from = reinterpret_cast<const TO*>(p.residual) + (long long)row[r] * p.ldr + col[h];
+        if (left >= 4) {
+          other[r][h] = *reinterpret_cast<const Quad*>(from);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (e < left) other[r][h].e[e] = from[e];
+        }
+      }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      Quad o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = p.alpha * sum[r][h][e] + of_row[r] + bias.v[h][e] + to_f32(other[r][h].e[e]);
+        o.e[e] = from_f32<TO>((p.flags & 16) != 0 && v < 0.0f ? 0.0f : v);
+      }
+      const int left = row[r] < p.M ? p.N - col[h] : 0;
+      TO* c = reinterpret_cast<TO*>(p.c) + (long long)row[r] * p.ldc + col[h];
+      if (left >= 4) {
+        *reinterpret_cast<Quad*>(c) = o;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+          if (e < left) c[e] = o.e[e];
+      }
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += to_f32(t[e]);
-  }
-  TO o[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = from_f32<TO>((p.flags & 16) != 0 && v[e] < 0.0f ? 0.0f : v[e]);
-  TO* c = reinterpret_cast<TO*>(p.c) + (long long)m * p.ldc + n;
-  if (whole) {
-    *reinterpret_cast<Quad*>(c) = *reinterpret_cast<const Quad*>(o);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < left) c[e] = o[e];
-  }
+}
+template <typename TO>
+__device__ __forceinline__ void finish4(const GemmArgs& p, int m, int n, const float (&sum)[4]) {
+  const int row[1] = {m}, col[1] = {n};
+  const float v[1][1][4] = {{{sum[0], sum[1], sum[2], sum[3]}}};
+  finish<TO, 1, 1>(p, row, col, ColumnBias<TO, 1>(p, col), v);
 }
 // f(a value of the type of C)
 template <class F>
@@ -251,12 +280,14 @@ struct Panel {
   }
 };
 
-// Which tile a workgroup takes: workgroups are handed to the 8 dies in turn; each die, which has an L2 of its own, gets one run of tiles, walked
-// 4 tile rows at a time.
+// Workgroups are handed to the 8 dies in turn; each die, which has an L2 of its own, gets one run of `total` places.
+__device__ __forceinline__ unsigned place_of(unsigned at, unsigned total) {
+  const unsigned xcd = at % 8u, each = total / 8u, extra = total % 8u;
+  return xcd * each + (xcd < extra ? xcd : extra) + at / 8u;
+}
+// Which tile a workgroup takes: runs of tiles, walked 4 tile rows at a time.
 __device__ __forceinline__ void tile_of(unsigned at, int tiles_m, int tiles_n, int& i, int& j) {
-  const unsigned total = (unsigned)tiles_m * (unsigned)tiles_n, xcd = at % 8u, slot = at / 8u;
-  const unsigned each = total / 8u, extra = total % 8u;
-  const unsigned w = xcd * each + (xcd < extra ? xcd : extra) + slot;
+  const unsigned w = place_of(at, (unsigned)tiles_m * (unsigned)tiles_n);
   const unsigned panel = w / (4u * tiles_n), first = panel * 4u, rows = min(4u, (unsigned)tiles_m - first), within = w - first * tiles_n;
   i = (int)(first + within % rows);
   j = (int)(within / rows);
@@ -265,23 +296,40 @@ __device__ __forceinline__ void tile_of(unsigned at, int tiles_m, int tiles_n, i
 // What a wavefront has summed: 64 GM x 64 GN from row m and column n on.
 template <int GM, int GN>
 __device__ __forceinline__ void finish_tile(const GemmArgs& p, int slice, int m, int n, int lane, const f32x4 (&acc)[4 * GM][4 * GN]) {
-  auto quads = [&](auto done) {
+  int col[GN];
+#pragma unroll
+  for (int h = 0; h < GN; ++h) col[h] = n + 64 * h + 4 * (lane % 16);
+  auto rows = [&](auto done) {  // four at a time
 #pragma unroll
     for (int g = 0; g < GM; ++g)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int f = 0; f < 4; ++f) {
+        int row[4];
+        float v[4][GN][4];
 #pragma unroll
-        for (int f = 0; f < 4; ++f)
+        for (int i = 0; i < 4; ++i) {
+          row[i] = m + 64 * g + 16 * (lane / 16) + 4 * i + f;
 #pragma unroll
-          for (int h = 0; h < GN; ++h) {
-            const float v[4] = {acc[4 * g + f][4 * h][i], acc[4 * g + f][4 * h + 1][i], acc[4 * g + f][4 * h + 2][i], acc[4 * g + f][4 * h + 3][i]};
-            done(m + 64 * g + 16 * (lane / 16) + 4 * i + f, n + 64 * h + 4 * (lane % 16), v);
-          }
+          for (int h = 0; h < GN; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][h][e] = acc[4 * g + f][4 * h + e][i];
+        }
+        done(row, v);
+      }
   };
   if (slices_of(p) > 1)
-    quads([&](int row, int col, const float (&v)[4]) { keep4(p, slice, row, col, v); });
+    rows([&](const int (&row)[4], const float (&v)[4][GN][4]) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int h = 0; h < GN; ++h) keep4(p, slice, row[i], col[h], v[i][h]);
+    });
   else
-    with_out_type(p, [&](auto type) { quads([&](int row, int col, const float (&v)[4]) { finish4<decltype(type)>(p, row, col, v); }); });
+    with_out_type(p, [&](auto type) {
+      using TO = decltype(type);
+      const ColumnBias<TO, GN> bias(p, col);
+      rows([&](const int (&row)[4], const float (&v)[4][GN][4]) { finish<TO, 4, GN>(p, row, col, bias, v); });
+    });
 }
 
 // Bytes of a stage, and of the LDS of tile_kernel.
@@ -485,10 +533,11 @@ struct Rows {
   }
 };
 
-// A workgroup takes 64 or 16 rows x 64 or 16 columns; its wavefronts take the steps of K in turn and add their sums in LDS, in order.
+// A workgroup takes 64 or 16 rows x 64 or 16 columns; its wavefronts take a run of K's steps each and add their sums in LDS, in order.
 //
 // Bound by memory's latency: B is read once, and with 8 wavefronts on 4 steps each all of K = 4096 is asked for at once.  4 x 8192 x 4096, 8 bits
-// by 4, with a residual: 8.7 us for 17.9 MB, which a stream reads in 2.8 behind a launch of 1.5.
+// by 4, with a residual: 7.1 us for 17.9 MB, which a stream reads in 2.8 behind a launch of 1.5.  (8.7 with the steps dealt to the wavefronts in turn,
+// tiles to the dies in turn, and rows finished one behind the other.)
 template <int FA, int FB, bool GROUP_M, bool GROUP_N, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
   constexpr int FM = GROUP_M ? 4 : 1, FN = GROUP_N ? 4 : 1, BM = 16 * FM, BN = 16 * FN;
@@ -496,7 +545,8 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
   __shared__ f32x4 meet[WAVES][FM * FN][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN, slices = slices_of(p);
-  const int tile = blockIdx.x / slices, slice = blockIdx.x - tile * slices;
+  // (neighbouring tiles of columns share lines of scales)
+  const int place = (int)place_of(blockIdx.x, gridDim.x), tile = place / slices, slice = place - tile * slices;
   const int m0 = tile % tiles_m * BM, n0 = tile / tiles_m * BN;
   (void)tiles_n;
   Rows<FA, GROUP_M> a;
@@ -529,27 +579,31 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
       });
     });
   };
-  const int end = (slice + 1) * p.slice, whole = min(p.blocks / 4, end);  // (p.slice is below 2^25)
-  int step = slice * p.slice + wave;
-  for (; step + (AT_ONCE - 1) * WAVES < whole; step += AT_ONCE * WAVES) {
+  // a run of steps for every wavefront, so that it takes whole lines of 4-bit rows; its last may be the one that K ends in
+  const int begin = slice * p.slice, end = min((p.blocks + 3) / 4, begin + p.slice), each_wave = (end - begin + WAVES - 1) / WAVES;
+  int step = begin + wave * each_wave;
+  const int last = min(step + each_wave, end), whole = min(last, p.blocks / 4);
+  for (; step + AT_ONCE <= whole; step += AT_ONCE) {
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
-      a.load(step + u * WAVES, lane, fa[u], sa[u]);
-      b.load(step + u * WAVES, lane, fb[u], sb[u]);
+      a.load(step + u, lane, fa[u], sa[u]);
+      b.load(step + u, lane, fb[u], sb[u]);
     }
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) product(u);
   }
-  for (; step < whole; step += WAVES) {
-    a.load(step, lane, fa[0], sa[0]);
-    b.load(step, lane, fb[0], sb[0]);
-    product(0);
-  }
-  if (step * 4 < p.blocks && step < end) {
-    a.load_end(step, lane, fa[0], sa[0]);
-    b.load_end(step, lane, fb[0], sb[0]);
-    product(0);
-  }
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u)
+    if (step + u < whole) {
+      a.load(step + u, lane, fa[u], sa[u]);
+      b.load(step + u, lane, fb[u], sb[u]);
+    } else if (step + u < last) {
+      a.load_end(step + u, lane, fa[u], sa[u]);
+      b.load_end(step + u, lane, fb[u], sb[u]);
+    }
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u)
+    if (step + u < last) product(u);
   asm volatile("" ::"v"(near));
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -565,28 +619,40 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) sum[j] += meet[w][i * FN + j][lane];
     }
+    if constexpr (GROUP_N) {
+      const int col[1] = {n0 + 4 * (lane % 16)};
+      int row[4];
+      float v[4][1][4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int row = m0 + (GROUP_M ? 16 * (lane / 16) + 4 * e + i : 4 * (lane / 16) + e);
-      if constexpr (GROUP_N) {
-        const float v[4] = {sum[0][e], sum[1][e], sum[2][e], sum[3][e]};
-        const int col = n0 + 4 * (lane % 16);
-        if (slices > 1)
-          keep4(p, slice, row, col, v);
-        else
-          with_out_type(p, [&](auto type) { finish4<decltype(type)>(p, row, col, v); });
-      } else {  // a column a lane: four lanes' make the four that are finished together
-        float v[4];
+      for (int e = 0; e < 4; ++e) {
+        row[e] = m0 + (GROUP_M ? 16 * (lane / 16) + 4 * e + i : 4 * (lane / 16) + e);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] = __shfl(sum[0][e], (lane & ~3) + c);
-        const int col = n0 + (lane % 16);
-        if (lane % 4 == 0) {
-          if (slices > 1)
-            keep4(p, slice, row, col, v);
-          else
-            with_out_type(p, [&](auto type) { finish4<decltype(type)>(p, row, col, v); });
-        }
+        for (int c = 0; c < 4; ++c) v[e][0][c] = sum[c][e];
       }
+      if (slices > 1) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) keep4(p, slice, row[e], col[0], v[e][0]);
+      } else {
+        with_out_type(p, [&](auto type) {
+          using TO = decltype(type);
+          finish<TO, 4, 1>(p, row, col, ColumnBias<TO, 1>(p, col), v);
+        });
+      }
+    } else {  // a column a lane, four rows: of four lanes, each takes the four columns of one row
+      static_assert(!GROUP_M, "one fragment");
+      float v[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float t[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = __shfl(sum[0][e], (lane & ~3) + c);
+        v[c] = lane & 2 ? (lane & 1 ? t[3] : t[2]) : (lane & 1 ? t[1] : t[0]);
+      }
+      const int row = m0 + 4 * (lane / 16) + lane % 4, col = n0 + lane % 16 / 4 * 4;
+      if (slices > 1)
+        keep4(p, slice, row, col, v);
+      else
+        with_out_type(p, [&](auto type) { finish4<decltype(type)>(p, row, col, v); });
     }
   }
 }
