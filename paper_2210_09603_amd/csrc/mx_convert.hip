@@ -1,7 +1,7 @@
 // Numbers into blocks of 32 that share a power of two, along rows, columns or both, and back.
 //
 // Memory bound: x is read once.  Along rows the lanes of a block (4, or 8 in fp32) find their maximum among themselves.  Along columns a tile
-// of 128 x 128 goes through LDS, where a thread takes 32 rows of two neighbouring columns; both outputs come from the same tile.  Scales lie
+// of 128 x 128 goes through LDS, where two lanes take 32 rows of two neighbouring columns; both outputs come from the same tile.  Scales lie
 // [block][row]: a tile collects those of its rows in LDS and writes words of 4.
 #include <algorithm>
 
@@ -79,20 +79,21 @@ __global__ __launch_bounds__(256) void rows_kernel(const QuantizeArgs p) {
   write_codes<COLS, TILE_ROWS>(p.by_rows, codes, row0, p.rows, tile_col * (COLS / kBlock), filled / kBlock);
 }
 
-// 32 rows of two neighbouring columns of a tile in LDS.
+// 16 rows, half a block, of two neighbouring columns of a tile in LDS.
 template <typename T>
 struct Pair {
-  unsigned raw[kBlock * (int)sizeof(T) / 2];
+  static constexpr int ROWS = kBlock / 2;
+  unsigned raw[ROWS * (int)sizeof(T) / 2];
   // the larger magnitude of either column
   __device__ __forceinline__ void largest(unsigned (&top)[2]) const {
     if constexpr (sizeof(T) == 4) {
       top[0] = top[1] = 0;
 #pragma unroll
-      for (int i = 0; i < 2 * kBlock; ++i) top[i & 1] = max(top[i & 1], raw[i] & 0x7fffffffu);
+      for (int i = 0; i < 2 * ROWS; ++i) top[i & 1] = max(top[i & 1], raw[i] & 0x7fffffffu);
     } else {
       unsigned m = 0;
 #pragma unroll
-      for (int i = 0; i < kBlock; ++i) m = larger_pair(m, raw[i]);
+      for (int i = 0; i < ROWS; ++i) m = larger_pair(m, raw[i]);
       top[0] = widened<T>(m & 0xffffu);
       top[1] = widened<T>(m >> 16);
     }
@@ -104,12 +105,12 @@ struct Pair {
       return to_f32(__builtin_bit_cast(T, (unsigned short)(column ? raw[row] >> 16 : raw[row] & 0xffffu)));
   }
 };
-// The elements of a column of them, 16 or 32 bytes of LDS
+// The elements of a column of them, 8 or 16 bytes of LDS
 template <typename T>
-__device__ __forceinline__ void put_block(unsigned char* to, int format, const Pair<T>& two, int column, int code) {
-  unsigned words[8];
+__device__ __forceinline__ void put_half(unsigned char* to, int format, const Pair<T>& two, int column, int code) {
+  unsigned words[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 2; ++i) {
     float part[8];
     unsigned out[2];
 #pragma unroll
@@ -118,19 +119,17 @@ __device__ __forceinline__ void put_block(unsigned char* to, int format, const P
     words[2 * i] = out[0];
     words[2 * i + 1] = out[1];
   }
-  if (format == HIDET_MX_E2M1) {
-    *reinterpret_cast<u32x4*>(to) = u32x4{words[0], words[2], words[4], words[6]};
-  } else {
+  if (format == HIDET_MX_E2M1)
+    *reinterpret_cast<u32x2*>(to) = u32x2{words[0], words[2]};
+  else
     *reinterpret_cast<u32x4*>(to) = u32x4{words[0], words[1], words[2], words[3]};
-    *reinterpret_cast<u32x4*>(to + 16) = u32x4{words[4], words[5], words[6], words[7]};
-  }
 }
 
-// 4096 x 4096 in 16 bits into 8 along both axes: 17.9 us, 3.8 TB/s, and 4099 x 1003 11.2.  Neither memory nor the vector unit (30 % busy) nor LDS (9 %)
-// bounds it, but four phases with a barrier between them, and 4 workgroups a compute unit to hide one behind another's.
+// 4096 x 4096 in bf16 into 8 bits along both axes: 16.4 us, 4.2 TB/s; 4099 x 1003 in fp16 8.5; 16384 x 8192 110 (4.9 TB/s).  Four phases with a barrier between
+// them: four workgroups of 512 threads a compute unit hide one behind another's.  (256 threads, each with whole blocks: 18.1, 11.1 and 111.)
 template <typename T, int TILE_ROWS, bool STREAM>
-__global__ __launch_bounds__(2 * TILE_ROWS) void columns_kernel(const QuantizeArgs p) {
-  constexpr int COLS = 128, THREADS = 2 * TILE_ROWS;  // (a thread for two columns of a block)
+__global__ __launch_bounds__(4 * TILE_ROWS) void columns_kernel(const QuantizeArgs p) {
+  constexpr int COLS = 128, THREADS = 4 * TILE_ROWS;  // (lanes l and l + 32 for two columns of a block)
   using W = Walk<T, COLS, THREADS>;
   constexpr int PASSES = TILE_ROWS / W::ROWS;
   __shared__ __attribute__((aligned(16))) T tile[TILE_ROWS * COLS];
@@ -157,15 +156,19 @@ __global__ __launch_bounds__(2 * TILE_ROWS) void columns_kernel(const QuantizeAr
   constexpr int PITCH = TILE_ROWS + 16;
   static_assert(COLS * PITCH <= (int)sizeof(tile), "the elements take the tile's place");
   const Side& s = p.by_columns;
-  const int pair = threadIdx.x % 64 * 2, block = threadIdx.x / 64, each = s.format == HIDET_MX_E2M1 ? 16 : 32;
+  const int wave = threadIdx.x / 64, half = threadIdx.x / 32 % 2, pair = (wave % 2 * 32 + threadIdx.x % 32) * 2, block = wave / 2;
+  const int each = s.format == HIDET_MX_E2M1 ? 16 : 32;
   const long long column = (long long)tile_col * COLS + pair;
   Pair<T> two;
 #pragma unroll
-  for (int r = 0; r < kBlock; ++r) __builtin_memcpy(two.raw + r * (int)sizeof(T) / 2, tile + (block * kBlock + r) * COLS + pair, 2 * sizeof(T));
+  for (int r = 0; r < Pair<T>::ROWS; ++r)
+    __builtin_memcpy(two.raw + r * (int)sizeof(T) / 2, tile + (block * kBlock + half * Pair<T>::ROWS + r) * COLS + pair, 2 * sizeof(T));
   unsigned top[2];
   two.largest(top);
+#pragma unroll
+  for (int c = 0; c < 2; ++c) top[c] = max(top[c], (unsigned)__shfl_xor((int)top[c], 32));
   const int code_a = scale_code(top[0], s.format), code_b = scale_code(top[1], s.format);
-  if (column < p.cols && row0 + block * kBlock < p.rows) {
+  if (half == 0 && column < p.cols && row0 + block * kBlock < p.rows) {
     unsigned char* scales = s.scales + (long long)(row0 / kBlock + block) * s.stride_scales + column;
     if (column + 1 < p.cols)
       *reinterpret_cast<unsigned short*>(scales) = (unsigned short)(code_a | code_b << 8);
@@ -174,8 +177,8 @@ __global__ __launch_bounds__(2 * TILE_ROWS) void columns_kernel(const QuantizeAr
   }
   __syncthreads();  // (the tile is read)
   unsigned char* out = reinterpret_cast<unsigned char*>(tile);
-  put_block(out + pair * PITCH + block * each, s.format, two, 0, code_a);
-  put_block(out + (pair + 1) * PITCH + block * each, s.format, two, 1, code_b);
+  put_half(out + pair * PITCH + block * each + half * each / 2, s.format, two, 0, code_a);
+  put_half(out + (pair + 1) * PITCH + block * each + half * each / 2, s.format, two, 1, code_b);
   __syncthreads();
   const int chunks = TILE_ROWS / kBlock * each / 16;  // of a row of the transposed matrix
   for (int i = threadIdx.x; i < COLS * chunks; i += THREADS) {
@@ -197,7 +200,7 @@ hipError_t launch_quantize(QuantizeArgs p, hipStream_t stream) {
   if (p.by_columns.values) {
     const long long tiles = grid(128, 128);
     if (tiles > kMaxTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((far ? columns_kernel<T, 128, true> : columns_kernel<T, 128, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((far ? columns_kernel<T, 128, true> : columns_kernel<T, 128, false>), dim3((unsigned)tiles), dim3(512), 0, stream, p);
     return hipGetLastError();
   }
   // Rows of 1 KB or more of a tile, four loads a thread in flight: 16384 x 4096 in bf16 into 4 bits 28.8 us (5.8 TB/s); 128 columns 32.1, two
