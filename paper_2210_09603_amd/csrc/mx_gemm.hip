@@ -37,56 +37,55 @@ constexpr TileCost kTiles[] = {
     {KERNEL_TILE_64, 64, 64, {0.28f, 0.24f, 0.18f}, {0.35f, 0.31f, 0.16f}, 2.0f},
 };
 constexpr float kJoin = 4.0f;  // us, of the second launch of a product in slices
+// The same of the workgroups of few rows, whose wavefronts take 8 steps at once; by rounds of one to a unit, and as far as they begin sooner than tiles.
+// (64 x 4096 x 4096, 8 bits by 4 and 4 by 4: 9.0 and 8.0 us, tiles 12.4 and 11.3; 32 x 8192 x 2048, both in 8 bits: 8.0 and 11.3; 48 x 8192 x 8192: 40 and
+// 21, 8 bits by 4 25 and 17; 256 x 1024 x 1024, 8 bits by 4: 4.8 and 7.8.  More than two rounds are left to the tiles.)
+constexpr float kStream[3] = {0.27f, 0.15f, 0.12f};
 
 long long tiles_of(long long M, long long N, long long rows, long long cols) { return (M + rows - 1) / rows * ((N + cols - 1) / cols); }
+
+// Cuts c along K where its workgroups leave units without work, and that saves more than the second launch takes.  each: steps that a slice is
+// made of; per: us of a step; most: slices that the workspace has room for.  Gives the us of what follows its first loads.
+float cut_slices(GemmCut& c, long long steps, long long each, float per, long long most) {
+  const float whole = (float)steps * per;
+  if (c.blocks > kUnits / 2) return whole * (float)((c.blocks + kUnits - 1) / kUnits);
+  const long long slices = std::min(std::min<long long>(kUnits / c.blocks, steps / (2 * each)), most);
+  if (slices < 2) return whole;
+  const long long slice = ((steps + slices - 1) / slices + each - 1) / each * each, cut = (steps + slice - 1) / slice;
+  if (cut < 2 || (float)(steps - slice) * per <= kJoin) return whole;
+  c.slices = (int)cut;
+  c.slice = (int)slice;
+  c.blocks *= cut;
+  return (float)slice * per + kJoin;
+}
 
 // `room`: bytes of workspace
 GemmCut cut_gemm(long long M, long long N, long long K, int format_a, int format_b, long long room) {
   const long long steps = std::max(1LL, (K + 127) / 128);
   const int kind = 2 - (int)is_wide(format_a) - (int)is_wide(format_b);
-  GemmCut c{KERNEL_STREAM_16, 1, 1 << 24, tiles_of(M, N, 16, 16)};
-  long long each = 1;  // steps that a slice is made of
-  float per = 0.0f;    // us that a slice of one step takes
+  const long long most = room / 4 / M / N;
   if (M <= 16) {
-    // (8 wavefronts of a workgroup take a step each: 0.5 us.)  4 x 8192 x 4096, 8 bits by 4: 7.0 us; 64 columns a workgroup 8.0, 64 x 64 tiles 13.8.
-    each = 8;
-    per = 0.06f;
-  } else if (M <= 64 && !is_wide(format_b)) {
-    // 64 x 4096 x 4096, 8 bits by 4 and 4 by 4: 9.6 and 9.2 us, 64 x 64 tiles 13.8 and 11.6.  (By 8 bits: 20.7 and 15.0.)
-    c.kernel = KERNEL_STREAM_16X64;
-    c.blocks = tiles_of(M, N, 16, 64);
-    each = 8;
-    per = 0.09f;
-  } else {
-    float best = 0.0f;
-    for (const TileCost& t : kTiles) {
-      const long long tiles = tiles_of(M, N, t.rows, t.cols);
-      const float rounds = (float)((tiles + kUnits - 1) / kUnits);
-      const float us = rounds * ((float)steps * (tiles <= kUnits ? t.alone[kind] : t.among[kind]) + t.once);
-      if (best == 0.0f || us < best) {
-        best = us;
-        c.kernel = t.kernel;
-        c.blocks = tiles;
-        per = t.alone[kind];
-      }
-    }
-    each = 4;
+    // (4 x 8192 x 4096, 8 bits by 4: 6.6 us; 64 columns a workgroup 7.9, 64 x 64 tiles 13.2.)
+    GemmCut c{KERNEL_STREAM_16, 1, 1 << 24, tiles_of(M, N, 16, 16)};
+    cut_slices(c, steps, 8, 0.06f, most);
+    return c;
   }
-  // Slices of K where that leaves units without work, and saves more than the second launch takes.
-  if (c.blocks <= kUnits / 2) {
-    long long slices = std::min<long long>(kUnits / c.blocks, steps / (2 * each));
-    slices = std::min(slices, room / (4 * M * N));
-    if (slices > 1) {
-      const long long slice = ((steps + slices - 1) / slices + each - 1) / each * each;
-      slices = (steps + slice - 1) / slice;
-      if (slices > 1 && (float)(steps - slice) * per > kJoin) {
-        c.slices = (int)slices;
-        c.slice = (int)slice;
-        c.blocks *= slices;
-      }
+  GemmCut tile{}, stream{KERNEL_STREAM_16X64, 1, 1 << 24, tiles_of(M, N, 16, 64)};
+  float best = 0.0f, alone = 0.0f, once = 0.0f;
+  for (const TileCost& t : kTiles) {
+    const long long tiles = tiles_of(M, N, t.rows, t.cols);
+    const float rounds = (float)((tiles + kUnits - 1) / kUnits);
+    const float us = rounds * ((float)steps * (tiles <= kUnits ? t.alone[kind] : t.among[kind]) + t.once);
+    if (best == 0.0f || us < best) {
+      best = us;
+      tile = GemmCut{t.kernel, 1, 1 << 24, tiles};
+      alone = t.alone[kind];
+      once = t.once;
     }
   }
-  return c;
+  if (const float us = cut_slices(tile, steps, 4, alone, most); tile.slices > 1) best = us + once;
+  if (stream.blocks > 2 * kUnits) return tile;
+  return cut_slices(stream, steps, 8, kStream[kind], most) < best ? stream : tile;
 }
 
 hidet_status_t check_epilogue(const hidet_epilogue_t* e, int out, long long M, long long N) {

@@ -156,6 +156,36 @@ def test_epilogues(size, out):
         _exact_case(*size, FORMATS[i % 3], FORMATS[(i + 1) % 3], out, 2 + i, **e)
 
 
+# (the tiles: 64 x 64, in slices too, 64 x 128, 128 x 128, 256 x 256)
+@pytest.mark.parametrize("formats", [(0, 0), (1, 2), (2, 0), (2, 2)], ids=str)
+@pytest.mark.parametrize("size", [(1000, 1020, 1060), (500, 1000, 8200), (129, 200, 9000), (1030, 1020, 2500), (700, 2805, 900), (1030, 2050, 700), (4000, 4090, 300)], ids=str)
+def test_products_on_tiles(size, formats):
+    _exact_case(*size, *formats, ("f32", "bf16", "f16")[sum(size) % 3], 1, odd=True)
+
+
+@pytest.mark.parametrize("size", [(517, 1030, 300), (700, 2805, 200), (1030, 2050, 200), (3900, 3850, 160)], ids=str)
+@pytest.mark.parametrize("out", ["f32", "f16", "bf16"])
+def test_epilogues_on_tiles(size, out):
+    for i, e in enumerate((dict(bias="col"), dict(bias="row", relu=True), dict(alpha=0.5, bias="col", residual=True, apart=3, relu=True, odd=True))):
+        _exact_case(*size, FORMATS[i % 3], FORMATS[(i + 1) % 3], out, 2 + i, **e)
+
+
+def test_a_residual_in_place():
+    for size in ((4, 300, 256), (40, 70, 130), (517, 1030, 300), (1030, 2050, 200)):
+        m, n, k = size
+        g = rng(m, n, k, 5)
+        a, b = _powers(g, m, k, 0), _powers(g, n, k, 2)
+        r = g.integers(-8, 8, (m, n)).astype(np.float64)
+        c = on_gpu(r, "f32")
+        hb.hidet_mx_gemm(matrix(*a, k, 0), matrix(*b, k, 2), c, epilogue=hb.make_epilogue(residual=c))
+        assert np.array_equal(f64(c), mx.numbers(*a, 0) @ mx.numbers(*b, 2).T + r), size
+
+
+@pytest.mark.parametrize("size", [(1000, 900, 0), (1030, 1020, 0), (1030, 2050, 0)], ids=str)
+def test_no_k_on_tiles(size):
+    test_no_k_is_the_epilogue_of_zero(size)
+
+
 @pytest.mark.parametrize("size", [(4, 48, 0), (100, 70, 0), (300, 300, 0)], ids=str)
 def test_no_k_is_the_epilogue_of_zero(size):
     m, n, _ = size
