@@ -288,7 +288,7 @@ static_assert(sizeof(GradArgs) <= 112, "a launch with more takes longer");
 
 // A workgroup takes every gridDim-th group of rows and keeps its part of the weight's gradient in registers: lanes hold the same columns of
 // every row.  AHEAD: the loads of the next rows are on their way while one group is worked on.  8192 x 5120 in bf16 with the residual's gradient:
-// 66.9 us for 336 MB, 5.0 TB/s, of which the parts of the weight's gradient, written and added, are 7.
+// 60.9 us for 336 MB, 5.5 TB/s, of which the parts of the weight's gradient, written and added, are 4.
 template <typename T, typename TW, int LANES, int CHUNKS, bool AHEAD, bool STREAM>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const GradArgs p) {
   constexpr int N = Chunk<T>::N, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES, COLS = LANES * CHUNKS * N;
@@ -417,14 +417,16 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, TW* out, 
   out[col] = from_f32<TW>(v);
 }
 
-// Lanes and chunks of a row's gradient, by its chunks; `most` workgroups, as many as the units hold at once by their registers (13107 x 5120 in bf16 with
-// the residual's gradient: 512 workgroups of 256 x 3 102 us, 768 127, 1024 110).  Workgroups are rows of the workspace: they follow from the
-// sizes alone.
+// Lanes and chunks of a row's gradient, by its chunks; `most` workgroups, as many as the units hold at once by their registers.  One chunk a lane where a
+// workgroup can have as many (bf16: 512 x 5120 by 768 lanes 12.2 us, by 256 of three chunks 18.1; 16384 x 5120 89 and 92, by 384 of two 127; 16384 x 8192 by
+// 1024 lanes 142, by 512 of two 161; fp32, 16384 x 5120, by 512 lanes of three chunks 163, by 768 of two 183); no more workgroups than one
+// to a unit, or two of 256 lanes (2048 x 2048: 512 workgroups 12.8, 1024 17.7), since each is a row to add up.  Workgroups are rows of the
+// workspace: they follow from the sizes alone.
 struct GradCut {
   int chunks, lanes, each, most;
 };
-constexpr GradCut kGradCuts[] = {{16, 16, 1, 512},   {64, 64, 1, 512},    {128, 64, 2, 512},   {256, 256, 1, 1024}, {512, 256, 2, 512},
-                                 {768, 256, 3, 512}, {1024, 512, 2, 256}, {1536, 512, 3, 256}, {4096, 1024, 4, 256}, {8192, 1024, 8, 256}};
+constexpr GradCut kGradCuts[] = {{16, 16, 1, 512},   {64, 64, 1, 512},    {128, 64, 2, 512},    {256, 256, 1, 512},   {512, 512, 1, 256},
+                                 {768, 768, 1, 256}, {1024, 1024, 1, 256}, {1536, 512, 3, 256}, {4096, 1024, 4, 256}, {8192, 1024, 8, 256}};
 int cut_of(long long cols, int per_chunk) {
   const long long chunks = (cols + per_chunk - 1) / per_chunk;
   int i = 0;
@@ -440,7 +442,7 @@ int parts_of(long long rows, long long cols, int per_chunk) {
 template <typename T, typename TW, int CUT>
 hipError_t launch_grad(const GradArgs& p, bool far, void* grad_weight, hipStream_t stream) {
   constexpr GradCut c = kGradCuts[CUT];
-  constexpr bool AHEAD = c.lanes < 1024;  // (1024 lanes have 128 registers each)
+  constexpr bool AHEAD = c.lanes < 1024 || c.each == 1;  // (1024 lanes have 128 registers each)
   const int parts = parts_of(p.rows, p.cols, Chunk<T>::N);
   const dim3 grid((unsigned)parts), block(c.lanes > 256 ? c.lanes : 256);
   if (far)

@@ -124,6 +124,11 @@ def test_rows_that_are_not_finite_or_zero_stay_alone():
     assert (scales[:, 1] == 255).all() and (scales[:6, 2] == 0).all() and scales[6, 2] == 255 and not scales[:, 3].any()
 
 
+@pytest.mark.parametrize("size,types", [(s, t) for s in ((260, 4000), (300, 5999), (515, 8192), (513, 2041)) for t in PAIRS], ids=str)
+def test_backward_of_rows_that_fill_a_workgroup(size, types):
+    test_backward(size, types)
+
+
 def test_no_rows_have_no_gradient():
     w = torch.ones(50, device="cuda")
     gw = torch.full((50,), 7.0, device="cuda")
