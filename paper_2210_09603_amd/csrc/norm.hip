@@ -267,8 +267,9 @@ hipError_t dispatch_norm(const NormArgs& p, bool far, hipStream_t stream) {
   if (chunks <= 1024) return launch_norm<T, TW, 512, 2>(p, far, stream);
   if (chunks <= 1536) return launch_norm<T, TW, 512, 3>(p, far, stream);
   if (chunks <= 2048) return launch_norm<T, TW, 1024, 2>(p, far, stream);
-  if (chunks <= 4096) return launch_norm<T, TW, 1024, 4>(p, far, stream);
-  return launch_norm<T, TW, 1024, 8>(p, far, stream);
+  if constexpr (Chunk<T>::N == 4)
+    if (chunks > 4096) return launch_norm<T, TW, 1024, 8>(p, far, stream);
+  return launch_norm<T, TW, 1024, 4>(p, far, stream);
 }
 
 // ---- gradients ------------------------------------------------------------------------------------------------------------
@@ -287,7 +288,8 @@ struct GradArgs {
 static_assert(sizeof(GradArgs) <= 112, "a launch with more takes longer");
 
 // A workgroup takes every gridDim-th group of rows and keeps its part of the weight's gradient in registers: lanes hold the same columns of
-// every row.  AHEAD: the loads of the next rows are on their way while one group is worked on.  8192 x 5120 in bf16 with the residual's gradient:
+// every row.  AHEAD: the loads of the next rows are on their way while one group is worked on, and the weight
+// stays in registers; without, it and the residual's gradient are read where they are needed.  8192 x 5120 in bf16 with the residual's gradient:
 // 60.9 us for 336 MB, 5.5 TB/s, of which the parts of the weight's gradient, written and added, are 4.
 template <typename T, typename TW, int LANES, int CHUNKS, bool AHEAD, bool STREAM>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const GradArgs p) {
@@ -296,15 +298,15 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
   __shared__ float meet[ROWS > 1 ? (ROWS - 1) * COLS : 1];
   const int tid = threadIdx.x, lane = tid % LANES, mine = tid / LANES;
   const TW* weight = reinterpret_cast<const TW*>(p.weight);
-  float w[CHUNKS][N], total[CHUNKS][N];
+  float w[AHEAD ? CHUNKS : 1][N], total[CHUNKS][N];
 #pragma unroll
   for (int i = 0; i < CHUNKS; ++i) {
-    load_weights<TW, N>(weight, (i * LANES + lane) * N, p.cols, p.offset, w[i]);
+    if (AHEAD) load_weights<TW, N>(weight, (i * LANES + lane) * N, p.cols, p.offset, w[i]);
 #pragma unroll
     for (int e = 0; e < N; ++e) total[i][e] = 0.0f;
   }
   const int groups = (p.rows + ROWS - 1) / ROWS;
-  u32x4 next_g[CHUNKS], next_h[CHUNKS], next_s[CHUNKS];
+  u32x4 next_g[CHUNKS], next_h[CHUNKS], next_s[AHEAD ? CHUNKS : 1];
   float next_rstd;
   auto load = [&](int group) {
     const long long at = min(group * ROWS + mine, p.rows - 1);  // (a thread without a row reads the last one, and nothing comes of it)
@@ -316,16 +318,13 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
       next_g[i] = load_chunk<T, STREAM>(gy + col, p.cols - col);
       next_h[i] = load_chunk<T, STREAM>(hh + col, p.cols - col);
     }
-    if (p.grad_sum) {
+    if (AHEAD) {
       const T* gs = reinterpret_cast<const T*>(p.grad_sum) + at * p.lds;
 #pragma unroll
       for (int i = 0; i < CHUNKS; ++i) {
         const int col = (i * LANES + lane) * N;
-        next_s[i] = load_chunk<T, STREAM>(gs + col, p.cols - col);
+        next_s[i] = p.grad_sum ? load_chunk<T, STREAM>(gs + col, p.cols - col) : u32x4{0, 0, 0, 0};
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < CHUNKS; ++i) next_s[i] = u32x4{0, 0, 0, 0};
     }
     next_rstd = p.rstd[at];
   };
@@ -335,12 +334,12 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
     const int row = group * ROWS + mine;
     const bool active = row < p.rows;
     if (!AHEAD) load(group);
-    u32x4 rg[CHUNKS], rh[CHUNKS], rs[CHUNKS];
+    u32x4 rg[CHUNKS], rh[CHUNKS], rs[AHEAD ? CHUNKS : 1];
 #pragma unroll
     for (int i = 0; i < CHUNKS; ++i) {
       rg[i] = next_g[i];
       rh[i] = next_h[i];
-      rs[i] = next_s[i];
+      if (AHEAD) rs[i] = next_s[i];
     }
     const float rstd = next_rstd;
     if (AHEAD && group + (int)gridDim.x < groups) load(group + gridDim.x);
@@ -350,10 +349,11 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
       float g[N], h[N];
       unpack<T>(rg[i], g);
       unpack<T>(rh[i], h);
+      if (!AHEAD) load_weights<TW, N>(weight, (i * LANES + lane) * N, p.cols, p.offset, w[0]);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         const float xhat = h[e] * rstd;
-        dot += g[e] * w[i][e] * xhat;
+        dot += g[e] * w[AHEAD ? i : 0][e] * xhat;
         if (active) total[i][e] += g[e] * xhat;
       }
     }
@@ -367,9 +367,14 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void grad_kernel(const G
       float g[N], h[N], s[N];
       unpack<T>(rg[i], g);
       unpack<T>(rh[i], h);
-      unpack<T>(rs[i], s);
+      if (!AHEAD) {
+        const T* gs = reinterpret_cast<const T*>(p.grad_sum) + (long long)row * p.lds;
+        rs[0] = p.grad_sum ? load_chunk<T, STREAM>(gs + col, p.cols - col) : u32x4{0, 0, 0, 0};
+        load_weights<TW, N>(weight, col, p.cols, p.offset, w[0]);
+      }
+      unpack<T>(rs[AHEAD ? i : 0], s);
 #pragma unroll
-      for (int e = 0; e < N; ++e) g[e] = rstd * (g[e] * w[i][e] - h[e] * rstd * mean) + s[e];
+      for (int e = 0; e < N; ++e) g[e] = rstd * (g[e] * w[AHEAD ? i : 0][e] - h[e] * rstd * mean) + s[e];
       store_chunk<T, STREAM>(out + col, p.cols - col, pack<T>(g));
     }
   }
@@ -419,14 +424,17 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, TW* out, 
 
 // Lanes and chunks of a row's gradient, by its chunks; `most` workgroups, as many as the units hold at once by their registers.  One chunk a lane where a
 // workgroup can have as many (bf16: 512 x 5120 by 768 lanes 12.2 us, by 256 of three chunks 18.1; 16384 x 5120 89 and 92, by 384 of two 127; 16384 x 8192 by
-// 1024 lanes 142, by 512 of two 161; fp32, 16384 x 5120, by 512 lanes of three chunks 163, by 768 of two 183); no more workgroups than one
+// 1024 lanes 142, by 512 of two 161; fp32, 16384 x 5120, by 512 lanes of three chunks 163, by 768 of two 183), then as many as 512
+// lanes have registers for (bf16, 4096 x 16384 by 512 lanes of four chunks 86, by 1024, whose registers do not hold two rows, 395); no more workgroups than one
 // to a unit, or two of 256 lanes (2048 x 2048: 512 workgroups 12.8, 1024 17.7), since each is a row to add up.  Workgroups are rows of the
 // workspace: they follow from the sizes alone.
 struct GradCut {
   int chunks, lanes, each, most;
 };
 constexpr GradCut kGradCuts[] = {{16, 16, 1, 512},   {64, 64, 1, 512},    {128, 64, 2, 512},    {256, 256, 1, 512},   {512, 512, 1, 256},
-                                 {768, 768, 1, 256}, {1024, 1024, 1, 256}, {1536, 512, 3, 256}, {4096, 1024, 4, 256}, {8192, 1024, 8, 256}};
+                                 {768, 768, 1, 256}, {1024, 1024, 1, 256}, {1536, 512, 3, 256}, {2048, 512, 4, 256},
+                                 {4096, 512, 8, 256}, {8192, 512, 16, 256}};
+constexpr GradCut kWideCut = {4096, 1024, 4, 256};  // of fp32 (4096 x 16384: 152 us, by 512 lanes 172; half the sums to a chunk)
 int cut_of(long long cols, int per_chunk) {
   const long long chunks = (cols + per_chunk - 1) / per_chunk;
   int i = 0;
@@ -441,8 +449,8 @@ int parts_of(long long rows, long long cols, int per_chunk) {
 
 template <typename T, typename TW, int CUT>
 hipError_t launch_grad(const GradArgs& p, bool far, void* grad_weight, hipStream_t stream) {
-  constexpr GradCut c = kGradCuts[CUT];
-  constexpr bool AHEAD = c.lanes < 1024 || c.each == 1;  // (1024 lanes have 128 registers each)
+  constexpr GradCut c = Chunk<T>::N == 4 && kGradCuts[CUT].chunks == kWideCut.chunks ? kWideCut : kGradCuts[CUT];
+  constexpr bool AHEAD = c.each <= (c.lanes > 768 ? 1 : 4);  // (512 lanes have 256 registers each, 1024 have 128)
   const int parts = parts_of(p.rows, p.cols, Chunk<T>::N);
   const dim3 grid((unsigned)parts), block(c.lanes > 256 ? c.lanes : 256);
   if (far)
@@ -456,7 +464,7 @@ hipError_t launch_grad(const GradArgs& p, bool far, void* grad_weight, hipStream
 }
 template <typename T, typename TW, int CUT = 0>
 hipError_t dispatch_grad(int cut, const GradArgs& p, bool far, void* grad_weight, hipStream_t stream) {
-  if constexpr (CUT + 1 < (int)(sizeof(kGradCuts) / sizeof(kGradCuts[0])))
+  if constexpr (CUT + 1 < (int)(sizeof(kGradCuts) / sizeof(kGradCuts[0])) && kGradCuts[CUT].chunks * Chunk<T>::N < kMaxCols)
     if (cut > CUT) return dispatch_grad<T, TW, CUT + 1>(cut, p, far, grad_weight, stream);
   return launch_grad<T, TW, CUT>(p, far, grad_weight, stream);
 }
