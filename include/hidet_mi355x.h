@@ -569,8 +569,8 @@ typedef struct {
  * infinity has the scale NaN and elements 0.
  * hidet_mx_dequantize: y [rows][cols] of dtype, rounded once.
  * Nothing that is written may overlap anything else.
- * rows or cols of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: rows or cols of 2^29 or more, rows * ld beyond 2^47 elements, 2^24 tiles or more (of
- * 16 x 128 elements at the smallest).
+ * rows or cols of 0 is an OK no-op.  HIDET_ERR_UNSUPPORTED: rows or cols of 2^29 or more, rows * ld beyond 2^47 elements, 2^24 tiles or more of
+ * 16 x 512 elements along rows (8 x 512 in fp32), of 16 x 128 in dequantize, 2^23 or more of 128 x 128 where by_columns is wanted.
  */
 hidet_status_t hidet_mx_quantize(int32_t dtype, int64_t rows, int64_t cols, const void* x, int64_t ldx, const hidet_mx_t* by_rows,
                                  const hidet_mx_t* by_columns, void* stream);

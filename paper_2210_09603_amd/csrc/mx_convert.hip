@@ -12,7 +12,8 @@ using namespace hidet::mx;
 
 namespace {
 
-constexpr long long kMaxTiles = (1LL << 24) - 1; // of 256 threads: below 2^32 work items
+// The most workgroups of a launch: it has fewer than 2^32 work items.
+constexpr long long most_tiles(int threads) { return ((1LL << 32) - 1) / threads; }
 
 struct Side {
   unsigned char* values;  // null: not wanted
@@ -198,19 +199,21 @@ hipError_t launch_quantize(QuantizeArgs p, hipStream_t stream) {
     return tiles;
   };
   if (p.by_columns.values) {
+    constexpr int THREADS = 512;
     const long long tiles = grid(128, 128);
-    if (tiles > kMaxTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((far ? columns_kernel<T, 128, true> : columns_kernel<T, 128, false>), dim3((unsigned)tiles), dim3(512), 0, stream, p);
+    if (tiles > most_tiles(THREADS)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((far ? columns_kernel<T, 128, true> : columns_kernel<T, 128, false>), dim3((unsigned)tiles), dim3(THREADS), 0, stream, p);
     return hipGetLastError();
   }
   // Rows of 1 KB or more of a tile, four loads a thread in flight: 16384 x 4096 in bf16 into 4 bits 28.8 us (5.8 TB/s); 128 columns 32.1, two
   // loads 30.4, all through the caches 36.2.  Few tiles of these: smaller ones.
   constexpr int FAR_ROWS = Walk<T, 512>::ROWS * 4, NEAR_ROWS = Walk<T, 128>::ROWS;
+  constexpr int THREADS = 256;
   if (const long long tiles = grid(FAR_ROWS, 512); tiles >= 1024) {
-    if (tiles > kMaxTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((far ? rows_kernel<T, 512, 4, true> : rows_kernel<T, 512, 4, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+    if (tiles > most_tiles(THREADS)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((far ? rows_kernel<T, 512, 4, true> : rows_kernel<T, 512, 4, false>), dim3((unsigned)tiles), dim3(THREADS), 0, stream, p);
   } else {
-    hipLaunchKernelGGL((rows_kernel<T, 128, 1, false>), dim3((unsigned)grid(NEAR_ROWS, 128)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((rows_kernel<T, 128, 1, false>), dim3((unsigned)grid(NEAR_ROWS, 128)), dim3(THREADS), 0, stream, p);
   }
   return hipGetLastError();
 }
@@ -255,10 +258,11 @@ hipError_t launch_dequantize(DequantizeArgs p, hipStream_t stream) {
   // (16384 x 4096 from 4 bits into bf16: 33.4 us, 5.0 TB/s, four fifths of it written; with two rows a thread 36.2, with four 39.7, all through the
   // caches 40.8)
   const long long col_tiles = (p.cols + 127LL) / 128, tiles = (p.rows + 15LL) / 16 * col_tiles;
-  if (tiles > kMaxTiles) return hipErrorInvalidValue;
+  constexpr int THREADS = 256;
+  if (tiles > most_tiles(THREADS)) return hipErrorInvalidValue;
   p.col_tiles = (int)col_tiles;
   const bool far = (long long)p.rows * p.cols * (int)sizeof(T) >= kFarBytes;
-  hipLaunchKernelGGL((far ? dequantize_kernel<T, true> : dequantize_kernel<T, false>), dim3((unsigned)tiles), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((far ? dequantize_kernel<T, true> : dequantize_kernel<T, false>), dim3((unsigned)tiles), dim3(THREADS), 0, stream, p);
   return hipGetLastError();
 }
 

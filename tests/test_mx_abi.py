@@ -95,6 +95,18 @@ def test_more_tiles_than_a_launch_has():
     assert gemm(M=16, N=rows, K=32, A=wide, B=wide, ldc=rows) == UNSUPPORTED
 
 
+def test_more_tiles_along_columns_than_a_launch_has():
+    # 512 threads to a tile of 128 x 128: 2^23 tiles are 2^32 threads (nothing is launched)
+    long = (1 << 29) - 32
+    one = blocks(stride_values=160, stride_scales=long)
+    assert quantize(rows=129, cols=long, ldx=long, by_rows=None, by_columns=one) == UNSUPPORTED
+    rows, cols = 1 << 19, 1 << 18
+    by_rows = blocks(format=hb.HIDET_MX_E2M1, stride_values=cols // 2, stride_scales=rows)
+    by_columns = blocks(format=hb.HIDET_MX_E2M1, values=0x8000, scales=0x9000, stride_values=rows // 2, stride_scales=cols)
+    assert quantize(rows=rows, cols=cols, ldx=cols, by_rows=by_rows, by_columns=by_columns) == UNSUPPORTED
+    assert quantize(rows=rows, cols=cols, ldx=cols, by_rows=None, by_columns=by_columns) == UNSUPPORTED
+
+
 def test_gemm():
     assert gemm(out=3) == INVALID and gemm(M=-1) == INVALID and gemm(K=-1) == INVALID and gemm(wb=-1) == INVALID
     for n in ("M", "N", "K"):
