@@ -1,0 +1,66 @@
+"""Block-scaled products on every tile and in slices of K, for every pair of formats: exact cases and bounds as in the tests of all sizes."""
+import numpy as np
+import pytest
+import torch
+
+from mx_helpers import FLOOR, FORMATS, TYPES, U, f64, matrix, rng
+from oracle import mx
+from paper_2210_09603_amd import binding as hb
+from test_gpu_mx import _exact_case
+
+pytestmark = pytest.mark.gpu
+
+PAIRS = [(a, b) for a in FORMATS for b in FORMATS]
+# (64 x 64 tiles, in two slices of K too, 64 x 128, 128 x 128, 256 x 256)
+TILES = [(1000, 1020, 1060), (500, 1000, 8200), (1030, 1020, 2500), (1030, 2050, 700), (4000, 4090, 300)]
+
+
+@pytest.mark.parametrize("formats", PAIRS, ids=str)
+@pytest.mark.parametrize("size", TILES + [(1024, 1024, 1024)], ids=str)
+def test_products_of_every_pair_on_tiles(size, formats):
+    _exact_case(*size, *formats, ("f32", "bf16", "f16")[(sum(size) + sum(formats)) % 3], 7, odd=bool(sum(formats) % 2))
+
+
+@pytest.mark.parametrize("formats", PAIRS, ids=str)
+@pytest.mark.parametrize("size", TILES, ids=str)
+def test_products_of_elements_of_all_sizes_on_tiles(size, formats):
+    """Every element code but NaN and infinity, and scales apart by 2^8, against float64 products of 40 rows and 40 columns, both ends and the middle
+    among them."""
+    m, n, k = size
+    g = rng(m, n, k, *formats)
+
+    def operand(rows, fmt):
+        top = {mx.E4M3: 0x7F, mx.E5M2: 0x7C, mx.E2M1: 8}[fmt]
+        width = mx.blocks(k) * 32
+        codes = g.integers(0, top, (rows, width)).astype(np.uint8)
+        codes = np.where(g.random((rows, width)) < 0.5, codes, codes + mx.sign_bit(fmt)).astype(np.uint8)
+        codes[:, k:] = 0
+        middle = 127 - mx.POWER[fmt]
+        return codes, g.integers(middle - 4, middle + 5, (mx.blocks(k), rows)).astype(np.uint8)
+
+    a, b = operand(m, formats[0]), operand(n, formats[1])
+    ma, mb = matrix(*a, k, formats[0]), matrix(*b, k, formats[1])
+
+    def some(count):
+        return np.unique(np.r_[0:3, count // 2:count // 2 + 2, count - 3:count, g.integers(0, count, 32)])
+
+    rows, cols = some(m), some(n)
+    na, nb = mx.numbers(a[0][rows], a[1][:, rows], formats[0]), mx.numbers(b[0][cols], b[1][:, cols], formats[1])
+    want, size_of = na @ nb.T, np.abs(na) @ np.abs(nb).T
+    bound = (mx.blocks(k) / 4 + 16) * 2.0 ** -24 * size_of
+    if formats != (mx.E2M1, mx.E2M1):
+        pa, pb = np.abs(na), np.abs(nb)  # (whole blocks: groups of 8 k)
+        for k8 in range(0, na.shape[1], 8):
+            bound += 8 * 2.0 ** -12 * (pa[:, None, k8:k8 + 8] * pb[None, :, k8:k8 + 8]).max(2)
+    for out in ("f32", "bf16"):
+        c = torch.empty((m, n), dtype=TYPES[out], device="cuda")
+        ws = torch.empty(max(4, hb.hidet_mx_gemm_workspace_bytes(ma, mb)), dtype=torch.uint8, device="cuda")
+        hb.hidet_mx_gemm(ma, mb, c, workspace=ws)
+        first = c.clone()
+        got = f64(c)[np.ix_(rows, cols)]
+        ratio = (np.abs(got - want) / (bound + U[out] * (np.abs(want) + bound) + FLOOR[out])).max()
+        assert ratio <= 1, ratio
+        for _ in range(3):  # the same bits again
+            c.fill_(7.0)
+            hb.hidet_mx_gemm(ma, mb, c, workspace=ws)
+            assert torch.equal(first, c)
