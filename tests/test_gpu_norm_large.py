@@ -152,3 +152,10 @@ BACKWARD = [(c, HALF[(i + j) % 4]) for i, c in enumerate((100, 501, 1003, 2040, 
 @pytest.mark.parametrize("cols,types", BACKWARD, ids=str)
 def test_backward_past_the_caches(cols, types):
     _check_backward(FAR // (3 * ES[types[0]] * cols) + 7, cols, types, cols % 2, 1)
+
+
+@pytest.mark.parametrize("size,types", [(s, t) for s in ((515, 20001), (515, 32768), (771, 16390)) for t in HALF] + [
+    (s, ("f32", "f32")) for s in ((515, 12003), (515, 16384), (300, 32768), (771, 20001), (515, 8200))], ids=str)
+def test_backward_of_several_long_rows_a_workgroup(size, types):
+    _check_backward(*size, types, 0, 0)
+    _check_backward(*size, types, 1, 2)
