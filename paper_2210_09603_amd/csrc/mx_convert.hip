@@ -128,9 +128,9 @@ __device__ __forceinline__ void put_half(unsigned char* to, int format, const Pa
 
 // 4096 x 4096 in bf16 into 8 bits along both axes: 16.4 us, 4.2 TB/s; 4099 x 1003 in fp16 8.5; 16384 x 8192 110 (4.9 TB/s).  Four phases with a barrier between
 // them: four workgroups of 512 threads a compute unit hide one behind another's.  (256 threads, each with whole blocks: 18.1, 11.1 and 111.)
-template <typename T, int TILE_ROWS, bool STREAM>
-__global__ __launch_bounds__(4 * TILE_ROWS) void columns_kernel(const QuantizeArgs p) {
-  constexpr int COLS = 128, THREADS = 4 * TILE_ROWS;  // (lanes l and l + 32 for two columns of a block)
+template <typename T, bool STREAM>
+__global__ __launch_bounds__(512) void columns_kernel(const QuantizeArgs p) {
+  constexpr int COLS = 128, TILE_ROWS = 128, THREADS = 512;  // (lanes l and l + 32 for two columns of a block)
   using W = Walk<T, COLS, THREADS>;
   constexpr int PASSES = TILE_ROWS / W::ROWS;
   __shared__ __attribute__((aligned(16))) T tile[TILE_ROWS * COLS];
@@ -202,7 +202,7 @@ hipError_t launch_quantize(QuantizeArgs p, hipStream_t stream) {
     constexpr int THREADS = 512;
     const long long tiles = grid(128, 128);
     if (tiles > most_tiles(THREADS)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((far ? columns_kernel<T, 128, true> : columns_kernel<T, 128, false>), dim3((unsigned)tiles), dim3(THREADS), 0, stream, p);
+    hipLaunchKernelGGL((far ? columns_kernel<T, true> : columns_kernel<T, false>), dim3((unsigned)tiles), dim3(THREADS), 0, stream, p);
     return hipGetLastError();
   }
   // Rows of 1 KB or more of a tile, four loads a thread in flight: 16384 x 4096 in bf16 into 4 bits 28.8 us (5.8 TB/s); 128 columns 32.1, two

@@ -20,7 +20,7 @@ hipError_t launch_gemm<HIDET_MX_E2M1>(int, const GemmCut&, const GemmArgs&, hipS
 namespace {
 
 constexpr long long kMaxLd = 1LL << 32;          // of C and the residual
-constexpr long long kMaxGrid = (1LL << 22) - 1;  // workgroups of up to 512 threads: below 2^32 work items
+constexpr long long kMaxGrid = (1LL << 22) - 1;  // workgroups of up to 1024 threads: below 2^32 work items
 
 constexpr int kUnits = 256;                      // compute units
 

@@ -73,33 +73,29 @@ __device__ __forceinline__ f32x4 multiply(const Fragment<FA>& a, const Fragment<
 }
 
 // ---- epilogue -----------------------------------------------------------------------------------------------------------
-// R rows of H times four neighbouring columns, as the other products finish theirs: alpha, bias, residual, ReLU, one rounding.  All that is read
+// R rows of four neighbouring columns, as the other products finish theirs: alpha, bias, residual, ReLU, one rounding.  All that is read
 // is asked for before anything is written, so that a thread waits once for all of it.
-template <typename TO, int H>
+template <typename TO>
 struct ColumnBias {
-  float v[H][4];  // 0 if there is none
-  __device__ __forceinline__ ColumnBias(const GemmArgs& p, const int (&col)[H]) {
+  float v[4];  // 0 if there is none
+  __device__ __forceinline__ ColumnBias(const GemmArgs& p, int col) {
     const bool any = ((p.flags >> 2) & 3) == HIDET_BIAS_PER_COL;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[h][e] = any ? to_f32(reinterpret_cast<const TO*>(p.bias)[min(col[h] + e, p.N - 1)]) : 0.0f;
+    for (int e = 0; e < 4; ++e) v[e] = any ? to_f32(reinterpret_cast<const TO*>(p.bias)[min(col + e, p.N - 1)]) : 0.0f;
   }
 };
-template <typename TO, int R, int H>
-__device__ __forceinline__ void finish(const GemmArgs& p, const int (&row)[R], const int (&col)[H], const ColumnBias<TO, H>& bias, const float (&sum)[R][H][4]) {
+template <typename TO, int R>
+__device__ __forceinline__ void finish(const GemmArgs& p, const int (&row)[R], int col, const ColumnBias<TO>& bias, const float (&sum)[R][4]) {
   struct __attribute__((packed, aligned(sizeof(TO)))) Quad {  // (one access, at element alignment)
     TO e[4];
   };
   float of_row[R];
-  Quad other[R][H];
+  Quad other[R];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     of_row[r] = 0.0f;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) other[r][h].e[e] = TO(0.0f);
+    for (int e = 0; e < 4; ++e) other[r].e[e] = TO(0.0f);
   }
   if (((p.flags >> 2) & 3) == HIDET_BIAS_PER_ROW) {
 #pragma unroll
@@ -107,46 +103,42 @@ __device__ __forceinline__ void finish(const GemmArgs& p, const int (&row)[R], c
   }
   if (p.residual) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int h = 0; h < H; ++h) {
-        const int left = row[r] < p.M ? p.N - col[h] : 0;
-        const TO* from = reinterpret_cast<const TO*>(p.residual) + (long long)row[r] * p.ldr + col[h];
-        if (left >= 4) {
-          other[r][h] = *reinterpret_cast<const Quad*>(from);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 3; ++e)
-            if (e < left) other[r][h].e[e] = from[e];
-        }
-      }
-  }
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      Quad o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v = p.alpha * sum[r][h][e] + of_row[r] + bias.v[h][e] + to_f32(other[r][h].e[e]);
-        o.e[e] = from_f32<TO>((p.flags & 16) != 0 && v < 0.0f ? 0.0f : v);
-      }
-      const int left = row[r] < p.M ? p.N - col[h] : 0;
-      TO* c = reinterpret_cast<TO*>(p.c) + (long long)row[r] * p.ldc + col[h];
+    for (int r = 0; r < R; ++r) {
+      const int left = row[r] < p.M ? p.N - col : 0;
+      const TO* from = reinterpret_cast<const TO*>(p.residual) + (long long)row[r] * p.ldr + col;
       if (left >= 4) {
-        *reinterpret_cast<Quad*>(c) = o;
+        other[r] = *reinterpret_cast<const Quad*>(from);
       } else {
 #pragma unroll
         for (int e = 0; e < 3; ++e)
-          if (e < left) c[e] = o.e[e];
+          if (e < left) other[r].e[e] = from[e];
       }
     }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    Quad o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float v = p.alpha * sum[r][e] + of_row[r] + bias.v[e] + to_f32(other[r].e[e]);
+      o.e[e] = from_f32<TO>((p.flags & 16) != 0 && v < 0.0f ? 0.0f : v);
+    }
+    const int left = row[r] < p.M ? p.N - col : 0;
+    TO* c = reinterpret_cast<TO*>(p.c) + (long long)row[r] * p.ldc + col;
+    if (left >= 4) {
+      *reinterpret_cast<Quad*>(c) = o;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < left) c[e] = o.e[e];
+    }
+  }
 }
 template <typename TO>
 __device__ __forceinline__ void finish4(const GemmArgs& p, int m, int n, const float (&sum)[4]) {
-  const int row[1] = {m}, col[1] = {n};
-  const float v[1][1][4] = {{{sum[0], sum[1], sum[2], sum[3]}}};
-  finish<TO, 1, 1>(p, row, col, ColumnBias<TO, 1>(p, col), v);
+  const int row[1] = {m};
+  const float v[1][4] = {{sum[0], sum[1], sum[2], sum[3]}};
+  finish<TO, 1>(p, row, n, ColumnBias<TO>(p, n), v);
 }
 // f(a value of the type of C)
 template <class F>
@@ -293,91 +285,84 @@ __device__ __forceinline__ void tile_of(unsigned at, int tiles_m, int tiles_n, i
   j = (int)(within / rows);
 }
 
-// What a wavefront has summed: 64 GM x 64 GN from row m and column n on.
-template <int GM, int GN>
-__device__ __forceinline__ void finish_tile(const GemmArgs& p, int slice, int m, int n, int lane, const f32x4 (&acc)[4 * GM][4 * GN]) {
-  int col[GN];
-#pragma unroll
-  for (int h = 0; h < GN; ++h) col[h] = n + 64 * h + 4 * (lane % 16);
+// What a wavefront has summed: 64 x 64 from row m and column n on.
+__device__ __forceinline__ void finish_tile(const GemmArgs& p, int slice, int m, int n, int lane, const f32x4 (&acc)[4][4]) {
+  const int col = n + 4 * (lane % 16);
   auto rows = [&](auto done) {  // four at a time
 #pragma unroll
-    for (int g = 0; g < GM; ++g)
+    for (int f = 0; f < 4; ++f) {
+      int row[4];
+      float v[4][4];
 #pragma unroll
-      for (int f = 0; f < 4; ++f) {
-        int row[4];
-        float v[4][GN][4];
+      for (int i = 0; i < 4; ++i) {
+        row[i] = m + 16 * (lane / 16) + 4 * i + f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          row[i] = m + 64 * g + 16 * (lane / 16) + 4 * i + f;
-#pragma unroll
-          for (int h = 0; h < GN; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[i][h][e] = acc[4 * g + f][4 * h + e][i];
-        }
-        done(row, v);
+        for (int e = 0; e < 4; ++e) v[i][e] = acc[f][e][i];
       }
+      done(row, v);
+    }
   };
   if (slices_of(p) > 1)
-    rows([&](const int (&row)[4], const float (&v)[4][GN][4]) {
+    rows([&](const int (&row)[4], const float (&v)[4][4]) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int h = 0; h < GN; ++h) keep4(p, slice, row[i], col[h], v[i][h]);
+      for (int i = 0; i < 4; ++i) keep4(p, slice, row[i], col, v[i]);
     });
   else
     with_out_type(p, [&](auto type) {
       using TO = decltype(type);
-      const ColumnBias<TO, GN> bias(p, col);
-      rows([&](const int (&row)[4], const float (&v)[4][GN][4]) { finish<TO, 4, GN>(p, row, col, bias, v); });
+      const ColumnBias<TO> bias(p, col);
+      rows([&](const int (&row)[4], const float (&v)[4][4]) { finish<TO, 4>(p, row, col, bias, v); });
     });
 }
 
+constexpr int PLACES = 2;  // of stages in LDS
+// (256 x 256 tiles of 8 by 4 bits need all of their 128 registers: with the first request written out in place of its loop they do not suffice, and
+// 4096 x 4096 x 4096 takes 129 us for 52.)
 // Bytes of a stage, and of the LDS of tile_kernel.
-template <int FA, int FB, int GM, int GN, int WM, int WN, int GROUPS>
+template <int FA, int FB, int WM, int WN, int GROUPS>
 struct TileShape {
   // steps of 128 k: of a wavefront, and of a stage.  (Rows of 128 bytes, a line, in a stage: with 64 every line is fetched twice.)
   static constexpr int EACH = !is_wide(FA) && !is_wide(FB) && GROUPS == 1 ? 2 : 1, STEPS = EACH * GROUPS;
-  static constexpr int WAVES = WM * WN * GROUPS, BM = 64 * GM * WM, BN = 64 * GN * WN;
+  static constexpr int WAVES = WM * WN * GROUPS, BM = 64 * WM, BN = 64 * WN;
   using A = Panel<FA, BM, STEPS, WAVES>;
   using B = Panel<FB, BN, STEPS, WAVES>;
   static constexpr int VALUES = A::BYTES + B::BYTES, STAGE = VALUES + A::SCALE_BYTES + B::SCALE_BYTES;
-  static constexpr int SUMS = (GROUPS - 1) * WM * WN * GM * GN * 16384;
-  static constexpr int lds(int places) { return places * STAGE > SUMS ? places * STAGE : SUMS; }
+  static constexpr int SUMS = (GROUPS - 1) * WM * WN * 16384, LDS = PLACES * STAGE > SUMS ? PLACES * STAGE : SUMS;
 };
 
-// Tiles from LDS: WM x WN wavefronts of 64 GM x 64 GN each, PLACES stages, all but one of them on their way.  GROUPS such sets of wavefronts take
-// a part of every stage's k each, and add their sums in LDS, in order.
+// Tiles from LDS: WM x WN wavefronts of 64 x 64 each, two stages, one of them on its way.  GROUPS such sets of wavefronts take a part of
+// every stage's k each, and add their sums in LDS, in order.
 //
 // 8192 x 8192 x 8192 into bf16 on 256 x 256 tiles: 4 bits by 4 264 us (4.2 PFLOP/s), 8 by 8 430 (2.6), 8 by 4 375 (2.9).  Of these the matrix
 // instructions alone, at the clock that the board's power leaves them, are 157, 260 and 250; the loads into LDS alone 151, 270 and 261; products
 // with their reads of LDS and no loads 209, 361 and 310: no one of the three bounds it, but they do not overlap wholly, since a compute
 // unit has room for one workgroup of two stages.  128 x 128 tiles of 4 wavefronts: 296, 514, 442 (half the products per byte loaded); 3 or 4
 // smaller stages, 8 wavefronts of 128 x 64 and wavefronts that only load: no shorter.
-template <int FA, int FB, int GM, int GN, int WM, int WN, int GROUPS, int PLACES>
+template <int FA, int FB, int WM, int WN, int GROUPS>
 __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tile_kernel(const GemmArgs p) {
-  using S = TileShape<FA, FB, GM, GN, WM, WN, GROUPS>;
+  using S = TileShape<FA, FB, WM, WN, GROUPS>;
   using A = typename S::A;
   using B = typename S::B;
-  constexpr int SET = WM * WN, PARTS = A::PARTS + B::PARTS, LOADS = A::LOADS + B::LOADS + S::STEPS;  // of a wavefront, a stage
-  static_assert(PARTS <= S::WAVES && (PLACES - 2) * LOADS < 64, "a load of scales a wavefront; loads in flight are counted in 6 bits");
+  constexpr int SET = WM * WN, PARTS = A::PARTS + B::PARTS;
+  static_assert(PARTS <= S::WAVES, "a load of scales a wavefront");
   // The loads of another stage are handed over behind a quarter of a wavefront's products, not before them: it is held up there for long
   // enough that the matrix cores should have work by then.  (Two operands of 8 bits have no registers left for it.)
   constexpr bool LATE = !(is_wide(FA) && is_wide(FB));
-  __shared__ __attribute__((aligned(16))) unsigned char smem[S::lds(PLACES)];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[S::LDS];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int group = wave / SET, member = wave % SET;
   const int slices = slices_of(p), slice = blockIdx.x % slices, first_block = slice * p.slice * 4;
   const int blocks = min(p.blocks - first_block, p.slice * 4);  // of this slice
   int ti, tj;
   tile_of(blockIdx.x / slices, (p.M + S::BM - 1) / S::BM, (p.N + S::BN - 1) / S::BN, ti, tj);
-  const int m0 = ti * S::BM, n0 = tj * S::BN, gm = member / WN * GM, gn = member % WN * GN;
+  const int m0 = ti * S::BM, n0 = tj * S::BN, gm = member / WN, gn = member % WN;
   const A a(p.a, p.scales_a, p.lda, p.ld_scales_a, m0, p.M, first_block, blocks, wave, lane);
   const B b(p.b, p.scales_b, p.ldb, p.ld_scales_b, n0, p.N, first_block, blocks, wave, lane);
-  f32x4 acc[4 * GM][4 * GN];
+  f32x4 acc[4][4];
 #pragma unroll
-  for (int i = 0; i < 4 * GM; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4 * GN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   const unsigned lds = lds_address(smem);
   // whole stages; what K ends in comes before them, in the first place
@@ -404,33 +389,22 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tile_kernel(const GemmA
 #pragma unroll
     for (int i = 0; i < S::EACH; ++i) {
       const int u = group * S::EACH + i;
-      Fragment<FA> fa[4 * GM];
-      Fragment<FB> fb[4 * GN];
-      unsigned sa[GM], sb[GN];
+      Fragment<FA> fa[4];
+      Fragment<FB> fb[4];
+      const unsigned sb = B::scale(stage + S::VALUES + A::SCALE_BYTES, u, gn, lane);
 #pragma unroll
-      for (int g = 0; g < GN; ++g) {
-        sb[g] = B::scale(stage + S::VALUES + A::SCALE_BYTES, u, gn + g, lane);
+      for (int f = 0; f < 4; ++f) fb[f] = B::fragment(stage + A::BYTES, u, gn, f, lane);
+      const unsigned sa = A::scale(stage + S::VALUES, u, gm, lane);
 #pragma unroll
-        for (int f = 0; f < 4; ++f) fb[4 * g + f] = B::fragment(stage + A::BYTES, u, gn + g, f, lane);
-      }
-#pragma unroll
-      for (int g = 0; g < GM; ++g) {
-        sa[g] = A::scale(stage + S::VALUES, u, gm + g, lane);
-#pragma unroll
-        for (int f = 0; f < 4; ++f) fa[4 * g + f] = A::fragment(stage, u, gm + g, f, lane);
-      }
-#pragma unroll
-      for (int g = 0; g < GM; ++g)
-        each<4>([&](auto f) {
-          constexpr int F = decltype(f)::value;
-          if (i == 0 && g == 0 && F == 1) between();
-#pragma unroll
-          for (int h = 0; h < GN; ++h)
-            each<4>([&](auto e) {
-              constexpr int E = decltype(e)::value;
-              acc[4 * g + F][4 * h + E] = multiply<FA, FB, F, E>(fa[4 * g + F], fb[4 * h + E], acc[4 * g + F][4 * h + E], sa[g], sb[h]);
-            });
+      for (int f = 0; f < 4; ++f) fa[f] = A::fragment(stage, u, gm, f, lane);
+      each<4>([&](auto f) {
+        constexpr int F = decltype(f)::value;
+        if (i == 0 && F == 1) between();
+        each<4>([&](auto e) {
+          constexpr int E = decltype(e)::value;
+          acc[F][E] = multiply<FA, FB, F, E>(fa[F], fb[E], acc[F][E], sa, sb);
         });
+      });
     }
   };
   if (ahead) {
@@ -448,14 +422,7 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tile_kernel(const GemmA
   int place = ahead, next = (PLACES - 1 + ahead) % PLACES;  // of this stage, and of the one that is requested
   for (int s = 0; s < stages; ++s) {
     __builtin_amdgcn_sched_barrier(0);
-    // the stage has arrived, and nobody reads the one before any more
-    if (PLACES > 2 && s + PLACES - 2 < stages) {
-      constexpr int YOUNGER = (PLACES - 2) * LOADS;
-      __builtin_amdgcn_s_waitcnt(0x0070 | (YOUNGER & 15) | ((YOUNGER >> 4) << 14));
-      __builtin_amdgcn_s_barrier();
-    } else {
-      wait_all_and_meet();
-    }
+    wait_all_and_meet();  // the stage has arrived, and nobody reads the one before any more
     __builtin_amdgcn_sched_barrier(0);
     const bool more = s + PLACES - 1 < stages;
     if (!LATE && more) request(s + PLACES - 1, next);
@@ -474,20 +441,20 @@ __global__ __launch_bounds__(64 * WM * WN * GROUPS) void tile_kernel(const GemmA
     __syncthreads();  // (the stages are read)
     if (group > 0) {
 #pragma unroll
-      for (int i = 0; i < 4 * GM; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4 * GN; ++j) meet[(((group - 1) * SET + member) * 16 * GM * GN + i * 4 * GN + j) * 64] = acc[i][j];
+        for (int j = 0; j < 4; ++j) meet[(((group - 1) * SET + member) * 16 + i * 4 + j) * 64] = acc[i][j];
     }
     __syncthreads();
     if (group > 0) return;
 #pragma unroll
     for (int k = 0; k < GROUPS - 1; ++k)
 #pragma unroll
-      for (int i = 0; i < 4 * GM; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4 * GN; ++j) acc[i][j] += meet[((k * SET + member) * 16 * GM * GN + i * 4 * GN + j) * 64];
+        for (int j = 0; j < 4; ++j) acc[i][j] += meet[((k * SET + member) * 16 + i * 4 + j) * 64];
   }
-  finish_tile<GM, GN>(p, slice, m0 + 64 * gm, n0 + 64 * gn, lane, acc);
+  finish_tile(p, slice, m0 + 64 * gm, n0 + 64 * gn, lane, acc);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------------
@@ -533,50 +500,45 @@ struct Rows {
   }
 };
 
-// A workgroup takes 64 or 16 rows x 64 or 16 columns; its wavefronts take a run of K's steps each and add their sums in LDS, in order.
+// A workgroup takes 16 rows x 64 (GROUP) or 16 columns; its 8 wavefronts take a run of K's steps each and add their sums in LDS, in order.
 //
 // Bound by memory's latency: B is read once, and with 8 wavefronts on 4 steps each all of K = 4096 is asked for at once.  4 x 8192 x 4096, 8 bits
 // by 4, with a residual: 7.1 us for 17.9 MB, which a stream reads in 2.8 behind a launch of 1.5.  (8.7 with the steps dealt to the wavefronts in turn,
 // tiles to the dies in turn, and rows finished one behind the other.)
-template <int FA, int FB, bool GROUP_M, bool GROUP_N, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
-  constexpr int FM = GROUP_M ? 4 : 1, FN = GROUP_N ? 4 : 1, BM = 16 * FM, BN = 16 * FN;
-  constexpr int AT_ONCE = FM * FN == 1 ? 4 : 2;  // steps whose loads are in flight
-  __shared__ f32x4 meet[WAVES][FM * FN][64];
+template <int FA, int FB, bool GROUP>
+__global__ __launch_bounds__(512) void stream_kernel(const GemmArgs p) {
+  constexpr int WAVES = 8, FN = GROUP ? 4 : 1;
+  constexpr int AT_ONCE = GROUP ? 2 : 4;  // steps whose loads are in flight
+  __shared__ f32x4 meet[WAVES][FN][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN, slices = slices_of(p);
+  const int tiles_m = (p.M + 15) / 16, slices = slices_of(p);
   // (neighbouring tiles of columns share lines of scales)
   const int place = (int)place_of(blockIdx.x, gridDim.x), tile = place / slices, slice = place - tile * slices;
-  const int m0 = tile % tiles_m * BM, n0 = tile / tiles_m * BN;
-  (void)tiles_n;
-  Rows<FA, GROUP_M> a;
-  Rows<FB, GROUP_N> b;
+  const int m0 = tile % tiles_m * 16, n0 = tile / tiles_m * 16 * FN;
+  Rows<FA, false> a;
+  Rows<FB, GROUP> b;
   a.init(p.a, p.scales_a, p.lda, p.ld_scales_a, m0, p.M, p.blocks, lane);
   b.init(p.b, p.scales_b, p.ldb, p.ld_scales_b, n0, p.N, p.blocks, lane);
   // (the residual is asked for before all else, so that it is at hand when the sums are)
   unsigned near = 0;
-  if (p.residual && slices == 1 && wave < FM) {
-    const int size = (p.flags & 3) == HIDET_F32 ? 4 : 2, col = n0 + (GROUP_N ? 4 : 1) * (lane % 16);
+  if (p.residual && slices == 1 && wave == 0) {
+    const int size = (p.flags & 3) == HIDET_F32 ? 4 : 2, col = n0 + (GROUP ? 4 : 1) * (lane % 16);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int row = m0 + (GROUP_M ? 16 * (lane / 16) + 4 * e + wave : 4 * (lane / 16) + e);
+      const int row = m0 + 4 * (lane / 16) + e;
       if (row < p.M && col < p.N) near |= *reinterpret_cast<const unsigned short*>(reinterpret_cast<const unsigned char*>(p.residual) + ((long long)row * p.ldr + col) * size);
     }
   }
-  f32x4 acc[FM][FN];
+  f32x4 acc[FN];
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  Fragment<FA> fa[AT_ONCE][FM];
+  for (int j = 0; j < FN; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  Fragment<FA> fa[AT_ONCE][1];
   Fragment<FB> fb[AT_ONCE][FN];
   unsigned sa[AT_ONCE], sb[AT_ONCE];
   auto product = [&](int u) {
-    each<FM>([&](auto f) {
-      each<FN>([&](auto e) {
-        constexpr int F = decltype(f)::value, E = decltype(e)::value;
-        acc[F][E] = multiply<FA, FB, F, E>(fa[u][F], fb[u][E], acc[F][E], sa[u], sb[u]);
-      });
+    each<FN>([&](auto e) {
+      constexpr int E = decltype(e)::value;
+      acc[E] = multiply<FA, FB, 0, E>(fa[u][0], fb[u][E], acc[E], sa[u], sb[u]);
     });
   };
   // a run of steps for every wavefront, so that it takes whole lines of 4-bit rows; its last may be the one that K ends in
@@ -606,54 +568,49 @@ __global__ __launch_bounds__(64 * WAVES) void stream_kernel(const GemmArgs p) {
     if (step + u < last) product(u);
   asm volatile("" ::"v"(near));
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j) meet[wave][i * FN + j][lane] = acc[i][j];
+  for (int j = 0; j < FN; ++j) meet[wave][j][lane] = acc[j];
   __syncthreads();
-  // every wavefront finishes some of the rows: those of fragment i, or (16 rows) the first does all
-  for (int i = wave; i < FM; i += WAVES) {
-    f32x4 sum[FN];
+  if (wave > 0) return;  // (the first finishes all rows)
+  f32x4 sum[FN];
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      sum[j] = meet[0][i * FN + j][lane];
+  for (int j = 0; j < FN; ++j) {
+    sum[j] = meet[0][j][lane];
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) sum[j] += meet[w][i * FN + j][lane];
+    for (int w = 1; w < WAVES; ++w) sum[j] += meet[w][j][lane];
+  }
+  if constexpr (GROUP) {
+    const int col = n0 + 4 * (lane % 16);
+    int row[4];
+    float v[4][4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      row[e] = m0 + 4 * (lane / 16) + e;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) v[e][c] = sum[c][e];
     }
-    if constexpr (GROUP_N) {
-      const int col[1] = {n0 + 4 * (lane % 16)};
-      int row[4];
-      float v[4][1][4];
+    if (slices > 1) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        row[e] = m0 + (GROUP_M ? 16 * (lane / 16) + 4 * e + i : 4 * (lane / 16) + e);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[e][0][c] = sum[c][e];
-      }
-      if (slices > 1) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) keep4(p, slice, row[e], col[0], v[e][0]);
-      } else {
-        with_out_type(p, [&](auto type) {
-          using TO = decltype(type);
-          finish<TO, 4, 1>(p, row, col, ColumnBias<TO, 1>(p, col), v);
-        });
-      }
-    } else {  // a column a lane, four rows: of four lanes, each takes the four columns of one row
-      static_assert(!GROUP_M, "one fragment");
-      float v[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        float t[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t[e] = __shfl(sum[0][e], (lane & ~3) + c);
-        v[c] = lane & 2 ? (lane & 1 ? t[3] : t[2]) : (lane & 1 ? t[1] : t[0]);
-      }
-      const int row = m0 + 4 * (lane / 16) + lane % 4, col = n0 + lane % 16 / 4 * 4;
-      if (slices > 1)
-        keep4(p, slice, row, col, v);
-      else
-        with_out_type(p, [&](auto type) { finish4<decltype(type)>(p, row, col, v); });
+      for (int e = 0; e < 4; ++e) keep4(p, slice, row[e], col, v[e]);
+    } else {
+      with_out_type(p, [&](auto type) {
+        using TO = decltype(type);
+        finish<TO, 4>(p, row, col, ColumnBias<TO>(p, col), v);
+      });
     }
+  } else {  // a column a lane, four rows: of four lanes, each takes the four columns of one row
+    float v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float t[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] = __shfl(sum[0][e], (lane & ~3) + c);
+      v[c] = lane & 2 ? (lane & 1 ? t[3] : t[2]) : (lane & 1 ? t[1] : t[0]);
+    }
+    const int row = m0 + 4 * (lane / 16) + lane % 4, col = n0 + lane % 16 / 4 * 4;
+    if (slices > 1)
+      keep4(p, slice, row, col, v);
+    else
+      with_out_type(p, [&](auto type) { finish4<decltype(type)>(p, row, col, v); });
   }
 }
 

@@ -8,12 +8,12 @@ template <int FA, int FB>
 hipError_t launch(const GemmCut& c, const GemmArgs& p, hipStream_t stream) {
   const dim3 grid((unsigned)c.blocks);
   switch (c.kernel) {
-    case KERNEL_TILE_256: hipLaunchKernelGGL((tile_kernel<FA, FB, 1, 1, 4, 4, 1, 2>), grid, dim3(1024), 0, stream, p); break;
-    case KERNEL_TILE_128: hipLaunchKernelGGL((tile_kernel<FA, FB, 1, 1, 2, 2, 1, 2>), grid, dim3(256), 0, stream, p); break;
-    case KERNEL_TILE_64X128: hipLaunchKernelGGL((tile_kernel<FA, FB, 1, 1, 1, 2, 2, 2>), grid, dim3(256), 0, stream, p); break;
-    case KERNEL_TILE_64: hipLaunchKernelGGL((tile_kernel<FA, FB, 1, 1, 1, 1, 4, 2>), grid, dim3(256), 0, stream, p); break;
-    case KERNEL_STREAM_16: hipLaunchKernelGGL((stream_kernel<FA, FB, false, false, 8>), grid, dim3(512), 0, stream, p); break;
-    default: hipLaunchKernelGGL((stream_kernel<FA, FB, false, true, 8>), grid, dim3(512), 0, stream, p); break;
+    case KERNEL_TILE_256: hipLaunchKernelGGL((tile_kernel<FA, FB, 4, 4, 1>), grid, dim3(1024), 0, stream, p); break;
+    case KERNEL_TILE_128: hipLaunchKernelGGL((tile_kernel<FA, FB, 2, 2, 1>), grid, dim3(256), 0, stream, p); break;
+    case KERNEL_TILE_64X128: hipLaunchKernelGGL((tile_kernel<FA, FB, 1, 2, 2>), grid, dim3(256), 0, stream, p); break;
+    case KERNEL_TILE_64: hipLaunchKernelGGL((tile_kernel<FA, FB, 1, 1, 4>), grid, dim3(256), 0, stream, p); break;
+    case KERNEL_STREAM_16: hipLaunchKernelGGL((stream_kernel<FA, FB, false>), grid, dim3(512), 0, stream, p); break;
+    default: hipLaunchKernelGGL((stream_kernel<FA, FB, true>), grid, dim3(512), 0, stream, p); break;
   }
   return hipGetLastError();
 }
