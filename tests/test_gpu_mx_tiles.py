@@ -1,4 +1,4 @@
-"""Block-scaled products on every tile and in slices of K, for every pair of formats: exact cases and bounds as in the tests of all sizes."""
+"""Block-scaled products on every tile and in slices of K, for every pair of formats."""
 import numpy as np
 import pytest
 import torch
@@ -24,8 +24,8 @@ def test_products_of_every_pair_on_tiles(size, formats):
 @pytest.mark.parametrize("formats", PAIRS, ids=str)
 @pytest.mark.parametrize("size", TILES, ids=str)
 def test_products_of_elements_of_all_sizes_on_tiles(size, formats):
-    """Every element code but NaN and infinity, and scales apart by 2^8, against float64 products of 40 rows and 40 columns, both ends and the middle
-    among them."""
+    """Every element code but NaN and infinity, and scales apart by 2^8, against sums of eights as the matrix cores cut them, for 40 rows and 40 columns,
+    both ends and the middle among them: a step of fp32 for every one of K / 128 + 16 additions, and half a step of the output's type."""
     m, n, k = size
     g = rng(m, n, k, *formats)
 
@@ -45,13 +45,8 @@ def test_products_of_elements_of_all_sizes_on_tiles(size, formats):
         return np.unique(np.r_[0:3, count // 2:count // 2 + 2, count - 3:count, g.integers(0, count, 32)])
 
     rows, cols = some(m), some(n)
-    na, nb = mx.numbers(a[0][rows], a[1][:, rows], formats[0]), mx.numbers(b[0][cols], b[1][:, cols], formats[1])
-    want, size_of = na @ nb.T, np.abs(na) @ np.abs(nb).T
+    want, size_of = mx.product_of_cut_eights((a[0][rows], a[1][:, rows]), formats[0], (b[0][cols], b[1][:, cols]), formats[1])
     bound = (mx.blocks(k) / 4 + 16) * 2.0 ** -24 * size_of
-    if formats != (mx.E2M1, mx.E2M1):
-        pa, pb = np.abs(na), np.abs(nb)  # (whole blocks: groups of 8 k)
-        for k8 in range(0, na.shape[1], 8):
-            bound += 8 * 2.0 ** -12 * (pa[:, None, k8:k8 + 8] * pb[None, :, k8:k8 + 8]).max(2)
     for out in ("f32", "bf16"):
         c = torch.empty((m, n), dtype=TYPES[out], device="cuda")
         ws = torch.empty(max(4, hb.hidet_mx_gemm_workspace_bytes(ma, mb)), dtype=torch.uint8, device="cuda")

@@ -75,3 +75,29 @@ def test_norm_and_its_gradient():
         b[i, j] -= step
         d = ((mx.rms_norm(a, w, 1e-3, 0.5)[0] - mx.rms_norm(b, w, 1e-3, 0.5)[0]) * gy).sum() / (2 * step)
         assert abs(d - gh[i, j]) < 1e-7
+
+
+def test_products_whose_eights_are_cut():
+    """By hand: e4m3, 2^8 * 2^8 beside 2^k; 4 by 4 bits and eights of one size lose nothing."""
+    def row(*codes):
+        c = np.zeros((1, 32), dtype=np.uint8)
+        c[0, :len(codes)] = codes
+        return c, np.full((1, 1), 127, dtype=np.uint8)
+
+    def power(e):
+        return (e + 7) << 3
+
+    for small, want in ((3, 2.0 ** 16 + 2.0 ** 3), (2, 2.0 ** 16)):
+        total, size = mx.product_of_cut_eights(row(power(8), power(small)), 0, row(power(8), power(0)), 0)
+        assert total[0, 0] == want and size[0, 0] == 2.0 ** 16 + 2.0 ** small
+    # the small one in another eight; 2^-9 counts as 2^-6: 2^-9 * 2^8 keeps 2^-11, and cuts 2^-12 towards zero
+    assert mx.product_of_cut_eights(row(power(8), 0, 0, 0, 0, 0, 0, 0, power(2)), 0, row(power(8), 0, 0, 0, 0, 0, 0, 0, power(0)), 0)[0][0, 0] == 2.0 ** 16 + 4
+    for small, want in ((-5, 0.5 + 2.0 ** -11), (-6, 0.5)):
+        assert mx.product_of_cut_eights(row(1, power(small)), 0, row(power(8), power(-6)), 0)[0][0, 0] == want
+        assert mx.product_of_cut_eights(row(1, power(small) | 128), 0, row(power(8), power(-6)), 0)[0][0, 0] == 1.0 - want
+    # elements that meet a 0 do not count
+    assert mx.product_of_cut_eights(row(0, power(-6), power(8)), 0, row(power(8), power(-6), 0), 0)[0][0, 0] == 2.0 ** -12
+    g = np.random.default_rng(2)
+    a, b = (g.integers(0, 16, (5, 64)).astype(np.uint8) for _ in range(2))
+    s = g.integers(120, 130, (2, 5)).astype(np.uint8)
+    assert np.array_equal(mx.product_of_cut_eights((a, s), 2, (b, s), 2)[0], mx.numbers(a, s, 2) @ mx.numbers(b, s, 2).T)
