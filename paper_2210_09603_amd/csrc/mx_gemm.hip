@@ -25,7 +25,17 @@ constexpr long long kMaxGrid = (1LL << 22) - 1;  // workgroups of up to 1024 thr
 constexpr int kUnits = 256;                      // compute units
 
 // What a tile takes for a step of 128 k, in us: where each unit has one of them, and, by the unit's time, where there are more.  Both operands in 8
-// bits, one, none.  (K = 4096; 333 x 5120, 1024 x 1024, 4096 x 4096 and 8192 x 8192.)
+// bits, one, none.  (K = 4096; 333 x 5120, 1024 x 1024, 4096 x 4096 and 8192 x 8192.)  What the kernels on both sides of a border take at
+// K = 4096 into bf16, 8 bits by 8, 8 by 4, 4 by 4, in us; * is the one that is chosen:
+//   1024 x 1024   64 x 64    15.5* 13.8* 12.1*   64 x 128   19.1  17.3  16.2
+//   1024 x 1536   64 x 64    27.7  25.3  14.5    64 x 128   18.9* 17.0* 15.3*
+//   1024 x 2048   64 x 128   19.5* 17.4* 15.6*   128 x 128  23.7  25.5  24.9
+//   2048 x 2048   64 x 128   37.4  23.2  20.6    128 x 128  27.0* 26.7* 19.5*
+//   3000 x 4096   128 x 128  57.9* 56.3* 38.6*   256 x 256  53.1  50.0  35.6
+//   4096 x 4096   128 x 128  70.3  66.7  47.3    256 x 256  60.2* 55.1* 38.9*
+// (with slices of K where cut_slices makes them).  Of 381 products of 17 to 8192 rows the choice is within 3 % of the fastest kernel in 311 and within
+// 10 % in 356.  It is off by most for 8 bits by 4, where two and three rounds of 64 x 128 tiles take less than the model has for them:
+// 512 x 8192 x 8192 on 128 x 128 tiles 47.6, on 64 x 128 37.3.
 struct TileCost {
   int kernel, rows, cols;
   float alone[3], among[3], once;  // once: of a tile, its first loads and its stores
@@ -38,8 +48,13 @@ constexpr TileCost kTiles[] = {
 };
 constexpr float kJoin = 4.0f;  // us, of the second launch of a product in slices
 // The same of the workgroups of few rows, whose wavefronts take 8 steps at once; by rounds of one to a unit, and as far as they begin sooner than tiles.
-// (64 x 4096 x 4096, 8 bits by 4 and 4 by 4: 9.0 and 8.0 us, tiles 12.4 and 11.3; 32 x 8192 x 2048, both in 8 bits: 8.0 and 11.3; 48 x 8192 x 8192: 40 and
-// 21, 8 bits by 4 25 and 17; 256 x 1024 x 1024, 8 bits by 4: 4.8 and 7.8.  More than two rounds are left to the tiles.)
+// Them and tiles (those that are chosen, else the fastest), as above:
+//   32 x 4096 x 4096    11.2  8.9* 8.1*   13.0* 11.0 10.6        64 x 4096 x 4096    12.9  9.4* 8.4*   14.2* 12.4 11.8
+//   100 x 4096 x 4096   22.6 14.8* 13.1*  14.1* 13.9 12.0        128 x 4096 x 4096   22.7 15.0* 13.2*  14.4* 13.5 11.7
+//   256 x 1024 x 1024   5.9* 5.1* 4.8*    8.3   8.1  7.3         512 x 1024 x 1024    9.1  6.6* 6.1*   8.4*  8.2  7.4
+//   64 x 8192 x 2048    14.1 9.4* 8.5*    11.3* 9.9  8.8         48 x 8192 x 8192    40.0 25.0 22.0    21.5* 18.3* 16.5*
+// (the last: 64 x 128 tiles 19.8, 16.1 and 14.9).  The time has no term for A, which every workgroup of columns reads again: at 100 and 128 rows it
+// is up to 14 % off.  More than two rounds are left to the tiles.
 constexpr float kStream[3] = {0.27f, 0.15f, 0.12f};
 
 long long tiles_of(long long M, long long N, long long rows, long long cols) { return (M + rows - 1) / rows * ((N + cols - 1) / cols); }

@@ -126,7 +126,8 @@ __device__ __forceinline__ S row_sum(S v, S* room) {
 }
 
 // LANES threads a row, CHUNKS chunks of 16 bytes a thread; 256 threads, or as many as a row has.  STREAM: x, residual and what is written pass
-// the caches by.  16384 x 8192 in bf16, x + residual into the stream and 8 bits: 165 us for 944 MB, 5.7 TB/s (a copy: 6.1); 4 x 4096: 2.4 us in the
+// the caches by.  16384 x 8192 in bf16, x + residual into the stream and 8 bits: 165 us for 944 MB, 5.7 TB/s (a copy: 6.1), into 4 bits 162;
+// 16384 x 4096 in fp32, into the stream and fp32 174 us for 1074 MB, 6.2 TB/s, and 8 bits 147; 4 x 4096: 2.4 us in the
 // kernel, a launch and one trip to memory: with one chunk a thread the weight is asked for with x (333 x 4096 into 8 bits and the product behind it
 // 22.65 us together, 22.86 with the weight behind the sum).
 template <typename T, typename TW, int LANES, int CHUNKS, bool STREAM>
@@ -427,7 +428,8 @@ __global__ __launch_bounds__(1024) void join_kernel(const float* part, TW* out, 
 // 1024 lanes 142, by 512 of two 161; fp32, 16384 x 5120, by 512 lanes of three chunks 163, by 768 of two 183), then as many as 512
 // lanes have registers for (bf16, 4096 x 16384 by 512 lanes of four chunks 86, by 1024, whose registers do not hold two rows, 395); no more workgroups than one
 // to a unit, or two of 256 lanes (2048 x 2048: 512 workgroups 12.8, 1024 17.7), since each is a row to add up.  Workgroups are rows of the
-// workspace: they follow from the sizes alone.
+// workspace: they follow from the sizes alone.  Where a row and the sums over rows are more than the registers of its lanes, some of it lies in scratch memory: 8 or
+// 16 bytes a lane in 16 bits above 16384 columns, 12 in bf16 with fp32 weights from 12289 on, 408 in fp32 above 16384 (4096 x 32768: 630 us, 2.6 TB/s).
 struct GradCut {
   int chunks, lanes, each, most;
 };
